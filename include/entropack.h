@@ -56,7 +56,8 @@ typedef enum {
     EP_ERR_CUDA = -4,        /* a CUDA runtime call failed */
     EP_ERR_NOMEM = -6,       /* host allocation failed */
     EP_ERR_SCRATCH = -7,     /* scratch buffer missing, misaligned or too small */
-    EP_ERR_STATIC_LIMIT = -8 /* ep_decode_tensor_static: the stream's tables exceed the built-in area */
+    EP_ERR_STATIC_LIMIT = -8, /* ep_decode_tensor_static: the stream's tables exceed the built-in area */
+    EP_ERR_BAD_PAGE = -9     /* a kernel met a page number outside the cache (ep_last_device_status) */
 } ep_status;
 
 /* Output element types of the decoder: snap_tau of Eq. 19. */
@@ -282,12 +283,86 @@ int ep_decode_tensor_static(const ep_info *info, const void *d_stream, const voi
 int ep_decode_gemm(const ep_info *info, const void *d_stream, const void *d_tile_index, const float *d_row_scales,
                    const void *d_tables, const void *d_x, uint32_t T, float *d_y, void *stream);
 
+/* ---- operators in the 8-bit container -------------------------------------------------------------------------------
+ *
+ * What a program does next with weights that it decodes to EP_FP8_E4M3 (the paper's FP8 route multiplies them in low
+ * precision, Sec. "FP8 and INT8 computation"; activations and keys / values are its future work).  Values q of the container
+ * stand for s q; the scales s made here are powers of two, the smallest with which the largest finite magnitude of a block
+ * fits 448 (at least 2^-126), so that scaling never rounds.  All calls are asynchronous on `stream`, allocate nothing, keep
+ * nothing between calls (ep_cache_append aside, whose cache it is) and can be recorded in a stream capture; the first
+ * call of a kind on a device also sets a kernel attribute.  Leading dimensions (`ld*`) are in elements. */
+
+/* q[i, j] = e4m3(x[i, j] / s), round to nearest even, one scale s per block of block_rows x 128 (block_rows 1: activations,
+ * 128: weights; blocks at the edges are smaller).  What is not finite becomes NaN and has no part in the scale; a block without
+ * a finite value but 0 has s = 1.
+ *   d_x       device, T x C of x_dtype (EP_BF16, EP_FP16, EP_FP32), any leading dimension >= C; aligned to its element
+ *             (rows that begin on 16 bytes are read fastest)
+ *   d_q       device, T x C E4M3 values, ldq >= C
+ *   d_scales  device, ceil(T / block_rows) x ceil(C / 128) E8M0 bytes (the scale is 2^(byte - 127)), lds >= ceil(C / 128) */
+int ep_quantize_blocks(const void *d_x, int32_t x_dtype, uint32_t T, uint32_t C, int64_t ldx, uint32_t block_rows, void *d_q,
+                       int64_t ldq, void *d_scales, int64_t lds, void *stream);
+
+/* y[t, r] = a[r] * sum_k (sx[t, k / 128] xq[t, k]) (sw[r / 128, k / 128] wq[r, k]), products exact, sums in fp32 on the tensor
+ * cores, one rounding to out_dtype (EP_BF16, EP_FP16, EP_FP32; EP_FP16 overflows to infinity).  NaN in either operand or
+ * scale (byte 255) gives NaN.  Results do not depend on what else runs: sums are taken in a fixed order.
+ *   d_x, d_x_scales   device, T x C E4M3 and T x ceil(C / 128) E8M0, as ep_quantize_blocks leaves them (block_rows 1)
+ *   d_w, d_w_scales   device, R x C E4M3 - a decoded weight, or one of ep_quantize_blocks (block_rows 128) - and its
+ *                     ceil(R / 128) x ceil(C / 128) E8M0 scales, or NULL: ones
+ *   d_row_scales      device, R floats a[r] (the scales with which the rows were brought into the container), or NULL: ones
+ *   d_y               device, T x R of out_dtype, aligned to its element, ldy >= R
+ * The copy engine reads the operands: d_x and d_w on 16 bytes, C, ldx and ldw multiples of 16, else EP_ERR_UNSUPPORTED.
+ * A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
+int ep_fp8_matmul(const void *d_x, int64_t ldx, const void *d_x_scales, int64_t ldsx, const void *d_w, int64_t ldw,
+                  const void *d_w_scales, int64_t ldsw, const float *d_row_scales, uint32_t T, uint32_t R, uint32_t C,
+                  int32_t out_dtype, void *d_y, int64_t ldy, void *stream);
+
+/* Keys and values of many requests in pages of E4M3, one scale for each page and head.  All pointers are device pointers. */
+typedef struct {
+    void *d_k, *d_v;                    /* [pages][heads][page][dim] E4M3; 16-byte aligned */
+    float *d_k_scales, *d_v_scales;     /* [pages][heads]; finite and >= 0 wherever a token lies */
+    uint32_t pages, heads, page, dim;   /* page: tokens of a page, 16, 32, 64, 128 or 256; dim: 64 or 128;
+                                           pages * heads * page < 2^31 - 256 */
+} ep_cache;
+
+/* Which tokens are whose, for both calls below: request b of B has d_seq_lens[b] tokens in the cache, its token j in row
+ * j % page of page d_table[b * ldt + j / page] (columns pages at most); rows d_starts[b] .. d_starts[b + 1] of the call's N
+ * rows are its newest tokens, the last of them token d_seq_lens[b] - 1.  The arrays are read on the device, so a captured
+ * call serves requests of any lengths.  Rows outside the requests are left alone.  Whatever the arrays hold, nothing outside
+ * the buffers is read or written: a page number outside the cache is passed over (the tokens are not written, and are left out
+ * of the attention) and raises EP_ERR_BAD_PAGE in the integrity word; lengths are cut to columns * page, starts to 0 .. N. */
+
+/* Writes the call's rows to the cache.  A page's scale only grows while the page fills: s' = max(s, the smallest power of two
+ * that holds the new tokens); where it grows the older tokens become e4m3(q s / s').  A page without older tokens gets the new
+ * tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request that has fewer
+ * tokens than rows is passed over, from the first on.
+ * A page that a call writes must belong to one request only; pages that are full may be shared.
+ *   d_k, d_v   device, N x heads x dim of dtype (EP_BF16, EP_FP16); `ld*` between rows, `ld*_head` between heads, all multiples
+ *              of 8 and the addresses on 16 bytes, else EP_ERR_UNSUPPORTED */
+int ep_cache_append(const ep_cache *cache, const void *d_k, int64_t ldk, int64_t ldk_head, const void *d_v, int64_t ldv,
+                    int64_t ldv_head, int32_t dtype, const int32_t *d_table, int64_t ldt, uint32_t columns,
+                    const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B, uint32_t N, void *stream);
+
+/* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row i of its n.
+ * Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token gives 0 (and -infinity in d_lse).
+ * Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values; a token's
+ * values count only for rows that see it.
+ *   d_q, d_o   device, N x q_heads x dim of dtype (EP_BF16, EP_FP16), strides as in ep_cache_append
+ *   d_lse      device, N x q_heads floats: the natural logarithm of the row's sum of exponentials, or NULL
+ *   d_workspace  device, ep_cache_attention_workspace_bytes() bytes, 16-byte aligned; may be NULL if columns * page <= 256.
+ *              Nothing in it outlives the call; calls that may overlap need one each.
+ * B <= 4096, else EP_ERR_UNSUPPORTED. */
+size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim);
+int ep_cache_attention(const ep_cache *cache, const void *d_q, int64_t ldq, int64_t ldq_head, int32_t dtype, uint32_t q_heads,
+                       const int32_t *d_table, int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts,
+                       uint32_t B, uint32_t N, float scale, int32_t causal, void *d_o, int64_t ldo, int64_t ldo_head, float *d_lse,
+                       void *d_workspace, size_t workspace_bytes, void *stream);
+
 /* Device-side integrity word (no counterpart in the paper; it uses the fact that the encoder of Eq. 17 starts
  * every state at 2^15, so a correct decode of Eq. 18 must end there).  The kernel ORs in a flag when a tile does
  * not end with every state at 2^15 and its word pointer at the next tile's offset (a damaged stream).  There is ONE
  * such word per device and process, shared by all streams and callers: the `stream` argument only says which
- * stream to wait for.  This call synchronises `stream`, returns EP_OK or EP_ERR_BAD_STREAM / EP_ERR_CUDA, and
- * clears the word.
+ * stream to wait for.  This call synchronises `stream`, returns EP_OK, EP_ERR_BAD_STREAM (also for a wait that ran out),
+ * EP_ERR_BAD_PAGE or EP_ERR_CUDA, and clears the word.
  * For tests and debugging; not needed on the hot path.  The decode kernels take every address bound
  * from `info` (sizes, counts, offsets), never from the stream's contents: damaged tables, tile records
  * or payload give wrong weights and this flag, not an access outside the buffers `info` describes.

@@ -6,6 +6,7 @@ their raw pointers; every step of the decode runs in the library's CUDA kernels.
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import os
 import weakref
@@ -58,6 +59,11 @@ class Info(C.Structure):
         return d
 
 
+class Cache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p),
+                ("pages", C.c_uint32), ("heads", C.c_uint32), ("page", C.c_uint32), ("dim", C.c_uint32)]
+
+
 class DecodeJob(C.Structure):
     _fields_ = [("info", C.POINTER(Info)), ("d_stream", C.c_void_p), ("d_tile_index", C.c_void_p),
                 ("d_row_scales", C.c_void_p), ("out_dtype", C.c_int32), ("d_out", C.c_void_p),
@@ -108,6 +114,17 @@ def load():
                                           C.c_void_p]
     L.ep_decode_gemm.argtypes = [C.POINTER(Info), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
                                  C.c_void_p, C.c_void_p]
+    L.ep_quantize_blocks.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint32, C.c_int64, C.c_uint32, C.c_void_p, C.c_int64,
+                                     C.c_void_p, C.c_int64, C.c_void_p]
+    L.ep_fp8_matmul.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
+                                C.c_uint32, C.c_uint32, C.c_uint32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
+    L.ep_cache_append.argtypes = [C.POINTER(Cache), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32,
+                                  C.c_void_p, C.c_int64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_void_p]
+    L.ep_cache_attention_workspace_bytes.restype = C.c_size_t
+    L.ep_cache_attention_workspace_bytes.argtypes = [C.c_uint32] * 5
+    L.ep_cache_attention.argtypes = [C.POINTER(Cache), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_uint32, C.c_void_p, C.c_int64,
+                                     C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_float, C.c_int32, C.c_void_p,
+                                     C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.ep_decode_batch.argtypes = [C.POINTER(DecodeJob), C.c_int32, C.c_void_p]
     L.ep_last_device_status.argtypes = [C.c_void_p]
     L.ep_strerror.restype = C.c_char_p
@@ -436,3 +453,169 @@ def decode_many(dblobs: list[DeviceBlob], out_dtype: int, outs: list, stream=Non
     for i in range(0, len(dblobs), MAX_BATCH):
         jobs = [d.job(out_dtype, o.data_ptr()) for d, o in zip(dblobs[i:i + MAX_BATCH], outs[i:i + MAX_BATCH])]
         decode_batch(jobs, h)
+
+
+# ---- operators in the 8-bit container -------------------------------------------------------------
+
+KVCache = collections.namedtuple("KVCache", "k v k_scales v_scales")
+KVCache.__doc__ = """Keys and values in pages of E4M3, one scale for each page and head: k, v [pages, heads, page, dim] float8_e4m3fn,
+k_scales, v_scales [pages, heads] float32, all contiguous.  A plain tuple of the four serves as well."""
+
+
+def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") -> KVCache:
+    """An empty cache: `pages` pages of `page` tokens."""
+    torch = _torch()
+    k, v = (torch.zeros((pages, heads, page, dim), dtype=torch.uint8, device=device).view(torch.float8_e4m3fn) for _ in range(2))
+    ks, vs = (torch.ones((pages, heads), dtype=torch.float32, device=device) for _ in range(2))
+    return KVCache(k, v, ks, vs)
+
+
+def _want(ok: bool, what: str):
+    if not ok:
+        raise ValueError(what)
+
+
+def _float_code(dtype):
+    torch = _torch()
+    return {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(dtype)
+
+
+def _launch(device, stream, call):
+    """call(stream handle) with `device` current, on the given torch stream or the device's current one."""
+    torch = _torch()
+    if device.index == torch.cuda.current_device():
+        call(_stream_handle(stream))
+    else:
+        with torch.cuda.device(device):
+            call(_stream_handle(stream))
+
+
+def _same_device(device, *tensors):
+    _want(device.type == "cuda" and all(t is None or t.device == device for t in tensors), "tensors must be on one CUDA device")
+
+
+def _rows_apart(m) -> int:
+    """Elements between the rows of a matrix; of a single row, whose stride means nothing, its length."""
+    return m.stride(0) if m.shape[0] > 1 else max(m.stride(0), m.shape[1])
+
+
+def quantize_blocks(x, block_rows: int = 1, out=None, stream=None):
+    """x [T, C] (bfloat16, float16 or float32) as E4M3 values and one power-of-two scale for each block of block_rows x 128
+    (1: activations, 128: weights): (float8_e4m3fn [T, C], float8_e8m0fnu [ceil(T / block_rows), ceil(C / 128)]).  `out`: such a
+    pair to fill.  See ep_quantize_blocks."""
+    torch = _torch()
+    code = _float_code(x.dtype)
+    _want(code is not None and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1), "x must be a matrix of bfloat16, float16 or float32 with contiguous rows")
+    _want(block_rows in (1, 128), "block_rows must be 1 or 128")
+    T, Cc = x.shape
+    shape = (-(-T // block_rows), -(-Cc // 128))
+    if out is None:
+        out = (torch.empty((T, Cc), dtype=torch.float8_e4m3fn, device=x.device), torch.empty(shape, dtype=torch.float8_e8m0fnu, device=x.device))
+    q, s = out
+    _want(q.dtype == torch.float8_e4m3fn and q.shape == (T, Cc) and (q.stride(1) == 1 or Cc == 1), "out[0] must be float8_e4m3fn of x's shape with contiguous rows")
+    _want(s.dtype == torch.float8_e8m0fnu and s.shape == shape and (s.stride(1) == 1 or shape[1] == 1), "out[1] must be float8_e8m0fnu, one scale per block")
+    _same_device(x.device, x, q, s)
+    _launch(x.device, stream, lambda h: _check(load().ep_quantize_blocks(
+        x.data_ptr(), code, T, Cc, _rows_apart(x), block_rows, q.data_ptr(), _rows_apart(q), s.data_ptr(), _rows_apart(s), h or None), "ep_quantize_blocks"))
+    return q, s
+
+
+def fp8_matmul(x, x_scales, w, w_scales=None, row_scale=None, out_dtype: int = BF16, out=None, stream=None):
+    """x [T, C] times w [R, C] transposed, both E4M3 with E8M0 scales per 1 x 128 (x_scales) and 128 x 128 (w_scales, None: ones),
+    row r of w times row_scale[r] (float32, None: ones): [T, R] of out_dtype (BF16, FP16 or FP32), or `out`.  See ep_fp8_matmul."""
+    torch = _torch()
+    e4m3, e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
+    _want(x.dtype == e4m3 and w.dtype == e4m3 and x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[1], "x and w must be float8_e4m3fn matrices of as many columns")
+    _want(x.stride(1) == 1 and w.stride(1) == 1, "rows of x and w must be contiguous")
+    (T, Cc), R = x.shape, w.shape[0]
+    blocks = -(-Cc // 128)
+    _want(x_scales.dtype == e8m0 and x_scales.shape == (T, blocks) and (x_scales.stride(1) == 1 or blocks == 1), "x_scales must be float8_e8m0fnu [T, ceil(C / 128)]")
+    _want(w_scales is None or w_scales.dtype == e8m0 and w_scales.shape == (-(-R // 128), blocks) and (w_scales.stride(1) == 1 or blocks == 1),
+          "w_scales must be float8_e8m0fnu [ceil(R / 128), ceil(C / 128)]")
+    _want(row_scale is None or row_scale.dtype == torch.float32 and row_scale.shape == (R,) and row_scale.is_contiguous(), "row_scale must be float32 [R]")
+    if out is None:
+        _want(out_dtype in (BF16, FP16, FP32), "out_dtype must be BF16, FP16 or FP32")
+        out = torch.empty((T, R), dtype=_out_torch_dtype(out_dtype), device=x.device)
+    code = _float_code(out.dtype)
+    _want(code is not None and out.shape == (T, R) and (out.stride(1) == 1 or R == 1), "out must be a [T, R] matrix of bfloat16, float16 or float32 with contiguous rows")
+    _same_device(x.device, x_scales, w, w_scales, row_scale, out)
+    _launch(x.device, stream, lambda h: _check(load().ep_fp8_matmul(
+        x.data_ptr(), _rows_apart(x), x_scales.data_ptr(), _rows_apart(x_scales), w.data_ptr(), _rows_apart(w), w_scales.data_ptr() if w_scales is not None else None,
+        _rows_apart(w_scales) if w_scales is not None else 0, row_scale.data_ptr() if row_scale is not None else None, T, R, Cc, code, out.data_ptr(), _rows_apart(out),
+        h or None), "ep_fp8_matmul"))
+    return out
+
+
+def _cache_of(cache):
+    torch = _torch()
+    k, v, ks, vs = cache
+    _want(k.dtype == torch.float8_e4m3fn and v.dtype == torch.float8_e4m3fn and k.dim() == 4 and v.shape == k.shape and k.is_contiguous() and v.is_contiguous(),
+          "the cache's keys and values must be contiguous float8_e4m3fn [pages, heads, page, dim]")
+    pages, heads, page, dim = k.shape
+    _want(ks.dtype == torch.float32 and vs.dtype == torch.float32 and ks.shape == (pages, heads) and vs.shape == (pages, heads) and ks.is_contiguous() and vs.is_contiguous(),
+          "the cache's scales must be contiguous float32 [pages, heads]")
+    _same_device(k.device, v, ks, vs)
+    return Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page, dim)
+
+
+def _requests(device, table, seq_lens, starts):
+    torch = _torch()
+    _want(table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1), "table must be an int32 matrix with contiguous rows")
+    B = table.shape[0]
+    _want(seq_lens.dtype == torch.int32 and seq_lens.shape == (B,) and seq_lens.is_contiguous(), "seq_lens must be int32, one per row of table")
+    _want(starts.dtype == torch.int32 and starts.shape == (B + 1,) and starts.is_contiguous(), "starts must be int32, one more than rows of table")
+    _same_device(device, table, seq_lens, starts)
+    return B
+
+
+def cache_append(cache, k, v, table, seq_lens, starts, stream=None) -> None:
+    """Writes k, v [N, heads, dim] (bfloat16 or float16) to a KVCache: rows starts[b] .. starts[b + 1] are the newest tokens of request b,
+    which has seq_lens[b] with them, in the pages table[b].  See ep_cache_append."""
+    c = _cache_of(cache)
+    code = _float_code(k.dtype)
+    _want(code in (BF16, FP16) and v.dtype == k.dtype and k.dim() == 3 and v.shape == k.shape and k.shape[1:] == (c.heads, c.dim), "k and v must be bfloat16 or float16 [N, heads, dim]")
+    _want(k.stride(2) == 1 and v.stride(2) == 1, "heads of k and v must be contiguous")
+    device = cache[0].device
+    B = _requests(device, table, seq_lens, starts)
+    _same_device(device, k, v)
+    _launch(device, stream, lambda h: _check(load().ep_cache_append(
+        C.byref(c), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), code, table.data_ptr(), _rows_apart(table), table.shape[1],
+        seq_lens.data_ptr(), starts.data_ptr(), B, k.shape[0], h or None), "ep_cache_append"))
+
+
+def cache_attention_workspace_bytes(N: int, B: int, q_heads: int, heads: int, dim: int) -> int:
+    """ep_cache_attention_workspace_bytes: of N rows of B requests, on the current device."""
+    return int(load().ep_cache_attention_workspace_bytes(N, B, q_heads, heads, dim))
+
+
+def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool = True, out=None, lse=None, workspace=None, stream=None):
+    """softmax(scale q K^T) V of q [N, q_heads, dim] (bfloat16 or float16) over a KVCache, rows, requests and pages as in cache_append;
+    scale: 1 / sqrt(dim) by default.  lse: float32 [N, q_heads] to fill.  workspace: a uint8 tensor of
+    cache_attention_workspace_bytes(), taken from torch's allocator if not given.  See ep_cache_attention."""
+    torch = _torch()
+    c = _cache_of(cache)
+    code = _float_code(q.dtype)
+    _want(code in (BF16, FP16) and q.dim() == 3 and q.shape[2] == c.dim and q.stride(2) == 1, "q must be bfloat16 or float16 [N, q_heads, dim] with contiguous heads")
+    N, Hq, D = q.shape
+    _want(Hq > 0 and Hq % c.heads == 0, "q's heads must be a multiple of the cache's")
+    device = cache[0].device
+    B = _requests(device, table, seq_lens, starts)
+    if out is None:
+        out = torch.empty((N, Hq, D), dtype=q.dtype, device=device)
+    _want(out.dtype == q.dtype and out.shape == q.shape and out.stride(2) == 1, "out must be of q's type and shape with contiguous heads")
+    _want(lse is None or lse.dtype == torch.float32 and lse.shape == (N, Hq) and lse.is_contiguous(), "lse must be contiguous float32 [N, q_heads]")
+    _same_device(device, q, out, lse, workspace)
+    scale = D ** -0.5 if scale is None else float(scale)
+
+    def call(h):
+        ws = workspace
+        if ws is None:
+            ws = torch.empty(cache_attention_workspace_bytes(N, B, Hq, c.heads, D), dtype=torch.uint8, device=device)
+            if stream is not None:
+                ws.record_stream(stream)
+        _check(load().ep_cache_attention(
+            C.byref(c), q.data_ptr(), q.stride(0), q.stride(1), code, Hq, table.data_ptr(), _rows_apart(table), table.shape[1], seq_lens.data_ptr(), starts.data_ptr(),
+            B, N, scale, int(causal), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr() if lse is not None else None, ws.data_ptr(),
+            ws.numel() * ws.element_size(), h or None), "ep_cache_attention")
+    _launch(device, stream, call)
+    return out

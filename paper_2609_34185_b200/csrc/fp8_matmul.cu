@@ -1,0 +1,472 @@
+// Rounding to E4M3 in blocks of 128 with power-of-two scales, and the matrix product of operands held that way.
+#include "op8.hpp"
+
+using namespace ep;
+
+namespace {
+
+constexpr uint32_t kBlock = 128;                 // columns (and rows, for weights) that share a scale
+__device__ unsigned int g_matmul_status = 0;
+
+// ======================================================================================================================
+// Quantisation.  For a block with largest finite magnitude a: s = the smallest power of two with a <= 448 s, q = e4m3(x / s).
+// x / s is exact (s is a power of two), so there is one rounding, E4M3's.  E4M3 has its three fraction bits at every magnitude from
+// 2^-6 to 448: a scale that is not a power of two would save at most one of fifteen binades and no rounding error.  What is
+// not finite becomes NaN and has no part in the scale.
+// Bound by memory: each value is read once into registers, where it waits for its block's maximum.
+// ======================================================================================================================
+struct QuantParams {
+    const void *x;
+    uint8_t *q, *s;
+    int64_t ldx, ldq, lds;
+    uint32_t T, C, blocks;        // blocks = ceil(C / 128)
+    uint32_t vec;                 // rows of x and q begin on 16 and 8 bytes
+};
+
+// N consecutive values of a row from column c on, as floats; zeros past the row's end
+template <class E>
+__device__ __forceinline__ void load_values(const typename E::T *row, uint32_t c, uint32_t C, bool vec, float (&v)[16 / sizeof(typename E::T)]) {
+    constexpr uint32_t N = 16 / sizeof(typename E::T);
+    if (vec && c + N <= C) {
+        const uint4 w = __ldcs(reinterpret_cast<const uint4 *>(row + c));
+        if constexpr (N == 4) {
+            v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+        } else {
+            v[0] = E::lo(w.x), v[1] = E::hi(w.x), v[2] = E::lo(w.y), v[3] = E::hi(w.y);
+            v[4] = E::lo(w.z), v[5] = E::hi(w.z), v[6] = E::lo(w.w), v[7] = E::hi(w.w);
+        }
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i) v[i] = c + i < C ? E::to(row[c + i]) : 0.0f;
+    }
+}
+template <uint32_t N>
+__device__ __forceinline__ float largest(const float (&v)[N]) {              // NaN has no part in it, infinity has
+    float a = 0.0f;
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i) a = fmaxf(a, fabsf(v[i]));
+    return a;
+}
+template <uint32_t N>
+__device__ __forceinline__ void only_finite(float (&v)[N]) {
+#pragma unroll
+    for (uint32_t i = 0; i < N; ++i)
+        if (!(fabsf(v[i]) < __uint_as_float(0x7F800000u))) v[i] = __uint_as_float(0x7FFFFFFFu);
+}
+template <uint32_t N>
+__device__ __forceinline__ void store_values(uint8_t *row, uint32_t c, uint32_t C, bool vec, const float (&v)[N], float inverse) {
+    uint32_t w[N / 4];
+#pragma unroll
+    for (uint32_t i = 0; i < N / 4; ++i)
+        w[i] = e4m3x2(v[4 * i] * inverse, v[4 * i + 1] * inverse) | e4m3x2(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse) << 16;
+    if (vec && c + N <= C) {
+        if constexpr (N == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
+        else *reinterpret_cast<uint32_t *>(row + c) = w[0];
+    } else {
+#pragma unroll
+        for (uint32_t i = 0; i < N; ++i)
+            if (c + i < C) row[c + i] = uint8_t(w[i / 4] >> (8 * (i % 4)));
+    }
+}
+
+// one scale per row and 128 columns: a warp takes four 16-byte loads per lane of one row
+template <class E>
+__global__ void __launch_bounds__(128) quantize_rows_kernel(const __grid_constant__ QuantParams P) {
+    using T = typename E::T;
+    constexpr uint32_t N = 16 / sizeof(T), kLanes = kBlock / N, kLoads = 4, kSpan = 32 * N;
+    op_wait_for_stream();
+    const uint32_t lane = threadIdx.x & 31u;
+    const uint32_t spans = (P.C + kLoads * kSpan - 1u) / (kLoads * kSpan);
+    const uint64_t unit = uint64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
+    if (unit >= uint64_t(P.T) * spans) return;
+    const uint32_t t = uint32_t(unit / spans), c0 = uint32_t(unit % spans) * (kLoads * kSpan) + lane * N;
+    const T *row = static_cast<const T *>(P.x) + int64_t(t) * P.ldx;
+    float v[kLoads][N];
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) load_values<E>(row, c0 + i * kSpan, P.C, P.vec, v[i]);
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        auto block_max = [&]() {
+            float a = largest(v[i]);
+#pragma unroll
+            for (uint32_t m = 1; m < kLanes; m <<= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, m));
+            return a;
+        };
+        float a = block_max();
+        if (__any_sync(0xFFFFFFFFu, !(a < __uint_as_float(0x7F800000u)))) {       // an infinity: without it
+            only_finite(v[i]);
+            a = block_max();
+        }
+        const uint32_t e = scale_exponent(a, 127u), c = c0 + i * kSpan;
+        store_values(P.q + int64_t(t) * P.ldq, c, P.C, P.vec, v[i], pow2_inverse(e));
+        if (c < P.C && (lane & (kLanes - 1u)) == 0) P.s[int64_t(t) * P.lds + c / kBlock] = uint8_t(e);
+    }
+}
+
+// one scale per 128 rows and 128 columns: a CTA of eight warps holds the block in registers, sixteen rows per warp
+template <class E>
+__global__ void __launch_bounds__(256) quantize_blocks_kernel(const __grid_constant__ QuantParams P) {
+    using T = typename E::T;
+    constexpr uint32_t N = 16 / sizeof(T), kLanes = kBlock / N, kRowsPerLoad = 32 / kLanes, kLoads = 16 / kRowsPerLoad;
+    __shared__ float largest_of[8];
+    op_wait_for_stream();
+    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5;
+    const uint32_t rb = blockIdx.x / P.blocks, cb = blockIdx.x % P.blocks;
+    const uint32_t t0 = rb * kBlock + warp * 16u + lane / kLanes, c = cb * kBlock + (lane % kLanes) * N;
+    float v[kLoads][N];
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t t = t0 + i * kRowsPerLoad;
+        if (t < P.T) load_values<E>(static_cast<const T *>(P.x) + int64_t(t) * P.ldx, c, P.C, P.vec, v[i]);
+        else
+#pragma unroll
+            for (uint32_t j = 0; j < N; ++j) v[i][j] = 0.0f;
+    }
+    auto block_max = [&]() {
+        float a = 0.0f;
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) a = fmaxf(a, largest(v[i]));
+        a = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a)));      // magnitudes order like their bits
+        if (lane == 0) largest_of[warp] = a;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) a = fmaxf(a, largest_of[i]);
+        return a;
+    };
+    float a = block_max();
+    if (!(a < __uint_as_float(0x7F800000u))) {                                        // the same for the whole CTA
+#pragma unroll
+        for (uint32_t i = 0; i < kLoads; ++i) only_finite(v[i]);
+        __syncthreads();
+        a = block_max();
+    }
+    const uint32_t e = scale_exponent(a, 127u);
+    const float inverse = pow2_inverse(e);
+#pragma unroll
+    for (uint32_t i = 0; i < kLoads; ++i) {
+        const uint32_t t = t0 + i * kRowsPerLoad;
+        if (t < P.T) store_values(P.q + int64_t(t) * P.ldq, c, P.C, P.vec, v[i], inverse);
+    }
+    if (threadIdx.x == 0) P.s[int64_t(rb) * P.lds + cb] = uint8_t(e);
+}
+
+template <class E>
+int launch_quantize(const QuantParams &P, uint32_t block_rows, cudaStream_t st) {
+    uint64_t grid;
+    if (block_rows == 1) {
+        const uint64_t span = 4u * 32u * (16u / sizeof(typename E::T));
+        grid = (uint64_t(P.T) * ((P.C + span - 1u) / span) + 3u) / 4u;
+    } else {
+        grid = uint64_t((P.T + kBlock - 1u) / kBlock) * P.blocks;
+    }
+    if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    const cudaError_t e = block_rows == 1 ? op_launch(quantize_rows_kernel<E>, uint32_t(grid), 128, 0, 1, st, P)
+                                          : op_launch(quantize_blocks_kernel<E>, uint32_t(grid), 256, 0, 1, st, P);
+    return e == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+}
+
+// ======================================================================================================================
+// y[t, r] = a[r] sum_k (sx[t, k / 128] xq[t, k]) (sw[r / 128, k / 128] wq[r, k])
+//
+// On the tensor cores as D = A B^T with A = 128 rows of the weight (so that a single token still fills the instruction's 128
+// lanes) and B = up to BN tokens: tcgen05.mma kind::mxf8f6f4 with one E8M0 scale for each row and 32 columns of both operands.
+// A block of 128 columns takes four instructions whose four scales are the same byte; four blocks' bytes make up the word
+// that tensor memory holds for a row, and the instruction's scale index picks the block's.  The products of two E4M3 numbers and the
+// scales are exact, sums are held in fp32 in tensor memory.
+// ======================================================================================================================
+struct MatmulParams {
+    const uint8_t *sx, *sw;       // sw may be null: ones
+    const float *a;               // may be null: ones
+    void *y;
+    int64_t ldsx, ldsw, ldy;
+    uint32_t T, R, blocks;        // blocks = ceil(C / 128)
+    uint32_t tiles_r;             // tiles of 128 rows of the weight; a grid walks them first
+    uint32_t split;               // CTAs (one cluster) that share a tile's columns
+};
+
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+// rows of 128 bytes, 128-byte swizzle, groups of eight rows 1024 bytes apart
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
+    return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+// 32 rows of 16 bytes without swizzle: eight rows, 128 bytes, are a unit
+__device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
+    return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
+}
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t addr) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scales_desc(addr)) : "memory");
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
+    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
+                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
+                 : "r"(tmem));
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+
+// E4M3 x E4M3, both K-major, E8M0 scales, M = 128, N = n; `word` = which byte of the scale words
+__host__ __device__ constexpr uint32_t scaled_idesc(uint32_t n, uint32_t word) {
+    return (word << 4) | ((n >> 3) << 17) | (1u << 23) | ((128u >> 4) << 24) | (word << 29);
+}
+
+// ---- one tile per CTA, its columns shared by a cluster --------------------------------------------------------------
+// Few tokens: the weight's bytes bound it, so every SM has to have some tens of KB of them in flight.  A cluster of up to
+// eight CTAs takes a tile of 128 rows, each a share of the columns; at the end the CTAs lay their fp32 tiles down in shared memory and
+// each adds up its share of the tokens over the cluster in rank order - no workspace, no atomics, the same bits every time.
+template <uint32_t BN>
+struct SplitShape {
+    static constexpr uint32_t kStages = BN <= 32 ? 5 : BN == 64 ? 4 : 3;
+    static constexpr uint32_t kA = kBlock * 128, kB = BN * 128, kStage = kA + kB;
+    static constexpr uint32_t kSlots = 4;                                             // scale words of four blocks each
+    static constexpr uint32_t kSlot = 512 + 512 * ((BN + 127) / 128);
+    static constexpr uint32_t kScales = kStages * kStage, kBars = kScales + kSlots * kSlot, kSmem = kBars + 256 + 1024;
+    static constexpr uint32_t kAcc = BN < 32 ? 32 : BN, kSlotCols = 4 + 4 * ((BN + 127) / 128);
+    static constexpr uint32_t kCols = kAcc + kSlots * kSlotCols <= 64 ? 64 : kAcc + kSlots * kSlotCols <= 128 ? 128 : 256;
+    static_assert(kAcc + kSlots * kSlotCols <= kCols && 128 * BN * 4 <= kScales);
+};
+
+template <uint32_t BN, class E>
+__global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant__ MatmulParams P, const __grid_constant__ CUtensorMap w_map,
+                                                           const __grid_constant__ CUtensorMap x_map) {
+    using G = SplitShape<BN>;
+    using T = typename E::T;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    const uint32_t full = base + G::kBars, empty = full + 8 * G::kStages, sfull = empty + 8 * G::kStages, sempty = sfull + 8 * G::kSlots,
+                   done = sempty + 8 * G::kSlots, slot_addr = done + 8, abort_word = slot_addr + 4;
+    if (tid == 0) {
+        for (uint32_t i = 0; i < G::kStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+        for (uint32_t i = 0; i < G::kSlots; ++i) bar_init(sfull + 8 * i, 64), bar_init(sempty + 8 * i, 1);
+        bar_init(done, 1);
+        st_smem(abort_word, 0);
+        bar_init_done();
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot_addr), "r"(G::kCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    tc_after();
+    op_wait_for_stream();
+    const uint32_t tmem = ld_smem(slot_addr), sf = tmem + G::kAcc;
+    const uint32_t tile = blockIdx.x / P.split, rank = blockIdx.x % P.split;
+    const uint32_t r0 = (tile % P.tiles_r) * kBlock, t0 = (tile / P.tiles_r) * BN;
+    const uint32_t kb0 = uint32_t(uint64_t(P.blocks) * rank / P.split), kb1 = uint32_t(uint64_t(P.blocks) * (rank + 1) / P.split), nk = kb1 - kb0;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            uint32_t k = 0;
+            for (; k < nk; ++k) {
+                const uint32_t s = k % G::kStages, at = base + s * G::kStage;
+                if (k >= G::kStages && !bar_wait(empty + 8 * s, (k / G::kStages - 1u) & 1u, abort_word)) break;
+                bar_expect(full + 8 * s, G::kStage);
+                tma_load_2d(at, &w_map, int32_t((kb0 + k) * 128u), int32_t(r0), full + 8 * s);
+                tma_load_2d(at + G::kA, &x_map, int32_t((kb0 + k) * 128u), int32_t(t0), full + 8 * s);
+            }
+            if (ld_smem(abort_word))                     // nothing may land after the CTA's end
+                for (uint32_t j = k > G::kStages ? k - G::kStages : 0; j < k; ++j) bar_drain(full + 8 * (j % G::kStages), (j / G::kStages) & 1u);
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            bool ok = true;
+            for (uint32_t k = 0; k < nk && ok; ++k) {
+                const uint32_t s = k % G::kStages, chunk = k / 4, slot = chunk % G::kSlots, sa = sf + slot * G::kSlotCols, sb = sa + 4;
+                if (k % 4 == 0) {
+                    ok = bar_wait(sfull + 8 * slot, (chunk / G::kSlots) & 1u, abort_word);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t at = base + G::kScales + slot * G::kSlot;
+                    copy_scales(sa, at);
+#pragma unroll
+                    for (uint32_t n = 0; n < (BN + 127) / 128; ++n) copy_scales(sb + 4 * n, at + 512 + 512 * n);
+                }
+                ok = bar_wait(full + 8 * s, (k / G::kStages) & 1u, abort_word);
+                if (!ok) break;
+                tc_after();
+                const uint64_t da = operand_desc(base + s * G::kStage), db = operand_desc(base + s * G::kStage + G::kA);
+                const uint32_t idesc = scaled_idesc(BN, k % 4);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) mma_scaled(tmem, da + 2 * i, db + 2 * i, idesc, sa, sb, (k | i) ? 1u : 0u);
+                tc_commit(empty + 8 * s);
+                if (k % 4 == 3) tc_commit(sempty + 8 * slot);
+            }
+            tc_commit(done);
+        }
+    } else {
+        // the scale words: byte i of a word is the scale of block 4 chunk + i; row r of 128 lies at 16 (r % 32) + 4 (r / 32)
+        const uint32_t l = tid - 64u;
+        for (uint32_t chunk = 0; 4 * chunk < nk; ++chunk) {
+            const uint32_t slot = chunk % G::kSlots, at = base + G::kScales + slot * G::kSlot, kb = kb0 + 4 * chunk, n = min(4u, nk - 4 * chunk);
+            if (chunk >= G::kSlots && !bar_wait(sempty + 8 * slot, (chunk / G::kSlots - 1u) & 1u, abort_word)) break;
+            uint32_t word = 0x7F7F7F7Fu;
+            if (P.sw) {
+                const uint8_t *p = P.sw + int64_t(r0 / kBlock) * P.ldsw + kb;
+                word = 0;
+                for (uint32_t i = 0; i < n; ++i) word |= uint32_t(__ldg(p + i)) << (8 * i);
+            }
+            for (uint32_t i = l; i < 128; i += 64) st_smem(at + 4 * i, word);
+            for (uint32_t t = l; t < (BN + 31u) / 32u * 32u; t += 64) {
+                uint32_t w = 0x7F7F7F7Fu;
+                if (t < BN && t0 + t < P.T) {
+                    const uint8_t *p = P.sx + int64_t(t0 + t) * P.ldsx + kb;
+                    w = 0;
+                    for (uint32_t i = 0; i < n; ++i) w |= uint32_t(__ldg(p + i)) << (8 * i);
+                }
+                st_smem(at + 512 + 512 * (t / 128) + 16 * (t % 32) + 4 * (t % 128 / 32), w);
+            }
+            fence_proxy_async();
+            bar_arrive(sfull + 8 * slot);
+        }
+    }
+    __syncwarp();
+    bar_wait(done, 0, abort_word);
+    if (ld_smem(abort_word)) bar_drain(done, 0);         // instructions in flight still read the stages
+    tc_after();
+
+    // lane = row of the weight, register = token
+    const uint32_t r = r0 + warp * 32u + lane;
+    const float a = P.a && r < P.R ? __ldg(P.a + r) : 1.0f;
+    T *y = static_cast<T *>(P.y) + r;
+    if (P.split == 1) {
+#pragma unroll
+        for (uint32_t c = 0; c < BN; c += 16) {
+            if (t0 + c >= P.T) break;
+            uint32_t v[16];
+            tc_load16(tmem + ((warp * 32u) << 16) + c, v);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i)
+                if (r < P.R && t0 + c + i < P.T) y[int64_t(t0 + c + i) * P.ldy] = E::of(__uint_as_float(v[i]) * a);
+        }
+    } else {
+        __syncthreads();                                 // (the stages are read no more: every thread has passed `done`)
+#pragma unroll
+        for (uint32_t c = 0; c < BN; c += 16) {
+            uint32_t v[16];
+            tc_load16(tmem + ((warp * 32u) << 16) + c, v);
+#pragma unroll
+            for (uint32_t i = 0; i < 16; ++i) st_smem(base + ((c + i) * 128u + tid) * 4u, v[i]);
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+        const uint32_t c0 = BN * rank / P.split, c1 = BN * (rank + 1) / P.split;
+        for (uint32_t c = c0; c < c1 && t0 + c < P.T; ++c) {
+            float sum = 0.0f;
+            for (uint32_t p = 0; p < P.split; ++p) {
+                uint32_t at, v;
+                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + (c * 128u + tid) * 4u), "r"(p));
+                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
+                sum += __uint_as_float(v);
+            }
+            if (r < P.R) y[int64_t(t0 + c) * P.ldy] = E::of(sum * a);
+        }
+        asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, 1u);
+    if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kCols) : "memory");
+}
+
+template <uint32_t BN, class E>
+int launch_split(MatmulParams P, const void *x, int64_t ldx, const void *w, int64_t ldw, uint32_t C, cudaStream_t st) {
+    using G = SplitShape<BN>;
+    static bool configured[64] = {};
+    int rc = op_configure(matmul_split_kernel<BN, E>, G::kSmem, configured);
+    if (rc) return rc;
+    const int sms = op_sms();
+    if (sms <= 0) return EP_ERR_CUDA;
+    CUtensorMap wm, xm;
+    if ((rc = byte_map(&wm, w, C, P.R, uint64_t(ldw), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+    if ((rc = byte_map(&xm, x, C, P.T, uint64_t(ldx), 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+    const uint64_t tiles = uint64_t(P.tiles_r) * ((P.T + BN - 1u) / BN);
+    // two CTAs fit an SM: as many as that allows share a tile, but none with fewer than two blocks of columns
+    P.split = 1;
+    while (P.split < 8 && tiles * P.split * 2 <= uint64_t(2 * sms) && P.split * 4 <= P.blocks) P.split *= 2;
+    if (tiles * P.split > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    return op_launch(matmul_split_kernel<BN, E>, uint32_t(tiles * P.split), 128, G::kSmem, P.split, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+}
+
+template <class E>
+int launch_matmul(const MatmulParams &P, const void *x, int64_t ldx, const void *w, int64_t ldw, uint32_t C, cudaStream_t st) {
+    if (P.T <= 16) return launch_split<16, E>(P, x, ldx, w, ldw, C, st);
+    if (P.T <= 32) return launch_split<32, E>(P, x, ldx, w, ldw, C, st);
+    if (P.T <= 64) return launch_split<64, E>(P, x, ldx, w, ldw, C, st);
+    return launch_split<128, E>(P, x, ldx, w, ldw, C, st);
+}
+
+bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+}  // namespace
+
+int ep::op8_status_matmul() {
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_matmul_status, sizeof(v)) != cudaSuccess) return -1;
+    if (v && cudaMemcpyToSymbol(g_matmul_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
+    return int(v);
+}
+
+extern "C" int ep_quantize_blocks(const void *d_x, int32_t x_dtype, uint32_t T, uint32_t C, int64_t ldx, uint32_t block_rows, void *d_q, int64_t ldq,
+                                  void *d_scales, int64_t lds, void *stream) {
+    if (T == 0) return EP_OK;
+    if (!d_x || !d_q || !d_scales || C == 0 || C > 0x7FFFFF00u || (block_rows != 1 && block_rows != kBlock)) return EP_ERR_BAD_ARG;
+    const uint32_t size = x_dtype == EP_FP32 ? 4 : x_dtype == EP_BF16 || x_dtype == EP_FP16 ? 2 : 0;
+    if (!size || !aligned(d_x, size)) return EP_ERR_BAD_ARG;
+    QuantParams P;
+    std::memset(&P, 0, sizeof(P));
+    P.blocks = (C + kBlock - 1u) / kBlock;
+    if (ldx < int64_t(C) || ldq < int64_t(C) || lds < int64_t(P.blocks)) return EP_ERR_BAD_ARG;
+    P.x = d_x;
+    P.q = static_cast<uint8_t *>(d_q);
+    P.s = static_cast<uint8_t *>(d_scales);
+    P.ldx = ldx;
+    P.ldq = ldq;
+    P.lds = lds;
+    P.T = T;
+    P.C = C;
+    P.vec = aligned(d_x, 16) && ldx * size % 16 == 0 && aligned(d_q, 8) && ldq % 8 == 0;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (x_dtype == EP_BF16) return launch_quantize<Bf16>(P, block_rows, st);
+    if (x_dtype == EP_FP16) return launch_quantize<Fp16>(P, block_rows, st);
+    return launch_quantize<Fp32>(P, block_rows, st);
+}
+
+extern "C" int ep_fp8_matmul(const void *d_x, int64_t ldx, const void *d_x_scales, int64_t ldsx, const void *d_w, int64_t ldw, const void *d_w_scales,
+                             int64_t ldsw, const float *d_row_scales, uint32_t T, uint32_t R, uint32_t C, int32_t out_dtype, void *d_y, int64_t ldy,
+                             void *stream) {
+    if (T == 0) return EP_OK;
+    if (!d_x || !d_x_scales || !d_w || !d_y || R == 0 || C == 0 || C > 0x7FFFFF00u || R > 0x7FFFFF00u || T > 0x7FFFFF00u) return EP_ERR_BAD_ARG;
+    const uint32_t size = out_dtype == EP_FP32 ? 4 : out_dtype == EP_BF16 || out_dtype == EP_FP16 ? 2 : 0;
+    const uint32_t blocks = (C + kBlock - 1u) / kBlock;
+    if (!size || !aligned(d_y, size) || (d_row_scales && !aligned(d_row_scales, 4)) || ldx < int64_t(C) || ldw < int64_t(C) || ldsx < int64_t(blocks) ||
+        (d_w_scales && ldsw < int64_t(blocks)) || ldy < int64_t(R))
+        return EP_ERR_BAD_ARG;
+    // the copy engine's rows begin on 16 bytes
+    if (C % 16 || ldx % 16 || ldw % 16 || !aligned(d_x, 16) || !aligned(d_w, 16) || ldx >= (int64_t(1) << 40) || ldw >= (int64_t(1) << 40)) return EP_ERR_UNSUPPORTED;
+    MatmulParams P;
+    std::memset(&P, 0, sizeof(P));
+    P.sx = static_cast<const uint8_t *>(d_x_scales);
+    P.sw = static_cast<const uint8_t *>(d_w_scales);
+    P.a = d_row_scales;
+    P.y = d_y;
+    P.ldsx = ldsx;
+    P.ldsw = ldsw;
+    P.ldy = ldy;
+    P.T = T;
+    P.R = R;
+    P.blocks = blocks;
+    P.tiles_r = (R + kBlock - 1u) / kBlock;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (out_dtype == EP_BF16) return launch_matmul<Bf16>(P, d_x, ldx, d_w, ldw, C, st);
+    if (out_dtype == EP_FP16) return launch_matmul<Fp16>(P, d_x, ldx, d_w, ldw, C, st);
+    return launch_matmul<Fp32>(P, d_x, ldx, d_w, ldw, C, st);
+}

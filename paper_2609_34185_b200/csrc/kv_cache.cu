@@ -1,0 +1,774 @@
+// Keys and values in pages of E4M3 with one scale for each page and head: writing new tokens, and the attention that
+// reads the pages.
+#include "op8.hpp"
+
+using namespace ep;
+
+namespace {
+
+__device__ unsigned int g_cache_status = 0;
+
+// What both operators read: where the requests' tokens stand.  Request b has seq_lens[b] tokens in the cache, the last
+// starts[b + 1] - starts[b] of which are its rows of the call; token j lies in page table[b][j / page], row j % page.
+struct Requests {
+    const int32_t *table, *seq_lens, *starts;
+    int64_t ldt;
+    uint32_t B, N, columns;       // requests; rows of the call; columns of the table
+    uint32_t pages, page, shift;  // pages of the cache, tokens of a page = 1 << shift
+    uint32_t H;                   // heads of the cache
+};
+// rows and tokens of request b; whatever the arrays hold, rows lie inside the call's and tokens inside the table
+struct Extent { uint32_t row, rows, len; };
+__device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
+    const uint32_t lo = uint32_t(min(max(__ldg(q.starts + b), 0), int32_t(q.N))), hi = uint32_t(min(max(__ldg(q.starts + b + 1), int32_t(lo)), int32_t(q.N)));
+    const uint64_t room = uint64_t(q.columns) << q.shift;
+    return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(__ldg(q.seq_lens + b), 0))), room))};
+}
+
+// ======================================================================================================================
+// Append.  For a page and head with scale s and older tokens q: s' = max(s, the smallest power of two that holds the new tokens), the
+// older tokens become e4m3(q s / s') if it grew, the new ones e4m3(x / s').  Powers of two: moving to a larger scale is exact but
+// for values that fall below E4M3's normal range, so a token is not rounded again each time its page's scale grows.  A page without
+// older tokens forgets what it held.  One warp (or CTA) per page, head and cache; a single new token that fits the scale costs one
+// read and write of its row.
+// ======================================================================================================================
+struct AppendParams {
+    Requests q;
+    const void *x[2];
+    int64_t ldx[2], ldh[2];
+    uint8_t *cache[2];
+    float *scales[2];
+    uint32_t D;
+    uint32_t spans;               // grid: spans pages side by side, x heads x 2 x requests
+};
+constexpr uint32_t kLeastScale = 127 - 100;      // of a page of zeros: 2^-100, which any value outgrows
+
+template <class E, uint32_t WARPS>
+__global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ AppendParams P) {
+    using T = typename E::T;
+    constexpr uint32_t kThreads = 32 * WARPS;
+    __shared__ float largest_of[4];
+    op_wait_for_stream();
+    const uint32_t tid = WARPS == 1 ? threadIdx.x & 31u : threadIdx.x, lane = tid & 31u;
+    const uint64_t unit = WARPS == 1 ? uint64_t(blockIdx.x) * 4u + (threadIdx.x >> 5) : blockIdx.x;
+    uint64_t rest = unit;
+    const uint32_t span = uint32_t(rest % P.spans); rest /= P.spans;
+    const uint32_t h = uint32_t(rest % P.q.H); rest /= P.q.H;
+    const uint32_t which = uint32_t(rest & 1u), b = uint32_t(rest >> 1);
+    if (b >= P.q.B) return;
+    const Extent r = extent_of(P.q, b);
+    const uint32_t rows = min(r.rows, r.len);             // (more rows than tokens: the first ones have no place)
+    if (rows == 0) return;
+    const uint32_t first = r.len - rows, lanes = P.D / 8u, at = tid % lanes * 8u, sub = tid / lanes, step = kThreads / lanes;
+    const T *x = static_cast<const T *>(P.x[which]) + int64_t(h) * P.ldh[which] + at;
+    for (uint32_t j = (first >> P.q.shift) + span; j <= (r.len - 1u) >> P.q.shift; j += P.spans) {
+        const int32_t id = __ldg(P.q.table + int64_t(b) * P.q.ldt + j);
+        if (id < 0 || uint32_t(id) >= P.q.pages) {
+            if (tid == 0) atomicOr(&g_cache_status, 2u);
+            continue;
+        }
+        const uint32_t p0 = j << P.q.shift, lo = max(first, p0), hi = min(r.len, p0 + P.q.page);        // new tokens of this page
+        const uint64_t block = uint64_t(uint32_t(id)) * P.q.H + h;
+        uint8_t *dst = P.cache[which] + (block << P.q.shift) * P.D + at;
+        auto row_of = [&](uint32_t pos) { return x + int64_t(r.row + (r.rows - rows) + pos - first) * P.ldx[which]; };
+        float a = 0.0f;
+        for (uint32_t pos = lo + sub; pos < hi; pos += step) {
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
+            const float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i)
+                if (fabsf(v[i]) < __uint_as_float(0x7F800000u)) a = fmaxf(a, fabsf(v[i]));
+        }
+        a = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a)));
+        if constexpr (WARPS > 1) {
+            if (lane == 0) largest_of[tid >> 5] = a;
+            __syncthreads();
+#pragma unroll
+            for (uint32_t i = 0; i < WARPS; ++i) a = fmaxf(a, largest_of[i]);
+            __syncthreads();
+        }
+        const float need = pow2_biased(max(scale_exponent(a, kLeastScale), kLeastScale));
+        float scale = need;
+        if (lo > p0) {                                    // older tokens
+            const float had = P.scales[which][block];
+            scale = fmaxf(need, had);
+            if (scale > had) {
+                const float ratio = __fdiv_rn(had, scale);
+                for (uint32_t i = sub; i < lo - p0; i += step) {
+                    uint2 w = *reinterpret_cast<uint2 *>(dst + i * P.D);
+                    auto moved = [&](uint32_t four) {
+                        uint32_t l, g;
+                        f16x4_of_e4m3x4(four, l, g);
+                        return e4m3x2(Fp16::lo(l) * ratio, Fp16::hi(l) * ratio) | e4m3x2(Fp16::lo(g) * ratio, Fp16::hi(g) * ratio) << 16;
+                    };
+                    w.x = moved(w.x), w.y = moved(w.y);
+                    *reinterpret_cast<uint2 *>(dst + i * P.D) = w;
+                }
+            }
+            if constexpr (WARPS > 1) __syncthreads();     // everyone has read the old scale
+            else __syncwarp();
+        }
+        for (uint32_t pos = lo + sub; pos < hi; pos += step) {
+            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
+            float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+#pragma unroll
+            for (uint32_t i = 0; i < 8; ++i) v[i] = fabsf(v[i]) < __uint_as_float(0x7F800000u) ? __fdiv_rn(v[i], scale) : __uint_as_float(0x7FFFFFFFu);
+            *reinterpret_cast<uint2 *>(dst + (pos - p0) * P.D) = make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+        }
+        if (tid == 0) P.scales[which][block] = scale;
+    }
+}
+
+// ======================================================================================================================
+// Attention.  o = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q . k_j - m), over the tokens that a row sees.
+//
+// A row is a query and one of the query heads that share a head of the cache; the rows of a request and head make tiles of 16 MT.
+// A tile of rows against all tokens of its request is a segment; a segment is cut into units of 256 tokens, the units of all segments form
+// one list, and every CTA takes an equal, contiguous share of it, whatever the requests' lengths (they are read on the device: a
+// captured launch serves any).  A CTA's eight warps take tiles of 32 tokens in turn, each with a running maximum and sum of its own and its own ring
+// of tiles brought in by the copy engine, so that nothing waits for another warp before the segment's end; there the warps' results
+// are joined in shared memory.  What crosses a CTA's share goes through the workspace: a CTA leaves at most two
+// pieces there, its first segment's and its last's, and a second launch joins them.
+//
+// Products are m16n8k16 with binary16 operands: E4M3 converts to binary16 exactly.  A row of q becomes binary16 times
+// a power of two that puts its largest magnitude at 2^13: exact for binary16 and bfloat16 alike but for elements 2^-27 and more
+// below the row's largest, whose rounding is below fp32's own.  The weights w carry a factor 2^14 (their largest, 2^14, is within binary16's range) so that
+// those down to 2^-28 of the largest keep 11 bits.  A page's value scale is moved onto w as v_scale / the largest so far.
+// ======================================================================================================================
+constexpr uint32_t kAttWarps = 8, kTile = 32, kUnit = kAttWarps * kTile, kMaxRequests = 4096;
+constexpr float kWeightShift = 14.0f;
+
+struct AttendParams {
+    Requests q;
+    const void *x;
+    void *o;
+    float *lse;                   // may be null
+    const float *ks, *vs;
+    int64_t ldq, ldqh, ldo, ldoh;
+    uint32_t Hq, G;               // query heads; per head of the cache
+    float scale_log2;             // scale * log2(e)
+    uint32_t causal;
+    float *workspace;             // null: no segment can cross a share
+    uint32_t grid;
+};
+
+// where a piece of a segment is left: O, then m and l of each row
+template <uint32_t MT, uint32_t D>
+constexpr uint32_t kPiece = 16 * MT * (D + 2);
+constexpr uint32_t kDescWords = 8;               // per CTA: the segment that it begins and does not end: request, row tile, head, last CTA + 1
+
+template <uint32_t MT, uint32_t D>
+struct AttendShape {
+    static constexpr uint32_t kTileBytes = kTile * D, kStage = 2 * kTileBytes;
+    static constexpr uint32_t kStages = D == 64 ? 6 : 3;
+    static constexpr uint32_t kRing = kStages * kStage;                                    // per warp
+    static constexpr uint32_t kMeta = kAttWarps * kRing;                                   // scales of the stages' pages: 2 x (key, value)
+    static constexpr uint32_t kBars = kMeta + kAttWarps * kStages * 16;
+    static constexpr uint32_t kJoin = kBars + kAttWarps * kStages * 8;                     // m, l, v scale of the warps' rows
+    static constexpr uint32_t kPrefix = kJoin + kAttWarps * 16 * MT * 16 + 16;
+    static constexpr uint32_t kSmem = kPrefix + 4 * (kMaxRequests + 32) + 1024;
+    static_assert(16 * MT * D * 4 <= kRing && kSmem <= 232448);
+};
+
+__device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float quad_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+    return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+}
+__device__ __forceinline__ float quad_sum(float v) {
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+    return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+}
+
+// prefix[b] = units of the requests before b; returns all
+__device__ __forceinline__ uint32_t units_of(const Extent &r, uint32_t G, uint32_t H, uint32_t rows_per_tile) {
+    const uint32_t tiles = (r.rows * G + rows_per_tile - 1u) / rows_per_tile;
+    return tiles * H * max(1u, (r.len + kUnit - 1u) / kUnit);
+}
+__device__ uint32_t prefix_units(const Requests &q, uint32_t G, uint32_t rows_per_tile, uint32_t *prefix, uint32_t *part) {
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, per = (q.B + blockDim.x - 1u) / blockDim.x;
+    const uint32_t b0 = min(tid * per, q.B), b1 = min(b0 + per, q.B);
+    uint32_t sum = 0;
+    for (uint32_t b = b0; b < b1; ++b) sum += units_of(extent_of(q, b), G, q.H, rows_per_tile);
+    uint32_t inc = sum;
+#pragma unroll
+    for (uint32_t d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) part[warp] = inc;
+    __syncthreads();
+    uint32_t at = inc - sum, all = 0;
+    for (uint32_t w = 0; w < (blockDim.x >> 5); ++w) {
+        if (w < warp) at += part[w];
+        all += part[w];
+    }
+    for (uint32_t b = b0; b < b1; ++b) {
+        prefix[b] = at;
+        at += units_of(extent_of(q, b), G, q.H, rows_per_tile);
+    }
+    if (tid == 0) prefix[q.B] = all;
+    __syncthreads();
+    return all;
+}
+
+template <class E, uint32_t MT, uint32_t D>
+__global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap k_map,
+                                                                   const __grid_constant__ CUtensorMap v_map) {
+    using S = AttendShape<MT, D>;
+    using T = typename E::T;
+    constexpr uint32_t kRows = 16 * MT, kSteps = D / 16, kPer = D / 4;       // k steps of q k^T; elements of a row that a lane of a quad holds
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    uint8_t *gen = raw + (base - smem_u32(raw));
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), quad = lane & 3u, oct = lane >> 2;
+    const uint32_t ring = base + warp * S::kRing, bars = base + S::kBars + warp * S::kStages * 8, meta = base + S::kMeta + warp * S::kStages * 16;
+    uint32_t *prefix = reinterpret_cast<uint32_t *>(gen + S::kPrefix);
+    float *join = reinterpret_cast<float *>(gen + S::kJoin);
+    const uint32_t abort_at = base + S::kPrefix - 16;
+    if (lane == 0) {
+        for (uint32_t i = 0; i < S::kStages; ++i) bar_init(bars + 8 * i, 3);
+        bar_init_done();
+    }
+    if (tid == 0) st_smem(abort_at, 0);
+    op_wait_for_stream();
+    const uint32_t all = prefix_units(P.q, P.G, kRows, prefix, reinterpret_cast<uint32_t *>(join));
+    const uint32_t ctas = min(P.grid, all);               // those with a share: none of theirs is empty
+    const uint32_t u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
+                   u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
+    uint32_t *desc = P.workspace ? reinterpret_cast<uint32_t *>(P.workspace) + blockIdx.x * kDescWords : nullptr;
+    float *pieces = P.workspace ? P.workspace + size_t(P.grid) * kDescWords + size_t(blockIdx.x) * 2u * kPiece<MT, D> : nullptr;
+    if (desc && tid == 0) desc[3] = 0;
+
+    uint32_t issued = 0, taken = 0;                       // tiles of this warp's ring
+    uint32_t b = 0;
+    for (uint32_t u = u_begin; u < u_end;) {
+        // ---- the segment of unit u ------------------------------------------------------------------------------------
+        {
+            uint32_t lo = b, hi = P.q.B;                  // the last request whose units begin at or before u
+            while (hi - lo > 1u) {
+                const uint32_t mid = (lo + hi) >> 1;
+                if (prefix[mid] <= u) lo = mid; else hi = mid;
+            }
+            b = lo;
+        }
+        const Extent r = extent_of(P.q, b);
+        const uint32_t per_seg = max(1u, (r.len + kUnit - 1u) / kUnit), seg = (u - prefix[b]) / per_seg, first_unit = (u - prefix[b]) % per_seg;
+        const uint32_t last_unit = min(per_seg, first_unit + (u_end - u));       // one past the share's last unit of the segment
+        const uint32_t h = seg % P.q.H, tile = seg / P.q.H;
+        const uint32_t n_rows = r.rows * P.G, row0 = tile * kRows;
+        const uint32_t t_begin = first_unit * kUnit, t_end = min(r.len, last_unit * kUnit);
+        const uint32_t n_tiles = t_end > t_begin + warp * kTile ? (t_end - t_begin - warp * kTile + kUnit - 1u) / kUnit : 0u;   // of this warp
+
+        // tile i of this warp begins at token t_begin + (i * 8 + warp) * 32
+        const int32_t *table = P.q.table + int64_t(b) * P.q.ldt;
+        const uint32_t per_tile = P.q.page < kTile ? 2u : 1u, box = P.q.page < kTile ? P.q.page : kTile;
+        auto page_of = [&](uint32_t i) {                  // lane 0 and 1: the page of the tile's first and second part, -1 if outside
+            const uint32_t t = t_begin + (i * kAttWarps + warp) * kTile + (lane & 1u) * box;
+            int32_t id = -1;
+            if (i < n_tiles && lane < per_tile && t < r.len) {
+                id = __ldg(table + (t >> P.q.shift));
+                if (id < 0 || uint32_t(id) >= P.q.pages) {
+                    atomicOr(&g_cache_status, 2u);
+                    id = -1;
+                }
+            }
+            return id;
+        };
+        auto issue = [&](uint32_t i, int32_t id) {
+            const uint32_t s = issued % S::kStages, bar = bars + 8 * s, at = ring + s * S::kStage;
+            if (lane == 0) bar_expect(bar, S::kStage);
+            __syncwarp();
+            if (lane < per_tile) {
+                // (a part without a page: rows past the cache's end, which arrive as zeros)
+                const uint32_t row = id < 0 ? P.q.pages * P.q.H << P.q.shift : ((uint32_t(id) * P.q.H + h) << P.q.shift) + ((t_begin + (i * kAttWarps + warp) * kTile) & (P.q.page - 1u));
+                tma_load_2d(at + lane * box * D, &k_map, 0, int32_t(row), bar);
+                tma_load_2d(at + S::kTileBytes + lane * box * D, &v_map, 0, int32_t(row), bar);
+            }
+            if (lane < 2) {
+                const uint32_t m = meta + s * 16 + lane * 8;
+                const int32_t first = __shfl_sync(0x3u, id, 0), mine = per_tile == 2 ? id : first;
+                if (mine >= 0) {
+                    const size_t block = size_t(uint32_t(mine)) * P.q.H + h;
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(m), "l"(P.ks + block) : "memory");
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(m + 4), "l"(P.vs + block) : "memory");
+                } else {
+                    st_smem(m, 0xBF800000u);              // -1: left out
+                    st_smem(m + 4, 0);
+                }
+                asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
+            }
+            __syncwarp();
+            ++issued;
+        };
+        int32_t next_page = page_of(0);
+        uint32_t asked = 0;
+        for (; asked < min(n_tiles, S::kStages); ++asked) {
+            const int32_t id = next_page;
+            next_page = page_of(asked + 1);
+            issue(asked, id);
+        }
+
+        // ---- rows of q as operands -----------------------------------------------------------------------------------
+        uint32_t qa[MT][kSteps][4];
+        float fac[MT][2];                                 // of a row's scores, without the keys' scale
+        uint32_t lim[MT][2];                              // tokens that a row sees
+        uint32_t lim_min = 0xFFFFFFFFu, lim_max = 0;
+#pragma unroll
+        for (uint32_t mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+                const uint32_t row = row0 + mt * 16 + half * 8 + oct, i = row / P.G, g = row % P.G;
+                const bool real = row < n_rows;
+                uint32_t w[kPer / 2];
+                const T *src = static_cast<const T *>(P.x) + int64_t(r.row + i) * P.ldq + int64_t(h * P.G + g) * P.ldqh + quad * kPer;
+#pragma unroll
+                for (uint32_t c = 0; c < kPer / 8; ++c) {
+                    const uint4 v = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
+                    w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
+                }
+                float a = 0.0f;
+#pragma unroll
+                for (uint32_t c = 0; c < kPer / 2; ++c) a = fmaxf(a, fmaxf(fabsf(E::lo(w[c])), fabsf(E::hi(w[c]))));
+                a = quad_max(a);
+                // 2^up puts the row's largest magnitude in [2^13, 2^14); a row of zeros or with an infinity stays as it is
+                const int32_t ea = int32_t(__float_as_uint(a) >> 23);
+                const int32_t up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
+                const float mul = pow2_biased(uint32_t(127 + up));
+                fac[mt][half] = P.scale_log2 * pow2_biased(uint32_t(127 - up));
+#pragma unroll
+                for (uint32_t st = 0; st < kSteps; ++st) {
+                    qa[mt][st][half] = Fp16::two(E::lo(w[2 * st]) * mul, E::hi(w[2 * st]) * mul);
+                    qa[mt][st][2 + half] = Fp16::two(E::lo(w[2 * st + 1]) * mul, E::hi(w[2 * st + 1]) * mul);
+                }
+                // query i of n sees tokens 0 .. len - n + i
+                const uint32_t sees = !real ? 0u : !P.causal ? r.len : r.len + i + 1u > r.rows ? min(r.len, r.len + i + 1u - r.rows) : 0u;
+                lim[mt][half] = sees;
+                lim_max = max(lim_max, sees);
+                lim_min = min(lim_min, real ? sees : 0xFFFFFFFFu);
+            }
+        lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
+        lim_max = __reduce_max_sync(0xFFFFFFFFu, lim_max);
+
+        float o[MT][D / 8][4], m[MT][2], l[MT][2], vref = 1e-37f;
+#pragma unroll
+        for (uint32_t mt = 0; mt < MT; ++mt) {
+            m[mt][0] = m[mt][1] = -INFINITY, l[mt][0] = l[mt][1] = 0.0f;
+#pragma unroll
+            for (uint32_t d = 0; d < D / 8; ++d) o[mt][d][0] = o[mt][d][1] = o[mt][d][2] = o[mt][d][3] = 0.0f;
+        }
+
+        for (uint32_t i = 0; i < n_tiles; ++i) {
+            const uint32_t s = taken % S::kStages, at = ring + s * S::kStage, t0 = t_begin + (i * kAttWarps + warp) * kTile;
+            const bool ok = bar_wait(bars + 8 * s, (taken / S::kStages) & 1u, abort_at);
+            ++taken;
+            if (__all_sync(0xFFFFFFFFu, ok) && t0 < lim_max) {
+                // ---- scores: n tile n holds tokens t0 + 8 n .. + 7 ---------------------------------------------------------
+                float sc[MT][4][4];
+#pragma unroll
+                for (uint32_t n = 0; n < 4; ++n) {
+                    const uint32_t row = n * 8 + oct;
+                    uint32_t kw[kPer / 4];
+#pragma unroll
+                    for (uint32_t c = 0; c < kPer / 16; ++c) {
+                        // 16-byte pieces of a row lie swizzled: of 128 bytes by the row's number mod 8, of 64 by half of it mod 4
+                        const uint32_t piece = quad * (kPer / 16) + c, sw = D == 128 ? piece ^ (row & 7u) : piece ^ ((row >> 1) & 3u);
+                        const uint4 v = ld_smem16(at + row * D + 16 * sw);
+                        kw[4 * c] = v.x, kw[4 * c + 1] = v.y, kw[4 * c + 2] = v.z, kw[4 * c + 3] = v.w;
+                    }
+#pragma unroll
+                    for (uint32_t mt = 0; mt < MT; ++mt) sc[mt][n][0] = sc[mt][n][1] = sc[mt][n][2] = sc[mt][n][3] = 0.0f;
+#pragma unroll
+                    for (uint32_t st = 0; st < kSteps; ++st) {
+                        uint32_t b0, b1;
+                        f16x4_of_e4m3x4(kw[st], b0, b1);
+#pragma unroll
+                        for (uint32_t mt = 0; mt < MT; ++mt) mma16816(sc[mt][n], qa[mt][st][0], qa[mt][st][1], qa[mt][st][2], qa[mt][st][3], b0, b1);
+                    }
+                }
+                float ks[2], vs[2];
+#pragma unroll
+                for (uint32_t p = 0; p < 2; ++p) {
+                    ks[p] = __uint_as_float(ld_smem(meta + s * 16 + 8 * p));
+                    vs[p] = __uint_as_float(ld_smem(meta + s * 16 + 8 * p + 4));
+                }
+                // ---- masks, running maximum, weights -----------------------------------------------------------------------
+                const bool edge = t0 + kTile > lim_min || ks[0] < 0.0f || ks[1] < 0.0f;
+                const float vnew = fmaxf(vref, fmaxf(vs[0], vs[1])), vmove = __fdiv_rn(vref, vnew);
+                const float vr[2] = {__fdiv_rn(vs[0], vnew), __fdiv_rn(vs[1], vnew)};
+                vref = vnew;
+                uint32_t pa[MT][2][4];
+#pragma unroll
+                for (uint32_t mt = 0; mt < MT; ++mt) {
+                    float top[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+                    for (uint32_t n = 0; n < 4; ++n)
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c) {
+                            const uint32_t half = c >> 1, t = t0 + n * 8 + quad * 2 + (c & 1u);
+                            float v = sc[mt][n][c] * (fac[mt][half] * ks[n >> 1]);
+                            if (edge && (t >= lim[mt][half] || ks[n >> 1] < 0.0f)) v = -INFINITY;
+                            sc[mt][n][c] = v;
+                            top[half] = fmaxf(top[half], v);
+                        }
+                    float alpha[2], sub[2];
+#pragma unroll
+                    for (uint32_t half = 0; half < 2; ++half) {
+                        const float now = fmaxf(m[mt][half], quad_max(top[half]));
+                        sub[half] = now == -INFINITY ? 0.0f : now - kWeightShift;        // no token yet: weights of 0
+                        alpha[half] = exp2_fast(m[mt][half] - (now == -INFINITY ? 0.0f : now));
+                        m[mt][half] = now;
+                        l[mt][half] *= alpha[half];
+                        alpha[half] *= vmove;
+                    }
+#pragma unroll
+                    for (uint32_t d = 0; d < D / 8; ++d) {
+                        o[mt][d][0] *= alpha[0], o[mt][d][1] *= alpha[0];
+                        o[mt][d][2] *= alpha[1], o[mt][d][3] *= alpha[1];
+                    }
+#pragma unroll
+                    for (uint32_t n = 0; n < 4; ++n) {
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c) {
+                            sc[mt][n][c] = exp2_fast(sc[mt][n][c] - sub[c >> 1]);
+                            l[mt][c >> 1] += sc[mt][n][c];
+                        }
+                        pa[mt][n >> 1][(n & 1u) * 2] = Fp16::two(sc[mt][n][0] * vr[n >> 1], sc[mt][n][1] * vr[n >> 1]);
+                        pa[mt][n >> 1][(n & 1u) * 2 + 1] = Fp16::two(sc[mt][n][2] * vr[n >> 1], sc[mt][n][3] * vr[n >> 1]);
+                    }
+                }
+                // ---- o += w v: k step st holds tokens t0 + 16 st .. + 15; a lane's columns are D / 8 oct .. + D / 8 - 1 ---------
+#pragma unroll
+                for (uint32_t st = 0; st < 2; ++st) {
+                    constexpr uint32_t kCols = D / 8;                                    // bytes of a row that a lane takes
+                    uint32_t vw[4][kCols / 4];
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) {
+                        const uint32_t row = st * 16 + quad * 2 + (j & 1u) + (j >> 1) * 8;
+                        if constexpr (D == 128) {
+                            const uint4 v = ld_smem16(at + S::kTileBytes + row * D + 16 * (oct ^ (row & 7u)));
+                            vw[j][0] = v.x, vw[j][1] = v.y, vw[j][2] = v.z, vw[j][3] = v.w;
+                        } else {
+                            const uint32_t a = at + S::kTileBytes + row * D + 16 * ((oct >> 1) ^ ((row >> 1) & 3u)) + 8 * (oct & 1u);
+                            asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[j][0]), "=r"(vw[j][1]) : "r"(a));
+                        }
+                        // a token past the request's end may hold anything, NaN included
+                        if (edge && t0 + row >= r.len)
+#pragma unroll
+                            for (uint32_t c = 0; c < kCols / 4; ++c) vw[j][c] = 0;
+                    }
+                    // a NaN counts for the rows that see its token and no others (0 * NaN is NaN): where some do not see it, it is
+                    // multiplied by who does, apart from the values
+                    uint32_t nan = 0;
+                    if (edge)
+#pragma unroll
+                        for (uint32_t j = 0; j < 4; ++j)
+#pragma unroll
+                            for (uint32_t c = 0; c < kCols / 4; ++c) nan |= __vcmpeq4(vw[j][c] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                    if (edge && __any_sync(0xFFFFFFFFu, nan != 0)) {
+                        uint32_t see[MT][4];
+#pragma unroll
+                        for (uint32_t mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e) {
+                                const uint32_t t = t0 + st * 16 + (e >> 1) * 8 + quad * 2, end = lim[mt][e & 1u];
+                                see[mt][e] = (t < end ? 0x3C00u : 0u) | (t + 1u < end ? 0x3C000000u : 0u);      // 1.0 twice
+                            }
+#pragma unroll
+                        for (uint32_t c = 0; c < kCols / 4; ++c) {
+                            uint32_t is[4];
+#pragma unroll
+                            for (uint32_t j = 0; j < 4; ++j) {
+                                is[j] = __vcmpeq4(vw[j][c] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
+                                vw[j][c] &= ~is[j];
+                                is[j] &= 0x38383838u;                                    // 1.0 in E4M3
+                            }
+                            uint32_t b0[4], b1[4];
+                            f16x4_of_e4m3x4(__byte_perm(is[0], is[1], 0x5140), b0[0], b0[1]);
+                            f16x4_of_e4m3x4(__byte_perm(is[0], is[1], 0x7362), b0[2], b0[3]);
+                            f16x4_of_e4m3x4(__byte_perm(is[2], is[3], 0x5140), b1[0], b1[1]);
+                            f16x4_of_e4m3x4(__byte_perm(is[2], is[3], 0x7362), b1[2], b1[3]);
+#pragma unroll
+                            for (uint32_t mt = 0; mt < MT; ++mt)
+#pragma unroll
+                                for (uint32_t e = 0; e < 4; ++e) {
+                                    float seen[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+                                    mma16816(seen, see[mt][0], see[mt][1], see[mt][2], see[mt][3], b0[e], b1[e]);
+#pragma unroll
+                                    for (uint32_t k = 0; k < 4; ++k)
+                                        if (seen[k] > 0.0f) o[mt][4 * c + e][k] = __uint_as_float(0x7FFFFFFFu);
+                                }
+                        }
+                    }
+#pragma unroll
+                    for (uint32_t c = 0; c < kCols / 4; ++c) {
+                        // bytes of two tokens side by side: columns 4 c, 4 c + 1 in the low word, 4 c + 2, 4 c + 3 in the high one
+                        const uint32_t lo0 = __byte_perm(vw[0][c], vw[1][c], 0x5140), hi0 = __byte_perm(vw[0][c], vw[1][c], 0x7362);
+                        const uint32_t lo1 = __byte_perm(vw[2][c], vw[3][c], 0x5140), hi1 = __byte_perm(vw[2][c], vw[3][c], 0x7362);
+                        uint32_t b0[4], b1[4];
+                        f16x4_of_e4m3x4(lo0, b0[0], b0[1]);
+                        f16x4_of_e4m3x4(hi0, b0[2], b0[3]);
+                        f16x4_of_e4m3x4(lo1, b1[0], b1[1]);
+                        f16x4_of_e4m3x4(hi1, b1[2], b1[3]);
+#pragma unroll
+                        for (uint32_t mt = 0; mt < MT; ++mt)
+#pragma unroll
+                            for (uint32_t e = 0; e < 4; ++e)
+                                mma16816(o[mt][4 * c + e], pa[mt][st][0], pa[mt][st][1], pa[mt][st][2], pa[mt][st][3], b0[e], b1[e]);
+                    }
+                }
+            }
+            __syncwarp();                                 // the stage has been read
+            if (asked < n_tiles) {
+                const int32_t id = next_page;
+                next_page = page_of(asked + 1);
+                issue(asked, id);
+                ++asked;
+            }
+        }
+
+        // ---- the warps' results, joined ------------------------------------------------------------------------------------
+        // (this warp's ring is empty: every tile asked for has been taken)
+        float *mine = reinterpret_cast<float *>(gen + warp * S::kRing);
+#pragma unroll
+        for (uint32_t mt = 0; mt < MT; ++mt)
+#pragma unroll
+            for (uint32_t half = 0; half < 2; ++half) {
+                const uint32_t row = mt * 16 + half * 8 + oct;
+                const float sum = quad_sum(l[mt][half]);
+                if (quad == 0) *reinterpret_cast<float4 *>(join + (warp * kRows + row) * 4) = make_float4(m[mt][half], sum, vref, 0.0f);
+#pragma unroll
+                for (uint32_t d = 0; d < D / 8; ++d)
+                    // accumulator columns 2 quad, 2 quad + 1 of n tile d are columns (D / 8) (2 quad) + d and (D / 8) (2 quad + 1) + d
+#pragma unroll
+                    for (uint32_t e = 0; e < 2; ++e) mine[row * D + (D / 8) * (2 * quad + e) + d] = o[mt][d][2 * half + e];
+            }
+        __syncthreads();
+        const bool whole = first_unit == 0 && last_unit == per_seg;
+        for (uint32_t e = tid; e < kRows * D; e += 32 * kAttWarps) {
+            const uint32_t row = e / D, d = e % D;
+            float top = -INFINITY;
+#pragma unroll
+            for (uint32_t w = 0; w < kAttWarps; ++w) top = fmaxf(top, join[(w * kRows + row) * 4]);
+            const float ref = top == -INFINITY ? 0.0f : top;
+            float sum = 0.0f, acc = 0.0f;
+#pragma unroll
+            for (uint32_t w = 0; w < kAttWarps; ++w) {
+                const float4 j = *reinterpret_cast<const float4 *>(join + (w * kRows + row) * 4);
+                const float f = exp2_fast(j.x - ref);
+                sum += f * j.y;
+                acc += f * j.z * *reinterpret_cast<const float *>(gen + w * S::kRing + (row * D + d) * 4);
+            }
+            if (whole) {
+                const uint32_t at = row0 + row, i = at / P.G, g = at % P.G;
+                if (at < n_rows) {
+                    const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+                    static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+                    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
+                }
+            } else {
+                float *piece = pieces + (u == u_begin ? 0u : kPiece<MT, D>);
+                piece[row * D + d] = acc;
+                if (d == 0) piece[kRows * D + row] = top, piece[kRows * D + kRows + row] = sum;
+            }
+        }
+        if (!whole && first_unit == 0 && tid == 0) {      // this CTA begins the segment: the second launch joins it from here
+            const uint32_t end = prefix[b] + (seg + 1u) * per_seg;                       // the segment's end in the list
+            uint32_t cta = uint32_t(uint64_t(end - 1u) * ctas / all);                    // the CTA that has its last unit
+            while (uint64_t(all) * (cta + 1u) / ctas < end) ++cta;
+            while (uint64_t(all) * cta / ctas >= end) --cta;
+            desc[0] = b, desc[1] = tile, desc[2] = h, desc[3] = cta + 1u, desc[4] = u == u_begin ? 0u : 1u;
+        }
+        // the rings are written by the copy engine next: the reads and writes above come first
+        fence_proxy_async();
+        __syncthreads();
+        u += last_unit - first_unit;
+    }
+    if (tid == 0 && ld_smem(abort_at)) atomicOr(&g_cache_status, 1u);
+    if (ld_smem(abort_at) && lane == 0)                   // (a wait ran out: what is still under way gets its time)
+        for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0u; j < issued; ++j) bar_drain(bars + 8 * (j % S::kStages), (j / S::kStages) & 1u);
+}
+
+// The segments that cross a share: CTA k takes the one that CTA k of the first launch began.  Its pieces are the first ones of the
+// CTAs after it, in order.
+template <class E, uint32_t MT, uint32_t D>
+__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttendParams P) {
+    using T = typename E::T;
+    constexpr uint32_t kRows = 16 * MT;
+    op_wait_for_stream();
+    const uint32_t *desc = reinterpret_cast<const uint32_t *>(P.workspace) + blockIdx.x * kDescWords;
+    const uint32_t end = desc[3];
+    if (end == 0) return;
+    const uint32_t b = desc[0], tile = desc[1], h = desc[2];
+    const Extent r = extent_of(P.q, b);
+    const float *all = P.workspace + size_t(P.grid) * kDescWords;
+    const float *own = all + (size_t(blockIdx.x) * 2u + desc[4]) * kPiece<MT, D>;
+    for (uint32_t e = threadIdx.x; e < kRows * D; e += blockDim.x) {
+        const uint32_t row = e / D, d = e % D, at = tile * kRows + row, i = at / P.G, g = at % P.G;
+        if (at >= r.rows * P.G) break;
+        float top = own[kRows * D + row], sum = own[kRows * D + kRows + row], acc = own[row * D + d];
+        for (uint32_t c = blockIdx.x + 1u; c < end; ++c) {
+            const float *p = all + size_t(c) * 2u * kPiece<MT, D>;
+            const float m = p[kRows * D + row], now = fmaxf(top, m), ref = now == -INFINITY ? 0.0f : now;
+            const float f = exp2_fast(top - ref), g2 = exp2_fast(m - ref);
+            sum = sum * f + p[kRows * D + kRows + row] * g2;
+            acc = acc * f + p[row * D + d] * g2;
+            top = now;
+        }
+        const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+        static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+        if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
+bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+// what both entry points check of the cache and the requests; fills q
+int check_cache(const ep_cache *c, const int32_t *table, int64_t ldt, uint32_t columns, const int32_t *seq_lens, const int32_t *starts, uint32_t B, uint32_t N,
+                Requests &q) {
+    if (!c || !c->d_k || !c->d_v || !c->d_k_scales || !c->d_v_scales || !table || !seq_lens || !starts) return EP_ERR_BAD_ARG;
+    if (c->pages == 0 || c->heads == 0 || columns == 0 || ldt < int64_t(columns) || N > 0x7FFFFFFFu) return EP_ERR_BAD_ARG;
+    if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !aligned(c->d_k_scales, 4) || !aligned(c->d_v_scales, 4) || !aligned(table, 4) || !aligned(seq_lens, 4) ||
+        !aligned(starts, 4))
+        return EP_ERR_BAD_ARG;
+    if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1u)) || (c->dim != 64 && c->dim != 128)) return EP_ERR_UNSUPPORTED;
+    if (c->pages >= (1u << 27) || c->heads >= (1u << 16) || uint64_t(c->pages) * c->heads * c->page >= (1ull << 31) - 256u || uint64_t(columns) * c->page >= (1ull << 31))
+        return EP_ERR_UNSUPPORTED;
+    q.table = table;
+    q.seq_lens = seq_lens;
+    q.starts = starts;
+    q.ldt = ldt;
+    q.B = B;
+    q.N = N;
+    q.columns = columns;
+    q.pages = c->pages;
+    q.page = c->page;
+    q.shift = 0;
+    while ((1u << q.shift) < c->page) ++q.shift;
+    q.H = c->heads;
+    return EP_OK;
+}
+
+template <class E>
+int launch_append(const AppendParams &P, cudaStream_t st) {
+    // many tokens per request: a CTA for each page and head, else a warp
+    const uint64_t units = uint64_t(P.spans) * P.q.H * 2u * P.q.B;
+    const bool wide = P.q.N >= 8ull * P.q.B;
+    const uint64_t grid = wide ? units : (units + 3u) / 4u;
+    if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    const cudaError_t e = wide ? op_launch(append_kernel<E, 4>, uint32_t(grid), 128, 0, 1, st, P) : op_launch(append_kernel<E, 1>, uint32_t(grid), 128, 0, 1, st, P);
+    return e == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+}
+
+uint32_t row_tiles_per_cta(uint32_t N, uint32_t G, uint32_t B) { return uint64_t(N) * G > 16ull * B ? 2u : 1u; }
+
+template <class E, uint32_t MT, uint32_t D>
+int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
+    using S = AttendShape<MT, D>;
+    static bool configured[64] = {};
+    int rc = op_configure(attend_kernel<E, MT, D>, S::kSmem, configured);
+    if (rc) return rc;
+    CUtensorMap km, vm;
+    const uint64_t rows = uint64_t(c.pages) * c.heads * c.page;
+    const CUtensorMapSwizzle sw = D == 128 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_64B;
+    const uint32_t box = c.page < kTile ? c.page : kTile;
+    if ((rc = byte_map(&km, c.d_k, D, rows, D, D, box, sw)) || (rc = byte_map(&vm, c.d_v, D, rows, D, D, box, sw))) return rc;
+    const bool joined = uint64_t(P.q.columns) * c.page > kUnit;             // else a segment is one unit and crosses no share
+    if (joined) {
+        const size_t need = size_t(P.grid) * (kDescWords + 2u * kPiece<MT, D>) * 4u;
+        if (!P.workspace || workspace_bytes < need || !aligned(P.workspace, 16)) return EP_ERR_SCRATCH;
+    } else {
+        P.workspace = nullptr;
+    }
+    if (op_launch(attend_kernel<E, MT, D>, P.grid, 32 * kAttWarps, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
+    if (joined && op_launch(join_kernel<E, MT, D>, P.grid, 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    return EP_OK;
+}
+
+template <class E>
+int launch_attend(const AttendParams &P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
+    if (row_tiles_per_cta(P.q.N, P.G, P.q.B) == 1)
+        return c.dim == 64 ? launch_attend<E, 1, 64>(P, c, workspace_bytes, st) : launch_attend<E, 1, 128>(P, c, workspace_bytes, st);
+    return c.dim == 64 ? launch_attend<E, 2, 64>(P, c, workspace_bytes, st) : launch_attend<E, 2, 128>(P, c, workspace_bytes, st);
+}
+
+}  // namespace
+
+int ep::op8_status_cache() {
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, g_cache_status, sizeof(v)) != cudaSuccess) return -1;
+    if (v && cudaMemcpyToSymbol(g_cache_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
+    return int(v);
+}
+
+extern "C" int ep_cache_append(const ep_cache *cache, const void *d_k, int64_t ldk, int64_t ldk_head, const void *d_v, int64_t ldv, int64_t ldv_head,
+                               int32_t dtype, const int32_t *d_table, int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B,
+                               uint32_t N, void *stream) {
+    if (B == 0 || N == 0) return EP_OK;
+    AppendParams P;
+    std::memset(&P, 0, sizeof(P));
+    const int rc = check_cache(cache, d_table, ldt, columns, d_seq_lens, d_starts, B, N, P.q);
+    if (rc) return rc;
+    if (!d_k || !d_v || (dtype != EP_BF16 && dtype != EP_FP16)) return EP_ERR_BAD_ARG;
+    if (!aligned(d_k, 16) || !aligned(d_v, 16) || ldk % 8 || ldk_head % 8 || ldv % 8 || ldv_head % 8) return EP_ERR_UNSUPPORTED;
+    P.x[0] = d_k, P.x[1] = d_v;
+    P.ldx[0] = ldk, P.ldx[1] = ldv;
+    P.ldh[0] = ldk_head, P.ldh[1] = ldv_head;
+    P.cache[0] = static_cast<uint8_t *>(cache->d_k), P.cache[1] = static_cast<uint8_t *>(cache->d_v);
+    P.scales[0] = cache->d_k_scales, P.scales[1] = cache->d_v_scales;
+    P.D = cache->dim;
+    // as many pages side by side as a request of average length touches; a longer one's take turns
+    const uint64_t average = (uint64_t(N) + B - 1u) / B;
+    P.spans = uint32_t(average > 1 ? (average - 1u) / cache->page + 2u : 1u);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == EP_BF16 ? launch_append<Bf16>(P, st) : launch_append<Fp16>(P, st);
+}
+
+extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim) {
+    const int sms = op_sms();
+    if (sms <= 0 || heads == 0 || B == 0) return 0;
+    const uint32_t rows = 16u * row_tiles_per_cta(N, q_heads / heads, B);
+    return size_t(sms) * (kDescWords + 2u * rows * (size_t(dim) + 2u)) * 4u;
+}
+
+extern "C" int ep_cache_attention(const ep_cache *cache, const void *d_q, int64_t ldq, int64_t ldq_head, int32_t dtype, uint32_t q_heads, const int32_t *d_table,
+                                  int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B, uint32_t N, float scale,
+                                  int32_t causal, void *d_o, int64_t ldo, int64_t ldo_head, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream) {
+    if (B == 0 || N == 0) return EP_OK;
+    AttendParams P;
+    std::memset(&P, 0, sizeof(P));
+    int rc = check_cache(cache, d_table, ldt, columns, d_seq_lens, d_starts, B, N, P.q);
+    if (rc) return rc;
+    if (!d_q || !d_o || (dtype != EP_BF16 && dtype != EP_FP16) || q_heads == 0 || q_heads % cache->heads || (d_lse && !aligned(d_lse, 4))) return EP_ERR_BAD_ARG;
+    if (!aligned(d_q, 16) || ldq % 8 || ldq_head % 8 || !aligned(d_o, 16) || ldo % 8 || ldo_head % 8 || B > kMaxRequests) return EP_ERR_UNSUPPORTED;
+    P.x = d_q;
+    P.o = d_o;
+    P.lse = d_lse;
+    P.ks = cache->d_k_scales;
+    P.vs = cache->d_v_scales;
+    P.ldq = ldq;
+    P.ldqh = ldq_head;
+    P.ldo = ldo;
+    P.ldoh = ldo_head;
+    P.Hq = q_heads;
+    P.G = q_heads / cache->heads;
+    P.scale_log2 = scale * 1.4426950408889634f;
+    P.causal = causal ? 1u : 0u;
+    P.workspace = static_cast<float *>(d_workspace);
+    // units are counted in 32 bits
+    const uint64_t rows = 16u * row_tiles_per_cta(N, P.G, B), units = ((uint64_t(columns) * cache->page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * cache->heads;
+    if (units >= (1ull << 31) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
+    const int sms = op_sms();
+    if (sms <= 0) return EP_ERR_CUDA;
+    P.grid = uint32_t(sms);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    return dtype == EP_BF16 ? launch_attend<Bf16>(P, *cache, workspace_bytes, st) : launch_attend<Fp16>(P, *cache, workspace_bytes, st);
+}
