@@ -294,27 +294,36 @@ int ep_decode_gemm(const ep_info *info, const void *d_stream, const void *d_tile
 
 /* q[i, j] = e4m3(x[i, j] / s), round to nearest even, one scale s per block of block_rows x 128 (block_rows 1: activations,
  * 128: weights; blocks at the edges are smaller).  What is not finite becomes NaN and has no part in the scale; a block without
- * a finite value but 0 has s = 1.
- *   d_x       device, T x C of x_dtype (EP_BF16, EP_FP16, EP_FP32), any leading dimension >= C; aligned to its element
- *             (rows that begin on 16 bytes are read fastest)
- *   d_q       device, T x C E4M3 values, ldq >= C
- *   d_scales  device, ceil(T / block_rows) x ceil(C / 128) E8M0 bytes (the scale is 2^(byte - 127)), lds >= ceil(C / 128) */
-int ep_quantize_blocks(const void *d_x, int32_t x_dtype, uint32_t T, uint32_t C, int64_t ldx, uint32_t block_rows, void *d_q,
-                       int64_t ldq, void *d_scales, int64_t lds, void *stream);
+ * a finite value but 0 has s = 1. */
+typedef struct {
+    const void *d_x;            /* device: T x C of x_dtype, any leading dimension >= C; aligned to its element (rows that begin on
+                                   16 bytes are read fastest) */
+    void *d_q;                  /* device: T x C E4M3 values, ldq >= C */
+    void *d_scales;             /* device: ceil(T / block_rows) x ceil(C / 128) E8M0 bytes (the scale is 2^(byte - 127)), lds >= ceil(C / 128) */
+    int64_t ldx, ldq, lds;
+    uint32_t T, C;
+    uint32_t block_rows;        /* 1 or 128 */
+    int32_t x_dtype;            /* EP_BF16, EP_FP16 or EP_FP32 */
+} ep_quantize_job;
+int ep_quantize_blocks(const ep_quantize_job *job, void *stream);
 
 /* y[t, r] = a[r] * sum_k (sx[t, k / 128] xq[t, k]) (sw[r / 128, k / 128] wq[r, k]), products exact, sums in fp32 on the tensor
- * cores, one rounding to out_dtype (EP_BF16, EP_FP16, EP_FP32; EP_FP16 overflows to infinity).  NaN in either operand or
- * scale (byte 255) gives NaN.  Results do not depend on what else runs: sums are taken in a fixed order.
- *   d_x, d_x_scales   device, T x C E4M3 and T x ceil(C / 128) E8M0, as ep_quantize_blocks leaves them (block_rows 1)
- *   d_w, d_w_scales   device, R x C E4M3 - a decoded weight, or one of ep_quantize_blocks (block_rows 128) - and its
- *                     ceil(R / 128) x ceil(C / 128) E8M0 scales, or NULL: ones
- *   d_row_scales      device, R floats a[r] (the scales with which the rows were brought into the container), or NULL: ones
- *   d_y               device, T x R of out_dtype, aligned to its element, ldy >= R
+ * cores, one rounding to out_dtype (EP_FP16 overflows to infinity).  NaN in either operand or scale (byte 255) gives NaN.
+ * Results do not depend on what else runs: sums are taken in a fixed order.
  * The copy engine reads the operands: d_x and d_w on 16 bytes, C, ldx and ldw multiples of 16, else EP_ERR_UNSUPPORTED.
  * A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
-int ep_fp8_matmul(const void *d_x, int64_t ldx, const void *d_x_scales, int64_t ldsx, const void *d_w, int64_t ldw,
-                  const void *d_w_scales, int64_t ldsw, const float *d_row_scales, uint32_t T, uint32_t R, uint32_t C,
-                  int32_t out_dtype, void *d_y, int64_t ldy, void *stream);
+typedef struct {
+    const void *d_x, *d_x_scales;   /* device: T x C E4M3 and T x ceil(C / 128) E8M0, as ep_quantize_blocks leaves them (block_rows 1) */
+    const void *d_w, *d_w_scales;   /* device: R x C E4M3 - a decoded weight, or one of ep_quantize_blocks (block_rows 128) - and its
+                                       ceil(R / 128) x ceil(C / 128) E8M0 scales, or NULL: ones */
+    const float *d_row_scales;      /* device: R floats a[r] (the scales with which the rows were brought into the container), or
+                                       NULL: ones */
+    void *d_y;                      /* device: T x R of out_dtype, aligned to its element, ldy >= R */
+    int64_t ldx, ldx_scales, ldw, ldw_scales, ldy;
+    uint32_t T, R, C;
+    int32_t out_dtype;              /* EP_BF16, EP_FP16 or EP_FP32 */
+} ep_matmul_job;
+int ep_fp8_matmul(const ep_matmul_job *job, void *stream);
 
 /* Keys and values of many requests in pages of E4M3, one scale for each page and head.  All pointers are device pointers. */
 typedef struct {
@@ -324,38 +333,55 @@ typedef struct {
                                            pages * heads * page < 2^31 - 256 */
 } ep_cache;
 
-/* Which tokens are whose, for both calls below: request b of B has d_seq_lens[b] tokens in the cache, its token j in row
- * j % page of page d_table[b * ldt + j / page] (columns pages at most); rows d_starts[b] .. d_starts[b + 1] of the call's N
- * rows are its newest tokens, the last of them token d_seq_lens[b] - 1.  The arrays are read on the device, so a captured
- * call serves requests of any lengths.  Rows outside the requests are left alone.  Whatever the arrays hold, nothing outside
- * the buffers is read or written: a page number outside the cache is passed over (the tokens are not written, and are left out
- * of the attention) and raises EP_ERR_BAD_PAGE in the integrity word; lengths are cut to columns * page, starts to 0 .. N. */
+/* Which tokens are whose: request b of B has d_seq_lens[b] tokens in the cache, its token j in row j % page of page
+ * d_table[b * ldt + j / page]; rows d_starts[b] .. d_starts[b + 1] of the call's N rows are its newest tokens, the last of
+ * them token d_seq_lens[b] - 1.  The arrays are read on the device, so a captured call serves requests of any lengths.  Rows outside
+ * the requests are left alone.  Whatever the arrays hold, nothing outside the buffers is read or written: a page number outside
+ * the cache is passed over (the tokens are not written, and are left out of the attention) and raises EP_ERR_BAD_PAGE in the
+ * integrity word; lengths are cut to columns * page, starts to 0 .. N. */
+typedef struct {
+    const int32_t *d_table, *d_seq_lens, *d_starts;   /* device: B x columns, B, B + 1 */
+    int64_t ldt;                                      /* between the table's rows */
+    uint32_t columns;                                 /* pages of a request, at most */
+    uint32_t B, N;                                    /* requests; rows of the call */
+} ep_requests;
 
 /* Writes the call's rows to the cache.  A page's scale only grows while the page fills: s' = max(s, the smallest power of two
  * that holds the new tokens); where it grows the older tokens become e4m3(q s / s').  A page without older tokens gets the new
- * tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request that has fewer
- * tokens than rows is passed over, from the first on.
- * A page that a call writes must belong to one request only; pages that are full may be shared.
- *   d_k, d_v   device, N x heads x dim of dtype (EP_BF16, EP_FP16); `ld*` between rows, `ld*_head` between heads, all multiples
- *              of 8 and the addresses on 16 bytes, else EP_ERR_UNSUPPORTED */
-int ep_cache_append(const ep_cache *cache, const void *d_k, int64_t ldk, int64_t ldk_head, const void *d_v, int64_t ldv,
-                    int64_t ldv_head, int32_t dtype, const int32_t *d_table, int64_t ldt, uint32_t columns,
-                    const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B, uint32_t N, void *stream);
+ * tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request
+ * that has fewer tokens than rows is passed over, from the first on.
+ * A page that a call writes must belong to one request only; pages that are full may be shared. */
+typedef struct {
+    ep_cache cache;
+    ep_requests requests;
+    const void *d_k, *d_v;          /* device: N x heads x dim of dtype */
+    int64_t ldk, ldk_head, ldv, ldv_head;   /* between rows, between heads: multiples of 8, the addresses on 16 bytes, else
+                                               EP_ERR_UNSUPPORTED */
+    int32_t dtype;                  /* EP_BF16 or EP_FP16 */
+} ep_append_job;
+int ep_cache_append(const ep_append_job *job, void *stream);
 
-/* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row i of its n.
- * Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token gives 0 (and -infinity in d_lse).
- * Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values; a token's
- * values count only for rows that see it.
- *   d_q, d_o   device, N x q_heads x dim of dtype (EP_BF16, EP_FP16), strides as in ep_cache_append
- *   d_lse      device, N x q_heads floats: the natural logarithm of the row's sum of exponentials, or NULL
- *   d_workspace  device, ep_cache_attention_workspace_bytes() bytes, 16-byte aligned; may be NULL if columns * page <= 256.
- *              Nothing in it outlives the call; calls that may overlap need one each.
- * B <= 4096, else EP_ERR_UNSUPPORTED. */
+/* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row
+ * i of its n.  Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token gives 0 (and -infinity
+ * in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values;
+ * a token's values count only for rows that see it.  B <= 4096, else EP_ERR_UNSUPPORTED. */
+typedef struct {
+    ep_cache cache;
+    ep_requests requests;
+    const void *d_q;                /* device: N x q_heads x dim of dtype */
+    void *d_o;                      /* device: the same; strides of both as in ep_append_job */
+    float *d_lse;                   /* device: N x q_heads floats, the natural logarithm of the row's sum of exponentials; or NULL */
+    void *d_workspace;              /* device: ep_cache_attention_workspace_bytes() bytes, 16-byte aligned; may be NULL if
+                                       columns * page <= 256.  Nothing in it outlives the call; calls that may overlap need one each */
+    size_t workspace_bytes;
+    int64_t ldq, ldq_head, ldo, ldo_head;
+    float scale;
+    uint32_t q_heads;
+    int32_t dtype;                  /* EP_BF16 or EP_FP16 */
+    int32_t causal;
+} ep_attention_job;
 size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim);
-int ep_cache_attention(const ep_cache *cache, const void *d_q, int64_t ldq, int64_t ldq_head, int32_t dtype, uint32_t q_heads,
-                       const int32_t *d_table, int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts,
-                       uint32_t B, uint32_t N, float scale, int32_t causal, void *d_o, int64_t ldo, int64_t ldo_head, float *d_lse,
-                       void *d_workspace, size_t workspace_bytes, void *stream);
+int ep_cache_attention(const ep_attention_job *job, void *stream);
 
 /* Device-side integrity word (no counterpart in the paper; it uses the fact that the encoder of Eq. 17 starts
  * every state at 2^15, so a correct decode of Eq. 18 must end there).  The kernel ORs in a flag when a tile does

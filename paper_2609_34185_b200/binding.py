@@ -9,6 +9,7 @@ from __future__ import annotations
 import collections
 import ctypes as C
 import os
+import struct
 import weakref
 
 import numpy as np
@@ -57,11 +58,6 @@ class Info(C.Structure):
         d["table_min"] = list(self.table_min)
         d["table_K"] = list(self.table_K)
         return d
-
-
-class Cache(C.Structure):
-    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scales", C.c_void_p), ("d_v_scales", C.c_void_p),
-                ("pages", C.c_uint32), ("heads", C.c_uint32), ("page", C.c_uint32), ("dim", C.c_uint32)]
 
 
 class DecodeJob(C.Structure):
@@ -114,17 +110,10 @@ def load():
                                           C.c_void_p]
     L.ep_decode_gemm.argtypes = [C.POINTER(Info), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
                                  C.c_void_p, C.c_void_p]
-    L.ep_quantize_blocks.argtypes = [C.c_void_p, C.c_int32, C.c_uint32, C.c_uint32, C.c_int64, C.c_uint32, C.c_void_p, C.c_int64,
-                                     C.c_void_p, C.c_int64, C.c_void_p]
-    L.ep_fp8_matmul.argtypes = [C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p, C.c_int64, C.c_void_p,
-                                C.c_uint32, C.c_uint32, C.c_uint32, C.c_int32, C.c_void_p, C.c_int64, C.c_void_p]
-    L.ep_cache_append.argtypes = [C.POINTER(Cache), C.c_void_p, C.c_int64, C.c_int64, C.c_void_p, C.c_int64, C.c_int64, C.c_int32,
-                                  C.c_void_p, C.c_int64, C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_void_p]
+    for f in (L.ep_quantize_blocks, L.ep_fp8_matmul, L.ep_cache_append, L.ep_cache_attention):
+        f.argtypes = [C.c_char_p, C.c_void_p]      # a job's bytes (see the *_JOB layouts), the stream
     L.ep_cache_attention_workspace_bytes.restype = C.c_size_t
     L.ep_cache_attention_workspace_bytes.argtypes = [C.c_uint32] * 5
-    L.ep_cache_attention.argtypes = [C.POINTER(Cache), C.c_void_p, C.c_int64, C.c_int64, C.c_int32, C.c_uint32, C.c_void_p, C.c_int64,
-                                     C.c_uint32, C.c_void_p, C.c_void_p, C.c_uint32, C.c_uint32, C.c_float, C.c_int32, C.c_void_p,
-                                     C.c_int64, C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
     L.ep_decode_batch.argtypes = [C.POINTER(DecodeJob), C.c_int32, C.c_void_p]
     L.ep_last_device_status.argtypes = [C.c_void_p]
     L.ep_strerror.restype = C.c_char_p
@@ -456,10 +445,42 @@ def decode_many(dblobs: list[DeviceBlob], out_dtype: int, outs: list, stream=Non
 
 
 # ---- operators in the 8-bit container -------------------------------------------------------------
+# These are called several times per layer and token, so what they cost on the host counts: a job is packed in one step
+# (a ctypes call takes 0.2 us per argument), and a tensor's properties are asked for once.
 
 KVCache = collections.namedtuple("KVCache", "k v k_scales v_scales")
 KVCache.__doc__ = """Keys and values in pages of E4M3, one scale for each page and head: k, v [pages, heads, page, dim] float8_e4m3fn,
 k_scales, v_scales [pages, heads] float32, all contiguous.  A plain tuple of the four serves as well."""
+
+# the C structs, field by field
+_CACHE, _REQUESTS = "PPPPIIII", "PPPqIIIxxxx"
+QUANTIZE_JOB = struct.Struct("@PPPqqqIIIi")
+MATMUL_JOB = struct.Struct("@PPPPPPqqqqqIIIi")
+APPEND_JOB = struct.Struct("@" + _CACHE + _REQUESTS + "PPqqqqixxxx")
+ATTENTION_JOB = struct.Struct("@" + _CACHE + _REQUESTS + "PPPPNqqqqfIii")
+
+_types = None
+
+
+def _float8():
+    """(torch, E4M3, E8M0, codes of the 16- and 32-bit types, int32)."""
+    global _types
+    if _types is None:
+        torch = _torch()
+        _types = (torch, torch.float8_e4m3fn, torch.float8_e8m0fnu, {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}, torch.int32)
+    return _types
+
+
+def _enqueue(f, name, job, dev, stream):
+    """f(job, the stream's handle) with device `dev` current."""
+    torch = _types[0]
+    if dev == torch.cuda.current_device():
+        rc = f(job, _stream_handle(stream) or None)
+    else:
+        with torch.cuda.device(dev):
+            rc = f(job, _stream_handle(stream) or None)
+    if rc:
+        raise EntroPackError(rc, name)
 
 
 def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") -> KVCache:
@@ -470,117 +491,111 @@ def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") ->
     return KVCache(k, v, ks, vs)
 
 
-def _want(ok: bool, what: str):
-    if not ok:
-        raise ValueError(what)
-
-
-def _float_code(dtype):
-    torch = _torch()
-    return {torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32}.get(dtype)
-
-
-def _launch(device, stream, call):
-    """call(stream handle) with `device` current, on the given torch stream or the device's current one."""
-    torch = _torch()
-    if device.index == torch.cuda.current_device():
-        call(_stream_handle(stream))
-    else:
-        with torch.cuda.device(device):
-            call(_stream_handle(stream))
-
-
-def _same_device(device, *tensors):
-    _want(device.type == "cuda" and all(t is None or t.device == device for t in tensors), "tensors must be on one CUDA device")
-
-
-def _rows_apart(m) -> int:
-    """Elements between the rows of a matrix; of a single row, whose stride means nothing, its length."""
-    return m.stride(0) if m.shape[0] > 1 else max(m.stride(0), m.shape[1])
+def _matrix(t, dtype, shape, dev, what):
+    """Distance between the rows of a [T, C] tensor on device `dev` with contiguous rows; of a single row, whose stride means
+    nothing, at least its length."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on the operands' CUDA device")
+    ld, one = t.stride()
+    if one != 1 and shape[1] > 1:
+        raise ValueError(f"rows of {what} must be contiguous")
+    return ld if shape[0] > 1 or ld > shape[1] else shape[1]
 
 
 def quantize_blocks(x, block_rows: int = 1, out=None, stream=None):
     """x [T, C] (bfloat16, float16 or float32) as E4M3 values and one power-of-two scale for each block of block_rows x 128
     (1: activations, 128: weights): (float8_e4m3fn [T, C], float8_e8m0fnu [ceil(T / block_rows), ceil(C / 128)]).  `out`: such a
     pair to fill.  See ep_quantize_blocks."""
-    torch = _torch()
-    code = _float_code(x.dtype)
-    _want(code is not None and x.dim() == 2 and (x.stride(1) == 1 or x.shape[1] == 1), "x must be a matrix of bfloat16, float16 or float32 with contiguous rows")
-    _want(block_rows in (1, 128), "block_rows must be 1 or 128")
-    T, Cc = x.shape
-    shape = (-(-T // block_rows), -(-Cc // 128))
+    torch, e4m3, e8m0, codes, _ = _float8()
+    dtype, shape, dev = x.dtype, x.shape, x.get_device()
+    code = codes.get(dtype)
+    if code is None or len(shape) != 2 or dev < 0:
+        raise ValueError("x must be a CUDA matrix of bfloat16, float16 or float32")
+    if block_rows != 1 and block_rows != 128:
+        raise ValueError("block_rows must be 1 or 128")
+    T, Cc = shape
+    blocks = (-(-T // block_rows), -(-Cc // 128))
     if out is None:
-        out = (torch.empty((T, Cc), dtype=torch.float8_e4m3fn, device=x.device), torch.empty(shape, dtype=torch.float8_e8m0fnu, device=x.device))
+        out = (torch.empty(shape, dtype=e4m3, device=x.device), torch.empty(blocks, dtype=e8m0, device=x.device))
     q, s = out
-    _want(q.dtype == torch.float8_e4m3fn and q.shape == (T, Cc) and (q.stride(1) == 1 or Cc == 1), "out[0] must be float8_e4m3fn of x's shape with contiguous rows")
-    _want(s.dtype == torch.float8_e8m0fnu and s.shape == shape and (s.stride(1) == 1 or shape[1] == 1), "out[1] must be float8_e8m0fnu, one scale per block")
-    _same_device(x.device, x, q, s)
-    _launch(x.device, stream, lambda h: _check(load().ep_quantize_blocks(
-        x.data_ptr(), code, T, Cc, _rows_apart(x), block_rows, q.data_ptr(), _rows_apart(q), s.data_ptr(), _rows_apart(s), h or None), "ep_quantize_blocks"))
-    return q, s
+    job = QUANTIZE_JOB.pack(x.data_ptr(), q.data_ptr(), s.data_ptr(), _matrix(x, dtype, shape, dev, "x"), _matrix(q, e4m3, shape, dev, "out[0]"),
+                            _matrix(s, e8m0, blocks, dev, "out[1]"), T, Cc, block_rows, code)
+    _enqueue(load().ep_quantize_blocks, "ep_quantize_blocks", job, dev, stream)
+    return out
 
 
 def fp8_matmul(x, x_scales, w, w_scales=None, row_scale=None, out_dtype: int = BF16, out=None, stream=None):
     """x [T, C] times w [R, C] transposed, both E4M3 with E8M0 scales per 1 x 128 (x_scales) and 128 x 128 (w_scales, None: ones),
     row r of w times row_scale[r] (float32, None: ones): [T, R] of out_dtype (BF16, FP16 or FP32), or `out`.  See ep_fp8_matmul."""
-    torch = _torch()
-    e4m3, e8m0 = torch.float8_e4m3fn, torch.float8_e8m0fnu
-    _want(x.dtype == e4m3 and w.dtype == e4m3 and x.dim() == 2 and w.dim() == 2 and x.shape[1] == w.shape[1], "x and w must be float8_e4m3fn matrices of as many columns")
-    _want(x.stride(1) == 1 and w.stride(1) == 1, "rows of x and w must be contiguous")
-    (T, Cc), R = x.shape, w.shape[0]
+    torch, e4m3, e8m0, codes, _ = _float8()
+    xs, wsh, dev = x.shape, w.shape, x.get_device()
+    if len(xs) != 2 or len(wsh) != 2 or xs[1] != wsh[1] or dev < 0:
+        raise ValueError("x and w must be CUDA matrices of as many columns")
+    (T, Cc), R = xs, wsh[0]
     blocks = -(-Cc // 128)
-    _want(x_scales.dtype == e8m0 and x_scales.shape == (T, blocks) and (x_scales.stride(1) == 1 or blocks == 1), "x_scales must be float8_e8m0fnu [T, ceil(C / 128)]")
-    _want(w_scales is None or w_scales.dtype == e8m0 and w_scales.shape == (-(-R // 128), blocks) and (w_scales.stride(1) == 1 or blocks == 1),
-          "w_scales must be float8_e8m0fnu [ceil(R / 128), ceil(C / 128)]")
-    _want(row_scale is None or row_scale.dtype == torch.float32 and row_scale.shape == (R,) and row_scale.is_contiguous(), "row_scale must be float32 [R]")
     if out is None:
-        _want(out_dtype in (BF16, FP16, FP32), "out_dtype must be BF16, FP16 or FP32")
+        if out_dtype not in (BF16, FP16, FP32):
+            raise ValueError("out_dtype must be BF16, FP16 or FP32")
         out = torch.empty((T, R), dtype=_out_torch_dtype(out_dtype), device=x.device)
-    code = _float_code(out.dtype)
-    _want(code is not None and out.shape == (T, R) and (out.stride(1) == 1 or R == 1), "out must be a [T, R] matrix of bfloat16, float16 or float32 with contiguous rows")
-    _same_device(x.device, x_scales, w, w_scales, row_scale, out)
-    _launch(x.device, stream, lambda h: _check(load().ep_fp8_matmul(
-        x.data_ptr(), _rows_apart(x), x_scales.data_ptr(), _rows_apart(x_scales), w.data_ptr(), _rows_apart(w), w_scales.data_ptr() if w_scales is not None else None,
-        _rows_apart(w_scales) if w_scales is not None else 0, row_scale.data_ptr() if row_scale is not None else None, T, R, Cc, code, out.data_ptr(), _rows_apart(out),
-        h or None), "ep_fp8_matmul"))
+    dtype = out.dtype
+    code = codes.get(dtype)
+    if code is None:
+        raise ValueError("out must be bfloat16, float16 or float32")
+    if row_scale is not None and (row_scale.dtype != torch.float32 or row_scale.shape != (R,) or not row_scale.is_contiguous() or row_scale.get_device() != dev):
+        raise ValueError("row_scale must be float32 [R], contiguous, on the operands' device")
+    job = MATMUL_JOB.pack(x.data_ptr(), x_scales.data_ptr(), w.data_ptr(), w_scales.data_ptr() if w_scales is not None else 0,
+                          row_scale.data_ptr() if row_scale is not None else 0, out.data_ptr(), _matrix(x, e4m3, xs, dev, "x"),
+                          _matrix(x_scales, e8m0, (T, blocks), dev, "x_scales"), _matrix(w, e4m3, wsh, dev, "w"),
+                          _matrix(w_scales, e8m0, (-(-R // 128), blocks), dev, "w_scales") if w_scales is not None else 0,
+                          _matrix(out, dtype, (T, R), dev, "out"), T, R, Cc, code)
+    _enqueue(load().ep_fp8_matmul, "ep_fp8_matmul", job, dev, stream)
     return out
 
 
-def _cache_of(cache):
-    torch = _torch()
+def _cache_and_requests(cache, table, seq_lens, starts, N):
+    """The fields of ep_cache and ep_requests, and the device."""
+    torch, e4m3, _, _, i32 = _float8()
     k, v, ks, vs = cache
-    _want(k.dtype == torch.float8_e4m3fn and v.dtype == torch.float8_e4m3fn and k.dim() == 4 and v.shape == k.shape and k.is_contiguous() and v.is_contiguous(),
-          "the cache's keys and values must be contiguous float8_e4m3fn [pages, heads, page, dim]")
-    pages, heads, page, dim = k.shape
-    _want(ks.dtype == torch.float32 and vs.dtype == torch.float32 and ks.shape == (pages, heads) and vs.shape == (pages, heads) and ks.is_contiguous() and vs.is_contiguous(),
-          "the cache's scales must be contiguous float32 [pages, heads]")
-    _same_device(k.device, v, ks, vs)
-    return Cache(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page, dim)
+    shape, dev = k.shape, k.get_device()
+    if (k.dtype != e4m3 or v.dtype != e4m3 or len(shape) != 4 or v.shape != shape or v.get_device() != dev or dev < 0 or not k.is_contiguous()
+            or not v.is_contiguous()):
+        raise ValueError("the cache's keys and values must be contiguous CUDA float8_e4m3fn [pages, heads, page, dim]")
+    pages, heads, page, dim = shape
+    f32, scales = torch.float32, (pages, heads)
+    if (ks.dtype != f32 or vs.dtype != f32 or ks.shape != scales or vs.shape != scales or ks.get_device() != dev or vs.get_device() != dev
+            or not ks.is_contiguous() or not vs.is_contiguous()):
+        raise ValueError("the cache's scales must be contiguous float32 [pages, heads] on its device")
+    rows = table.shape
+    if len(rows) != 2 or seq_lens.dtype != i32 or seq_lens.shape != rows[:1] or not seq_lens.is_contiguous() or seq_lens.get_device() != dev:
+        raise ValueError("table must be a matrix, seq_lens contiguous int32, one per row of table, on the cache's device")
+    B, columns = rows
+    if starts.dtype != i32 or starts.shape != (B + 1,) or not starts.is_contiguous() or starts.get_device() != dev:
+        raise ValueError("starts must be contiguous int32, one more than rows of table, on the cache's device")
+    return (k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr(), pages, heads, page, dim, table.data_ptr(), seq_lens.data_ptr(),
+            starts.data_ptr(), _matrix(table, i32, rows, dev, "table"), columns, B, N), dev
 
 
-def _requests(device, table, seq_lens, starts):
-    torch = _torch()
-    _want(table.dtype == torch.int32 and table.dim() == 2 and (table.stride(1) == 1 or table.shape[1] == 1), "table must be an int32 matrix with contiguous rows")
-    B = table.shape[0]
-    _want(seq_lens.dtype == torch.int32 and seq_lens.shape == (B,) and seq_lens.is_contiguous(), "seq_lens must be int32, one per row of table")
-    _want(starts.dtype == torch.int32 and starts.shape == (B + 1,) and starts.is_contiguous(), "starts must be int32, one more than rows of table")
-    _same_device(device, table, seq_lens, starts)
-    return B
+def _heads(t, dtype, shape, dev, what):
+    """Distances between rows and between heads of [N, heads, dim] whose heads are contiguous."""
+    if t.dtype != dtype or t.shape != shape or t.get_device() != dev:
+        raise ValueError(f"{what} must be {dtype} {list(shape)} on the cache's CUDA device")
+    row, head, one = t.stride()
+    if one != 1:
+        raise ValueError(f"heads of {what} must be contiguous")
+    return row, head
 
 
 def cache_append(cache, k, v, table, seq_lens, starts, stream=None) -> None:
     """Writes k, v [N, heads, dim] (bfloat16 or float16) to a KVCache: rows starts[b] .. starts[b + 1] are the newest tokens of request b,
     which has seq_lens[b] with them, in the pages table[b].  See ep_cache_append."""
-    c = _cache_of(cache)
-    code = _float_code(k.dtype)
-    _want(code in (BF16, FP16) and v.dtype == k.dtype and k.dim() == 3 and v.shape == k.shape and k.shape[1:] == (c.heads, c.dim), "k and v must be bfloat16 or float16 [N, heads, dim]")
-    _want(k.stride(2) == 1 and v.stride(2) == 1, "heads of k and v must be contiguous")
-    device = cache[0].device
-    B = _requests(device, table, seq_lens, starts)
-    _same_device(device, k, v)
-    _launch(device, stream, lambda h: _check(load().ep_cache_append(
-        C.byref(c), k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(), v.stride(0), v.stride(1), code, table.data_ptr(), _rows_apart(table), table.shape[1],
-        seq_lens.data_ptr(), starts.data_ptr(), B, k.shape[0], h or None), "ep_cache_append"))
+    shape = k.shape
+    fields, dev = _cache_and_requests(cache, table, seq_lens, starts, shape[0])
+    dtype = k.dtype
+    code = _types[3].get(dtype)
+    if code is None or code == FP32 or shape[1:] != (fields[5], fields[7]):
+        raise ValueError("k must be bfloat16 or float16 [N, heads, dim] of the cache's heads")
+    job = APPEND_JOB.pack(*fields, k.data_ptr(), v.data_ptr(), *_heads(k, dtype, shape, dev, "k"), *_heads(v, dtype, shape, dev, "v"), code)
+    _enqueue(load().ep_cache_append, "ep_cache_append", job, dev, stream)
 
 
 def cache_attention_workspace_bytes(N: int, B: int, q_heads: int, heads: int, dim: int) -> int:
@@ -592,30 +607,32 @@ def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool 
     """softmax(scale q K^T) V of q [N, q_heads, dim] (bfloat16 or float16) over a KVCache, rows, requests and pages as in cache_append;
     scale: 1 / sqrt(dim) by default.  lse: float32 [N, q_heads] to fill.  workspace: a uint8 tensor of
     cache_attention_workspace_bytes(), taken from torch's allocator if not given.  See ep_cache_attention."""
-    torch = _torch()
-    c = _cache_of(cache)
-    code = _float_code(q.dtype)
-    _want(code in (BF16, FP16) and q.dim() == 3 and q.shape[2] == c.dim and q.stride(2) == 1, "q must be bfloat16 or float16 [N, q_heads, dim] with contiguous heads")
-    N, Hq, D = q.shape
-    _want(Hq > 0 and Hq % c.heads == 0, "q's heads must be a multiple of the cache's")
-    device = cache[0].device
-    B = _requests(device, table, seq_lens, starts)
+    shape = q.shape
+    fields, dev = _cache_and_requests(cache, table, seq_lens, starts, shape[0])
+    torch, dtype = _types[0], q.dtype
+    code = _types[3].get(dtype)
+    heads, page, dim, columns, B = fields[5], fields[6], fields[7], fields[12], fields[13]
+    if code is None or code == FP32 or len(shape) != 3 or shape[2] != dim or shape[1] == 0 or shape[1] % heads:
+        raise ValueError("q must be bfloat16 or float16 [N, q_heads, dim], its heads a multiple of the cache's")
     if out is None:
-        out = torch.empty((N, Hq, D), dtype=q.dtype, device=device)
-    _want(out.dtype == q.dtype and out.shape == q.shape and out.stride(2) == 1, "out must be of q's type and shape with contiguous heads")
-    _want(lse is None or lse.dtype == torch.float32 and lse.shape == (N, Hq) and lse.is_contiguous(), "lse must be contiguous float32 [N, q_heads]")
-    _same_device(device, q, out, lse, workspace)
-    scale = D ** -0.5 if scale is None else float(scale)
-
-    def call(h):
-        ws = workspace
-        if ws is None:
-            ws = torch.empty(cache_attention_workspace_bytes(N, B, Hq, c.heads, D), dtype=torch.uint8, device=device)
-            if stream is not None:
-                ws.record_stream(stream)
-        _check(load().ep_cache_attention(
-            C.byref(c), q.data_ptr(), q.stride(0), q.stride(1), code, Hq, table.data_ptr(), _rows_apart(table), table.shape[1], seq_lens.data_ptr(), starts.data_ptr(),
-            B, N, scale, int(causal), out.data_ptr(), out.stride(0), out.stride(1), lse.data_ptr() if lse is not None else None, ws.data_ptr(),
-            ws.numel() * ws.element_size(), h or None), "ep_cache_attention")
-    _launch(device, stream, call)
+        out = torch.empty(shape, dtype=dtype, device=q.device)
+    at = 0
+    if lse is not None:
+        if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != dev:
+            raise ValueError("lse must be contiguous float32 [N, q_heads] on the cache's device")
+        at = lse.data_ptr()
+    size = room = 0
+    if workspace is not None:
+        if workspace.get_device() != dev or not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous, on the cache's device")
+        room, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+    elif columns * page > 256:
+        with torch.cuda.device(dev):
+            workspace = torch.empty(cache_attention_workspace_bytes(shape[0], B, shape[1], heads, dim), dtype=torch.uint8, device=q.device)
+        if stream is not None:
+            workspace.record_stream(stream)
+        room, size = workspace.data_ptr(), workspace.numel()
+    job = ATTENTION_JOB.pack(*fields, q.data_ptr(), out.data_ptr(), at, room, size, *_heads(q, dtype, shape, dev, "q"), *_heads(out, dtype, shape, dev, "out"),
+                             dim ** -0.5 if scale is None else scale, shape[1], code, 1 if causal else 0)
+    _enqueue(load().ep_cache_attention, "ep_cache_attention", job, dev, stream)
     return out

@@ -20,7 +20,7 @@ struct QuantParams {
     uint8_t *q, *s;
     int64_t ldx, ldq, lds;
     uint32_t T, C, blocks;        // blocks = ceil(C / 128)
-    uint32_t vec;                 // rows of x and q begin on 16 and 8 bytes
+    uint32_t vec;                 // rows of x and of q begin on 16 bytes
 };
 
 // N consecutive values of a row from column c on, as floats; zeros past the row's end
@@ -53,6 +53,7 @@ __device__ __forceinline__ void only_finite(float (&v)[N]) {
     for (uint32_t i = 0; i < N; ++i)
         if (!(fabsf(v[i]) < __uint_as_float(0x7F800000u))) v[i] = __uint_as_float(0x7FFFFFFFu);
 }
+// N of 4, 8 or 16 values; `vec`: the place is aligned to N bytes
 template <uint32_t N>
 __device__ __forceinline__ void store_values(uint8_t *row, uint32_t c, uint32_t C, bool vec, const float (&v)[N], float inverse) {
     uint32_t w[N / 4];
@@ -60,7 +61,8 @@ __device__ __forceinline__ void store_values(uint8_t *row, uint32_t c, uint32_t 
     for (uint32_t i = 0; i < N / 4; ++i)
         w[i] = e4m3x2(v[4 * i] * inverse, v[4 * i + 1] * inverse) | e4m3x2(v[4 * i + 2] * inverse, v[4 * i + 3] * inverse) << 16;
     if (vec && c + N <= C) {
-        if constexpr (N == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
+        if constexpr (N == 16) *reinterpret_cast<uint4 *>(row + c) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (N == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(w[0], w[1]);
         else *reinterpret_cast<uint32_t *>(row + c) = w[0];
     } else {
 #pragma unroll
@@ -69,37 +71,74 @@ __device__ __forceinline__ void store_values(uint8_t *row, uint32_t c, uint32_t 
     }
 }
 
-// one scale per row and 128 columns: a warp takes four 16-byte loads per lane of one row
-template <class E>
+// One scale per row and 128 columns.  A lane takes 32 bytes, so that a block of 16-bit values is eight lanes' (three
+// exchanges for its maximum instead of four); a warp takes LOADS such pieces, counted through the rows.  Magnitudes are compared as
+// integers, two 16-bit ones at a time.
+template <class E, uint32_t LOADS>
 __global__ void __launch_bounds__(128) quantize_rows_kernel(const __grid_constant__ QuantParams P) {
     using T = typename E::T;
-    constexpr uint32_t N = 16 / sizeof(T), kLanes = kBlock / N, kLoads = 4, kSpan = 32 * N;
+    constexpr uint32_t N = 32 / sizeof(T), kLanes = kBlock / N, kSpan = 32 * N;
     op_wait_for_stream();
     const uint32_t lane = threadIdx.x & 31u;
-    const uint32_t spans = (P.C + kLoads * kSpan - 1u) / (kLoads * kSpan);
-    const uint64_t unit = uint64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    if (unit >= uint64_t(P.T) * spans) return;
-    const uint32_t t = uint32_t(unit / spans), c0 = uint32_t(unit % spans) * (kLoads * kSpan) + lane * N;
-    const T *row = static_cast<const T *>(P.x) + int64_t(t) * P.ldx;
-    float v[kLoads][N];
+    const uint32_t spans = (P.C + kSpan - 1u) / kSpan;
+    uint64_t unit = (uint64_t(blockIdx.x) * (blockDim.x >> 5) + (threadIdx.x >> 5)) * LOADS;
+    uint32_t t0 = uint32_t(unit / spans), s0 = uint32_t(unit - uint64_t(t0) * spans);
+    uint32_t w[LOADS][8], row[LOADS], col[LOADS];
 #pragma unroll
-    for (uint32_t i = 0; i < kLoads; ++i) load_values<E>(row, c0 + i * kSpan, P.C, P.vec, v[i]);
+    for (uint32_t i = 0; i < LOADS; ++i) {
+        row[i] = t0, col[i] = s0 * kSpan + lane * N;
+        if (++s0 == spans) s0 = 0, ++t0;
+        const T *src = static_cast<const T *>(P.x) + int64_t(row[i]) * P.ldx;
+        if (row[i] < P.T && P.vec && col[i] + N <= P.C) {
+            const uint4 lo = __ldcs(reinterpret_cast<const uint4 *>(src + col[i])), hi = __ldcs(reinterpret_cast<const uint4 *>(src + col[i]) + 1);
+            w[i][0] = lo.x, w[i][1] = lo.y, w[i][2] = lo.z, w[i][3] = lo.w, w[i][4] = hi.x, w[i][5] = hi.y, w[i][6] = hi.z, w[i][7] = hi.w;
+        } else {
 #pragma unroll
-    for (uint32_t i = 0; i < kLoads; ++i) {
-        auto block_max = [&]() {
-            float a = largest(v[i]);
+            for (uint32_t j = 0; j < 8; ++j) {
+                w[i][j] = 0;
 #pragma unroll
-            for (uint32_t m = 1; m < kLanes; m <<= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, m));
-            return a;
-        };
-        float a = block_max();
-        if (__any_sync(0xFFFFFFFFu, !(a < __uint_as_float(0x7F800000u)))) {       // an infinity: without it
-            only_finite(v[i]);
-            a = block_max();
+                for (uint32_t k = 0; k < 4 / sizeof(T); ++k) {
+                    const uint32_t c = col[i] + j * (4 / sizeof(T)) + k;
+                    if (row[i] < P.T && c < P.C) w[i][j] |= E::bits(src[c]) << (16 * k);
+                }
+            }
         }
-        const uint32_t e = scale_exponent(a, 127u), c = c0 + i * kSpan;
-        store_values(P.q + int64_t(t) * P.ldq, c, P.C, P.vec, v[i], pow2_inverse(e));
-        if (c < P.C && (lane & (kLanes - 1u)) == 0) P.s[int64_t(t) * P.lds + c / kBlock] = uint8_t(e);
+    }
+#pragma unroll
+    for (uint32_t i = 0; i < LOADS; ++i) {
+        // the largest magnitude's bits; what is not finite is the largest of all
+        uint32_t a;
+        if constexpr (N == 16) {
+            a = w[i][0] & 0x7FFF7FFFu;
+#pragma unroll
+            for (uint32_t j = 1; j < 8; ++j) a = __vmaxu2(a, w[i][j] & 0x7FFF7FFFu);
+#pragma unroll
+            for (uint32_t m = 1; m < kLanes; m <<= 1) a = __vmaxu2(a, __shfl_xor_sync(0xFFFFFFFFu, a, m));
+            a = max(a & 0xFFFFu, a >> 16);
+        } else {
+            a = w[i][0] & 0x7FFFFFFFu;
+#pragma unroll
+            for (uint32_t j = 1; j < 8; ++j) a = max(a, w[i][j] & 0x7FFFFFFFu);
+#pragma unroll
+            for (uint32_t m = 1; m < kLanes; m <<= 1) a = max(a, __shfl_xor_sync(0xFFFFFFFFu, a, m));
+        }
+        float top = E::of_bits(a);
+        float v[N];
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) {
+            if constexpr (N == 16) v[2 * j] = E::lo(w[i][j]), v[2 * j + 1] = E::hi(w[i][j]);
+            else v[j] = __uint_as_float(w[i][j]);
+        }
+        if (__any_sync(0xFFFFFFFFu, !(top < __uint_as_float(0x7F800000u)))) {     // without what is not finite
+            only_finite(v);
+            top = largest(v);
+#pragma unroll
+            for (uint32_t m = 1; m < kLanes; m <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
+        }
+        const uint32_t e = scale_exponent(top, 127u);
+        if (row[i] >= P.T) continue;
+        store_values(P.q + int64_t(row[i]) * P.ldq, col[i], P.C, P.vec, v, pow2_inverse(e));
+        if (col[i] < P.C && (lane & (kLanes - 1u)) == 0) P.s[int64_t(row[i]) * P.lds + col[i] / kBlock] = uint8_t(e);
     }
 }
 
@@ -152,16 +191,20 @@ __global__ void __launch_bounds__(256) quantize_blocks_kernel(const __grid_const
 
 template <class E>
 int launch_quantize(const QuantParams &P, uint32_t block_rows, cudaStream_t st) {
-    uint64_t grid;
+    cudaError_t e;
     if (block_rows == 1) {
-        const uint64_t span = 4u * 32u * (16u / sizeof(typename E::T));
-        grid = (uint64_t(P.T) * ((P.C + span - 1u) / span) + 3u) / 4u;
+        constexpr uint32_t kSpan = 32u * (32u / sizeof(typename E::T));
+        const uint64_t pieces = uint64_t(P.T) * ((P.C + kSpan - 1u) / kSpan);
+        // one piece per warp while that does not fill the GPU (4096 warps are seven for each scheduler)
+        const bool few = pieces <= 4096;
+        const uint64_t grid = (pieces + (few ? 3u : 15u)) / (few ? 4u : 16u);
+        if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+        e = few ? op_launch(quantize_rows_kernel<E, 1>, uint32_t(grid), 128, 0, 1, st, P) : op_launch(quantize_rows_kernel<E, 4>, uint32_t(grid), 128, 0, 1, st, P);
     } else {
-        grid = uint64_t((P.T + kBlock - 1u) / kBlock) * P.blocks;
+        const uint64_t grid = uint64_t((P.T + kBlock - 1u) / kBlock) * P.blocks;
+        if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+        e = op_launch(quantize_blocks_kernel<E>, uint32_t(grid), 256, 0, 1, st, P);
     }
-    if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
-    const cudaError_t e = block_rows == 1 ? op_launch(quantize_rows_kernel<E>, uint32_t(grid), 128, 0, 1, st, P)
-                                          : op_launch(quantize_blocks_kernel<E>, uint32_t(grid), 256, 0, 1, st, P);
     return e == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
@@ -415,58 +458,60 @@ int ep::op8_status_matmul() {
     return int(v);
 }
 
-extern "C" int ep_quantize_blocks(const void *d_x, int32_t x_dtype, uint32_t T, uint32_t C, int64_t ldx, uint32_t block_rows, void *d_q, int64_t ldq,
-                                  void *d_scales, int64_t lds, void *stream) {
-    if (T == 0) return EP_OK;
-    if (!d_x || !d_q || !d_scales || C == 0 || C > 0x7FFFFF00u || (block_rows != 1 && block_rows != kBlock)) return EP_ERR_BAD_ARG;
-    const uint32_t size = x_dtype == EP_FP32 ? 4 : x_dtype == EP_BF16 || x_dtype == EP_FP16 ? 2 : 0;
-    if (!size || !aligned(d_x, size)) return EP_ERR_BAD_ARG;
+extern "C" int ep_quantize_blocks(const ep_quantize_job *job, void *stream) {
+    if (!job) return EP_ERR_BAD_ARG;
+    const ep_quantize_job &j = *job;
+    if (j.T == 0) return EP_OK;
+    if (!j.d_x || !j.d_q || !j.d_scales || j.C == 0 || j.C > 0x7FFFFF00u || (j.block_rows != 1 && j.block_rows != kBlock)) return EP_ERR_BAD_ARG;
+    const uint32_t size = j.x_dtype == EP_FP32 ? 4 : j.x_dtype == EP_BF16 || j.x_dtype == EP_FP16 ? 2 : 0;
+    if (!size || !aligned(j.d_x, size)) return EP_ERR_BAD_ARG;
     QuantParams P;
     std::memset(&P, 0, sizeof(P));
-    P.blocks = (C + kBlock - 1u) / kBlock;
-    if (ldx < int64_t(C) || ldq < int64_t(C) || lds < int64_t(P.blocks)) return EP_ERR_BAD_ARG;
-    P.x = d_x;
-    P.q = static_cast<uint8_t *>(d_q);
-    P.s = static_cast<uint8_t *>(d_scales);
-    P.ldx = ldx;
-    P.ldq = ldq;
-    P.lds = lds;
-    P.T = T;
-    P.C = C;
-    P.vec = aligned(d_x, 16) && ldx * size % 16 == 0 && aligned(d_q, 8) && ldq % 8 == 0;
+    P.blocks = (j.C + kBlock - 1u) / kBlock;
+    if (j.ldx < int64_t(j.C) || j.ldq < int64_t(j.C) || j.lds < int64_t(P.blocks)) return EP_ERR_BAD_ARG;
+    P.x = j.d_x;
+    P.q = static_cast<uint8_t *>(j.d_q);
+    P.s = static_cast<uint8_t *>(j.d_scales);
+    P.ldx = j.ldx;
+    P.ldq = j.ldq;
+    P.lds = j.lds;
+    P.T = j.T;
+    P.C = j.C;
+    P.vec = aligned(j.d_x, 16) && j.ldx * size % 16 == 0 && aligned(j.d_q, 16) && j.ldq % 16 == 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (x_dtype == EP_BF16) return launch_quantize<Bf16>(P, block_rows, st);
-    if (x_dtype == EP_FP16) return launch_quantize<Fp16>(P, block_rows, st);
-    return launch_quantize<Fp32>(P, block_rows, st);
+    if (j.x_dtype == EP_BF16) return launch_quantize<Bf16>(P, j.block_rows, st);
+    if (j.x_dtype == EP_FP16) return launch_quantize<Fp16>(P, j.block_rows, st);
+    return launch_quantize<Fp32>(P, j.block_rows, st);
 }
 
-extern "C" int ep_fp8_matmul(const void *d_x, int64_t ldx, const void *d_x_scales, int64_t ldsx, const void *d_w, int64_t ldw, const void *d_w_scales,
-                             int64_t ldsw, const float *d_row_scales, uint32_t T, uint32_t R, uint32_t C, int32_t out_dtype, void *d_y, int64_t ldy,
-                             void *stream) {
-    if (T == 0) return EP_OK;
-    if (!d_x || !d_x_scales || !d_w || !d_y || R == 0 || C == 0 || C > 0x7FFFFF00u || R > 0x7FFFFF00u || T > 0x7FFFFF00u) return EP_ERR_BAD_ARG;
-    const uint32_t size = out_dtype == EP_FP32 ? 4 : out_dtype == EP_BF16 || out_dtype == EP_FP16 ? 2 : 0;
-    const uint32_t blocks = (C + kBlock - 1u) / kBlock;
-    if (!size || !aligned(d_y, size) || (d_row_scales && !aligned(d_row_scales, 4)) || ldx < int64_t(C) || ldw < int64_t(C) || ldsx < int64_t(blocks) ||
-        (d_w_scales && ldsw < int64_t(blocks)) || ldy < int64_t(R))
+extern "C" int ep_fp8_matmul(const ep_matmul_job *job, void *stream) {
+    if (!job) return EP_ERR_BAD_ARG;
+    const ep_matmul_job &j = *job;
+    if (j.T == 0) return EP_OK;
+    if (!j.d_x || !j.d_x_scales || !j.d_w || !j.d_y || j.R == 0 || j.C == 0 || j.C > 0x7FFFFF00u || j.R > 0x7FFFFF00u || j.T > 0x7FFFFF00u) return EP_ERR_BAD_ARG;
+    const uint32_t size = j.out_dtype == EP_FP32 ? 4 : j.out_dtype == EP_BF16 || j.out_dtype == EP_FP16 ? 2 : 0;
+    const uint32_t blocks = (j.C + kBlock - 1u) / kBlock;
+    if (!size || !aligned(j.d_y, size) || (j.d_row_scales && !aligned(j.d_row_scales, 4)) || j.ldx < int64_t(j.C) || j.ldw < int64_t(j.C) ||
+        j.ldx_scales < int64_t(blocks) || (j.d_w_scales && j.ldw_scales < int64_t(blocks)) || j.ldy < int64_t(j.R))
         return EP_ERR_BAD_ARG;
     // the copy engine's rows begin on 16 bytes
-    if (C % 16 || ldx % 16 || ldw % 16 || !aligned(d_x, 16) || !aligned(d_w, 16) || ldx >= (int64_t(1) << 40) || ldw >= (int64_t(1) << 40)) return EP_ERR_UNSUPPORTED;
+    if (j.C % 16 || j.ldx % 16 || j.ldw % 16 || !aligned(j.d_x, 16) || !aligned(j.d_w, 16) || j.ldx >= (int64_t(1) << 40) || j.ldw >= (int64_t(1) << 40))
+        return EP_ERR_UNSUPPORTED;
     MatmulParams P;
     std::memset(&P, 0, sizeof(P));
-    P.sx = static_cast<const uint8_t *>(d_x_scales);
-    P.sw = static_cast<const uint8_t *>(d_w_scales);
-    P.a = d_row_scales;
-    P.y = d_y;
-    P.ldsx = ldsx;
-    P.ldsw = ldsw;
-    P.ldy = ldy;
-    P.T = T;
-    P.R = R;
+    P.sx = static_cast<const uint8_t *>(j.d_x_scales);
+    P.sw = static_cast<const uint8_t *>(j.d_w_scales);
+    P.a = j.d_row_scales;
+    P.y = j.d_y;
+    P.ldsx = j.ldx_scales;
+    P.ldsw = j.ldw_scales;
+    P.ldy = j.ldy;
+    P.T = j.T;
+    P.R = j.R;
     P.blocks = blocks;
-    P.tiles_r = (R + kBlock - 1u) / kBlock;
+    P.tiles_r = (j.R + kBlock - 1u) / kBlock;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (out_dtype == EP_BF16) return launch_matmul<Bf16>(P, d_x, ldx, d_w, ldw, C, st);
-    if (out_dtype == EP_FP16) return launch_matmul<Fp16>(P, d_x, ldx, d_w, ldw, C, st);
-    return launch_matmul<Fp32>(P, d_x, ldx, d_w, ldw, C, st);
+    if (j.out_dtype == EP_BF16) return launch_matmul<Bf16>(P, j.d_x, j.ldx, j.d_w, j.ldw, j.C, st);
+    if (j.out_dtype == EP_FP16) return launch_matmul<Fp16>(P, j.d_x, j.ldx, j.d_w, j.ldw, j.C, st);
+    return launch_matmul<Fp32>(P, j.d_x, j.ldx, j.d_w, j.ldw, j.C, st);
 }

@@ -46,7 +46,7 @@ constexpr uint32_t kLeastScale = 127 - 100;      // of a page of zeros: 2^-100, 
 template <class E, uint32_t WARPS>
 __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ AppendParams P) {
     using T = typename E::T;
-    constexpr uint32_t kThreads = 32 * WARPS;
+    constexpr uint32_t kThreads = 32 * WARPS, kHeld = WARPS == 1 ? 2 : 8;
     __shared__ float largest_of[4];
     op_wait_for_stream();
     const uint32_t tid = WARPS == 1 ? threadIdx.x & 31u : threadIdx.x, lane = tid & 31u;
@@ -71,14 +71,22 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
         const uint64_t block = uint64_t(uint32_t(id)) * P.q.H + h;
         uint8_t *dst = P.cache[which] + (block << P.q.shift) * P.D + at;
         auto row_of = [&](uint32_t pos) { return x + int64_t(r.row + (r.rows - rows) + pos - first) * P.ldx[which]; };
+        // kHeld rows of a lane at a time; a page of up to 64 tokens of 128 dimensions (by a CTA) is held whole and read once
         float a = 0.0f;
-        for (uint32_t pos = lo + sub; pos < hi; pos += step) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
-            const float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+        uint4 held[kHeld];
+        for (uint32_t from = lo + sub; from < hi; from += kHeld * step) {
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i)
-                if (fabsf(v[i]) < __uint_as_float(0x7F800000u)) a = fmaxf(a, fabsf(v[i]));
+            for (uint32_t i = 0; i < kHeld; ++i) held[i] = from + i * step < hi ? __ldg(reinterpret_cast<const uint4 *>(row_of(from + i * step))) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (uint32_t i = 0; i < kHeld; ++i) {
+                const uint4 w = held[i];
+                const float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k)
+                    if (fabsf(v[k]) < __uint_as_float(0x7F800000u)) a = fmaxf(a, fabsf(v[k]));
+            }
         }
+        const bool once = hi - lo <= kHeld * step;
         a = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a)));
         if constexpr (WARPS > 1) {
             if (lane == 0) largest_of[tid >> 5] = a;
@@ -108,12 +116,20 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
             if constexpr (WARPS > 1) __syncthreads();     // everyone has read the old scale
             else __syncwarp();
         }
-        for (uint32_t pos = lo + sub; pos < hi; pos += step) {
-            const uint4 w = __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
-            float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+        const bool power = (__float_as_uint(scale) & 0x7FFFFFu) == 0 && scale >= 1e-30f && scale <= 1e30f;
+        const float inverse = __fdiv_rn(1.0f, scale);     // exact for a power of two; other scales (a caller's own) are divided by
+        for (uint32_t from = lo + sub; from < hi; from += kHeld * step) {
 #pragma unroll
-            for (uint32_t i = 0; i < 8; ++i) v[i] = fabsf(v[i]) < __uint_as_float(0x7F800000u) ? __fdiv_rn(v[i], scale) : __uint_as_float(0x7FFFFFFFu);
-            *reinterpret_cast<uint2 *>(dst + (pos - p0) * P.D) = make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+            for (uint32_t i = 0; i < kHeld; ++i) {
+                const uint32_t pos = from + i * step;
+                if (pos >= hi) break;
+                const uint4 w = once ? held[i] : __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
+                float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+#pragma unroll
+                for (uint32_t k = 0; k < 8; ++k)
+                    v[k] = !(fabsf(v[k]) < __uint_as_float(0x7F800000u)) ? __uint_as_float(0x7FFFFFFFu) : power ? v[k] * inverse : __fdiv_rn(v[k], scale);
+                *reinterpret_cast<uint2 *>(dst + (pos - p0) * P.D) = make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+            }
         }
         if (tid == 0) P.scales[which][block] = scale;
     }
@@ -125,7 +141,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // A row is a query and one of the query heads that share a head of the cache; the rows of a request and head make tiles of 16 MT.
 // A tile of rows against all tokens of its request is a segment; a segment is cut into units of 256 tokens, the units of all segments form
 // one list, and every CTA takes an equal, contiguous share of it, whatever the requests' lengths (they are read on the device: a
-// captured launch serves any).  A CTA's eight warps take tiles of 32 tokens in turn, each with a running maximum and sum of its own and its own ring
+// captured launch serves any).  A CTA's warps take tiles of 32 tokens in turn, each with a running maximum and sum of its own and its own ring
 // of tiles brought in by the copy engine, so that nothing waits for another warp before the segment's end; there the warps' results
 // are joined in shared memory.  What crosses a CTA's share goes through the workspace: a CTA leaves at most two
 // pieces there, its first segment's and its last's, and a second launch joins them.
@@ -135,7 +151,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // below the row's largest, whose rounding is below fp32's own.  The weights w carry a factor 2^14 (their largest, 2^14, is within binary16's range) so that
 // those down to 2^-28 of the largest keep 11 bits.  A page's value scale is moved onto w as v_scale / the largest so far.
 // ======================================================================================================================
-constexpr uint32_t kAttWarps = 8, kTile = 32, kUnit = kAttWarps * kTile, kMaxRequests = 4096;
+constexpr uint32_t kTile = 32, kUnit = 256, kMaxRequests = 4096;
 constexpr float kWeightShift = 14.0f;
 
 struct AttendParams {
@@ -157,15 +173,15 @@ template <uint32_t MT, uint32_t D>
 constexpr uint32_t kPiece = 16 * MT * (D + 2);
 constexpr uint32_t kDescWords = 8;               // per CTA: the segment that it begins and does not end: request, row tile, head, last CTA + 1
 
-template <uint32_t MT, uint32_t D>
+template <uint32_t MT, uint32_t D, uint32_t W>
 struct AttendShape {
     static constexpr uint32_t kTileBytes = kTile * D, kStage = 2 * kTileBytes;
-    static constexpr uint32_t kStages = D == 64 ? 6 : 3;
+    static constexpr uint32_t kStages = 24 / W * (128 / D);
     static constexpr uint32_t kRing = kStages * kStage;                                    // per warp
-    static constexpr uint32_t kMeta = kAttWarps * kRing;                                   // scales of the stages' pages: 2 x (key, value)
-    static constexpr uint32_t kBars = kMeta + kAttWarps * kStages * 16;
-    static constexpr uint32_t kJoin = kBars + kAttWarps * kStages * 8;                     // m, l, v scale of the warps' rows
-    static constexpr uint32_t kPrefix = kJoin + kAttWarps * 16 * MT * 16 + 16;
+    static constexpr uint32_t kMeta = W * kRing;                                   // scales of the stages' pages: 2 x (key, value)
+    static constexpr uint32_t kBars = kMeta + W * kStages * 16;
+    static constexpr uint32_t kJoin = kBars + W * kStages * 8;                     // m, l, v scale of the warps' rows
+    static constexpr uint32_t kPrefix = kJoin + W * 16 * MT * 16 + 16;
     static constexpr uint32_t kSmem = kPrefix + 4 * (kMaxRequests + 32) + 1024;
     static_assert(16 * MT * D * 4 <= kRing && kSmem <= 232448);
 };
@@ -220,10 +236,10 @@ __device__ uint32_t prefix_units(const Requests &q, uint32_t G, uint32_t rows_pe
     return all;
 }
 
-template <class E, uint32_t MT, uint32_t D>
-__global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap k_map,
+template <class E, uint32_t MT, uint32_t D, uint32_t W>
+__global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap k_map,
                                                                    const __grid_constant__ CUtensorMap v_map) {
-    using S = AttendShape<MT, D>;
+    using S = AttendShape<MT, D, W>;
     using T = typename E::T;
     constexpr uint32_t kRows = 16 * MT, kSteps = D / 16, kPer = D / 4;       // k steps of q k^T; elements of a row that a lane of a quad holds
     extern __shared__ uint8_t raw[];
@@ -266,13 +282,13 @@ __global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_
         const uint32_t h = seg % P.q.H, tile = seg / P.q.H;
         const uint32_t n_rows = r.rows * P.G, row0 = tile * kRows;
         const uint32_t t_begin = first_unit * kUnit, t_end = min(r.len, last_unit * kUnit);
-        const uint32_t n_tiles = t_end > t_begin + warp * kTile ? (t_end - t_begin - warp * kTile + kUnit - 1u) / kUnit : 0u;   // of this warp
+        const uint32_t n_tiles = t_end > t_begin + warp * kTile ? (t_end - t_begin - warp * kTile + W * kTile - 1u) / (W * kTile) : 0u;   // of this warp
 
         // tile i of this warp begins at token t_begin + (i * 8 + warp) * 32
         const int32_t *table = P.q.table + int64_t(b) * P.q.ldt;
         const uint32_t per_tile = P.q.page < kTile ? 2u : 1u, box = P.q.page < kTile ? P.q.page : kTile;
         auto page_of = [&](uint32_t i) {                  // lane 0 and 1: the page of the tile's first and second part, -1 if outside
-            const uint32_t t = t_begin + (i * kAttWarps + warp) * kTile + (lane & 1u) * box;
+            const uint32_t t = t_begin + (i * W + warp) * kTile + (lane & 1u) * box;
             int32_t id = -1;
             if (i < n_tiles && lane < per_tile && t < r.len) {
                 id = __ldg(table + (t >> P.q.shift));
@@ -289,7 +305,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_
             __syncwarp();
             if (lane < per_tile) {
                 // (a part without a page: rows past the cache's end, which arrive as zeros)
-                const uint32_t row = id < 0 ? P.q.pages * P.q.H << P.q.shift : ((uint32_t(id) * P.q.H + h) << P.q.shift) + ((t_begin + (i * kAttWarps + warp) * kTile) & (P.q.page - 1u));
+                const uint32_t row = id < 0 ? P.q.pages * P.q.H << P.q.shift : ((uint32_t(id) * P.q.H + h) << P.q.shift) + ((t_begin + (i * W + warp) * kTile) & (P.q.page - 1u));
                 tma_load_2d(at + lane * box * D, &k_map, 0, int32_t(row), bar);
                 tma_load_2d(at + S::kTileBytes + lane * box * D, &v_map, 0, int32_t(row), bar);
             }
@@ -367,7 +383,7 @@ __global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_
         }
 
         for (uint32_t i = 0; i < n_tiles; ++i) {
-            const uint32_t s = taken % S::kStages, at = ring + s * S::kStage, t0 = t_begin + (i * kAttWarps + warp) * kTile;
+            const uint32_t s = taken % S::kStages, at = ring + s * S::kStage, t0 = t_begin + (i * W + warp) * kTile;
             const bool ok = bar_wait(bars + 8 * s, (taken / S::kStages) & 1u, abort_at);
             ++taken;
             if (__all_sync(0xFFFFFFFFu, ok) && t0 < lim_max) {
@@ -429,10 +445,12 @@ __global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_
                         l[mt][half] *= alpha[half];
                         alpha[half] *= vmove;
                     }
+                    if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {          // (a maximum moves a few times per segment)
 #pragma unroll
-                    for (uint32_t d = 0; d < D / 8; ++d) {
-                        o[mt][d][0] *= alpha[0], o[mt][d][1] *= alpha[0];
-                        o[mt][d][2] *= alpha[1], o[mt][d][3] *= alpha[1];
+                        for (uint32_t d = 0; d < D / 8; ++d) {
+                            o[mt][d][0] *= alpha[0], o[mt][d][1] *= alpha[0];
+                            o[mt][d][2] *= alpha[1], o[mt][d][3] *= alpha[1];
+                        }
                     }
 #pragma unroll
                     for (uint32_t n = 0; n < 4; ++n) {
@@ -553,15 +571,15 @@ __global__ void __launch_bounds__(32 * kAttWarps, 1) attend_kernel(const __grid_
             }
         __syncthreads();
         const bool whole = first_unit == 0 && last_unit == per_seg;
-        for (uint32_t e = tid; e < kRows * D; e += 32 * kAttWarps) {
+        for (uint32_t e = tid; e < kRows * D; e += 32 * W) {
             const uint32_t row = e / D, d = e % D;
             float top = -INFINITY;
 #pragma unroll
-            for (uint32_t w = 0; w < kAttWarps; ++w) top = fmaxf(top, join[(w * kRows + row) * 4]);
+            for (uint32_t w = 0; w < W; ++w) top = fmaxf(top, join[(w * kRows + row) * 4]);
             const float ref = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f, acc = 0.0f;
 #pragma unroll
-            for (uint32_t w = 0; w < kAttWarps; ++w) {
+            for (uint32_t w = 0; w < W; ++w) {
                 const float4 j = *reinterpret_cast<const float4 *>(join + (w * kRows + row) * 4);
                 const float f = exp2_fast(j.x - ref);
                 sum += f * j.y;
@@ -611,49 +629,52 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
     const Extent r = extent_of(P.q, b);
     const float *all = P.workspace + size_t(P.grid) * kDescWords;
     const float *own = all + (size_t(blockIdx.x) * 2u + desc[4]) * kPiece<MT, D>;
-    for (uint32_t e = threadIdx.x; e < kRows * D; e += blockDim.x) {
-        const uint32_t row = e / D, d = e % D, at = tile * kRows + row, i = at / P.G, g = at % P.G;
-        if (at >= r.rows * P.G) break;
-        float top = own[kRows * D + row], sum = own[kRows * D + kRows + row], acc = own[row * D + d];
-        for (uint32_t c = blockIdx.x + 1u; c < end; ++c) {
-            const float *p = all + size_t(c) * 2u * kPiece<MT, D>;
-            const float m = p[kRows * D + row], now = fmaxf(top, m), ref = now == -INFINITY ? 0.0f : now;
-            const float f = exp2_fast(top - ref), g2 = exp2_fast(m - ref);
-            sum = sum * f + p[kRows * D + kRows + row] * g2;
-            acc = acc * f + p[row * D + d] * g2;
-            top = now;
-        }
-        const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
-        static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
-        if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
+    const uint32_t e = blockIdx.y * blockDim.x + threadIdx.x, row = e / D, d = e % D, at = tile * kRows + row, i = at / P.G, g = at % P.G;
+    if (at >= r.rows * P.G) return;
+    const float *first = all + size_t(blockIdx.x + 1u) * 2u * kPiece<MT, D>;
+    const uint32_t n = end - blockIdx.x - 1u;
+    const float own_top = own[kRows * D + row];
+    float top = own_top;
+#pragma unroll 8
+    for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPiece<MT, D> + kRows * D + row]);
+    const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(own_top - ref);
+    float sum = own[kRows * D + kRows + row] * f0, acc = own[row * D + d] * f0;
+#pragma unroll 8
+    for (uint32_t c = 0; c < n; ++c) {
+        const float *p = first + size_t(c) * 2u * kPiece<MT, D>;
+        const float f = exp2_fast(p[kRows * D + row] - ref);
+        sum += p[kRows * D + kRows + row] * f;
+        acc += p[row * D + d] * f;
     }
+    const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+    static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
 }
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
 
 // what both entry points check of the cache and the requests; fills q
-int check_cache(const ep_cache *c, const int32_t *table, int64_t ldt, uint32_t columns, const int32_t *seq_lens, const int32_t *starts, uint32_t B, uint32_t N,
-                Requests &q) {
-    if (!c || !c->d_k || !c->d_v || !c->d_k_scales || !c->d_v_scales || !table || !seq_lens || !starts) return EP_ERR_BAD_ARG;
-    if (c->pages == 0 || c->heads == 0 || columns == 0 || ldt < int64_t(columns) || N > 0x7FFFFFFFu) return EP_ERR_BAD_ARG;
-    if (!aligned(c->d_k, 16) || !aligned(c->d_v, 16) || !aligned(c->d_k_scales, 4) || !aligned(c->d_v_scales, 4) || !aligned(table, 4) || !aligned(seq_lens, 4) ||
-        !aligned(starts, 4))
+int check_cache(const ep_cache &c, const ep_requests &r, Requests &q) {
+    if (!c.d_k || !c.d_v || !c.d_k_scales || !c.d_v_scales || !r.d_table || !r.d_seq_lens || !r.d_starts) return EP_ERR_BAD_ARG;
+    if (c.pages == 0 || c.heads == 0 || r.columns == 0 || r.ldt < int64_t(r.columns) || r.N > 0x7FFFFFFFu) return EP_ERR_BAD_ARG;
+    if (!aligned(c.d_k, 16) || !aligned(c.d_v, 16) || !aligned(c.d_k_scales, 4) || !aligned(c.d_v_scales, 4) || !aligned(r.d_table, 4) ||
+        !aligned(r.d_seq_lens, 4) || !aligned(r.d_starts, 4))
         return EP_ERR_BAD_ARG;
-    if (c->page < 16 || c->page > 256 || (c->page & (c->page - 1u)) || (c->dim != 64 && c->dim != 128)) return EP_ERR_UNSUPPORTED;
-    if (c->pages >= (1u << 27) || c->heads >= (1u << 16) || uint64_t(c->pages) * c->heads * c->page >= (1ull << 31) - 256u || uint64_t(columns) * c->page >= (1ull << 31))
+    if (c.page < 16 || c.page > 256 || (c.page & (c.page - 1u)) || (c.dim != 64 && c.dim != 128)) return EP_ERR_UNSUPPORTED;
+    if (c.pages >= (1u << 27) || c.heads >= (1u << 16) || uint64_t(c.pages) * c.heads * c.page >= (1ull << 31) - 256u || uint64_t(r.columns) * c.page >= (1ull << 31))
         return EP_ERR_UNSUPPORTED;
-    q.table = table;
-    q.seq_lens = seq_lens;
-    q.starts = starts;
-    q.ldt = ldt;
-    q.B = B;
-    q.N = N;
-    q.columns = columns;
-    q.pages = c->pages;
-    q.page = c->page;
+    q.table = r.d_table;
+    q.seq_lens = r.d_seq_lens;
+    q.starts = r.d_starts;
+    q.ldt = r.ldt;
+    q.B = r.B;
+    q.N = r.N;
+    q.columns = r.columns;
+    q.pages = c.pages;
+    q.page = c.page;
     q.shift = 0;
-    while ((1u << q.shift) < c->page) ++q.shift;
-    q.H = c->heads;
+    while ((1u << q.shift) < c.page) ++q.shift;
+    q.H = c.heads;
     return EP_OK;
 }
 
@@ -672,9 +693,13 @@ uint32_t row_tiles_per_cta(uint32_t N, uint32_t G, uint32_t B) { return uint64_t
 
 template <class E, uint32_t MT, uint32_t D>
 int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
-    using S = AttendShape<MT, D>;
+#ifndef EP_W
+#define EP_W 8
+#endif
+    constexpr uint32_t W = MT == 1 ? EP_W : 8;
+    using S = AttendShape<MT, D, W>;
     static bool configured[64] = {};
-    int rc = op_configure(attend_kernel<E, MT, D>, S::kSmem, configured);
+    int rc = op_configure(attend_kernel<E, MT, D, W>, S::kSmem, configured);
     if (rc) return rc;
     CUtensorMap km, vm;
     const uint64_t rows = uint64_t(c.pages) * c.heads * c.page;
@@ -688,8 +713,8 @@ int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cud
     } else {
         P.workspace = nullptr;
     }
-    if (op_launch(attend_kernel<E, MT, D>, P.grid, 32 * kAttWarps, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
-    if (joined && op_launch(join_kernel<E, MT, D>, P.grid, 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    if (op_launch(attend_kernel<E, MT, D, W>, P.grid, 32 * W, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
+    if (joined && op_launch(join_kernel<E, MT, D>, dim3(P.grid, 16 * MT * D / 256), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
     return EP_OK;
 }
 
@@ -709,27 +734,28 @@ int ep::op8_status_cache() {
     return int(v);
 }
 
-extern "C" int ep_cache_append(const ep_cache *cache, const void *d_k, int64_t ldk, int64_t ldk_head, const void *d_v, int64_t ldv, int64_t ldv_head,
-                               int32_t dtype, const int32_t *d_table, int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B,
-                               uint32_t N, void *stream) {
+extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
+    if (!job) return EP_ERR_BAD_ARG;
+    const ep_append_job &j = *job;
+    const uint32_t B = j.requests.B, N = j.requests.N;
     if (B == 0 || N == 0) return EP_OK;
     AppendParams P;
     std::memset(&P, 0, sizeof(P));
-    const int rc = check_cache(cache, d_table, ldt, columns, d_seq_lens, d_starts, B, N, P.q);
+    const int rc = check_cache(j.cache, j.requests, P.q);
     if (rc) return rc;
-    if (!d_k || !d_v || (dtype != EP_BF16 && dtype != EP_FP16)) return EP_ERR_BAD_ARG;
-    if (!aligned(d_k, 16) || !aligned(d_v, 16) || ldk % 8 || ldk_head % 8 || ldv % 8 || ldv_head % 8) return EP_ERR_UNSUPPORTED;
-    P.x[0] = d_k, P.x[1] = d_v;
-    P.ldx[0] = ldk, P.ldx[1] = ldv;
-    P.ldh[0] = ldk_head, P.ldh[1] = ldv_head;
-    P.cache[0] = static_cast<uint8_t *>(cache->d_k), P.cache[1] = static_cast<uint8_t *>(cache->d_v);
-    P.scales[0] = cache->d_k_scales, P.scales[1] = cache->d_v_scales;
-    P.D = cache->dim;
+    if (!j.d_k || !j.d_v || (j.dtype != EP_BF16 && j.dtype != EP_FP16)) return EP_ERR_BAD_ARG;
+    if (!aligned(j.d_k, 16) || !aligned(j.d_v, 16) || j.ldk % 8 || j.ldk_head % 8 || j.ldv % 8 || j.ldv_head % 8) return EP_ERR_UNSUPPORTED;
+    P.x[0] = j.d_k, P.x[1] = j.d_v;
+    P.ldx[0] = j.ldk, P.ldx[1] = j.ldv;
+    P.ldh[0] = j.ldk_head, P.ldh[1] = j.ldv_head;
+    P.cache[0] = static_cast<uint8_t *>(j.cache.d_k), P.cache[1] = static_cast<uint8_t *>(j.cache.d_v);
+    P.scales[0] = j.cache.d_k_scales, P.scales[1] = j.cache.d_v_scales;
+    P.D = j.cache.dim;
     // as many pages side by side as a request of average length touches; a longer one's take turns
     const uint64_t average = (uint64_t(N) + B - 1u) / B;
-    P.spans = uint32_t(average > 1 ? (average - 1u) / cache->page + 2u : 1u);
+    P.spans = uint32_t(average > 1 ? (average - 1u) / j.cache.page + 2u : 1u);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return dtype == EP_BF16 ? launch_append<Bf16>(P, st) : launch_append<Fp16>(P, st);
+    return j.dtype == EP_BF16 ? launch_append<Bf16>(P, st) : launch_append<Fp16>(P, st);
 }
 
 extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim) {
@@ -739,36 +765,39 @@ extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uin
     return size_t(sms) * (kDescWords + 2u * rows * (size_t(dim) + 2u)) * 4u;
 }
 
-extern "C" int ep_cache_attention(const ep_cache *cache, const void *d_q, int64_t ldq, int64_t ldq_head, int32_t dtype, uint32_t q_heads, const int32_t *d_table,
-                                  int64_t ldt, uint32_t columns, const int32_t *d_seq_lens, const int32_t *d_starts, uint32_t B, uint32_t N, float scale,
-                                  int32_t causal, void *d_o, int64_t ldo, int64_t ldo_head, float *d_lse, void *d_workspace, size_t workspace_bytes, void *stream) {
+extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
+    if (!job) return EP_ERR_BAD_ARG;
+    const ep_attention_job &j = *job;
+    const ep_cache &c = j.cache;
+    const uint32_t B = j.requests.B, N = j.requests.N;
     if (B == 0 || N == 0) return EP_OK;
     AttendParams P;
     std::memset(&P, 0, sizeof(P));
-    int rc = check_cache(cache, d_table, ldt, columns, d_seq_lens, d_starts, B, N, P.q);
+    const int rc = check_cache(c, j.requests, P.q);
     if (rc) return rc;
-    if (!d_q || !d_o || (dtype != EP_BF16 && dtype != EP_FP16) || q_heads == 0 || q_heads % cache->heads || (d_lse && !aligned(d_lse, 4))) return EP_ERR_BAD_ARG;
-    if (!aligned(d_q, 16) || ldq % 8 || ldq_head % 8 || !aligned(d_o, 16) || ldo % 8 || ldo_head % 8 || B > kMaxRequests) return EP_ERR_UNSUPPORTED;
-    P.x = d_q;
-    P.o = d_o;
-    P.lse = d_lse;
-    P.ks = cache->d_k_scales;
-    P.vs = cache->d_v_scales;
-    P.ldq = ldq;
-    P.ldqh = ldq_head;
-    P.ldo = ldo;
-    P.ldoh = ldo_head;
-    P.Hq = q_heads;
-    P.G = q_heads / cache->heads;
-    P.scale_log2 = scale * 1.4426950408889634f;
-    P.causal = causal ? 1u : 0u;
-    P.workspace = static_cast<float *>(d_workspace);
+    if (!j.d_q || !j.d_o || (j.dtype != EP_BF16 && j.dtype != EP_FP16) || j.q_heads == 0 || j.q_heads % c.heads || (j.d_lse && !aligned(j.d_lse, 4))) return EP_ERR_BAD_ARG;
+    if (!aligned(j.d_q, 16) || j.ldq % 8 || j.ldq_head % 8 || !aligned(j.d_o, 16) || j.ldo % 8 || j.ldo_head % 8 || B > kMaxRequests) return EP_ERR_UNSUPPORTED;
+    P.x = j.d_q;
+    P.o = j.d_o;
+    P.lse = j.d_lse;
+    P.ks = c.d_k_scales;
+    P.vs = c.d_v_scales;
+    P.ldq = j.ldq;
+    P.ldqh = j.ldq_head;
+    P.ldo = j.ldo;
+    P.ldoh = j.ldo_head;
+    P.Hq = j.q_heads;
+    P.G = j.q_heads / c.heads;
+    P.scale_log2 = j.scale * 1.4426950408889634f;
+    P.causal = j.causal ? 1u : 0u;
+    P.workspace = static_cast<float *>(j.d_workspace);
     // units are counted in 32 bits
-    const uint64_t rows = 16u * row_tiles_per_cta(N, P.G, B), units = ((uint64_t(columns) * cache->page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * cache->heads;
+    const uint64_t rows = 16u * row_tiles_per_cta(N, P.G, B),
+                   units = ((uint64_t(P.q.columns) * c.page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * c.heads;
     if (units >= (1ull << 31) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
     P.grid = uint32_t(sms);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    return dtype == EP_BF16 ? launch_attend<Bf16>(P, *cache, workspace_bytes, st) : launch_attend<Fp16>(P, *cache, workspace_bytes, st);
+    return j.dtype == EP_BF16 ? launch_attend<Bf16>(P, c, j.workspace_bytes, st) : launch_attend<Fp16>(P, c, j.workspace_bytes, st);
 }

@@ -51,6 +51,8 @@ struct Bf16 {
     static __device__ __forceinline__ float hi(uint32_t w) { return __uint_as_float(w & 0xFFFF0000u); }
     static __device__ __forceinline__ T of(float f) { return __float2bfloat16_rn(f); }
     static __device__ __forceinline__ float to(T v) { return __bfloat162float(v); }
+    static __device__ __forceinline__ uint32_t bits(T v) { return __bfloat16_as_ushort(v); }
+    static __device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b << 16); }
     static __device__ __forceinline__ uint32_t two(float lo, float hi) {
         uint32_t r;
         asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -63,6 +65,8 @@ struct Fp16 {
     static __device__ __forceinline__ float hi(uint32_t w) { return __half2float(__ushort_as_half(uint16_t(w >> 16))); }
     static __device__ __forceinline__ T of(float f) { return __float2half_rn(f); }
     static __device__ __forceinline__ float to(T v) { return __half2float(v); }
+    static __device__ __forceinline__ uint32_t bits(T v) { return __half_as_ushort(v); }
+    static __device__ __forceinline__ float of_bits(uint32_t b) { return __half2float(__ushort_as_half(uint16_t(b))); }
     static __device__ __forceinline__ uint32_t two(float lo, float hi) {
         uint32_t r;
         asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
@@ -73,6 +77,8 @@ struct Fp32 {
     using T = float;
     static __device__ __forceinline__ T of(float f) { return f; }
     static __device__ __forceinline__ float to(T v) { return v; }
+    static __device__ __forceinline__ uint32_t bits(T v) { return __float_as_uint(v); }
+    static __device__ __forceinline__ float of_bits(uint32_t b) { return __uint_as_float(b); }
 };
 
 // ---- shared memory, barriers -----------------------------------------------------------------------------------------
@@ -132,7 +138,7 @@ __device__ __forceinline__ void op_wait_for_stream() {
 // A launch that may come up while the kernel before it still runs (`kernel` begins with op_wait_for_stream), in clusters of
 // `cluster` CTAs.
 template <class... A>
-inline cudaError_t op_launch(void (*kernel)(A...), uint32_t grid, uint32_t threads, uint32_t smem, uint32_t cluster, cudaStream_t st, const A &...args) {
+inline cudaError_t op_launch(void (*kernel)(A...), dim3 grid, uint32_t threads, uint32_t smem, uint32_t cluster, cudaStream_t st, const A &...args) {
     cudaLaunchAttribute attr[2]{};
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
@@ -140,7 +146,7 @@ inline cudaError_t op_launch(void (*kernel)(A...), uint32_t grid, uint32_t threa
     attr[1].val.clusterDim.x = cluster;
     attr[1].val.clusterDim.y = attr[1].val.clusterDim.z = 1;
     cudaLaunchConfig_t cfg{};
-    cfg.gridDim = dim3(grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(threads);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = st;

@@ -646,24 +646,36 @@ def test_refusals():
 
 def test_entry_points_refuse_without_a_gpu():
     """The C entry points check their arguments before they touch a device: statuses, not crashes."""
-    L = ep.load()
+    L, B = ep.load(), ep.binding
     p = 1 << 20                                           # an address that is never read
-    assert L.ep_quantize_blocks(None, ep.BF16, 4, 4, 4, 1, p, 4, p, 1, None) == -1
-    assert L.ep_quantize_blocks(p, ep.INT8, 4, 4, 4, 1, p, 4, p, 1, None) == -1
-    assert L.ep_quantize_blocks(p, ep.BF16, 4, 4, 3, 1, p, 4, p, 1, None) == -1
-    assert L.ep_quantize_blocks(p, ep.BF16, 4, 4, 4, 2, p, 4, p, 1, None) == -1
-    assert L.ep_quantize_blocks(p + 1, ep.BF16, 4, 4, 4, 1, p, 4, p, 1, None) == -1
-    assert L.ep_quantize_blocks(None, ep.BF16, 0, 4, 4, 1, None, 4, None, 1, None) == 0
-    mm = lambda x=p, ldx=256, w=p, ldw=256, C=256, dt=ep.BF16, ldy=64, lds=2, T=4: L.ep_fp8_matmul(x, ldx, p, lds, w, ldw, None, 0, None, T, 64, C, dt, p, ldy, None)  # noqa: E731
-    assert mm(x=None) == -1 and mm(ldx=255) == -1 and mm(dt=ep.INT8) == -1 and mm(ldy=63) == -1 and mm(lds=1) == -1 and mm(T=0) == 0
-    assert mm(C=248) == -3 and mm(ldx=264) == -3 and mm(w=p + 8) == -3
-    c = ep.binding.Cache(p, p, p, p, 4, 2, 16, 64)
-    ap = lambda c=c, ldk=128, ldh=64, dt=ep.BF16, t=p, cols=2, B=1, N=1: L.ep_cache_append(c, p, ldk, ldh, p, ldk, ldh, dt, t, 2, cols, p, p, B, N, None)  # noqa: E731
-    assert ap(t=None) == -1 and ap(cols=3) == -1 and ap(dt=ep.FP32) == -1 and ap(ldk=129) == -3 and ap(B=0) == 0 and ap(N=0) == 0
-    for field, value, status in (("page", 24, -3), ("page", 512, -3), ("dim", 96, -3), ("pages", 0, -1), ("pages", 1 << 28, -3), ("d_k", p + 8, -1)):
-        odd = ep.binding.Cache(p, p, p, p, 4, 2, 16, 64)
-        setattr(odd, field, value)
-        assert ap(c=odd) == status, field
-    at = lambda heads=4, ldq=256, B=1, dt=ep.BF16: L.ep_cache_attention(c, p, ldq, 64, dt, heads, p, 2, 2, p, p, B, 1, 1.0, 1, p, 256, 64, None, None, 0, None)  # noqa: E731
-    assert at(heads=3) == -1 and at(heads=0) == -1 and at(dt=ep.FP32) == -1 and at(ldq=255) == -3 and at(B=5000) == -3
+
+    def checked(layout, call, names, **fine):
+        def f(**other):
+            values = {**fine, **other}
+            return call(layout.pack(*(values[n] for n in names.split())), None)
+        return f
+
+    quantize = checked(B.QUANTIZE_JOB, L.ep_quantize_blocks, "x q s ldx ldq lds T C rows dtype", x=p, q=p, s=p, ldx=4, ldq=4, lds=1, T=4, C=4, rows=1, dtype=ep.BF16)
+    for other in ({"x": 0}, {"q": 0}, {"s": 0}, {"dtype": ep.INT8}, {"ldx": 3}, {"ldq": 3}, {"lds": 0}, {"rows": 2}, {"x": p + 1}, {"C": 0}):
+        assert quantize(**other) == -1, other
+    assert quantize(T=0, x=0) == 0 and L.ep_quantize_blocks(None, None) == -1
+    matmul = checked(B.MATMUL_JOB, L.ep_fp8_matmul, "x xs w ws a y ldx ldxs ldw ldws ldy T R C dtype", x=p, xs=p, w=p, ws=0, a=0, y=p, ldx=256, ldxs=2, ldw=256, ldws=0, ldy=64,
+                     T=4, R=64, C=256, dtype=ep.BF16)
+    for other in ({"x": 0}, {"xs": 0}, {"w": 0}, {"y": 0}, {"ldx": 255}, {"dtype": ep.INT8}, {"ldy": 63}, {"ldxs": 1}, {"ws": p, "ldws": 1}, {"y": p + 1}, {"a": p + 2}):
+        assert matmul(**other) == -1, other
+    for other in ({"C": 248}, {"ldx": 264}, {"ldw": 264}, {"w": p + 8}, {"x": p + 8}):
+        assert matmul(**other) == -3, other
+    assert matmul(T=0) == 0 and L.ep_fp8_matmul(None, None) == -1
+    shared = dict(k=p, v=p, ks=p, vs=p, pages=4, heads=2, page=16, dim=64, table=p, lens=p, starts=p, ldt=2, columns=2, B=1, N=1)
+    head = "k v ks vs pages heads page dim table lens starts ldt columns B N "
+    append = checked(B.APPEND_JOB, L.ep_cache_append, head + "xk xv ldk ldkh ldv ldvh dtype", xk=p, xv=p, ldk=128, ldkh=64, ldv=128, ldvh=64, dtype=ep.BF16, **shared)
+    attend = checked(B.ATTENTION_JOB, L.ep_cache_attention, head + "q o lse ws bytes ldq ldqh ldo ldoh scale Hq dtype causal", q=p, o=p, lse=0, ws=0, bytes=0, ldq=256, ldqh=64,
+                     ldo=256, ldoh=64, scale=1.0, Hq=4, dtype=ep.BF16, causal=1, **shared)
+    for call in (append, attend):
+        for other, status in (({"k": 0}, -1), ({"vs": 0}, -1), ({"table": 0}, -1), ({"columns": 3}, -1), ({"columns": 0}, -1), ({"dtype": ep.FP32}, -1), ({"pages": 0}, -1), ({"k": p + 8}, -1),
+                              ({"lens": p + 2}, -1), ({"page": 24}, -3), ({"page": 512}, -3), ({"page": 8}, -3), ({"dim": 96}, -3), ({"pages": 1 << 28}, -3), ({"heads": 1 << 20}, -3)):
+            assert call(**other) == status, other
+        assert call(B=0) == 0 and call(N=0, k=0) == 0
+    assert append(ldk=129) == -3 and append(ldvh=4) == -3 and append(xk=p + 8) == -3 and append(xv=0) == -1 and L.ep_cache_append(None, None) == -1
+    assert attend(Hq=3) == -1 and attend(Hq=0) == -1 and attend(ldq=255) == -3 and attend(o=p + 8) == -3 and attend(B=5000, ldt=2) == -3 and L.ep_cache_attention(None, None) == -1
     assert "page" in ep.strerror(-9)
