@@ -227,12 +227,6 @@ struct MatmulParams {
     uint32_t split;               // CTAs (one cluster) that share a tile's columns
 };
 
-__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-// rows of 128 bytes, 128-byte swizzle, groups of eight rows 1024 bytes apart
-__device__ __forceinline__ uint64_t operand_desc(uint32_t addr) {
-    return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
-}
 // 32 rows of 16 bytes without swizzle: eight rows, 128 bytes, are a unit
 __device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
     return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
@@ -245,17 +239,6 @@ __device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, u
                  "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
 }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
-    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
-                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7]), "=r"(v[8]), "=r"(v[9]),
-                   "=r"(v[10]), "=r"(v[11]), "=r"(v[12]), "=r"(v[13]), "=r"(v[14]), "=r"(v[15])
-                 : "r"(tmem));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
-}
-
 // E4M3 x E4M3, both K-major, E8M0 scales, M = 128, N = n; `word` = which byte of the scale words
 __host__ __device__ constexpr uint32_t scaled_idesc(uint32_t n, uint32_t word) {
     return (word << 4) | ((n >> 3) << 17) | (1u << 23) | ((128u >> 4) << 24) | (word << 29);
@@ -387,6 +370,7 @@ __global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant
             if (t0 + c >= P.T) break;
             uint32_t v[16];
             tc_load16(tmem + ((warp * 32u) << 16) + c, v);
+            tc_loaded();
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i)
                 if (r < P.R && t0 + c + i < P.T) y[int64_t(t0 + c + i) * P.ldy] = E::of(__uint_as_float(v[i]) * a);
@@ -397,6 +381,7 @@ __global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant
         for (uint32_t c = 0; c < BN; c += 16) {
             uint32_t v[16];
             tc_load16(tmem + ((warp * 32u) << 16) + c, v);
+            tc_loaded();
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i) st_smem(base + ((c + i) * 128u + tid) * 4u, v[i]);
         }

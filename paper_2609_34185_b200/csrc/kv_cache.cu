@@ -1,29 +1,12 @@
 // Keys and values in pages of E4M3 with one scale for each page and head: writing new tokens, and the attention that
 // reads the pages.
-#include "op8.hpp"
+#include "kv_cache.hpp"
 
 using namespace ep;
 
 namespace {
 
 __device__ unsigned int g_cache_status = 0;
-
-// What both operators read: where the requests' tokens stand.  Request b has seq_lens[b] tokens in the cache, the last
-// starts[b + 1] - starts[b] of which are its rows of the call; token j lies in page table[b][j / page], row j % page.
-struct Requests {
-    const int32_t *table, *seq_lens, *starts;
-    int64_t ldt;
-    uint32_t B, N, columns;       // requests; rows of the call; columns of the table
-    uint32_t pages, page, shift;  // pages of the cache, tokens of a page = 1 << shift
-    uint32_t H;                   // heads of the cache
-};
-// rows and tokens of request b; whatever the arrays hold, rows lie inside the call's and tokens inside the table
-struct Extent { uint32_t row, rows, len; };
-__device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
-    const uint32_t lo = uint32_t(min(max(__ldg(q.starts + b), 0), int32_t(q.N))), hi = uint32_t(min(max(__ldg(q.starts + b + 1), int32_t(lo)), int32_t(q.N)));
-    const uint64_t room = uint64_t(q.columns) << q.shift;
-    return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(__ldg(q.seq_lens + b), 0))), room))};
-}
 
 // ======================================================================================================================
 // Append.  For a page and head with scale s and older tokens q: s' = max(s, the smallest power of two that holds the new tokens), the
@@ -151,22 +134,8 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // below the row's largest, whose rounding is below fp32's own.  The weights w carry a factor 2^14 (their largest, 2^14, is within binary16's range) so that
 // those down to 2^-28 of the largest keep 11 bits.  A page's value scale is moved onto w as v_scale / the largest so far.
 // ======================================================================================================================
-constexpr uint32_t kTile = 32, kUnit = 256, kMaxRequests = 4096;
+constexpr uint32_t kTile = 32, kUnit = 256;
 constexpr float kWeightShift = 14.0f;
-
-struct AttendParams {
-    Requests q;
-    const void *x;
-    void *o;
-    float *lse;                   // may be null
-    const float *ks, *vs;
-    int64_t ldq, ldqh, ldo, ldoh;
-    uint32_t Hq, G;               // query heads; per head of the cache
-    float scale_log2;             // scale * log2(e)
-    uint32_t causal;
-    float *workspace;             // null: no segment can cross a share
-    uint32_t grid;
-};
 
 // where a piece of a segment is left: O, then m and l of each row
 template <uint32_t MT, uint32_t D>
@@ -190,11 +159,6 @@ __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float exp2_fast(float x) {
-    float r;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
-    return r;
-}
 __device__ __forceinline__ float quad_max(float v) {
     v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
     return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
@@ -204,36 +168,9 @@ __device__ __forceinline__ float quad_sum(float v) {
     return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
 }
 
-// prefix[b] = units of the requests before b; returns all
 __device__ __forceinline__ uint32_t units_of(const Extent &r, uint32_t G, uint32_t H, uint32_t rows_per_tile) {
     const uint32_t tiles = (r.rows * G + rows_per_tile - 1u) / rows_per_tile;
     return tiles * H * max(1u, (r.len + kUnit - 1u) / kUnit);
-}
-__device__ uint32_t prefix_units(const Requests &q, uint32_t G, uint32_t rows_per_tile, uint32_t *prefix, uint32_t *part) {
-    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, per = (q.B + blockDim.x - 1u) / blockDim.x;
-    const uint32_t b0 = min(tid * per, q.B), b1 = min(b0 + per, q.B);
-    uint32_t sum = 0;
-    for (uint32_t b = b0; b < b1; ++b) sum += units_of(extent_of(q, b), G, q.H, rows_per_tile);
-    uint32_t inc = sum;
-#pragma unroll
-    for (uint32_t d = 1; d < 32; d <<= 1) {
-        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
-        if (lane >= d) inc += o;
-    }
-    if (lane == 31) part[warp] = inc;
-    __syncthreads();
-    uint32_t at = inc - sum, all = 0;
-    for (uint32_t w = 0; w < (blockDim.x >> 5); ++w) {
-        if (w < warp) at += part[w];
-        all += part[w];
-    }
-    for (uint32_t b = b0; b < b1; ++b) {
-        prefix[b] = at;
-        at += units_of(extent_of(q, b), G, q.H, rows_per_tile);
-    }
-    if (tid == 0) prefix[q.B] = all;
-    __syncthreads();
-    return all;
 }
 
 template <class E, uint32_t MT, uint32_t D, uint32_t W>
@@ -256,7 +193,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
     }
     if (tid == 0) st_smem(abort_at, 0);
     op_wait_for_stream();
-    const uint32_t all = prefix_units(P.q, P.G, kRows, prefix, reinterpret_cast<uint32_t *>(join));
+    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t i) { return units_of(extent_of(P.q, i), P.G, P.q.H, kRows); }, prefix, reinterpret_cast<uint32_t *>(join));
     const uint32_t ctas = min(P.grid, all);               // those with a share: none of theirs is empty
     const uint32_t u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
                    u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
@@ -268,14 +205,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
     uint32_t b = 0;
     for (uint32_t u = u_begin; u < u_end;) {
         // ---- the segment of unit u ------------------------------------------------------------------------------------
-        {
-            uint32_t lo = b, hi = P.q.B;                  // the last request whose units begin at or before u
-            while (hi - lo > 1u) {
-                const uint32_t mid = (lo + hi) >> 1;
-                if (prefix[mid] <= u) lo = mid; else hi = mid;
-            }
-            b = lo;
-        }
+        b = request_of(prefix, b, P.q.B, u);
         const Extent r = extent_of(P.q, b);
         const uint32_t per_seg = max(1u, (r.len + kUnit - 1u) / kUnit), seg = (u - prefix[b]) / per_seg, first_unit = (u - prefix[b]) % per_seg;
         const uint32_t last_unit = min(per_seg, first_unit + (u_end - u));       // one past the share's last unit of the segment
@@ -728,10 +658,12 @@ int launch_attend(const AttendParams &P, const ep_cache &c, size_t workspace_byt
 }  // namespace
 
 int ep::op8_status_cache() {
+    const int more = op8_status_prompts();
+    if (more < 0) return more;
     unsigned int v = 0, zero = 0;
     if (cudaMemcpyFromSymbol(&v, g_cache_status, sizeof(v)) != cudaSuccess) return -1;
     if (v && cudaMemcpyToSymbol(g_cache_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
-    return int(v);
+    return int(v) | more;
 }
 
 extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
@@ -798,6 +730,9 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
     P.grid = uint32_t(sms);
+    P.k = static_cast<const uint8_t *>(c.d_k);
+    P.v = static_cast<const uint8_t *>(c.d_v);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (prompts_serve(N, B, P.G, c.heads)) return launch_prompts(P, c.dim, j.dtype, st);
     return j.dtype == EP_BF16 ? launch_attend<Bf16>(P, c, j.workspace_bytes, st) : launch_attend<Fp16>(P, c, j.workspace_bytes, st);
 }

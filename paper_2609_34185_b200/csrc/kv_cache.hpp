@@ -1,0 +1,94 @@
+// What the kernels of the paged cache share.
+#pragma once
+#include "op8.hpp"
+
+namespace ep {
+
+#ifdef __CUDACC__
+
+// What both operators read: where the requests' tokens stand.  Request b has seq_lens[b] tokens in the cache, the last
+// starts[b + 1] - starts[b] of which are its rows of the call; token j lies in page table[b][j / page], row j % page.
+struct Requests {
+    const int32_t *table, *seq_lens, *starts;
+    int64_t ldt;
+    uint32_t B, N, columns;       // requests; rows of the call; columns of the table
+    uint32_t pages, page, shift;  // pages of the cache, tokens of a page = 1 << shift
+    uint32_t H;                   // heads of the cache
+};
+// rows and tokens of request b; whatever the arrays hold, rows lie inside the call's and tokens inside the table
+struct Extent { uint32_t row, rows, len; };
+__device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
+    const uint32_t lo = uint32_t(min(max(__ldg(q.starts + b), 0), int32_t(q.N))), hi = uint32_t(min(max(__ldg(q.starts + b + 1), int32_t(lo)), int32_t(q.N)));
+    const uint64_t room = uint64_t(q.columns) << q.shift;
+    return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(__ldg(q.seq_lens + b), 0))), room))};
+}
+
+// ---- softmax in powers of two -------------------------------------------------------------------------------------------
+__device__ __forceinline__ float exp2_fast(float x) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+
+// prefix[b] = the sum of units(b') over b' < b, prefix[B] = all; by a whole CTA of at most 32 warps.  Returns all.
+template <class F>
+__device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t *prefix, uint32_t *part) {
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, per = (B + blockDim.x - 1u) / blockDim.x;
+    const uint32_t b0 = min(tid * per, B), b1 = min(b0 + per, B);
+    uint32_t sum = 0;
+    for (uint32_t b = b0; b < b1; ++b) sum += units(b);
+    uint32_t inc = sum;
+#pragma unroll
+    for (uint32_t d = 1; d < 32; d <<= 1) {
+        const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+        if (lane >= d) inc += o;
+    }
+    if (lane == 31) part[warp] = inc;
+    __syncthreads();
+    uint32_t at = inc - sum, all = 0;
+    for (uint32_t w = 0; w < (blockDim.x >> 5); ++w) {
+        if (w < warp) at += part[w];
+        all += part[w];
+    }
+    for (uint32_t b = b0; b < b1; ++b) {
+        prefix[b] = at;
+        at += units(b);
+    }
+    if (tid == 0) prefix[B] = all;
+    __syncthreads();
+    return all;
+}
+// the last b in [lo, B) with prefix[b] <= u (prefix[lo] <= u < prefix[B]): its units hold u
+__device__ __forceinline__ uint32_t request_of(const uint32_t *prefix, uint32_t lo, uint32_t B, uint32_t u) {
+    uint32_t hi = B;
+    while (hi - lo > 1u) {
+        const uint32_t mid = (lo + hi) >> 1;
+        if (prefix[mid] <= u) lo = mid; else hi = mid;
+    }
+    return lo;
+}
+constexpr uint32_t kMaxRequests = 4096;
+
+struct AttendParams {
+    Requests q;
+    const void *x;
+    void *o;
+    float *lse;                   // may be null
+    const float *ks, *vs;
+    const uint8_t *k, *v;
+    int64_t ldq, ldqh, ldo, ldoh;
+    uint32_t Hq, G;               // query heads; per head of the cache
+    float scale_log2;             // scale * log2(e)
+    uint32_t causal;
+    float *workspace;             // null: no segment can cross a share
+    uint32_t grid;
+};
+
+// many rows per request (attend_prompts.cu): true if this call's shape is worth it
+bool prompts_serve(uint32_t N, uint32_t B, uint32_t G, uint32_t H);
+int launch_prompts(const AttendParams &P, uint32_t dim, int32_t dtype, cudaStream_t st);
+int op8_status_prompts();
+
+#endif  // __CUDACC__
+
+}  // namespace ep

@@ -8,6 +8,7 @@
 
 #include <cstdint>
 #include <cstring>
+#include <type_traits>
 
 #include "entropack.h"
 
@@ -127,6 +128,42 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
+
+
+// ---- tensor cores ------------------------------------------------------------------------------------------------------
+__device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void tc_commit(uint32_t bar) {
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+// Operands of rows of 128 bytes with 128-byte swizzle, groups of eight rows 1024 bytes apart.  K-major: a row is a row of the
+// operand.  MN-major: a row is one k, its 128 bytes 64 16-bit values along M or N; `lead` bytes to the next 64 of those.
+__device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lead = 16) {
+    return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(lead >> 4) << 16) | (uint64_t(1024 >> 4) << 32) | (uint64_t(1) << 46) | (uint64_t(2) << 61);
+}
+#define EP_R8(v, i) "=r"(v[i]), "=r"(v[i + 1]), "=r"(v[i + 2]), "=r"(v[i + 3]), "=r"(v[i + 4]), "=r"(v[i + 5]), "=r"(v[i + 6]), "=r"(v[i + 7])
+#define EP_I8(v, i) "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]), "r"(v[i + 4]), "r"(v[i + 5]), "r"(v[i + 6]), "r"(v[i + 7])
+// a warp's quarter of tensor memory: lane = row, registers = columns.  Loads are complete after tc_loaded, stores after tc_stored
+__device__ __forceinline__ void tc_load16(uint32_t tmem, uint32_t (&v)[16]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+                 : EP_R8(v, 0), EP_R8(v, 8) : "r"(tmem));
+}
+__device__ __forceinline__ void tc_load32(uint32_t tmem, uint32_t (&v)[32]) {
+    asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
+                 "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+                 : EP_R8(v, 0), EP_R8(v, 8), EP_R8(v, 16), EP_R8(v, 24) : "r"(tmem));
+}
+__device__ __forceinline__ void tc_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ void tc_store16(uint32_t tmem, const uint32_t (&v)[16]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
+                 ::EP_I8(v, 0), EP_I8(v, 8), "r"(tmem) : "memory");
+}
+__device__ __forceinline__ void tc_store32(uint32_t tmem, const uint32_t (&v)[32]) {
+    asm volatile("tcgen05.st.sync.aligned.32x32b.x32.b32 [%32], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, "
+                 "%21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31};"
+                 ::EP_I8(v, 0), EP_I8(v, 8), EP_I8(v, 16), EP_I8(v, 24), "r"(tmem) : "memory");
+}
+__device__ __forceinline__ void tc_stored() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 
 // ends when everything earlier in the stream has; before it nothing is read or written
 __device__ __forceinline__ void op_wait_for_stream() {

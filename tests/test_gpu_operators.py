@@ -679,3 +679,93 @@ def test_entry_points_refuse_without_a_gpu():
     assert append(ldk=129) == -3 and append(ldvh=4) == -3 and append(xk=p + 8) == -3 and append(xv=0) == -1 and L.ep_cache_append(None, None) == -1
     assert attend(Hq=3) == -1 and attend(Hq=0) == -1 and attend(ldq=255) == -3 and attend(o=p + 8) == -3 and attend(B=5000, ldt=2) == -3 and L.ep_cache_attention(None, None) == -1
     assert "page" in ep.strerror(-9)
+
+
+PROMPTS = [  # heads per group, heads, dim, page, tokens, rows: enough rows for the kernel of prompts
+    (8, 4, 128, 64, [300], [300]), (5, 8, 128, 64, [1000], [260]), (4, 8, 64, 16, [129, 700, 300], [129, 200, 1]), (1, 16, 128, 16, [700, 0, 640], [650, 3, 0]),
+    (8, 8, 128, 256, [140, 128], [140, 128]), (16, 16, 64, 32, [257], [70]), (3, 16, 128, 128, [90, 555], [200, 300]), (2, 32, 64, 64, [385], [384]),
+]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("G,H,D,page,lens,news", PROMPTS)
+@pytest.mark.parametrize("causal", [True, False])
+def test_attention_of_prompts(G, H, D, page, lens, news, causal, dtype):
+    # (a few heads are looked at: the oracle is slow)
+    cache, table = filled(lens, H, D, page, seed=G + D + page + len(lens))
+    starts = offsets(news)
+    q = torch.randn(starts[-1], G * H, D, generator=cuda(D), device="cuda").mul_(1.5).to(dtype)
+    lse = torch.full((starts[-1], G * H), 7.0, device="cuda")
+    out = torch.full_like(q, 9.0)
+    ep.cache_attention(q, cache, ints(table), ints(lens), ints(starts), scale=-0.2 if H == 4 else 0.2, causal=causal, out=out, lse=lse)
+    for h in {0, H // 2, H - 1}:
+        part = [t[:, h:h + 1].contiguous() for t in cache]
+        at = slice(h * G, (h + 1) * G)
+        want, bound, want_lse = attended(q[:, at], part, table, lens, starts, -0.2 if H == 4 else 0.2, causal)
+        check_attention(out[:, at], want, bound)
+        seen = want_lse > -math.inf
+        assert torch.equal(lse[:, at].cpu() > -math.inf, seen)
+        assert bool(((lse[:, at].double().cpu() - want_lse)[seen].abs() <= 1e-3).all())
+    assert ep.last_device_status() == 0
+
+
+@gpu
+def test_attention_of_prompts_with_nan_and_pages_outside():
+    G, H, lens, news = 8, 8, [300, 200, 420], [160, 140, 130]
+    starts = offsets(news)
+    cache, table = filled(lens, H, 128, 32, seed=31)
+    for t in (cache.k, cache.v):
+        t.view(torch.uint8)[table[0][8], :, 5, 9] = 0x7F       # token 261 of the first request: seen by its last 39 rows
+    cache.v.view(torch.uint8)[table[0][9], :, 3, 100] = 0xFF   # token 291, another column
+    cache.v.view(torch.uint8)[table[2][1], :, 0, 77] = 0x7F    # token 32 of the third: every row sees it
+    bad = [row[:] for row in table]
+    bad[1][2], bad[1][6] = 10 ** 8, -1
+    q = torch.randn(starts[-1], G * H, 128, generator=cuda(9), device="cuda").to(torch.bfloat16)
+    out = ep.cache_attention(q, cache, ints(bad), ints(lens), ints(starts))
+    assert ep.last_device_status() == -9
+    for h in (0, 5):
+        at = slice(h * G, (h + 1) * G)
+        want, bound, _ = attended(q[:, at], [t[:, h:h + 1].contiguous() for t in cache], bad, lens, starts, 128 ** -0.5, True, dead=(10 ** 8, -1))
+        assert want[121:160].isnan().all() and not want[:121].isnan().any() and want[-130:, :, 77].isnan().all() and want[-130:].isnan().sum() == 130 * G
+        check_attention(out[:, at], want, bound)
+
+
+@gpu
+def test_attention_of_prompts_scores_far_apart():
+    lens, news, G, H = [700], [260], 8, 8
+    cache, table = filled(lens, H, 128, 64, seed=13)
+    cache.k.view(torch.uint8)[table[0][5], :, 60] = 0x70       # 128 everywhere, in a late tile: the reference moves
+    cache.k.view(torch.uint8)[table[0][0], :, 3] = 0xF0        # -128 everywhere
+    size = torch.exp2(torch.linspace(-60, 6, 260, device="cuda"))[:, None, None]
+    for dtype in (torch.bfloat16, torch.float16):
+        q = (torch.randn(260, G * H, 128, generator=cuda(4), device="cuda").abs() * size).to(dtype)
+        out = ep.cache_attention(q, cache, ints(table), ints(lens), ints([0, 260]))
+        for h in (0, 7):
+            at = slice(h * G, (h + 1) * G)
+            want, bound, _ = attended(q[:, at], [t[:, h:h + 1].contiguous() for t in cache], table, lens, [0, 260], 128 ** -0.5, True)
+            check_attention(out[:, at], want, bound)
+
+
+@gpu
+def test_attention_of_prompts_many_units_and_captured():
+    # more units than SMs, several per CTA; the same bits again, from a graph and with other lengths
+    lens, news, G, H = [900, 300, 450, 130], [400, 300, 350, 64], 4, 32
+    cache, table = filled(lens, H, 64, 64, seed=17)
+    starts = offsets(news)
+    q = torch.randn(starts[-1], G * H, 64, generator=cuda(2), device="cuda").to(torch.bfloat16)
+    t, sl, st = ints(table), ints(lens), ints(starts)
+    first = ep.cache_attention(q, cache, t, sl, st)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = ep.cache_attention(q, cache, t, sl, st)
+    for now, rows in ((lens, starts), ([500, 300, 0, 64], starts), ([900, 20, 450, 130], [0, 1, 21, 400, 401])):
+        sl.copy_(ints(now)), st.copy_(ints(rows))
+        for _ in range(3):
+            graph.replay()
+        for h in (0, 31):
+            at = slice(h * G, (h + 1) * G)
+            want, bound, _ = attended(q[:, at], [c[:, h:h + 1].contiguous() for c in cache], table, now, rows, 0.125, True)
+            check_attention(out[:rows[-1], at], want[:rows[-1]], bound[:rows[-1]])
+        if now is lens:
+            assert torch.equal(out, first)
