@@ -18,11 +18,18 @@ __device__ unsigned int g_prompts_status = 0;
 //   warp 12              issues the products.  While one tile's softmax runs, the other's products do.
 // (Warps 13 - 15 have nothing to do: registers go from one group of four warps to another.)
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
-// than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into
-// the exponent, t = score + log2(v_scale), and out of the row's sum again.
+// than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
+// t = score + log2(v_scale), and out of the row's sum again.
+// The loops are short on purpose: three roles run side by side, and what they execute over and over has to fit the SM's instruction
+// cache (with everything unrolled, 170 KB, six of ten fetches hit it and a tile took 13 700 cycles).
+// The tiles of tokens of all units form one list; every CTA takes an equal, contiguous share of it, as in kv_cache.cu, and what
+// crosses a share goes through the workspace: units are few and long, and 640 of unequal length on 148 SMs left a third of them idle.
 // ======================================================================================================================
 constexpr uint32_t kUnitRows = 256, kKeys = 128, kThreads = 32 * 16, kNanUnits = 8;
 constexpr float kSlack = 8.0f, kShift = 7.0f;
+// a piece of a unit in the workspace: O, then m and l of each row
+template <uint32_t D>
+constexpr uint32_t kPromptPiece = kUnitRows * (D + 2);
 
 template <uint32_t D>
 struct PromptShape {
@@ -31,7 +38,7 @@ struct PromptShape {
     static constexpr uint32_t kMeta = kV + 2 * kTile;                  // four slots of eight groups of 16 tokens: key scale, log2 value scale, its inverse
     static constexpr uint32_t kNan = kMeta + 4 * 8 * 16;               // some units' first NaN token of each column, then their flags
     static constexpr uint32_t kBars = kNan + kNanUnits * (D + 1) * 4;
-    static constexpr uint32_t kPart = kBars + 256, kPrefix = kPart + 128;
+    static constexpr uint32_t kPart = kBars + 256, kPrefix = kPart + 128;      // (64 bytes for the sums' parts, then the share's first place)
     static constexpr uint32_t kSmem = kPrefix + 4 * (kMaxRequests + 32) + 1024;
     static_assert(kSmem <= 232448);
 };
@@ -47,27 +54,48 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
 // binary16 x binary16 to fp32, M = 128, N = n; `mn` = the right operand is MN-major
 __host__ __device__ constexpr uint32_t f16_idesc(uint32_t n, uint32_t mn) { return (1u << 4) | (mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 
-struct Unit {
-    uint32_t b, h, row0;          // request, head of the cache, first of its rows
-    Extent r;
-    uint32_t n_rows;              // rows of the request
-    uint32_t least, most;         // tokens that the unit's first and last rows see
-};
 __device__ __forceinline__ uint32_t sees(const AttendParams &P, const Extent &r, uint32_t query) {
     return !P.causal ? r.len : r.len + query + 1u > r.rows ? min(r.len, r.len + query + 1u - r.rows) : 0u;
 }
-__device__ __forceinline__ Unit unit_of(const AttendParams &P, const uint32_t *prefix, uint32_t u) {
-    Unit x;
-    x.b = request_of(prefix, 0, P.q.B, u);
-    const uint32_t rest = u - prefix[x.b];
-    x.h = rest % P.q.H;
-    x.row0 = rest / P.q.H * kUnitRows;
-    x.r = extent_of(P.q, x.b);
-    x.n_rows = x.r.rows * P.G;
-    x.least = sees(P, x.r, x.row0 / P.G);
-    x.most = sees(P, x.r, (min(x.row0 + kUnitRows, x.n_rows) - 1u) / P.G);
-    return x;
-}
+// row tile j of a request: tokens that its last row sees; tiles of tokens, at least one, so that rows that see nothing are written too
+__device__ __forceinline__ uint32_t most_of(const AttendParams &P, const Extent &r, uint32_t j) { return sees(P, r, (min((j + 1u) * kUnitRows, r.rows * P.G) - 1u) / P.G); }
+__device__ __forceinline__ uint32_t tiles_of(const AttendParams &P, const Extent &r, uint32_t j) { return max(1u, (most_of(P, r, j) + kKeys - 1u) / kKeys); }
+__device__ __forceinline__ uint32_t row_tiles_of(const AttendParams &P, const Extent &r) { return (r.rows * P.G + kUnitRows - 1u) / kUnitRows; }
+
+// a place in the list: requests, in them row tiles, in them heads, in them tiles of tokens
+struct Place { uint32_t b, j, h, off, at, left; };        // at: number of tile `off`; left: tiles of the share from there on
+
+// What a CTA does next: tiles [first, first + count) of a unit.  Every role of the CTA walks its share alone.
+struct Cursor {
+    const AttendParams &P;
+    Place p;
+    Extent r;
+    uint32_t total;               // tiles of the unit
+    uint32_t first, count;
+    __device__ __forceinline__ Cursor(const AttendParams &P_, const Place &start) : P(P_), p(start) { enter(); }
+    __device__ __forceinline__ void enter() {
+        if (!p.left) return;
+        for (;; ++p.b, p.j = 0) {                         // (p.left: there is one)
+            r = extent_of(P.q, p.b);
+            if (p.j < row_tiles_of(P, r)) break;
+        }
+        total = tiles_of(P, r, p.j);
+        first = p.off;
+        count = P.workspace ? min(total - p.off, p.left) : total;
+    }
+    __device__ __forceinline__ bool more() const { return p.left != 0; }
+    __device__ __forceinline__ void next() {
+        p.left -= min(p.left, count);
+        p.at += count;
+        p.off = 0;
+        if (++p.h == P.q.H) p.h = 0, ++p.j;
+        enter();
+    }
+    // tiles that take part in products (none where no row sees a token)
+    __device__ __forceinline__ uint32_t products() const { return most_of(P, r, p.j) ? count : 0u; }
+    __device__ __forceinline__ uint32_t row0() const { return p.j * kUnitRows; }
+    __device__ __forceinline__ uint32_t least() const { return sees(P, r, row0() / P.G); }
+};
 
 template <class E, uint32_t D>
 __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_constant__ AttendParams P) {
@@ -100,14 +128,62 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     tc_after();
     op_wait_for_stream();
     const uint32_t tmem = ld_smem(slot_addr);
-    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t b) { return (extent_of(P.q, b).rows * P.G + kUnitRows - 1u) / kUnitRows * P.q.H; }, prefix,
-                                     reinterpret_cast<uint32_t *>(gen + S::kPart));
+    // tiles of a request: a warp adds up its row tiles; then sums over requests
+    for (uint32_t b = warp; b < P.q.B; b += kThreads / 32u) {
+        const Extent r = extent_of(P.q, b);
+        uint32_t n = 0;
+        for (uint32_t j = lane; j < row_tiles_of(P, r); j += 32u) n += tiles_of(P, r, j);
+        n = __reduce_add_sync(0xFFFFFFFFu, n);
+        if (lane == 0) prefix[b] = n * P.q.H;
+    }
+    __syncthreads();
+    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t b) { return prefix[b]; }, prefix, reinterpret_cast<uint32_t *>(gen + S::kPart));
+    const uint32_t ctas = min(P.grid, all), u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
+                   u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
+    Place *start = reinterpret_cast<Place *>(gen + S::kPart + 64);
+    if (warp == 0) {
+        Place p{0, 0, 0, 0, u_begin, u_end - u_begin};
+        if (p.left) {
+            p.b = request_of(prefix, 0, P.q.B, u_begin);
+            const Extent r = extent_of(P.q, p.b);
+            const uint32_t v = u_begin - prefix[p.b];
+            uint32_t before = 0;                          // tiles of the row tiles before
+            for (uint32_t j0 = 0;; j0 += 32u) {
+                const uint32_t mine = j0 + lane < row_tiles_of(P, r) ? tiles_of(P, r, j0 + lane) * P.q.H : 0u;
+                uint32_t inc = mine;
+#pragma unroll
+                for (uint32_t d = 1; d < 32; d <<= 1) {
+                    const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
+                    if (lane >= d) inc += o;
+                }
+                const uint32_t here = __ballot_sync(0xFFFFFFFFu, mine && before + inc > v);
+                if (here) {
+                    const uint32_t k = __ffs(int(here)) - 1u, per_head = __shfl_sync(0xFFFFFFFFu, mine, k) / P.q.H, from = before + __shfl_sync(0xFFFFFFFFu, inc - mine, k);
+                    p.j = j0 + k, p.h = (v - from) / per_head, p.off = (v - from) % per_head;
+                    if (!P.workspace && p.off) {          // units are not cut: the next one that begins in this share
+                        const uint32_t skip = per_head - p.off;
+                        p.left -= min(p.left, skip);
+                        p.at += skip, p.off = 0;
+                        if (++p.h == P.q.H) p.h = 0, ++p.j;
+                    }
+                    break;
+                }
+                before += __shfl_sync(0xFFFFFFFFu, inc, 31);
+                if (j0 >= row_tiles_of(P, r)) { p.left = 0; break; }         // (never)
+            }
+        }
+        if (lane == 0) *start = p;
+    }
+    __syncthreads();
+    const Place begin = *start;
+    uint32_t *desc = P.workspace ? reinterpret_cast<uint32_t *>(P.workspace) + blockIdx.x * 8u : nullptr;
+    if (desc && tid == 0) desc[3] = 0;
+    __syncthreads();
     // tensor memory: scores (and weights) of the two tiles, then their accumulators
     const uint32_t s_col[2] = {tmem, tmem + 128u}, o_col[2] = {tmem + 256u, tmem + 384u};
     uint32_t it = 0, n_unit = 0;                          // tiles of tokens and units so far
     bool ok = true;
 
-    // units from the last one on: a request's last rows see the most tokens, and the longest units come first
     // registers: 512 threads x 128 at launch = 128 x (168 + 168 + 104 + 72)
     if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
@@ -115,20 +191,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         if (warp == 12 && lane == 0) {
             constexpr uint32_t kScores = f16_idesc(kKeys, 0), kValues = f16_idesc(D, 1);
             auto scores = [&](uint32_t t, uint32_t stage) {
-#pragma unroll
+                // (descriptors differ in their address, 16 bytes a step of it: 32 bytes further along the swizzled rows, then the next 64 columns)
+                const uint64_t a = operand_desc(base + S::kQ + t * S::kTile), b = operand_desc(base + S::kK + stage * S::kTile);
+#pragma unroll 2
                 for (uint32_t k = 0; k < D / 16; ++k) {
-                    const uint32_t at = k / 4 * S::kHalf + k % 4 * 32;
-                    mma_f16_ss(s_col[t], operand_desc(base + S::kQ + t * S::kTile + at), operand_desc(base + S::kK + stage * S::kTile + at), kScores, k ? 1u : 0u);
+                    const uint32_t at = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
+                    mma_f16_ss(t ? s_col[1] : s_col[0], a + at, b + at, kScores, k ? 1u : 0u);
                 }
             };
             auto values = [&](uint32_t t, uint32_t stage, uint32_t accumulate) {
-#pragma unroll
+                const uint64_t b = operand_desc(base + S::kV + stage * S::kTile, S::kHalf);
+#pragma unroll 2
                 for (uint32_t k = 0; k < kKeys / 16; ++k)
-                    mma_f16_ts(o_col[t], s_col[t] + 8 * k, operand_desc(base + S::kV + stage * S::kTile + k * 2048, S::kHalf), kValues, accumulate | (k ? 1u : 0u));
+                    mma_f16_ts(t ? o_col[1] : o_col[0], (t ? s_col[1] : s_col[0]) + 8 * k, b + k * (2048 >> 4), kValues, accumulate | (k ? 1u : 0u));
             };
-            for (uint32_t u = blockIdx.x; u < all && ok; u += gridDim.x) {
-                const Unit x = unit_of(P, prefix, all - 1u - u);
-                const uint32_t tiles = (x.most + kKeys - 1u) / kKeys;
+            for (Cursor x(P, begin); x.more() && ok; x.next()) {
+                const uint32_t tiles = x.products();
                 if (tiles == 0) continue;
                 for (uint32_t i = 0; i < tiles && ok; ++i, ++it) {
                     const uint32_t stage = it & 1u, turn = (it >> 1) & 1u, before = it - 1u;
@@ -175,11 +253,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         // ---- keys and values ----------------------------------------------------------------------------------------------
         constexpr uint32_t kLanes = D / 16, kPer = 32 / kLanes, kLoads = 32 / kPer;          // lanes of a token; tokens of a load; loads of a warp's 32 tokens
         const uint32_t w = warp - 8u, l = tid - 256u, piece = lane % kLanes, half = piece >> 2;
-        for (uint32_t u = blockIdx.x; u < all && ok; u += gridDim.x) {
-            const Unit x = unit_of(P, prefix, all - 1u - u);
-            const uint32_t tiles = (x.most + kKeys - 1u) / kKeys;
+        // where a lane's first piece goes, of even and odd loads: its row's number mod 8 swizzles the 16-byte pieces
+        uint32_t to[2];
+#pragma unroll
+        for (uint32_t odd = 0; odd < 2; ++odd) {
+            const uint32_t row = w * 32u + lane / kLanes, sw = (row + odd * 4u) & 7u;
+            to[odd] = half * S::kHalf + row * 128u + (((2u * (piece & 3u) + (half ? 1u : 0u)) ^ sw) << 4);
+        }
+        for (Cursor x(P, begin); x.more() && ok; x.next()) {
+            const uint32_t tiles = x.products(), t_first = x.first * kKeys, least = x.least();
             if (tiles == 0) continue;
-            const int32_t *table = P.q.table + int64_t(x.b) * P.q.ldt;
+            const int32_t *table = P.q.table + int64_t(x.p.b) * P.q.ldt;
             // The record of NaN two units on is cleared here.  These warps run at most two tiles ahead of the products, so the unit that
             // used it six units ago has long been written; and a warp that is at that unit's first tile has seen a stage freed
             // that all of them filled after this.
@@ -195,15 +279,18 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 atomicOr(&g_prompts_status, 2u);
                 return -1;
             };
-            auto load = [&](const uint8_t *cache, uint32_t t0, int32_t id, uint4 (&v)[kLoads]) {
+            // a warp's 32 tokens lie in one page or two, 16 in each
+            auto load = [&](const uint8_t *cache, uint32_t t0, int32_t id0, int32_t id1, uint4 (&v)[kLoads]) {
 #pragma unroll
-                for (uint32_t j = 0; j < kLoads; ++j) {
-                    const uint32_t sub = j * kPer + lane / kLanes, t = t0 + w * 32u + sub;
-                    const int32_t page = __shfl_sync(0xFFFFFFFFu, id, sub);
-                    v[j] = make_uint4(0, 0, 0, 0);
-                    if (page >= 0) {
-                        const uint8_t *src = cache + (((uint64_t(uint32_t(page)) * P.q.H + x.h) << P.q.shift) + (t & (P.q.page - 1u))) * D + piece * 16u;
-                        asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w) : "l"(src));
+                for (uint32_t side = 0; side < 2; ++side) {
+                    const int32_t page = side ? id1 : id0;
+                    const uint8_t *src = cache + (((uint64_t(uint32_t(page)) * P.q.H + x.p.h) << P.q.shift) + ((t0 + w * 32u + side * 16u) & (P.q.page - 1u)) + lane / kLanes) * D + piece * 16u;
+#pragma unroll
+                    for (uint32_t j = side * kLoads / 2; j < (side + 1) * kLoads / 2; ++j) {
+                        v[j] = make_uint4(0, 0, 0, 0);
+                        if (page >= 0)
+                            asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];"
+                                         : "=r"(v[j].x), "=r"(v[j].y), "=r"(v[j].z), "=r"(v[j].w) : "l"(src + (j - side * kLoads / 2) * kPer * D));
                     }
                 }
             };
@@ -212,19 +299,40 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             auto store = [&](uint32_t at, const uint4 (&v)[kLoads]) {
 #pragma unroll
                 for (uint32_t j = 0; j < kLoads; ++j) {
-                    const uint32_t row = w * 32u + j * kPer + lane / kLanes;
-                    uint32_t f[8];
-                    f16x4_of_e4m3x4(v[j].x, f[0], f[1]);
-                    f16x4_of_e4m3x4(v[j].y, f[2], f[3]);
-                    f16x4_of_e4m3x4(v[j].z, f[4], f[5]);
-                    f16x4_of_e4m3x4(v[j].w, f[6], f[7]);
-                    const uint32_t to = at + half * S::kHalf + row * 128u, c = 2u * (piece & 3u), sw = row & 7u;
-                    const uint32_t a0 = to + ((c ^ sw) << 4), a1 = to + (((c + 1u) ^ sw) << 4);
                     const bool flip = half != 0;
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(flip ? a1 : a0), "r"(flip ? f[4] : f[0]), "r"(flip ? f[5] : f[1]), "r"(flip ? f[6] : f[2]), "r"(flip ? f[7] : f[3]) : "memory");
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(flip ? a0 : a1), "r"(flip ? f[0] : f[4]), "r"(flip ? f[1] : f[5]), "r"(flip ? f[2] : f[6]), "r"(flip ? f[3] : f[7]) : "memory");
+                    uint32_t f[8];
+                    f16x4_of_e4m3x4(flip ? v[j].z : v[j].x, f[0], f[1]);
+                    f16x4_of_e4m3x4(flip ? v[j].w : v[j].y, f[2], f[3]);
+                    f16x4_of_e4m3x4(flip ? v[j].x : v[j].z, f[4], f[5]);
+                    f16x4_of_e4m3x4(flip ? v[j].y : v[j].w, f[6], f[7]);
+                    const uint32_t a0 = at + to[kPer == 4 ? j & 1u : 0u] + j * kPer * 128u;
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a0), "r"(f[0]), "r"(f[1]), "r"(f[2]), "r"(f[3]) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(a0 ^ 16u), "r"(f[4]), "r"(f[5]), "r"(f[6]), "r"(f[7]) : "memory");
                 }
-                fence_proxy_async();
+            };
+            // Values of a tile that some rows do not see all of: tokens past the request's end may hold anything and become zeros, and a
+            // NaN counts for the rows that see its token only - it is taken out here and put into those rows at the unit's end.
+            auto scrub = [&](uint32_t at, uint32_t t0) {
+#pragma unroll 1
+                for (uint32_t j = 0; j < 2 * kLoads; ++j) {
+                    const uint32_t load_no = j >> 1, token = t0 + w * 32u + load_no * kPer + lane / kLanes;
+                    const uint32_t a0 = (at + (kPer == 4 && load_no & 1u ? to[1] : to[0]) + load_no * kPer * 128u) ^ (j & 1u ? 16u : 0u);
+                    const uint4 v = ld_smem16(a0);
+                    if (token >= x.r.len) {
+                        asm volatile("st.shared.v4.u32 [%0], {%1, %1, %1, %1};" ::"r"(a0), "r"(0u) : "memory");
+                    } else {
+                        const uint32_t word[4] = {v.x, v.y, v.z, v.w};
+                        const uint32_t first = piece * 16u + ((j & 1u) != half ? 8u : 0u);           // (see store: which eight of the sixteen)
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c)
+                            if ((word[c] & 0x7FFFu) > 0x7C00u || (word[c] & 0x7FFF0000u) > 0x7C000000u) {
+                                *has_nan = 1;
+                                if ((word[c] & 0x7FFFu) > 0x7C00u) atomicMin(first_nan + first + 2u * c, token);
+                                if ((word[c] & 0x7FFF0000u) > 0x7C000000u) atomicMin(first_nan + first + 2u * c + 1u, token);
+                                st_smem(a0 + 4u * c, ((word[c] & 0x7FFFu) > 0x7C00u ? 0u : word[c] & 0xFFFFu) | ((word[c] & 0x7FFF0000u) > 0x7C000000u ? 0u : word[c] & 0xFFFF0000u));
+                            }
+                    }
+                }
             };
             // a group's scales (threads 0 - 7), a tile ahead
             float ks = -1.0f, vs = 1.0f;
@@ -233,54 +341,42 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 const int32_t page = page_at(t0 + 16u * l);
                 ks = -1.0f, vs = 1.0f;
                 if (page >= 0) {
-                    const size_t block = size_t(uint32_t(page)) * P.q.H + x.h;
+                    const size_t block = size_t(uint32_t(page)) * P.q.H + x.p.h;
                     ks = __ldg(P.ks + block), vs = __ldg(P.vs + block);
                 }
             };
             uint4 kv[kLoads], vv[kLoads];
-            int32_t id = page_at(w * 32u + lane), id_next;
-            load(P.k, 0, id, kv);
-            scales_of(0);
+            int32_t id0 = page_at(t_first + w * 32u), id1 = page_at(t_first + w * 32u + 16u);
+            load(P.k, t_first, id0, id1, kv);
+            load(P.v, t_first, id0, id1, vv);
+            scales_of(t_first);
+            if (tiles > 1) id0 = page_at(t_first + kKeys + w * 32u), id1 = page_at(t_first + kKeys + w * 32u + 16u);
+#pragma unroll 1
             for (uint32_t i = 0; i < tiles; ++i, ++it) {
-                const uint32_t stage = it & 1u, turn = (it >> 1) & 1u, t0 = i * kKeys;
-                load(P.v, t0, id, vv);
-                id_next = i + 1u < tiles ? page_at(t0 + kKeys + w * 32u + lane) : -1;
+                const uint32_t stage = it & 1u, turn = (it >> 1) & 1u, t0 = t_first + i * kKeys;
                 if (it > 1u) ok = __all_sync(0xFFFFFFFFu, bar_wait(k_free + 8 * stage, turn ^ 1u, abort_word));
                 if (!ok) break;
                 store(base + S::kK + stage * S::kTile, kv);
+                fence_proxy_async();
                 if (l < 8) {
                     const float some = fmaxf(vs, 1e-30f);
                     *reinterpret_cast<float4 *>(gen + S::kMeta + ((it & 3u) * 8u + l) * 16u) = make_float4(ks, log2f(some), __fdiv_rn(1.0f, some), 0.0f);
                 }
                 bar_arrive(k_full + 8 * stage);
                 if (i + 1u < tiles) {
-                    load(P.k, t0 + kKeys, id_next, kv);
+                    load(P.k, t0 + kKeys, id0, id1, kv);
                     scales_of(t0 + kKeys);
-                }
-                // a NaN counts for the rows that see its token and no others: where some do not, it is taken out here and put into
-                // those rows at the unit's end
-                if (t0 + kKeys > x.least) {
-#pragma unroll
-                    for (uint32_t j = 0; j < kLoads; ++j) {
-                        uint32_t *word = reinterpret_cast<uint32_t *>(&vv[j]);
-#pragma unroll
-                        for (uint32_t c = 0; c < 4; ++c) {
-                            const uint32_t is = __vcmpeq4(word[c] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                            if (is) {
-#pragma unroll
-                                for (uint32_t e = 0; e < 4; ++e)
-                                    if (is >> (8 * e) & 1u) atomicMin(first_nan + piece * 16u + 4u * c + e, t0 + w * 32u + j * kPer + lane / kLanes);
-                                *has_nan = 1;
-                                word[c] &= ~is;
-                            }
-                        }
-                    }
                 }
                 if (it > 1u) ok = __all_sync(0xFFFFFFFFu, bar_wait(v_free + 8 * stage, turn ^ 1u, abort_word));
                 if (!ok) break;
                 store(base + S::kV + stage * S::kTile, vv);
+                if (t0 + kKeys > least) scrub(base + S::kV + stage * S::kTile, t0);
+                fence_proxy_async();
                 bar_arrive(v_full + 8 * stage);
-                id = id_next;
+                if (i + 1u < tiles) {
+                    load(P.v, t0 + kKeys, id0, id1, vv);
+                    if (i + 2u < tiles) id0 = page_at(t0 + 2 * kKeys + w * 32u), id1 = page_at(t0 + 2 * kKeys + w * 32u + 16u);
+                }
             }
             ++n_unit;
         }
@@ -288,34 +384,33 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         // ---- softmax --------------------------------------------------------------------------------------------------------
         const uint32_t t = warp >> 2, l = tid & 127u, quarter = (warp & 3u) * 32u;
-        const uint32_t s_mine = s_col[t] + (quarter << 16), o_mine = o_col[t] + (quarter << 16);
-        for (uint32_t u = blockIdx.x; u < all && ok; u += gridDim.x) {
-            const Unit x = unit_of(P, prefix, all - 1u - u);
-            const uint32_t tiles = (x.most + kKeys - 1u) / kKeys;
-            const uint32_t row = x.row0 + t * 128u + l, i_row = row / P.G, g = row % P.G;
-            const bool real = row < x.n_rows, any_real = __any_sync(0xFFFFFFFFu, real);
-            const uint32_t lim = real ? sees(P, x.r, i_row) : x.most;
+        const uint32_t s_mine = (t ? s_col[1] : s_col[0]) + (quarter << 16), o_mine = (t ? o_col[1] : o_col[0]) + (quarter << 16);
+        for (Cursor x(P, begin); x.more() && ok; x.next()) {
+            const uint32_t tiles = x.products(), n_rows = x.r.rows * P.G;
+            const uint32_t row = x.row0() + t * 128u + l, i_row = row / P.G, g = row % P.G;
+            const bool real = row < n_rows, any_real = __any_sync(0xFFFFFFFFu, real);
+            const uint32_t lim = real ? sees(P, x.r, i_row) : most_of(P, x.r, x.p.j);
             const uint32_t lim_least = __reduce_min_sync(0xFFFFFFFFu, lim);
-            const int64_t head = int64_t(x.h * P.G + g);
+            const int64_t head = int64_t(x.p.h * P.G + g);
             float m = -INFINITY, sum = 0.0f;
             if (tiles) {
                 // the row as binary16, times a power of two that puts its largest magnitude in [2^13, 2^14) (see kv_cache.cu), with the sign of the scale
-                uint4 w[D / 8];
                 const T *src = static_cast<const T *>(P.x) + int64_t(x.r.row + i_row) * P.ldq + head * P.ldqh;
                 float a = 0.0f;
-#pragma unroll
+#pragma unroll 4
                 for (uint32_t c = 0; c < D / 8; ++c) {
-                    w[c] = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
-                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w[c].x)), fabsf(E::hi(w[c].x))), fmaxf(fabsf(E::lo(w[c].y)), fabsf(E::hi(w[c].y)))));
-                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w[c].z)), fabsf(E::hi(w[c].z))), fmaxf(fabsf(E::lo(w[c].w)), fabsf(E::hi(w[c].w)))));
+                    const uint4 w = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
+                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w.x)), fabsf(E::hi(w.x))), fmaxf(fabsf(E::lo(w.y)), fabsf(E::hi(w.y)))));
+                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w.z)), fabsf(E::hi(w.z))), fmaxf(fabsf(E::lo(w.w)), fabsf(E::hi(w.w)))));
                 }
                 const int32_t ea = int32_t(__float_as_uint(a) >> 23), up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
                 const float mul = copysignf(pow2_biased(uint32_t(127 + up)), P.scale_log2), fac = fabsf(P.scale_log2) * pow2_biased(uint32_t(127 - up));
-#pragma unroll
+#pragma unroll 2
                 for (uint32_t c = 0; c < D / 8; ++c) {
+                    const uint4 w = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
                     const uint32_t at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + l * 128u + (((c & 7u) ^ (l & 7u)) << 4);
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w[c].x) * mul, E::hi(w[c].x) * mul)), "r"(Fp16::two(E::lo(w[c].y) * mul, E::hi(w[c].y) * mul)),
-                                 "r"(Fp16::two(E::lo(w[c].z) * mul, E::hi(w[c].z) * mul)), "r"(Fp16::two(E::lo(w[c].w) * mul, E::hi(w[c].w) * mul)) : "memory");
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w.x) * mul, E::hi(w.x) * mul)), "r"(Fp16::two(E::lo(w.y) * mul, E::hi(w.y) * mul)),
+                                 "r"(Fp16::two(E::lo(w.z) * mul, E::hi(w.z) * mul)), "r"(Fp16::two(E::lo(w.w) * mul, E::hi(w.w) * mul)) : "memory");
                 }
                 fence_proxy_async();
                 bar_arrive(q_ready + 8 * t);
@@ -323,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     ok = bar_wait(s_full + 8 * t, it & 1u, abort_word);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                     tc_after();
-                    const uint32_t t0 = i * kKeys;
+                    const uint32_t t0 = (x.first + i) * kKeys;
                     const float4 *meta = reinterpret_cast<const float4 *>(gen + S::kMeta) + (it & 3u) * 8u;
                     if (any_real) {
                         float low = 0.0f;
@@ -332,11 +427,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                         auto tile = [&](auto edge_tag) {
                             constexpr bool kEdge = decltype(edge_tag)::value;
                             float top = -INFINITY;
-#pragma unroll
-                            for (uint32_t c = 0; c < 4; ++c) {
-                                uint32_t v[32];
-                                tc_load32(s_mine + 32 * c, v);
-                                tc_loaded();
+                            uint32_t v[2][32];
+                            auto highest = [&](const uint32_t (&v)[32], uint32_t c) {
 #pragma unroll
                                 for (uint32_t k = 0; k < 2; ++k) {
                                     const float4 s = meta[2 * c + k];
@@ -349,6 +441,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                                     const float here = fmaf(best, fac * s.x, s.y);
                                     top = fmaxf(top, kEdge && best == -INFINITY ? -INFINITY : here);
                                 }
+                            };
+                            tc_load32(s_mine, v[0]);
+#pragma unroll 1
+                            for (uint32_t c = 0; c < 4; c += 2) {
+                                tc_loaded32(v[0]);
+                                tc_load32(s_mine + 32 * (c + 1), v[1]);
+                                highest(v[0], c);
+                                tc_loaded32(v[1]);
+                                tc_load32(s_mine + 32 * ((c + 2) & 3u), v[0]);           // (at the end the first ones again, for the second pass)
+                                highest(v[1], c + 1);
                             }
                             const bool move = top > m + kSlack;                          // (also from -infinity)
                             if (__any_sync(0xFFFFFFFFu, move)) {
@@ -356,28 +458,25 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                                 if (move) m = top;
                                 sum *= f;
                                 if (i) {
-#pragma unroll
+                                    tc_loaded32(v[0]);
+#pragma unroll 1
                                     for (uint32_t c = 0; c < D / 32; ++c) {
-                                        uint32_t v[32];
-                                        tc_load32(o_mine + 32 * c, v);
-                                        tc_loaded();
+                                        tc_load32(o_mine + 32 * c, v[1]);
+                                        tc_loaded32(v[1]);
 #pragma unroll
-                                        for (uint32_t e = 0; e < 32; ++e) v[e] = __float_as_uint(__uint_as_float(v[e]) * f);
-                                        tc_store32(o_mine + 32 * c, v);
+                                        for (uint32_t e = 0; e < 32; ++e) v[1][e] = __float_as_uint(__uint_as_float(v[1][e]) * f);
+                                        tc_store32(o_mine + 32 * c, v[1]);
                                     }
                                 }
                             }
                             const float sub = m == -INFINITY ? 0.0f : m - kShift;
-#pragma unroll
-                            for (uint32_t c = 0; c < 4; ++c) {
-                                uint32_t v[32], p[16];
-                                tc_load32(s_mine + 32 * c, v);
-                                tc_loaded();
+                            auto weigh = [&](const uint32_t (&v)[32], uint32_t c) {
+                                uint32_t p[16];
 #pragma unroll
                                 for (uint32_t k = 0; k < 2; ++k) {
                                     const float4 s = meta[2 * c + k];
                                     const float by = fac * s.x, off = s.y - sub;
-                                    float part = 0.0f;
+                                    float part[2] = {0.0f, 0.0f};
 #pragma unroll
                                     for (uint32_t e = 0; e < 16; e += 2) {
                                         float f[2];
@@ -386,13 +485,22 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                                             float d = fmaf(__uint_as_float(v[16 * k + e + z]), by, off);
                                             if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) d = -INFINITY;
                                             f[z] = exp2_fast(d);
-                                            part += f[z];
+                                            part[z] += f[z];
                                         }
                                         p[8 * k + e / 2] = Fp16::two(f[0], f[1]);
                                     }
-                                    sum += part * s.z;
+                                    sum = fmaf(part[0] + part[1], s.z, sum);
                                 }
                                 tc_store16(s_mine + 16 * c, p);
+                            };
+#pragma unroll 1
+                            for (uint32_t c = 0; c < 4; c += 2) {                        // (weights of columns 32 c .. go over scores 16 c .., which have been read)
+                                tc_loaded32(v[0]);
+                                tc_load32(s_mine + 32 * (c + 1), v[1]);
+                                weigh(v[0], c);
+                                tc_loaded32(v[1]);
+                                if (c == 0) tc_load32(s_mine + 64, v[0]);
+                                weigh(v[1], c + 1);
                             }
                             tc_stored();
                         };
@@ -407,33 +515,52 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_after();
             }
-            // ---- the unit's rows --------------------------------------------------------------------------------------------
+            // ---- the unit's rows, or a piece of them --------------------------------------------------------------------------
+            const bool whole = x.count == x.total;
             const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
             T *dst = static_cast<T *>(P.o) + int64_t(x.r.row + i_row) * P.ldo + head * P.ldoh;
+            float *piece = whole ? nullptr : P.workspace + size_t(P.grid) * 8u + (size_t(blockIdx.x) * 2u + (x.p.at == u_begin ? 0u : 1u)) * kPromptPiece<D>;
             const uint32_t *first_nan = nan_at + n_unit % kNanUnits * D;
             const bool has_nan = tiles && nan_at[kNanUnits * D + n_unit % kNanUnits] != 0;
             if (any_real) {
-#pragma unroll
+#pragma unroll 1
                 for (uint32_t c = 0; c < D / 32; ++c) {
                     uint32_t v[32];
                     if (tiles) {
                         tc_load32(o_mine + 32 * c, v);
-                        tc_loaded();
+                        tc_loaded32(v);
                     }
 #pragma unroll
                     for (uint32_t e = 0; e < 32; ++e) {
-                        float f = tiles && sum != 0.0f ? __uint_as_float(v[e]) * inverse : 0.0f;
+                        float f = tiles && sum != 0.0f ? __uint_as_float(v[e]) * (whole ? inverse : 1.0f) : 0.0f;
                         if (has_nan && first_nan[32 * c + e] < lim) f = __uint_as_float(0x7FFFFFFFu);
                         v[e] = __float_as_uint(f);
                     }
-                    if (real)
+                    if (!whole) {
+#pragma unroll
+                        for (uint32_t e = 0; e < 32; e += 4)
+                            *reinterpret_cast<uint4 *>(piece + (t * 128u + l) * D + 32 * c + e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    } else if (real) {
 #pragma unroll
                         for (uint32_t e = 0; e < 32; e += 8)
                             *reinterpret_cast<uint4 *>(dst + 32 * c + e) =
                                 make_uint4(E::two(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), E::two(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])),
                                            E::two(__uint_as_float(v[e + 4]), __uint_as_float(v[e + 5])), E::two(__uint_as_float(v[e + 6]), __uint_as_float(v[e + 7])));
+                    }
                 }
-                if (real && P.lse) P.lse[int64_t(x.r.row + i_row) * P.Hq + head] = sum == 0.0f ? -INFINITY : (m - kShift + log2f(sum)) * 0.69314718055994531f;
+                if (!whole) {
+                    piece[kUnitRows * D + t * 128u + l] = m;
+                    piece[kUnitRows * (D + 1) + t * 128u + l] = sum;
+                } else if (real && P.lse) {
+                    P.lse[int64_t(x.r.row + i_row) * P.Hq + head] = sum == 0.0f ? -INFINITY : (m - kShift + log2f(sum)) * 0.69314718055994531f;
+                }
+            }
+            if (!whole && x.first == 0 && tid == 0) {     // this CTA begins the unit: the second launch joins it from here
+                const uint32_t end = x.p.at + x.total;
+                uint32_t cta = uint32_t(uint64_t(end - 1u) * ctas / all);
+                while (uint64_t(all) * (cta + 1u) / ctas < end) ++cta;
+                while (uint64_t(all) * cta / ctas >= end) --cta;
+                desc[0] = x.p.b, desc[1] = x.p.j, desc[2] = x.p.h, desc[3] = cta + 1u, desc[4] = x.p.at == u_begin ? 0u : 1u;
             }
             tc_before();
             if (tiles) ++n_unit;
@@ -448,20 +575,65 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     }
 }
 
+// The units that cross a share: CTA column k takes the one that CTA k of the first launch began; its pieces are the first ones of the CTAs
+// after it, in order.  A thread has four columns of a row.
+template <class E, uint32_t D>
+__global__ void __launch_bounds__(256) prompts_join_kernel(const __grid_constant__ AttendParams P) {
+    using T = typename E::T;
+    op_wait_for_stream();
+    const uint32_t *desc = reinterpret_cast<const uint32_t *>(P.workspace) + blockIdx.x * 8u;
+    const uint32_t end = desc[3];
+    if (end == 0) return;
+    const uint32_t b = desc[0], j = desc[1], h = desc[2], n = end - blockIdx.x - 1u;
+    const Extent r = extent_of(P.q, b);
+    const float *pieces = P.workspace + size_t(P.grid) * 8u;
+    const float *own = pieces + (size_t(blockIdx.x) * 2u + desc[4]) * kPromptPiece<D>, *first = pieces + size_t(blockIdx.x + 1u) * 2u * kPromptPiece<D>;
+    for (uint32_t e = blockIdx.y * blockDim.x + threadIdx.x; e < kUnitRows * D / 4u; e += gridDim.y * blockDim.x) {
+        const uint32_t row = e / (D / 4u), d = e % (D / 4u) * 4u, at = j * kUnitRows + row, i = at / P.G, g = at % P.G;
+        if (at >= r.rows * P.G) return;
+        const float own_top = own[kUnitRows * D + row];
+        float top = own_top;
+#pragma unroll 4
+        for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPromptPiece<D> + kUnitRows * D + row]);
+        const float ref = top == -INFINITY ? 0.0f : top;
+        float f = exp2_fast(own_top - ref), sum = own[kUnitRows * (D + 1) + row] * f;
+        float4 acc = *reinterpret_cast<const float4 *>(own + row * D + d);
+        acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+#pragma unroll 4
+        for (uint32_t c = 0; c < n; ++c) {
+            const float *p = first + size_t(c) * 2u * kPromptPiece<D>;
+            f = exp2_fast(p[kUnitRows * D + row] - ref);
+            sum += p[kUnitRows * (D + 1) + row] * f;
+            const float4 v = *reinterpret_cast<const float4 *>(p + row * D + d);
+            acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
+        }
+        const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+        const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+        *reinterpret_cast<uint2 *>(static_cast<T *>(P.o) + t * P.ldo + head * P.ldoh + d) = make_uint2(E::two(acc.x * inverse, acc.y * inverse), E::two(acc.z * inverse, acc.w * inverse));
+        if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
+    }
+}
+
 template <class E, uint32_t D>
 int launch(const AttendParams &P, cudaStream_t st) {
     static bool configured[64] = {};
     const int rc = op_configure(prompts_kernel<E, D>, PromptShape<D>::kSmem, configured);
     if (rc) return rc;
-    return op_launch(prompts_kernel<E, D>, P.grid, kThreads, PromptShape<D>::kSmem, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+    if (op_launch(prompts_kernel<E, D>, P.grid, kThreads, PromptShape<D>::kSmem, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    if (P.workspace && op_launch(prompts_join_kernel<E, D>, dim3(P.grid, 8), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    return EP_OK;
 }
 
 }  // namespace
 
-// Units of 256 rows run one to an SM.  The other kernel takes 32 rows at a time, reads the cache again for each 32 and cuts along the tokens.
-bool ep::prompts_serve(uint32_t N, uint32_t B, uint32_t G, uint32_t H) { return uint64_t(N) * G >= 128ull * B && uint64_t(N) * G * H >= 32ull * kUnitRows; }
+// Rows enough to fill the products' 256: the other kernel takes 32 at a time and reads the cache again for each 32.
+bool ep::prompts_serve(uint32_t N, uint32_t B, uint32_t G) { return uint64_t(N) * G >= 96ull * B; }
 
-int ep::launch_prompts(const AttendParams &P, uint32_t dim, int32_t dtype, cudaStream_t st) {
+size_t ep::prompts_workspace_bytes(uint32_t grid, uint32_t dim) { return size_t(grid) * (8u + 2u * kUnitRows * (size_t(dim) + 2u)) * 4u; }
+
+int ep::launch_prompts(AttendParams P, size_t workspace_bytes, bool cut, uint32_t dim, int32_t dtype, cudaStream_t st) {
+    if (!cut) P.workspace = nullptr;
+    else if (!P.workspace || workspace_bytes < prompts_workspace_bytes(P.grid, dim) || (reinterpret_cast<uintptr_t>(P.workspace) & 15u)) return EP_ERR_SCRATCH;
     if (dtype == EP_BF16) return dim == 64 ? launch<Bf16, 64>(P, st) : launch<Bf16, 128>(P, st);
     return dim == 64 ? launch<Fp16, 64>(P, st) : launch<Fp16, 128>(P, st);
 }

@@ -693,6 +693,7 @@ extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
 extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim) {
     const int sms = op_sms();
     if (sms <= 0 || heads == 0 || B == 0) return 0;
+    if (prompts_serve(N, B, q_heads / heads)) return prompts_workspace_bytes(uint32_t(sms), dim);
     const uint32_t rows = 16u * row_tiles_per_cta(N, q_heads / heads, B);
     return size_t(sms) * (kDescWords + 2u * rows * (size_t(dim) + 2u)) * 4u;
 }
@@ -723,16 +724,16 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     P.scale_log2 = j.scale * 1.4426950408889634f;
     P.causal = j.causal ? 1u : 0u;
     P.workspace = static_cast<float *>(j.d_workspace);
-    // units are counted in 32 bits
+    // units (of 256 tokens here, of 128 for prompts) are counted in 32 bits
     const uint64_t rows = 16u * row_tiles_per_cta(N, P.G, B),
                    units = ((uint64_t(P.q.columns) * c.page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * c.heads;
-    if (units >= (1ull << 31) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
+    if (units >= (1ull << 30) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
     P.grid = uint32_t(sms);
     P.k = static_cast<const uint8_t *>(c.d_k);
     P.v = static_cast<const uint8_t *>(c.d_v);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    if (prompts_serve(N, B, P.G, c.heads)) return launch_prompts(P, c.dim, j.dtype, st);
+    if (prompts_serve(N, B, P.G)) return launch_prompts(P, j.workspace_bytes, uint64_t(P.q.columns) * c.page > kUnit, c.dim, j.dtype, st);
     return j.dtype == EP_BF16 ? launch_attend<Bf16>(P, c, j.workspace_bytes, st) : launch_attend<Fp16>(P, c, j.workspace_bytes, st);
 }

@@ -84,9 +84,10 @@ struct AttendParams {
     uint32_t grid;
 };
 
-// many rows per request (attend_prompts.cu): true if this call's shape is worth it
-bool prompts_serve(uint32_t N, uint32_t B, uint32_t G, uint32_t H);
-int launch_prompts(const AttendParams &P, uint32_t dim, int32_t dtype, cudaStream_t st);
+// many rows per request (attend_prompts.cu): whether a call's shape is for it; `cut`: segments may be cut (a workspace is there)
+bool prompts_serve(uint32_t N, uint32_t B, uint32_t G);
+size_t prompts_workspace_bytes(uint32_t grid, uint32_t dim);
+int launch_prompts(AttendParams P, size_t workspace_bytes, bool cut, uint32_t dim, int32_t dtype, cudaStream_t st);
 int op8_status_prompts();
 
 #endif  // __CUDACC__

@@ -110,7 +110,7 @@ __device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity) {
 }
 // waits for the phase of this parity to end; false, and the CTA's abort word set, if it does not within the limit
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t abort_word) {
-    if (bar_try(bar, parity)) return true;
+#pragma unroll 1
     for (uint32_t i = 0; i < kOpSpinLimit; ++i) {
         if (bar_try(bar, parity)) return true;
         if ((i & 63u) == 63u && ld_smem(abort_word)) return false;
@@ -120,6 +120,7 @@ __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity, uint32_t
 }
 // the same for the end of a kernel whose abort word may be set already: what is in flight gets its time to land
 __device__ __forceinline__ void bar_drain(uint32_t bar, uint32_t parity) {
+#pragma unroll 1
     for (uint32_t i = 0; i < kOpSpinLimit; ++i)
         if (bar_try(bar, parity)) return;
 }
@@ -152,6 +153,11 @@ __device__ __forceinline__ void tc_load32(uint32_t tmem, uint32_t (&v)[32]) {
     asm volatile("tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16, %17, %18, %19, %20, %21, "
                  "%22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
                  : EP_R8(v, 0), EP_R8(v, 8), EP_R8(v, 16), EP_R8(v, 24) : "r"(tmem));
+}
+// the same, and what uses v comes after it
+#define EP_U8(v, i) "+r"(v[i]), "+r"(v[i + 1]), "+r"(v[i + 2]), "+r"(v[i + 3]), "+r"(v[i + 4]), "+r"(v[i + 5]), "+r"(v[i + 6]), "+r"(v[i + 7])
+__device__ __forceinline__ void tc_loaded32(uint32_t (&v)[32]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;" : EP_U8(v, 0), EP_U8(v, 8), EP_U8(v, 16), EP_U8(v, 24)::"memory");
 }
 __device__ __forceinline__ void tc_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_store16(uint32_t tmem, const uint32_t (&v)[16]) {
