@@ -43,13 +43,13 @@ struct PromptShape {
     static_assert(kSmem <= 232448);
 };
 
-__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
-                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}"
+                 ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
 }
 // binary16 x binary16 to fp32, M = 128, N = n; `mn` = the right operand is MN-major
 __host__ __device__ constexpr uint32_t f16_idesc(uint32_t n, uint32_t mn) { return (1u << 4) | (mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
@@ -188,64 +188,65 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     if (warp >= 12) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
         // ---- products -----------------------------------------------------------------------------------------------------
-        if (warp == 12 && lane == 0) {
+        if (warp == 12) {
+            const uint32_t lead = elected();
             constexpr uint32_t kScores = f16_idesc(kKeys, 0), kValues = f16_idesc(D, 1);
             auto scores = [&](uint32_t t, uint32_t stage) {
                 // (descriptors differ in their address, 16 bytes a step of it: 32 bytes further along the swizzled rows, then the next 64 columns)
                 const uint64_t a = operand_desc(base + S::kQ + t * S::kTile), b = operand_desc(base + S::kK + stage * S::kTile);
-#pragma unroll 2
+#pragma unroll
                 for (uint32_t k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
-                    mma_f16_ss(t ? s_col[1] : s_col[0], a + at, b + at, kScores, k ? 1u : 0u);
+                    mma_f16_ss(t ? s_col[1] : s_col[0], a + at, b + at, kScores, k ? 1u : 0u, lead);
                 }
             };
             auto values = [&](uint32_t t, uint32_t stage, uint32_t accumulate) {
                 const uint64_t b = operand_desc(base + S::kV + stage * S::kTile, S::kHalf);
-#pragma unroll 2
+#pragma unroll
                 for (uint32_t k = 0; k < kKeys / 16; ++k)
-                    mma_f16_ts(t ? o_col[1] : o_col[0], (t ? s_col[1] : s_col[0]) + 8 * k, b + k * (2048 >> 4), kValues, accumulate | (k ? 1u : 0u));
+                    mma_f16_ts(t ? o_col[1] : o_col[0], (t ? s_col[1] : s_col[0]) + 8 * k, b + k * (2048 >> 4), kValues, accumulate | (k ? 1u : 0u), lead);
             };
             for (Cursor x(P, begin); x.more() && ok; x.next()) {
                 const uint32_t tiles = x.products();
                 if (tiles == 0) continue;
                 for (uint32_t i = 0; i < tiles && ok; ++i, ++it) {
                     const uint32_t stage = it & 1u, turn = (it >> 1) & 1u, before = it - 1u;
-                    ok = bar_wait(k_full + 8 * stage, turn, abort_word) && (i || bar_wait(q_ready, n_unit & 1u, abort_word));
+                    ok = bar_wait_warp(k_full + 8 * stage, turn, abort_word) && (i || bar_wait_warp(q_ready, n_unit & 1u, abort_word));
                     if (!ok) break;
                     tc_after();
                     scores(0, stage);
-                    tc_commit(s_full);
+                    tc_commit(s_full, lead);
                     if (i) {
-                        ok = bar_wait(p_ready + 8, before & 1u, abort_word);
+                        ok = bar_wait_warp(p_ready + 8, before & 1u, abort_word);
                         if (!ok) break;
                         tc_after();
                         values(1, before & 1u, i > 1u);
-                        tc_commit(v_free + 8 * (before & 1u));
+                        tc_commit(v_free + 8 * (before & 1u), lead);
                     } else {
-                        ok = bar_wait(q_ready + 8, n_unit & 1u, abort_word);
+                        ok = bar_wait_warp(q_ready + 8, n_unit & 1u, abort_word);
                         if (!ok) break;
                         tc_after();
                     }
                     scores(1, stage);
-                    tc_commit(s_full + 8);
-                    tc_commit(k_free + 8 * stage);
-                    ok = bar_wait(v_full + 8 * stage, turn, abort_word) && bar_wait(p_ready, it & 1u, abort_word);
+                    tc_commit(s_full + 8, lead);
+                    tc_commit(k_free + 8 * stage, lead);
+                    ok = bar_wait_warp(v_full + 8 * stage, turn, abort_word) && bar_wait_warp(p_ready, it & 1u, abort_word);
                     if (!ok) break;
                     tc_after();
                     values(0, stage, i ? 1u : 0u);
-                    if (i + 1u == tiles) tc_commit(o_full);
+                    if (i + 1u == tiles) tc_commit(o_full, lead);
                 }
                 if (!ok) break;
                 const uint32_t before = it - 1u;
-                ok = bar_wait(p_ready + 8, before & 1u, abort_word);
+                ok = bar_wait_warp(p_ready + 8, before & 1u, abort_word);
                 if (!ok) break;
                 tc_after();
                 values(1, before & 1u, tiles > 1u);
-                tc_commit(v_free + 8 * (before & 1u));
-                tc_commit(o_full + 8);
+                tc_commit(v_free + 8 * (before & 1u), lead);
+                tc_commit(o_full + 8, lead);
                 ++n_unit;
             }
-            tc_commit(drained);
+            tc_commit(drained, lead);
             bar_drain(drained, 0);                        // nothing is in flight when tensor memory is given back
         }
     } else if (warp >= 8) {

@@ -231,13 +231,14 @@ struct MatmulParams {
 __device__ __forceinline__ uint64_t scales_desc(uint32_t addr) {
     return uint64_t((addr >> 4) & 0x3FFFu) | (uint64_t(1) << 16) | (uint64_t(128 >> 4) << 32) | (uint64_t(1) << 46);
 }
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t addr) {
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(scales_desc(addr)) : "memory");
+__device__ __forceinline__ void copy_scales(uint32_t tmem, uint32_t addr, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(tmem), "l"(scales_desc(addr)), "r"(lead) : "memory");
 }
-__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
-                 "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
-                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate) : "memory");
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(lead) : "memory");
 }
 // E4M3 x E4M3, both K-major, E8M0 scales, M = 128, N = n; `word` = which byte of the scale words
 __host__ __device__ constexpr uint32_t scaled_idesc(uint32_t n, uint32_t word) {
@@ -304,30 +305,31 @@ __global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant
                 for (uint32_t j = k > G::kStages ? k - G::kStages : 0; j < k; ++j) bar_drain(full + 8 * (j % G::kStages), (j / G::kStages) & 1u);
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        {
+            const uint32_t lead = elected();
             bool ok = true;
             for (uint32_t k = 0; k < nk && ok; ++k) {
                 const uint32_t s = k % G::kStages, chunk = k / 4, slot = chunk % G::kSlots, sa = sf + slot * G::kSlotCols, sb = sa + 4;
                 if (k % 4 == 0) {
-                    ok = bar_wait(sfull + 8 * slot, (chunk / G::kSlots) & 1u, abort_word);
+                    ok = bar_wait_warp(sfull + 8 * slot, (chunk / G::kSlots) & 1u, abort_word);
                     if (!ok) break;
                     tc_after();
                     const uint32_t at = base + G::kScales + slot * G::kSlot;
-                    copy_scales(sa, at);
+                    copy_scales(sa, at, lead);
 #pragma unroll
-                    for (uint32_t n = 0; n < (BN + 127) / 128; ++n) copy_scales(sb + 4 * n, at + 512 + 512 * n);
+                    for (uint32_t n = 0; n < (BN + 127) / 128; ++n) copy_scales(sb + 4 * n, at + 512 + 512 * n, lead);
                 }
-                ok = bar_wait(full + 8 * s, (k / G::kStages) & 1u, abort_word);
+                ok = bar_wait_warp(full + 8 * s, (k / G::kStages) & 1u, abort_word);
                 if (!ok) break;
                 tc_after();
                 const uint64_t da = operand_desc(base + s * G::kStage), db = operand_desc(base + s * G::kStage + G::kA);
                 const uint32_t idesc = scaled_idesc(BN, k % 4);
 #pragma unroll
-                for (uint32_t i = 0; i < 4; ++i) mma_scaled(tmem, da + 2 * i, db + 2 * i, idesc, sa, sb, (k | i) ? 1u : 0u);
-                tc_commit(empty + 8 * s);
-                if (k % 4 == 3) tc_commit(sempty + 8 * slot);
+                for (uint32_t i = 0; i < 4; ++i) mma_scaled(tmem, da + 2 * i, db + 2 * i, idesc, sa, sb, (k | i) ? 1u : 0u, lead);
+                tc_commit(empty + 8 * s, lead);
+                if (k % 4 == 3) tc_commit(sempty + 8 * slot, lead);
             }
-            tc_commit(done);
+            tc_commit(done, lead);
         }
     } else {
         // the scale words: byte i of a word is the scale of block 4 chunk + i; row r of 128 lies at 16 (r % 32) + 4 (r / 32)

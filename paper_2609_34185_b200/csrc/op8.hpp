@@ -134,9 +134,19 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tc_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
-__device__ __forceinline__ void tc_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+// The warp that issues matrix instructions runs as a whole and one elected lane of it issues: its addresses then stay in uniform
+// registers (issued from a branch of one lane, each instruction took some 150 cycles to be put together).
+__device__ __forceinline__ uint32_t elected() {
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r;
 }
+__device__ __forceinline__ void tc_commit(uint32_t bar, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar), "r"(lead) : "memory");
+}
+// bar_wait by a whole warp, the same answer for all of it
+__device__ __forceinline__ bool bar_wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_word) { return __all_sync(0xFFFFFFFFu, bar_wait(bar, parity, abort_word)); }
 // Operands of rows of 128 bytes with 128-byte swizzle, groups of eight rows 1024 bytes apart.  K-major: a row is a row of the
 // operand.  MN-major: a row is one k, its 128 bytes 64 16-bit values along M or N; `lead` bytes to the next 64 of those.
 __device__ __forceinline__ uint64_t operand_desc(uint32_t addr, uint32_t lead = 16) {
