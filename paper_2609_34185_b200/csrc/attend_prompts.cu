@@ -386,7 +386,39 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         // ---- softmax --------------------------------------------------------------------------------------------------------
         const uint32_t t = warp >> 2, l = tid & 127u, quarter = (warp & 3u) * 32u;
         const uint32_t s_mine = (t ? s_col[1] : s_col[0]) + (quarter << 16), o_mine = (t ? o_col[1] : o_col[0]) + (quarter << 16);
+        // Rows of a unit's tile as binary16, times a power of two that puts a row's largest magnitude in [2^13, 2^14) (see kv_cache.cu),
+        // with the sign of the scale; returns the factor of the row's scores.  They go in as soon as the scores of the unit before are done.
+        auto rows_in = [&](const Cursor &y) {
+            const uint32_t row = y.row0() + t * 128u + l, i_row = row / P.G;
+            const bool real = row < y.r.rows * P.G;
+            const T *src = static_cast<const T *>(P.x) + int64_t(y.r.row + i_row) * P.ldq + int64_t(y.p.h * P.G + row % P.G) * P.ldqh;
+            uint4 w[D / 8];
+#pragma unroll
+            for (uint32_t c = 0; c < D / 8; ++c) w[c] = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
+            float a = 0.0f;
+#pragma unroll
+            for (uint32_t c = 0; c < D / 8; ++c) {
+                a = max3(a, max3(fabsf(E::lo(w[c].x)), fabsf(E::hi(w[c].x)), fabsf(E::lo(w[c].y))), fabsf(E::hi(w[c].y)));
+                a = max3(a, max3(fabsf(E::lo(w[c].z)), fabsf(E::hi(w[c].z)), fabsf(E::lo(w[c].w))), fabsf(E::hi(w[c].w)));
+            }
+            const int32_t ea = int32_t(__float_as_uint(a) >> 23), up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
+            const float mul = copysignf(pow2_biased(uint32_t(127 + up)), P.scale_log2);
+#pragma unroll
+            for (uint32_t c = 0; c < D / 8; ++c) {
+                const uint32_t at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + l * 128u + (((c & 7u) ^ (l & 7u)) << 4);
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w[c].x) * mul, E::hi(w[c].x) * mul)), "r"(Fp16::two(E::lo(w[c].y) * mul, E::hi(w[c].y) * mul)),
+                             "r"(Fp16::two(E::lo(w[c].z) * mul, E::hi(w[c].z) * mul)), "r"(Fp16::two(E::lo(w[c].w) * mul, E::hi(w[c].w) * mul)) : "memory");
+            }
+            fence_proxy_async();
+            bar_arrive(q_ready + 8 * t);
+            return fabsf(P.scale_log2) * pow2_biased(uint32_t(127 - up));
+        };
+        float fac_next = 0.0f;
+        bool rows_there = false;                          // of the unit that comes
+        Cursor y(P, begin);                               // the unit after x
+#pragma unroll 1
         for (Cursor x(P, begin); x.more() && ok; x.next()) {
+            y.next();
             const uint32_t tiles = x.products(), n_rows = x.r.rows * P.G;
             const uint32_t row = x.row0() + t * 128u + l, i_row = row / P.G, g = row % P.G;
             const bool real = row < n_rows, any_real = __any_sync(0xFFFFFFFFu, real);
@@ -395,26 +427,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             const int64_t head = int64_t(x.p.h * P.G + g);
             float m = -INFINITY, sum = 0.0f;
             if (tiles) {
-                // the row as binary16, times a power of two that puts its largest magnitude in [2^13, 2^14) (see kv_cache.cu), with the sign of the scale
-                const T *src = static_cast<const T *>(P.x) + int64_t(x.r.row + i_row) * P.ldq + head * P.ldqh;
-                float a = 0.0f;
-#pragma unroll 4
-                for (uint32_t c = 0; c < D / 8; ++c) {
-                    const uint4 w = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
-                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w.x)), fabsf(E::hi(w.x))), fmaxf(fabsf(E::lo(w.y)), fabsf(E::hi(w.y)))));
-                    a = fmaxf(a, fmaxf(fmaxf(fabsf(E::lo(w.z)), fabsf(E::hi(w.z))), fmaxf(fabsf(E::lo(w.w)), fabsf(E::hi(w.w)))));
-                }
-                const int32_t ea = int32_t(__float_as_uint(a) >> 23), up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
-                const float mul = copysignf(pow2_biased(uint32_t(127 + up)), P.scale_log2), fac = fabsf(P.scale_log2) * pow2_biased(uint32_t(127 - up));
-#pragma unroll 2
-                for (uint32_t c = 0; c < D / 8; ++c) {
-                    const uint4 w = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
-                    const uint32_t at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + l * 128u + (((c & 7u) ^ (l & 7u)) << 4);
-                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w.x) * mul, E::hi(w.x) * mul)), "r"(Fp16::two(E::lo(w.y) * mul, E::hi(w.y) * mul)),
-                                 "r"(Fp16::two(E::lo(w.z) * mul, E::hi(w.z) * mul)), "r"(Fp16::two(E::lo(w.w) * mul, E::hi(w.w) * mul)) : "memory");
-                }
-                fence_proxy_async();
-                bar_arrive(q_ready + 8 * t);
+                if (!rows_there) fac_next = rows_in(x);
+                const float fac = fac_next;
+                rows_there = false;
                 for (uint32_t i = 0; i < tiles; ++i, ++it) {
                     ok = bar_wait(s_full + 8 * t, it & 1u, abort_word);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
@@ -435,9 +450,14 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                                     const float4 s = meta[2 * c + k];
                                     float best = -INFINITY;
 #pragma unroll
-                                    for (uint32_t e = 0; e < 16; ++e) {
-                                        const float f = __uint_as_float(v[16 * k + e]);
-                                        best = fmaxf(best, !kEdge || (t0 + 32 * c + 16 * k + e < lim && s.x >= 0.0f) ? f : -INFINITY);
+                                    for (uint32_t e = 0; e < 16; e += 2) {
+                                        float f[2];
+#pragma unroll
+                                        for (uint32_t z = 0; z < 2; ++z) {
+                                            f[z] = __uint_as_float(v[16 * k + e + z]);
+                                            if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) f[z] = -INFINITY;
+                                        }
+                                        best = max3(best, f[0], f[1]);
                                     }
                                     const float here = fmaf(best, fac * s.x, s.y);
                                     top = fmaxf(top, kEdge && best == -INFINITY ? -INFINITY : here);
@@ -477,20 +497,23 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                                 for (uint32_t k = 0; k < 2; ++k) {
                                     const float4 s = meta[2 * c + k];
                                     const float by = fac * s.x, off = s.y - sub;
-                                    float part[2] = {0.0f, 0.0f};
+                                    const uint64_t by2 = pair_of(by, by), off2 = pair_of(off, off);
+                                    uint64_t part = 0;
 #pragma unroll
                                     for (uint32_t e = 0; e < 16; e += 2) {
                                         float f[2];
+                                        pair_to(fma2(pair_of(__uint_as_float(v[16 * k + e]), __uint_as_float(v[16 * k + e + 1])), by2, off2), f[0], f[1]);
 #pragma unroll
                                         for (uint32_t z = 0; z < 2; ++z) {
-                                            float d = fmaf(__uint_as_float(v[16 * k + e + z]), by, off);
-                                            if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) d = -INFINITY;
-                                            f[z] = exp2_fast(d);
-                                            part[z] += f[z];
+                                            if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) f[z] = -INFINITY;
+                                            f[z] = exp2_fast(f[z]);
                                         }
+                                        part = add2(part, pair_of(f[0], f[1]));
                                         p[8 * k + e / 2] = Fp16::two(f[0], f[1]);
                                     }
-                                    sum = fmaf(part[0] + part[1], s.z, sum);
+                                    float odd, even;
+                                    pair_to(part, even, odd);
+                                    sum = fmaf(even + odd, s.z, sum);
                                 }
                                 tc_store16(s_mine + 16 * c, p);
                             };
@@ -512,6 +535,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     bar_arrive(p_ready + 8 * t);
                 }
                 if (!ok) break;
+                if (y.more() && y.products()) {
+                    fac_next = rows_in(y);
+                    rows_there = true;
+                }
                 ok = bar_wait(o_full + 8 * t, n_unit & 1u, abort_word);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_after();
