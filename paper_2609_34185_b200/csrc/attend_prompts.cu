@@ -19,7 +19,8 @@ __device__ unsigned int g_prompts_status = 0;
 // (Warps 13 - 15 have nothing to do: registers go from one group of four warps to another.)
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
 // than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
-// t = score + log2(v_scale), and out of the row's sum again.
+// t = score + log2(v_scale), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
+// instead of the maximum first: 379 -> 462 us.)
 // The loops are short on purpose: three roles run side by side, and what they execute over and over has to fit the SM's instruction
 // cache (with everything unrolled, 170 KB, six of ten fetches hit it and a tile took 13 700 cycles).
 // The tiles of tokens of all units form one list; every CTA takes an equal, contiguous share of it, as in kv_cache.cu, and what
@@ -62,8 +63,11 @@ __device__ __forceinline__ uint32_t most_of(const AttendParams &P, const Extent 
 __device__ __forceinline__ uint32_t tiles_of(const AttendParams &P, const Extent &r, uint32_t j) { return max(1u, (most_of(P, r, j) + kKeys - 1u) / kKeys); }
 __device__ __forceinline__ uint32_t row_tiles_of(const AttendParams &P, const Extent &r) { return (r.rows * P.G + kUnitRows - 1u) / kUnitRows; }
 
-// a place in the list: requests, in them row tiles, in them heads, in them tiles of tokens
-struct Place { uint32_t b, j, h, off, at, left; };        // at: number of tile `off`; left: tiles of the share from there on
+// A unit's place in the list is its tiles and kStart before them, which is about what its start and end cost (rows in, the first
+// tile and those at the diagonal the careful way, rows out).
+constexpr uint32_t kStart = 3;
+// a place in the list: requests, in them row tiles, in them heads, in them kStart and tiles of tokens
+struct Place { uint32_t b, j, h, off, at, left; };        // at: number of place `off`; left: places of the share from there on
 
 // What a CTA does next: tiles [first, first + count) of a unit.  Every role of the CTA walks its share alone.
 struct Cursor {
@@ -71,7 +75,7 @@ struct Cursor {
     Place p;
     Extent r;
     uint32_t total;               // tiles of the unit
-    uint32_t first, count;
+    uint32_t first, count, taken; // taken: places of the share
     __device__ __forceinline__ Cursor(const AttendParams &P_, const Place &start) : P(P_), p(start) { enter(); }
     __device__ __forceinline__ void enter() {
         if (!p.left) return;
@@ -80,13 +84,14 @@ struct Cursor {
             if (p.j < row_tiles_of(P, r)) break;
         }
         total = tiles_of(P, r, p.j);
-        first = p.off;
-        count = P.workspace ? min(total - p.off, p.left) : total;
+        taken = P.workspace ? min(total + kStart - p.off, p.left) : total + kStart;
+        first = max(p.off, kStart) - kStart;
+        count = max(p.off + taken, kStart) - kStart - first;
     }
     __device__ __forceinline__ bool more() const { return p.left != 0; }
     __device__ __forceinline__ void next() {
-        p.left -= min(p.left, count);
-        p.at += count;
+        p.left -= min(p.left, taken);
+        p.at += taken;
         p.off = 0;
         if (++p.h == P.q.H) p.h = 0, ++p.j;
         enter();
@@ -128,11 +133,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     tc_after();
     op_wait_for_stream();
     const uint32_t tmem = ld_smem(slot_addr);
-    // tiles of a request: a warp adds up its row tiles; then sums over requests
+    // places of a request: a warp adds up its row tiles; then sums over requests
     for (uint32_t b = warp; b < P.q.B; b += kThreads / 32u) {
         const Extent r = extent_of(P.q, b);
         uint32_t n = 0;
-        for (uint32_t j = lane; j < row_tiles_of(P, r); j += 32u) n += tiles_of(P, r, j);
+        for (uint32_t j = lane; j < row_tiles_of(P, r); j += 32u) n += tiles_of(P, r, j) + kStart;
         n = __reduce_add_sync(0xFFFFFFFFu, n);
         if (lane == 0) prefix[b] = n * P.q.H;
     }
@@ -147,9 +152,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             p.b = request_of(prefix, 0, P.q.B, u_begin);
             const Extent r = extent_of(P.q, p.b);
             const uint32_t v = u_begin - prefix[p.b];
-            uint32_t before = 0;                          // tiles of the row tiles before
+            uint32_t before = 0;                          // places of the row tiles before
             for (uint32_t j0 = 0;; j0 += 32u) {
-                const uint32_t mine = j0 + lane < row_tiles_of(P, r) ? tiles_of(P, r, j0 + lane) * P.q.H : 0u;
+                const uint32_t mine = j0 + lane < row_tiles_of(P, r) ? (tiles_of(P, r, j0 + lane) + kStart) * P.q.H : 0u;
                 uint32_t inc = mine;
 #pragma unroll
                 for (uint32_t d = 1; d < 32; d <<= 1) {
@@ -544,10 +549,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 tc_after();
             }
             // ---- the unit's rows, or a piece of them --------------------------------------------------------------------------
+            if (x.count == 0) continue;                   // (a share that ends before the unit's first tile)
             const bool whole = x.count == x.total;
             const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
             T *dst = static_cast<T *>(P.o) + int64_t(x.r.row + i_row) * P.ldo + head * P.ldoh;
-            float *piece = whole ? nullptr : P.workspace + size_t(P.grid) * 8u + (size_t(blockIdx.x) * 2u + (x.p.at == u_begin ? 0u : 1u)) * kPromptPiece<D>;
+            float *piece = whole ? nullptr : P.workspace + size_t(P.grid) * 8u + (size_t(blockIdx.x) * 2u + (x.first ? 0u : 1u)) * kPromptPiece<D>;
             const uint32_t *first_nan = nan_at + n_unit % kNanUnits * D;
             const bool has_nan = tiles && nan_at[kNanUnits * D + n_unit % kNanUnits] != 0;
             if (any_real) {
@@ -584,11 +590,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 }
             }
             if (!whole && x.first == 0 && tid == 0) {     // this CTA begins the unit: the second launch joins it from here
-                const uint32_t end = x.p.at + x.total;
+                const uint32_t end = x.p.at - x.p.off + x.total + kStart;
                 uint32_t cta = uint32_t(uint64_t(end - 1u) * ctas / all);
                 while (uint64_t(all) * (cta + 1u) / ctas < end) ++cta;
                 while (uint64_t(all) * cta / ctas >= end) --cta;
-                desc[0] = x.p.b, desc[1] = x.p.j, desc[2] = x.p.h, desc[3] = cta + 1u, desc[4] = x.p.at == u_begin ? 0u : 1u;
+                desc[0] = x.p.b, desc[1] = x.p.j, desc[2] = x.p.h, desc[3] = cta + 1u;
             }
             tc_before();
             if (tiles) ++n_unit;
@@ -603,8 +609,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     }
 }
 
-// The units that cross a share: CTA column k takes the one that CTA k of the first launch began; its pieces are the first ones of the CTAs
-// after it, in order.  A thread has four columns of a row.
+// The units that cross a share: CTA column k takes the one that CTA k of the first launch began; its other pieces are those of the CTAs
+// after it, in order (a CTA's first piece continues a unit, its second begins one).  A thread has four columns of a row.
 template <class E, uint32_t D>
 __global__ void __launch_bounds__(256) prompts_join_kernel(const __grid_constant__ AttendParams P) {
     using T = typename E::T;
@@ -615,7 +621,7 @@ __global__ void __launch_bounds__(256) prompts_join_kernel(const __grid_constant
     const uint32_t b = desc[0], j = desc[1], h = desc[2], n = end - blockIdx.x - 1u;
     const Extent r = extent_of(P.q, b);
     const float *pieces = P.workspace + size_t(P.grid) * 8u;
-    const float *own = pieces + (size_t(blockIdx.x) * 2u + desc[4]) * kPromptPiece<D>, *first = pieces + size_t(blockIdx.x + 1u) * 2u * kPromptPiece<D>;
+    const float *own = pieces + (size_t(blockIdx.x) * 2u + 1u) * kPromptPiece<D>, *first = pieces + size_t(blockIdx.x + 1u) * 2u * kPromptPiece<D>;
     for (uint32_t e = blockIdx.y * blockDim.x + threadIdx.x; e < kUnitRows * D / 4u; e += gridDim.y * blockDim.x) {
         const uint32_t row = e / (D / 4u), d = e % (D / 4u) * 4u, at = j * kUnitRows + row, i = at / P.G, g = at % P.G;
         if (at >= r.rows * P.G) return;
