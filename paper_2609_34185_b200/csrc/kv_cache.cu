@@ -121,7 +121,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // ======================================================================================================================
 // Attention.  o = sum_j w_j v_j / sum_j w_j, w_j = exp(scale q . k_j - m), over the tokens that a row sees.
 //
-// A row is a query and one of the query heads that share a head of the cache; the rows of a request and head make tiles of 16 MT.
+// A row is a query and one of the query heads that share a head of the cache; the rows of a request and head make tiles of 8 NT.
 // A tile of rows against all tokens of its request is a segment; a segment is cut into units of 256 tokens, the units of all segments form
 // one list, and every CTA takes an equal, contiguous share of it, whatever the requests' lengths (they are read on the device: a
 // captured launch serves any).  A CTA's warps take tiles of 32 tokens in turn, each with a running maximum and sum of its own and its own ring
@@ -129,76 +129,97 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // are joined in shared memory.  What crosses a CTA's share goes through the workspace: a CTA leaves at most two
 // pieces there, its first segment's and its last's, and a second launch joins them.
 //
-// Products are m16n8k16 with binary16 operands: E4M3 converts to binary16 exactly.  A row of q becomes binary16 times
-// a power of two that puts its largest magnitude at 2^13: exact for binary16 and bfloat16 alike but for elements 2^-27 and more
-// below the row's largest, whose rounding is below fp32's own.  The weights w carry a factor 2^14 (their largest, 2^14, is within binary16's range) so that
-// those down to 2^-28 of the largest keep 11 bits.  A page's value scale is moved onto w as v_scale / the largest so far.
+// Products are m16n8k16 with binary16 operands (E4M3 converts to binary16 exactly) and tokens, then value columns, along M: a
+// handful of rows fills N = 8, where along M they would be half padding, with twice the scores, accumulators and instructions.
+// A row of q becomes binary16 times a power of two that puts its largest magnitude at 2^13: exact for binary16 and bfloat16 alike but for elements 2^-27 and
+// more below the row's largest, whose rounding is below fp32's own.  A page's value scale is taken into the exponent, t = score +
+// log2(v_scale), and out of the row's sum again.  The reference m of a row moves, and its accumulators with it, only when some t exceeds it by
+// more than 8; weights are 2^(t - m + 7): at most 2^15, and down to 2^-21 of what m stands for with 11 bits.
 // ======================================================================================================================
 constexpr uint32_t kTile = 32, kUnit = 256;
-constexpr float kWeightShift = 14.0f;
+constexpr float kSlack = 8.0f, kShift = 7.0f;
 
 // where a piece of a segment is left: O, then m and l of each row
-template <uint32_t MT, uint32_t D>
-constexpr uint32_t kPiece = 16 * MT * (D + 2);
+template <uint32_t NT, uint32_t D>
+constexpr uint32_t kPiece = 8 * NT * (D + 2);
 constexpr uint32_t kDescWords = 8;               // per CTA: the segment that it begins and does not end: request, row tile, head, last CTA + 1
 
-template <uint32_t MT, uint32_t D, uint32_t W>
+template <uint32_t NT, uint32_t D, uint32_t W>
 struct AttendShape {
     static constexpr uint32_t kTileBytes = kTile * D, kStage = 2 * kTileBytes;
     static constexpr uint32_t kStages = 24 / W * (128 / D);
     static constexpr uint32_t kRing = kStages * kStage;                                    // per warp
-    static constexpr uint32_t kMeta = W * kRing;                                   // scales of the stages' pages: 2 x (key, value)
+    static constexpr uint32_t kMeta = W * kRing;                                           // scales of the stages' pages: 2 x (key, value)
     static constexpr uint32_t kBars = kMeta + W * kStages * 16;
-    static constexpr uint32_t kJoin = kBars + W * kStages * 8;                     // m, l, v scale of the warps' rows
-    static constexpr uint32_t kPrefix = kJoin + W * 16 * MT * 16 + 16;
+    static constexpr uint32_t kJoin = kBars + W * kStages * 8;                             // m, l of the warps' rows
+    static constexpr uint32_t kNan = kJoin + W * 8 * NT * 8;                               // the first NaN token of each column, then the abort word
+    static constexpr uint32_t kPrefix = kNan + D * 4 + 16;
     static constexpr uint32_t kSmem = kPrefix + 4 * (kMaxRequests + 32) + 1024;
-    static_assert(16 * MT * D * 4 <= kRing && kSmem <= 232448);
+    static_assert(8 * NT * D * 4 <= kRing && kSmem <= 232448);
 };
 
 __device__ __forceinline__ void mma16816(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-__device__ __forceinline__ float quad_max(float v) {
-    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
-    return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+__device__ __forceinline__ uint32_t transposed(uint32_t v) {       // an 8 x 8 matrix of 16-bit values over the warp
+    uint32_t r;
+    asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
 }
-__device__ __forceinline__ float quad_sum(float v) {
-    v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
-    return v + __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+__device__ __forceinline__ float log2_fast(float x) {
+    float r;
+    asm("lg2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// over the lanes of equal lane % 4
+__device__ __forceinline__ float octs_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+    return fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
+}
+__device__ __forceinline__ float octs_sum(float v) {
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+    v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+    return v + __shfl_xor_sync(0xFFFFFFFFu, v, 16);
 }
 
 __device__ __forceinline__ uint32_t units_of(const Extent &r, uint32_t G, uint32_t H, uint32_t rows_per_tile) {
     const uint32_t tiles = (r.rows * G + rows_per_tile - 1u) / rows_per_tile;
     return tiles * H * max(1u, (r.len + kUnit - 1u) / kUnit);
 }
+// query i of n sees tokens 0 .. len - n + i
+__device__ __forceinline__ uint32_t seen_by(const AttendParams &P, const Extent &r, uint32_t i) {
+    return !P.causal ? r.len : r.len + i + 1u > r.rows ? min(r.len, r.len + i + 1u - r.rows) : 0u;
+}
 
-template <class E, uint32_t MT, uint32_t D, uint32_t W>
+template <class E, uint32_t NT, uint32_t D, uint32_t W>
 __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant__ AttendParams P, const __grid_constant__ CUtensorMap k_map,
-                                                                   const __grid_constant__ CUtensorMap v_map) {
-    using S = AttendShape<MT, D, W>;
+                                                           const __grid_constant__ CUtensorMap v_map) {
+    using S = AttendShape<NT, D, W>;
     using T = typename E::T;
-    constexpr uint32_t kRows = 16 * MT, kSteps = D / 16, kPer = D / 4;       // k steps of q k^T; elements of a row that a lane of a quad holds
+    constexpr uint32_t kRows = 8 * NT, kSteps = D / 16, kPer = D / 4;        // k steps of q k^T; elements of a row that a lane of a quad holds
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     uint8_t *gen = raw + (base - smem_u32(raw));
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0), quad = lane & 3u, oct = lane >> 2;
     const uint32_t ring = base + warp * S::kRing, bars = base + S::kBars + warp * S::kStages * 8, meta = base + S::kMeta + warp * S::kStages * 16;
-    uint32_t *prefix = reinterpret_cast<uint32_t *>(gen + S::kPrefix);
-    float *join = reinterpret_cast<float *>(gen + S::kJoin);
-    const uint32_t abort_at = base + S::kPrefix - 16;
+    uint32_t *prefix = reinterpret_cast<uint32_t *>(gen + S::kPrefix), *first_nan = reinterpret_cast<uint32_t *>(gen + S::kNan);
+    float2 *join = reinterpret_cast<float2 *>(gen + S::kJoin);
+    const uint32_t abort_at = base + S::kNan + D * 4;
     if (lane == 0) {
         for (uint32_t i = 0; i < S::kStages; ++i) bar_init(bars + 8 * i, 3);
         bar_init_done();
     }
     if (tid == 0) st_smem(abort_at, 0);
+    for (uint32_t i = tid; i < D; i += 32 * W) first_nan[i] = 0xFFFFFFFFu;
     op_wait_for_stream();
     const uint32_t all = prefix_sums(P.q.B, [&](uint32_t i) { return units_of(extent_of(P.q, i), P.G, P.q.H, kRows); }, prefix, reinterpret_cast<uint32_t *>(join));
     const uint32_t ctas = min(P.grid, all);               // those with a share: none of theirs is empty
     const uint32_t u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
                    u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
     uint32_t *desc = P.workspace ? reinterpret_cast<uint32_t *>(P.workspace) + blockIdx.x * kDescWords : nullptr;
-    float *pieces = P.workspace ? P.workspace + size_t(P.grid) * kDescWords + size_t(blockIdx.x) * 2u * kPiece<MT, D> : nullptr;
+    float *pieces = P.workspace ? P.workspace + size_t(P.grid) * kDescWords + size_t(blockIdx.x) * 2u * kPiece<NT, D> : nullptr;
     if (desc && tid == 0) desc[3] = 0;
 
     uint32_t issued = 0, taken = 0;                       // tiles of this warp's ring
@@ -214,7 +235,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         const uint32_t t_begin = first_unit * kUnit, t_end = min(r.len, last_unit * kUnit);
         const uint32_t n_tiles = t_end > t_begin + warp * kTile ? (t_end - t_begin - warp * kTile + W * kTile - 1u) / (W * kTile) : 0u;   // of this warp
 
-        // tile i of this warp begins at token t_begin + (i * 8 + warp) * 32
+        // tile i of this warp begins at token t_begin + (i * W + warp) * 32
         const int32_t *table = P.q.table + int64_t(b) * P.q.ldt;
         const uint32_t per_tile = P.q.page < kTile ? 2u : 1u, box = P.q.page < kTile ? P.q.page : kTile;
         auto page_of = [&](uint32_t i) {                  // lane 0 and 1: the page of the tile's first and second part, -1 if outside
@@ -248,7 +269,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
                     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(m + 4), "l"(P.vs + block) : "memory");
                 } else {
                     st_smem(m, 0xBF800000u);              // -1: left out
-                    st_smem(m + 4, 0);
+                    st_smem(m + 4, 0x3F800000u);
                 }
                 asm volatile("cp.async.mbarrier.arrive.noinc.shared::cta.b64 [%0];" ::"r"(bar) : "memory");
             }
@@ -257,150 +278,150 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         };
         int32_t next_page = page_of(0);
         uint32_t asked = 0;
+#pragma unroll 1
         for (; asked < min(n_tiles, S::kStages); ++asked) {
             const int32_t id = next_page;
             next_page = page_of(asked + 1);
             issue(asked, id);
         }
 
-        // ---- rows of q as operands -----------------------------------------------------------------------------------
-        uint32_t qa[MT][kSteps][4];
-        float fac[MT][2];                                 // of a row's scores, without the keys' scale
-        uint32_t lim[MT][2];                              // tokens that a row sees
+        // ---- rows of q as right operands: lane 4 oct + quad holds a quarter of row 8 n + oct, and in the accumulators rows 8 n + 2 quad, + 1 ------
+        uint32_t qb[NT][kSteps][2];
+        float fac[NT][2];                                 // of a row's scores, without the keys' scale
+        uint32_t lim[NT][2];                              // tokens that a row sees
         uint32_t lim_min = 0xFFFFFFFFu, lim_max = 0;
 #pragma unroll
-        for (uint32_t mt = 0; mt < MT; ++mt)
+        for (uint32_t n = 0; n < NT; ++n) {
+            const uint32_t row = row0 + n * 8 + oct, i = row / P.G, g = row % P.G;
+            const bool real = row < n_rows;
+            uint32_t w[kPer / 2];
+            const T *src = static_cast<const T *>(P.x) + int64_t(r.row + i) * P.ldq + int64_t(h * P.G + g) * P.ldqh + quad * kPer;
 #pragma unroll
-            for (uint32_t half = 0; half < 2; ++half) {
-                const uint32_t row = row0 + mt * 16 + half * 8 + oct, i = row / P.G, g = row % P.G;
-                const bool real = row < n_rows;
-                uint32_t w[kPer / 2];
-                const T *src = static_cast<const T *>(P.x) + int64_t(r.row + i) * P.ldq + int64_t(h * P.G + g) * P.ldqh + quad * kPer;
-#pragma unroll
-                for (uint32_t c = 0; c < kPer / 8; ++c) {
-                    const uint4 v = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
-                    w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
-                }
-                float a = 0.0f;
-#pragma unroll
-                for (uint32_t c = 0; c < kPer / 2; ++c) a = fmaxf(a, fmaxf(fabsf(E::lo(w[c])), fabsf(E::hi(w[c]))));
-                a = quad_max(a);
-                // 2^up puts the row's largest magnitude in [2^13, 2^14); a row of zeros or with an infinity stays as it is
-                const int32_t ea = int32_t(__float_as_uint(a) >> 23);
-                const int32_t up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
-                const float mul = pow2_biased(uint32_t(127 + up));
-                fac[mt][half] = P.scale_log2 * pow2_biased(uint32_t(127 - up));
-#pragma unroll
-                for (uint32_t st = 0; st < kSteps; ++st) {
-                    qa[mt][st][half] = Fp16::two(E::lo(w[2 * st]) * mul, E::hi(w[2 * st]) * mul);
-                    qa[mt][st][2 + half] = Fp16::two(E::lo(w[2 * st + 1]) * mul, E::hi(w[2 * st + 1]) * mul);
-                }
-                // query i of n sees tokens 0 .. len - n + i
-                const uint32_t sees = !real ? 0u : !P.causal ? r.len : r.len + i + 1u > r.rows ? min(r.len, r.len + i + 1u - r.rows) : 0u;
-                lim[mt][half] = sees;
-                lim_max = max(lim_max, sees);
-                lim_min = min(lim_min, real ? sees : 0xFFFFFFFFu);
+            for (uint32_t c = 0; c < kPer / 8; ++c) {
+                const uint4 v = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
+                w[4 * c] = v.x, w[4 * c + 1] = v.y, w[4 * c + 2] = v.z, w[4 * c + 3] = v.w;
             }
+            float a = 0.0f;
+#pragma unroll
+            for (uint32_t c = 0; c < kPer / 2; ++c) a = max3(a, fabsf(E::lo(w[c])), fabsf(E::hi(w[c])));
+            a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 1));
+            a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, 2));
+            // 2^up puts the row's largest magnitude in [2^13, 2^14); a row of zeros or with an infinity stays as it is
+            const int32_t ea = int32_t(__float_as_uint(a) >> 23);
+            const int32_t up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
+            const float mul = pow2_biased(uint32_t(127 + up)), f = P.scale_log2 * pow2_biased(uint32_t(127 - up));
+#pragma unroll
+            for (uint32_t st = 0; st < kSteps; ++st) {
+                qb[n][st][0] = Fp16::two(E::lo(w[2 * st]) * mul, E::hi(w[2 * st]) * mul);
+                qb[n][st][1] = Fp16::two(E::lo(w[2 * st + 1]) * mul, E::hi(w[2 * st + 1]) * mul);
+            }
+#pragma unroll
+            for (uint32_t e = 0; e < 2; ++e) {
+                fac[n][e] = __shfl_sync(0xFFFFFFFFu, f, int(4u * (2u * quad + e)));
+                const uint32_t mine = row0 + n * 8 + 2 * quad + e;
+                lim[n][e] = mine < n_rows ? seen_by(P, r, mine / P.G) : 0u;
+                lim_max = max(lim_max, lim[n][e]);
+                lim_min = min(lim_min, mine < n_rows ? lim[n][e] : 0xFFFFFFFFu);
+            }
+        }
         lim_min = __reduce_min_sync(0xFFFFFFFFu, lim_min);
         lim_max = __reduce_max_sync(0xFFFFFFFFu, lim_max);
 
-        float o[MT][D / 8][4], m[MT][2], l[MT][2], vref = 1e-37f;
+        // o: value columns oct D / 8 + 2 j (and + 1) of rows 8 n + 2 quad, + 1
+        float o[D / 16][NT][4], m[NT][2], l[NT][2];
 #pragma unroll
-        for (uint32_t mt = 0; mt < MT; ++mt) {
-            m[mt][0] = m[mt][1] = -INFINITY, l[mt][0] = l[mt][1] = 0.0f;
+        for (uint32_t n = 0; n < NT; ++n) {
+            m[n][0] = m[n][1] = -INFINITY, l[n][0] = l[n][1] = 0.0f;
 #pragma unroll
-            for (uint32_t d = 0; d < D / 8; ++d) o[mt][d][0] = o[mt][d][1] = o[mt][d][2] = o[mt][d][3] = 0.0f;
+            for (uint32_t j = 0; j < D / 16; ++j) o[j][n][0] = o[j][n][1] = o[j][n][2] = o[j][n][3] = 0.0f;
         }
 
+#pragma unroll 1
         for (uint32_t i = 0; i < n_tiles; ++i) {
             const uint32_t s = taken % S::kStages, at = ring + s * S::kStage, t0 = t_begin + (i * W + warp) * kTile;
-            const bool ok = bar_wait(bars + 8 * s, (taken / S::kStages) & 1u, abort_at);
+            const bool ok = bar_wait_warp(bars + 8 * s, (taken / S::kStages) & 1u, abort_at);
             ++taken;
-            if (__all_sync(0xFFFFFFFFu, ok) && t0 < lim_max) {
-                // ---- scores: n tile n holds tokens t0 + 8 n .. + 7 ---------------------------------------------------------
-                float sc[MT][4][4];
-#pragma unroll
-                for (uint32_t n = 0; n < 4; ++n) {
-                    const uint32_t row = n * 8 + oct;
-                    uint32_t kw[kPer / 4];
-#pragma unroll
-                    for (uint32_t c = 0; c < kPer / 16; ++c) {
-                        // 16-byte pieces of a row lie swizzled: of 128 bytes by the row's number mod 8, of 64 by half of it mod 4
-                        const uint32_t piece = quad * (kPer / 16) + c, sw = D == 128 ? piece ^ (row & 7u) : piece ^ ((row >> 1) & 3u);
-                        const uint4 v = ld_smem16(at + row * D + 16 * sw);
-                        kw[4 * c] = v.x, kw[4 * c + 1] = v.y, kw[4 * c + 2] = v.z, kw[4 * c + 3] = v.w;
-                    }
-#pragma unroll
-                    for (uint32_t mt = 0; mt < MT; ++mt) sc[mt][n][0] = sc[mt][n][1] = sc[mt][n][2] = sc[mt][n][3] = 0.0f;
-#pragma unroll
-                    for (uint32_t st = 0; st < kSteps; ++st) {
-                        uint32_t b0, b1;
-                        f16x4_of_e4m3x4(kw[st], b0, b1);
-#pragma unroll
-                        for (uint32_t mt = 0; mt < MT; ++mt) mma16816(sc[mt][n], qa[mt][st][0], qa[mt][st][1], qa[mt][st][2], qa[mt][st][3], b0, b1);
-                    }
-                }
+            if (ok && t0 < lim_max) {
                 float ks[2], vs[2];
 #pragma unroll
                 for (uint32_t p = 0; p < 2; ++p) {
                     ks[p] = __uint_as_float(ld_smem(meta + s * 16 + 8 * p));
-                    vs[p] = __uint_as_float(ld_smem(meta + s * 16 + 8 * p + 4));
+                    vs[p] = fmaxf(__uint_as_float(ld_smem(meta + s * 16 + 8 * p + 4)), 1e-30f);
                 }
-                // ---- masks, running maximum, weights -----------------------------------------------------------------------
                 const bool edge = t0 + kTile > lim_min || ks[0] < 0.0f || ks[1] < 0.0f;
-                const float vnew = fmaxf(vref, fmaxf(vs[0], vs[1])), vmove = __fdiv_rn(vref, vnew);
-                const float vr[2] = {__fdiv_rn(vs[0], vnew), __fdiv_rn(vs[1], vnew)};
-                vref = vnew;
-                uint32_t pa[MT][2][4];
+                // ---- scores: c0, c1 of m tile x are token t0 + 16 x + oct against rows 8 n + 2 quad, + 1; c2, c3 token + 8 -------
+                float sc[2][NT][4];
 #pragma unroll
-                for (uint32_t mt = 0; mt < MT; ++mt) {
-                    float top[2] = {-INFINITY, -INFINITY};
+                for (uint32_t x = 0; x < 2; ++x) {
+                    uint32_t kw[2][kPer / 4];
 #pragma unroll
-                    for (uint32_t n = 0; n < 4; ++n)
+                    for (uint32_t half = 0; half < 2; ++half)
 #pragma unroll
-                        for (uint32_t c = 0; c < 4; ++c) {
-                            const uint32_t half = c >> 1, t = t0 + n * 8 + quad * 2 + (c & 1u);
-                            float v = sc[mt][n][c] * (fac[mt][half] * ks[n >> 1]);
-                            if (edge && (t >= lim[mt][half] || ks[n >> 1] < 0.0f)) v = -INFINITY;
-                            sc[mt][n][c] = v;
-                            top[half] = fmaxf(top[half], v);
+                        for (uint32_t c = 0; c < kPer / 16; ++c) {
+                            // 16-byte pieces of a row lie swizzled: of 128 bytes by the row's number mod 8, of 64 by half of it mod 4
+                            const uint32_t row = x * 16 + half * 8 + oct, piece = quad * (kPer / 16) + c, sw = D == 128 ? piece ^ (row & 7u) : piece ^ ((row >> 1) & 3u);
+                            const uint4 v = ld_smem16(at + row * D + 16 * sw);
+                            kw[half][4 * c] = v.x, kw[half][4 * c + 1] = v.y, kw[half][4 * c + 2] = v.z, kw[half][4 * c + 3] = v.w;
                         }
-                    float alpha[2], sub[2];
 #pragma unroll
-                    for (uint32_t half = 0; half < 2; ++half) {
-                        const float now = fmaxf(m[mt][half], quad_max(top[half]));
-                        sub[half] = now == -INFINITY ? 0.0f : now - kWeightShift;        // no token yet: weights of 0
-                        alpha[half] = exp2_fast(m[mt][half] - (now == -INFINITY ? 0.0f : now));
-                        m[mt][half] = now;
-                        l[mt][half] *= alpha[half];
-                        alpha[half] *= vmove;
-                    }
-                    if (__any_sync(0xFFFFFFFFu, alpha[0] != 1.0f || alpha[1] != 1.0f)) {          // (a maximum moves a few times per segment)
+                    for (uint32_t n = 0; n < NT; ++n) sc[x][n][0] = sc[x][n][1] = sc[x][n][2] = sc[x][n][3] = 0.0f;
 #pragma unroll
-                        for (uint32_t d = 0; d < D / 8; ++d) {
-                            o[mt][d][0] *= alpha[0], o[mt][d][1] *= alpha[0];
-                            o[mt][d][2] *= alpha[1], o[mt][d][3] *= alpha[1];
-                        }
-                    }
+                    for (uint32_t st = 0; st < kSteps; ++st) {
+                        uint32_t a0, a1, a2, a3;
+                        f16x4_of_e4m3x4(kw[0][st], a0, a2);
+                        f16x4_of_e4m3x4(kw[1][st], a1, a3);
 #pragma unroll
-                    for (uint32_t n = 0; n < 4; ++n) {
-#pragma unroll
-                        for (uint32_t c = 0; c < 4; ++c) {
-                            sc[mt][n][c] = exp2_fast(sc[mt][n][c] - sub[c >> 1]);
-                            l[mt][c >> 1] += sc[mt][n][c];
-                        }
-                        pa[mt][n >> 1][(n & 1u) * 2] = Fp16::two(sc[mt][n][0] * vr[n >> 1], sc[mt][n][1] * vr[n >> 1]);
-                        pa[mt][n >> 1][(n & 1u) * 2 + 1] = Fp16::two(sc[mt][n][2] * vr[n >> 1], sc[mt][n][3] * vr[n >> 1]);
+                        for (uint32_t n = 0; n < NT; ++n) mma16816(sc[x][n], a0, a1, a2, a3, qb[n][st][0], qb[n][st][1]);
                     }
                 }
-                // ---- o += w v: k step st holds tokens t0 + 16 st .. + 15; a lane's columns are D / 8 oct .. + D / 8 - 1 ---------
+                // ---- t = score + log2(v_scale), the reference, weights -------------------------------------------------------------
+                const float lift[2] = {log2_fast(vs[0]), log2_fast(vs[1])}, sink[2] = {__frcp_rn(vs[0]), __frcp_rn(vs[1])};
+                bool move = false;
 #pragma unroll
-                for (uint32_t st = 0; st < 2; ++st) {
+                for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+                    for (uint32_t x = 0; x < 2; ++x)
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c) {
+                            float t = fmaf(sc[x][n][c], fac[n][c & 1u] * ks[x], lift[x]);
+                            if (edge && (t0 + x * 16 + oct + (c >> 1) * 8 >= lim[n][c & 1u] || ks[x] < 0.0f)) t = -INFINITY;
+                            sc[x][n][c] = t;
+                            move |= t > m[n][c & 1u] + kSlack;                    // (also from -infinity)
+                        }
+                if (__any_sync(0xFFFFFFFFu, move)) {
+#pragma unroll
+                    for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+                        for (uint32_t e = 0; e < 2; ++e) {
+                            const float top = octs_max(fmaxf(fmaxf(sc[0][n][e], sc[0][n][e + 2]), fmaxf(sc[1][n][e], sc[1][n][e + 2])));
+                            const float now = fmaxf(m[n][e], top), f = now == -INFINITY ? 1.0f : exp2_fast(m[n][e] - now);
+                            m[n][e] = now;
+                            l[n][e] *= f;
+#pragma unroll
+                            for (uint32_t j = 0; j < D / 16; ++j) o[j][n][e] *= f, o[j][n][e + 2] *= f;
+                        }
+                }
+                uint32_t pb[2][NT][2];
+#pragma unroll
+                for (uint32_t n = 0; n < NT; ++n)
+#pragma unroll
+                    for (uint32_t x = 0; x < 2; ++x) {
+#pragma unroll
+                        for (uint32_t c = 0; c < 4; ++c) sc[x][n][c] = exp2_fast(sc[x][n][c] - (m[n][c & 1u] == -INFINITY ? 0.0f : m[n][c & 1u] - kShift));
+#pragma unroll
+                        for (uint32_t e = 0; e < 2; ++e) l[n][e] = fmaf(sc[x][n][e] + sc[x][n][e + 2], sink[x], l[n][e]);
+                        // tokens by rows, turned to rows by tokens: the right operand of the second product
+                        pb[x][n][0] = transposed(Fp16::two(sc[x][n][0], sc[x][n][1]));
+                        pb[x][n][1] = transposed(Fp16::two(sc[x][n][2], sc[x][n][3]));
+                    }
+                // ---- o += v w: k step x holds tokens t0 + 16 x .. + 15 -----------------------------------------------------------------
+#pragma unroll
+                for (uint32_t x = 0; x < 2; ++x) {
                     constexpr uint32_t kCols = D / 8;                                    // bytes of a row that a lane takes
                     uint32_t vw[4][kCols / 4];
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) {
-                        const uint32_t row = st * 16 + quad * 2 + (j & 1u) + (j >> 1) * 8;
+                        const uint32_t row = x * 16 + quad * 2 + (j & 1u) + (j >> 1) * 8;
                         if constexpr (D == 128) {
                             const uint4 v = ld_smem16(at + S::kTileBytes + row * D + 16 * (oct ^ (row & 7u)));
                             vw[j][0] = v.x, vw[j][1] = v.y, vw[j][2] = v.z, vw[j][3] = v.w;
@@ -408,69 +429,37 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
                             const uint32_t a = at + S::kTileBytes + row * D + 16 * ((oct >> 1) ^ ((row >> 1) & 3u)) + 8 * (oct & 1u);
                             asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(vw[j][0]), "=r"(vw[j][1]) : "r"(a));
                         }
-                        // a token past the request's end may hold anything, NaN included
-                        if (edge && t0 + row >= r.len)
-#pragma unroll
-                            for (uint32_t c = 0; c < kCols / 4; ++c) vw[j][c] = 0;
                     }
-                    // a NaN counts for the rows that see its token and no others (0 * NaN is NaN): where some do not see it, it is
-                    // multiplied by who does, apart from the values
-                    uint32_t nan = 0;
+                    // Where some rows do not see all of the tile's tokens: tokens past the request's end may hold anything and count as zeros, and
+                    // a NaN counts for the rows that see its token only (0 * NaN is NaN) - it is taken out here and put into those rows at the end.
                     if (edge)
 #pragma unroll
-                        for (uint32_t j = 0; j < 4; ++j)
+                        for (uint32_t j = 0; j < 4; ++j) {
+                            const uint32_t token = t0 + x * 16 + quad * 2 + (j & 1u) + (j >> 1) * 8;
 #pragma unroll
-                            for (uint32_t c = 0; c < kCols / 4; ++c) nan |= __vcmpeq4(vw[j][c] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                    if (edge && __any_sync(0xFFFFFFFFu, nan != 0)) {
-                        uint32_t see[MT][4];
-#pragma unroll
-                        for (uint32_t mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (uint32_t e = 0; e < 4; ++e) {
-                                const uint32_t t = t0 + st * 16 + (e >> 1) * 8 + quad * 2, end = lim[mt][e & 1u];
-                                see[mt][e] = (t < end ? 0x3C00u : 0u) | (t + 1u < end ? 0x3C000000u : 0u);      // 1.0 twice
-                            }
-#pragma unroll
-                        for (uint32_t c = 0; c < kCols / 4; ++c) {
-                            uint32_t is[4];
-#pragma unroll
-                            for (uint32_t j = 0; j < 4; ++j) {
-                                is[j] = __vcmpeq4(vw[j][c] & 0x7F7F7F7Fu, 0x7F7F7F7Fu);
-                                vw[j][c] &= ~is[j];
-                                is[j] &= 0x38383838u;                                    // 1.0 in E4M3
-                            }
-                            uint32_t b0[4], b1[4];
-                            f16x4_of_e4m3x4(__byte_perm(is[0], is[1], 0x5140), b0[0], b0[1]);
-                            f16x4_of_e4m3x4(__byte_perm(is[0], is[1], 0x7362), b0[2], b0[3]);
-                            f16x4_of_e4m3x4(__byte_perm(is[2], is[3], 0x5140), b1[0], b1[1]);
-                            f16x4_of_e4m3x4(__byte_perm(is[2], is[3], 0x7362), b1[2], b1[3]);
-#pragma unroll
-                            for (uint32_t mt = 0; mt < MT; ++mt)
-#pragma unroll
-                                for (uint32_t e = 0; e < 4; ++e) {
-                                    float seen[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-                                    mma16816(seen, see[mt][0], see[mt][1], see[mt][2], see[mt][3], b0[e], b1[e]);
-#pragma unroll
-                                    for (uint32_t k = 0; k < 4; ++k)
-                                        if (seen[k] > 0.0f) o[mt][4 * c + e][k] = __uint_as_float(0x7FFFFFFFu);
+                            for (uint32_t c = 0; c < kCols / 4; ++c) {
+                                if (token >= r.len) vw[j][c] = 0;
+                                uint32_t is = ((vw[j][c] & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u;
+                                if (is) {
+                                    vw[j][c] &= ~((is >> 7) * 255u);
+#pragma unroll 1
+                                    for (; is; is &= is - 1u) atomicMin(first_nan + oct * kCols + 4u * c + (uint32_t(__ffs(int(is)) - 1) >> 3), token);
                                 }
+                            }
                         }
-                    }
 #pragma unroll
                     for (uint32_t c = 0; c < kCols / 4; ++c) {
-                        // bytes of two tokens side by side: columns 4 c, 4 c + 1 in the low word, 4 c + 2, 4 c + 3 in the high one
-                        const uint32_t lo0 = __byte_perm(vw[0][c], vw[1][c], 0x5140), hi0 = __byte_perm(vw[0][c], vw[1][c], 0x7362);
-                        const uint32_t lo1 = __byte_perm(vw[2][c], vw[3][c], 0x5140), hi1 = __byte_perm(vw[2][c], vw[3][c], 0x7362);
-                        uint32_t b0[4], b1[4];
-                        f16x4_of_e4m3x4(lo0, b0[0], b0[1]);
-                        f16x4_of_e4m3x4(hi0, b0[2], b0[3]);
-                        f16x4_of_e4m3x4(lo1, b1[0], b1[1]);
-                        f16x4_of_e4m3x4(hi1, b1[2], b1[3]);
+                        // bytes of two tokens side by side: columns 4 c, 4 c + 1 in the low words, 4 c + 2, 4 c + 3 in the high ones
+                        uint32_t lo[4], hi[4];
+                        f16x4_of_e4m3x4(__byte_perm(vw[0][c], vw[1][c], 0x5140), lo[0], lo[1]);
+                        f16x4_of_e4m3x4(__byte_perm(vw[2][c], vw[3][c], 0x5140), lo[2], lo[3]);
+                        f16x4_of_e4m3x4(__byte_perm(vw[0][c], vw[1][c], 0x7362), hi[0], hi[1]);
+                        f16x4_of_e4m3x4(__byte_perm(vw[2][c], vw[3][c], 0x7362), hi[2], hi[3]);
 #pragma unroll
-                        for (uint32_t mt = 0; mt < MT; ++mt)
-#pragma unroll
-                            for (uint32_t e = 0; e < 4; ++e)
-                                mma16816(o[mt][4 * c + e], pa[mt][st][0], pa[mt][st][1], pa[mt][st][2], pa[mt][st][3], b0[e], b1[e]);
+                        for (uint32_t n = 0; n < NT; ++n) {
+                            mma16816(o[2 * c][n], lo[0], lo[1], lo[2], lo[3], pb[x][n][0], pb[x][n][1]);
+                            mma16816(o[2 * c + 1][n], hi[0], hi[1], hi[2], hi[3], pb[x][n][0], pb[x][n][1]);
+                        }
                     }
                 }
             }
@@ -487,43 +476,40 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         // (this warp's ring is empty: every tile asked for has been taken)
         float *mine = reinterpret_cast<float *>(gen + warp * S::kRing);
 #pragma unroll
-        for (uint32_t mt = 0; mt < MT; ++mt)
+        for (uint32_t n = 0; n < NT; ++n)
 #pragma unroll
-            for (uint32_t half = 0; half < 2; ++half) {
-                const uint32_t row = mt * 16 + half * 8 + oct;
-                const float sum = quad_sum(l[mt][half]);
-                if (quad == 0) *reinterpret_cast<float4 *>(join + (warp * kRows + row) * 4) = make_float4(m[mt][half], sum, vref, 0.0f);
+            for (uint32_t e = 0; e < 2; ++e) {
+                const uint32_t row = n * 8 + 2 * quad + e;
+                const float sum = octs_sum(l[n][e]);
+                if (oct == 0) join[warp * kRows + row] = make_float2(m[n][e], sum);
 #pragma unroll
-                for (uint32_t d = 0; d < D / 8; ++d)
-                    // accumulator columns 2 quad, 2 quad + 1 of n tile d are columns (D / 8) (2 quad) + d and (D / 8) (2 quad + 1) + d
-#pragma unroll
-                    for (uint32_t e = 0; e < 2; ++e) mine[row * D + (D / 8) * (2 * quad + e) + d] = o[mt][d][2 * half + e];
+                for (uint32_t j = 0; j < D / 16; ++j) *reinterpret_cast<float2 *>(mine + row * D + oct * (D / 8) + 2 * j) = make_float2(o[j][n][e], o[j][n][e + 2]);
             }
         __syncthreads();
         const bool whole = first_unit == 0 && last_unit == per_seg;
+#pragma unroll 1
         for (uint32_t e = tid; e < kRows * D; e += 32 * W) {
-            const uint32_t row = e / D, d = e % D;
+            const uint32_t row = e / D, d = e % D, at = row0 + row, i = at / P.G, g = at % P.G;
+            if (at >= n_rows) break;
             float top = -INFINITY;
 #pragma unroll
-            for (uint32_t w = 0; w < W; ++w) top = fmaxf(top, join[(w * kRows + row) * 4]);
+            for (uint32_t w = 0; w < W; ++w) top = fmaxf(top, join[w * kRows + row].x);
             const float ref = top == -INFINITY ? 0.0f : top;
             float sum = 0.0f, acc = 0.0f;
 #pragma unroll
             for (uint32_t w = 0; w < W; ++w) {
-                const float4 j = *reinterpret_cast<const float4 *>(join + (w * kRows + row) * 4);
+                const float2 j = join[w * kRows + row];
                 const float f = exp2_fast(j.x - ref);
-                sum += f * j.y;
-                acc += f * j.z * *reinterpret_cast<const float *>(gen + w * S::kRing + (row * D + d) * 4);
+                sum = fmaf(f, j.y, sum);
+                acc = fmaf(f, *reinterpret_cast<const float *>(gen + w * S::kRing + (row * D + d) * 4), acc);
             }
+            if (first_nan[d] < seen_by(P, r, i)) acc = __uint_as_float(0x7FFFFFFFu);
             if (whole) {
-                const uint32_t at = row0 + row, i = at / P.G, g = at % P.G;
-                if (at < n_rows) {
-                    const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
-                    static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
-                    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
-                }
+                const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+                static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+                if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
             } else {
-                float *piece = pieces + (u == u_begin ? 0u : kPiece<MT, D>);
+                float *piece = pieces + (u == u_begin ? 0u : kPiece<NT, D>);
                 piece[row * D + d] = acc;
                 if (d == 0) piece[kRows * D + row] = top, piece[kRows * D + kRows + row] = sum;
             }
@@ -538,6 +524,8 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         // the rings are written by the copy engine next: the reads and writes above come first
         fence_proxy_async();
         __syncthreads();
+        for (uint32_t i = tid; i < D; i += 32 * W) first_nan[i] = 0xFFFFFFFFu;
+        if (u + last_unit - first_unit < u_end) __syncthreads();
         u += last_unit - first_unit;
     }
     if (tid == 0 && ld_smem(abort_at)) atomicOr(&g_cache_status, 1u);
@@ -547,10 +535,10 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
 
 // The segments that cross a share: CTA k takes the one that CTA k of the first launch began.  Its pieces are the first ones of the
 // CTAs after it, in order.
-template <class E, uint32_t MT, uint32_t D>
+template <class E, uint32_t NT, uint32_t D>
 __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttendParams P) {
     using T = typename E::T;
-    constexpr uint32_t kRows = 16 * MT;
+    constexpr uint32_t kRows = 8 * NT;
     op_wait_for_stream();
     const uint32_t *desc = reinterpret_cast<const uint32_t *>(P.workspace) + blockIdx.x * kDescWords;
     const uint32_t end = desc[3];
@@ -558,27 +546,27 @@ __global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ Atten
     const uint32_t b = desc[0], tile = desc[1], h = desc[2];
     const Extent r = extent_of(P.q, b);
     const float *all = P.workspace + size_t(P.grid) * kDescWords;
-    const float *own = all + (size_t(blockIdx.x) * 2u + desc[4]) * kPiece<MT, D>;
+    const float *own = all + (size_t(blockIdx.x) * 2u + desc[4]) * kPiece<NT, D>;
     const uint32_t e = blockIdx.y * blockDim.x + threadIdx.x, row = e / D, d = e % D, at = tile * kRows + row, i = at / P.G, g = at % P.G;
     if (at >= r.rows * P.G) return;
-    const float *first = all + size_t(blockIdx.x + 1u) * 2u * kPiece<MT, D>;
+    const float *first = all + size_t(blockIdx.x + 1u) * 2u * kPiece<NT, D>;
     const uint32_t n = end - blockIdx.x - 1u;
     const float own_top = own[kRows * D + row];
     float top = own_top;
 #pragma unroll 8
-    for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPiece<MT, D> + kRows * D + row]);
+    for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPiece<NT, D> + kRows * D + row]);
     const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(own_top - ref);
     float sum = own[kRows * D + kRows + row] * f0, acc = own[row * D + d] * f0;
 #pragma unroll 8
     for (uint32_t c = 0; c < n; ++c) {
-        const float *p = first + size_t(c) * 2u * kPiece<MT, D>;
+        const float *p = first + size_t(c) * 2u * kPiece<NT, D>;
         const float f = exp2_fast(p[kRows * D + row] - ref);
         sum += p[kRows * D + kRows + row] * f;
         acc += p[row * D + d] * f;
     }
     const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
     static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
-    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kWeightShift + log2f(sum)) * 0.69314718055994531f;
+    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
 }
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
@@ -619,17 +607,18 @@ int launch_append(const AppendParams &P, cudaStream_t st) {
     return e == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
-uint32_t row_tiles_per_cta(uint32_t N, uint32_t G, uint32_t B) { return uint64_t(N) * G > 16ull * B ? 2u : 1u; }
+// tiles of eight rows that a warp takes together: as many as a request of average size has, at most four
+uint32_t row_tiles(uint32_t N, uint32_t G, uint32_t B) { return uint64_t(N) * G <= 8ull * B ? 1u : uint64_t(N) * G <= 16ull * B ? 2u : 4u; }
 
-template <class E, uint32_t MT, uint32_t D>
+template <class E, uint32_t NT, uint32_t D>
 int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
 #ifndef EP_W
-#define EP_W 8
+#define EP_W 12
 #endif
-    constexpr uint32_t W = MT == 1 ? EP_W : 8;
-    using S = AttendShape<MT, D, W>;
+    constexpr uint32_t W = NT == 1 ? EP_W : 8;
+    using S = AttendShape<NT, D, W>;
     static bool configured[64] = {};
-    int rc = op_configure(attend_kernel<E, MT, D, W>, S::kSmem, configured);
+    int rc = op_configure(attend_kernel<E, NT, D, W>, S::kSmem, configured);
     if (rc) return rc;
     CUtensorMap km, vm;
     const uint64_t rows = uint64_t(c.pages) * c.heads * c.page;
@@ -638,21 +627,23 @@ int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cud
     if ((rc = byte_map(&km, c.d_k, D, rows, D, D, box, sw)) || (rc = byte_map(&vm, c.d_v, D, rows, D, D, box, sw))) return rc;
     const bool joined = uint64_t(P.q.columns) * c.page > kUnit;             // else a segment is one unit and crosses no share
     if (joined) {
-        const size_t need = size_t(P.grid) * (kDescWords + 2u * kPiece<MT, D>) * 4u;
+        const size_t need = size_t(P.grid) * (kDescWords + 2u * kPiece<NT, D>) * 4u;
         if (!P.workspace || workspace_bytes < need || !aligned(P.workspace, 16)) return EP_ERR_SCRATCH;
     } else {
         P.workspace = nullptr;
     }
-    if (op_launch(attend_kernel<E, MT, D, W>, P.grid, 32 * W, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
-    if (joined && op_launch(join_kernel<E, MT, D>, dim3(P.grid, 16 * MT * D / 256), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    if (op_launch(attend_kernel<E, NT, D, W>, P.grid, 32 * W, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
+    if (joined && op_launch(join_kernel<E, NT, D>, dim3(P.grid, (8 * NT * D + 255) / 256), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
     return EP_OK;
 }
 
 template <class E>
 int launch_attend(const AttendParams &P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
-    if (row_tiles_per_cta(P.q.N, P.G, P.q.B) == 1)
-        return c.dim == 64 ? launch_attend<E, 1, 64>(P, c, workspace_bytes, st) : launch_attend<E, 1, 128>(P, c, workspace_bytes, st);
-    return c.dim == 64 ? launch_attend<E, 2, 64>(P, c, workspace_bytes, st) : launch_attend<E, 2, 128>(P, c, workspace_bytes, st);
+    switch (row_tiles(P.q.N, P.G, P.q.B)) {
+    case 1: return c.dim == 64 ? launch_attend<E, 1, 64>(P, c, workspace_bytes, st) : launch_attend<E, 1, 128>(P, c, workspace_bytes, st);
+    case 2: return c.dim == 64 ? launch_attend<E, 2, 64>(P, c, workspace_bytes, st) : launch_attend<E, 2, 128>(P, c, workspace_bytes, st);
+    default: return c.dim == 64 ? launch_attend<E, 4, 64>(P, c, workspace_bytes, st) : launch_attend<E, 4, 128>(P, c, workspace_bytes, st);
+    }
 }
 
 }  // namespace
@@ -694,7 +685,7 @@ extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uin
     const int sms = op_sms();
     if (sms <= 0 || heads == 0 || B == 0) return 0;
     if (prompts_serve(N, B, q_heads / heads)) return prompts_workspace_bytes(uint32_t(sms), dim);
-    const uint32_t rows = 16u * row_tiles_per_cta(N, q_heads / heads, B);
+    const uint32_t rows = 8u * row_tiles(N, q_heads / heads, B);
     return size_t(sms) * (kDescWords + 2u * rows * (size_t(dim) + 2u)) * 4u;
 }
 
@@ -725,7 +716,7 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     P.causal = j.causal ? 1u : 0u;
     P.workspace = static_cast<float *>(j.d_workspace);
     // units (of 256 tokens here, of 128 for prompts) are counted in 32 bits
-    const uint64_t rows = 16u * row_tiles_per_cta(N, P.G, B),
+    const uint64_t rows = 8u * row_tiles(N, P.G, B),
                    units = ((uint64_t(P.q.columns) * c.page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * c.heads;
     if (units >= (1ull << 30) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
     const int sms = op_sms();
