@@ -99,6 +99,8 @@ struct Cursor {
     // tiles that take part in products (none where no row sees a token)
     __device__ __forceinline__ uint32_t products() const { return most_of(P, r, p.j) ? count : 0u; }
     __device__ __forceinline__ uint32_t row0() const { return p.j * kUnitRows; }
+    // a unit of up to 128 rows has one tile of rows: nothing is done for the other
+    __device__ __forceinline__ bool both() const { return row0() + kUnitRows / 2u < r.rows * P.G; }
     __device__ __forceinline__ uint32_t least() const { return sees(P, r, row0() / P.G); }
 };
 
@@ -112,7 +114,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     uint32_t *prefix = reinterpret_cast<uint32_t *>(gen + S::kPrefix), *nan_at = reinterpret_cast<uint32_t *>(gen + S::kNan);
     const uint32_t bars = base + S::kBars, k_full = bars, k_free = bars + 16, v_full = bars + 32, v_free = bars + 48, s_full = bars + 64, p_ready = bars + 80,
-                   q_ready = bars + 96, o_full = bars + 112, drained = bars + 128, slot_addr = bars + 136, abort_word = bars + 140;
+                   q_ready = bars + 96, o_full = bars + 112, drained = bars + 128, rows_out = bars + 136, slot_addr = bars + 144, abort_word = bars + 148;
     if (tid == 0) {
         for (uint32_t i = 0; i < 2; ++i) {
             bar_init(k_full + 8 * i, 128), bar_init(v_full + 8 * i, 128);
@@ -120,6 +122,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             bar_init(p_ready + 8 * i, 128), bar_init(q_ready + 8 * i, 128);
         }
         bar_init(drained, 1);
+        bar_init(rows_out, 128);
         st_smem(abort_word, 0);
         bar_init_done();
     }
@@ -211,44 +214,55 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 for (uint32_t k = 0; k < kKeys / 16; ++k)
                     mma_f16_ts(t ? o_col[1] : o_col[0], (t ? s_col[1] : s_col[0]) + 8 * k, b + k * (2048 >> 4), kValues, accumulate | (k ? 1u : 0u), lead);
             };
+            uint32_t it1 = 0, n_unit1 = 0;                // of the second tile of rows
             for (Cursor x(P, begin); x.more() && ok; x.next()) {
                 const uint32_t tiles = x.products();
+                const bool both = x.both();
                 if (tiles == 0) continue;
+                // Units of one tile of rows: the second tile's warps take no part in them, and must have done with the unit before (its
+                // record of NaN is cleared some units later).
+                if (!both && n_unit1) ok = bar_wait_warp(rows_out, (n_unit1 - 1u) & 1u, abort_word);
                 for (uint32_t i = 0; i < tiles && ok; ++i, ++it) {
-                    const uint32_t stage = it & 1u, turn = (it >> 1) & 1u, before = it - 1u;
+                    const uint32_t stage = it & 1u, turn = (it >> 1) & 1u;
                     ok = bar_wait_warp(k_full + 8 * stage, turn, abort_word) && (i || bar_wait_warp(q_ready, n_unit & 1u, abort_word));
                     if (!ok) break;
                     tc_after();
                     scores(0, stage);
                     tc_commit(s_full, lead);
-                    if (i) {
-                        ok = bar_wait_warp(p_ready + 8, before & 1u, abort_word);
-                        if (!ok) break;
-                        tc_after();
-                        values(1, before & 1u, i > 1u);
-                        tc_commit(v_free + 8 * (before & 1u), lead);
-                    } else {
-                        ok = bar_wait_warp(q_ready + 8, n_unit & 1u, abort_word);
-                        if (!ok) break;
-                        tc_after();
+                    if (both) {
+                        if (i) {
+                            ok = bar_wait_warp(p_ready + 8, (it1 - 1u) & 1u, abort_word);
+                            if (!ok) break;
+                            tc_after();
+                            values(1, stage ^ 1u, i > 1u);
+                            tc_commit(v_free + 8 * (stage ^ 1u), lead);
+                        } else {
+                            ok = bar_wait_warp(q_ready + 8, n_unit1 & 1u, abort_word);
+                            if (!ok) break;
+                            tc_after();
+                        }
+                        scores(1, stage);
+                        tc_commit(s_full + 8, lead);
+                        ++it1;
                     }
-                    scores(1, stage);
-                    tc_commit(s_full + 8, lead);
                     tc_commit(k_free + 8 * stage, lead);
                     ok = bar_wait_warp(v_full + 8 * stage, turn, abort_word) && bar_wait_warp(p_ready, it & 1u, abort_word);
                     if (!ok) break;
                     tc_after();
                     values(0, stage, i ? 1u : 0u);
+                    if (!both) tc_commit(v_free + 8 * stage, lead);
                     if (i + 1u == tiles) tc_commit(o_full, lead);
                 }
                 if (!ok) break;
-                const uint32_t before = it - 1u;
-                ok = bar_wait_warp(p_ready + 8, before & 1u, abort_word);
-                if (!ok) break;
-                tc_after();
-                values(1, before & 1u, tiles > 1u);
-                tc_commit(v_free + 8 * (before & 1u), lead);
-                tc_commit(o_full + 8, lead);
+                if (both) {
+                    ok = bar_wait_warp(p_ready + 8, (it1 - 1u) & 1u, abort_word);
+                    if (!ok) break;
+                    tc_after();
+                    values(1, (it - 1u) & 1u, tiles > 1u);
+                    tc_commit(v_free + 8 * ((it - 1u) & 1u), lead);
+                    tc_commit(o_full + 8, lead);
+                    ++n_unit1;
+                }
                 ++n_unit;
             }
             tc_commit(drained, lead);
@@ -420,11 +434,17 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         };
         float fac_next = 0.0f;
         bool rows_there = false;                          // of the unit that comes
+        uint32_t done = 0, n_done = 0;                    // tiles and units that this tile of rows took part in (it, n_unit: all)
         Cursor y(P, begin);                               // the unit after x
 #pragma unroll 1
         for (Cursor x(P, begin); x.more() && ok; x.next()) {
             y.next();
             const uint32_t tiles = x.products(), n_rows = x.r.rows * P.G;
+            if (t && !x.both()) {
+                it += tiles;
+                if (tiles) ++n_unit;
+                continue;
+            }
             const uint32_t row = x.row0() + t * 128u + l, i_row = row / P.G, g = row % P.G;
             const bool real = row < n_rows, any_real = __any_sync(0xFFFFFFFFu, real);
             const uint32_t lim = real ? sees(P, x.r, i_row) : most_of(P, x.r, x.p.j);
@@ -435,8 +455,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (!rows_there) fac_next = rows_in(x);
                 const float fac = fac_next;
                 rows_there = false;
-                for (uint32_t i = 0; i < tiles; ++i, ++it) {
-                    ok = bar_wait(s_full + 8 * t, it & 1u, abort_word);
+                for (uint32_t i = 0; i < tiles; ++i, ++it, ++done) {
+                    ok = bar_wait(s_full + 8 * t, done & 1u, abort_word);
                     if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                     tc_after();
                     const uint32_t t0 = (x.first + i) * kKeys;
@@ -540,11 +560,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     bar_arrive(p_ready + 8 * t);
                 }
                 if (!ok) break;
-                if (y.more() && y.products()) {
+                if (y.more() && y.products() && (!t || y.both())) {
                     fac_next = rows_in(y);
                     rows_there = true;
                 }
-                ok = bar_wait(o_full + 8 * t, n_unit & 1u, abort_word);
+                ok = bar_wait(o_full + 8 * t, n_done & 1u, abort_word);
                 if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
                 tc_after();
             }
@@ -597,7 +617,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 desc[0] = x.p.b, desc[1] = x.p.j, desc[2] = x.p.h, desc[3] = cta + 1u;
             }
             tc_before();
-            if (tiles) ++n_unit;
+            if (tiles) {
+                ++n_unit, ++n_done;
+                if (t) bar_arrive(rows_out);
+            }
         }
     }
     tc_before();
@@ -661,7 +684,7 @@ int launch(const AttendParams &P, cudaStream_t st) {
 }  // namespace
 
 // Rows enough to fill the products' 256: the other kernel takes 32 at a time and reads the cache again for each 32.
-bool ep::prompts_serve(uint32_t N, uint32_t B, uint32_t G) { return uint64_t(N) * G >= 96ull * B; }
+bool ep::prompts_serve(uint32_t N, uint32_t B, uint32_t G) { return uint64_t(N) * G > 16ull * B; }
 
 size_t ep::prompts_workspace_bytes(uint32_t grid, uint32_t dim) { return size_t(grid) * (8u + 2u * kUnitRows * (size_t(dim) + 2u)) * 4u; }
 
