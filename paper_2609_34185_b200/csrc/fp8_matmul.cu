@@ -426,11 +426,256 @@ int launch_split(MatmulParams P, const void *x, int64_t ldx, const void *w, int6
     return op_launch(matmul_split_kernel<BN, E>, uint32_t(tiles * P.split), 128, G::kSmem, P.split, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
+// ---- many tokens: a pair of CTAs per tile -----------------------------------------------------------------------------------
+// Two CTAs share tiles of 256 rows of the weight by 192 tokens (tcgen05 cta_group::2): each has half of the weight's rows and half of the
+// tokens in its shared memory, and keeps the sums of its 128 rows with all tokens in its tensor memory, twice, so that a tile is read out while the
+// next one is summed.  What bounds one CTA per tile of 128 x 128 is the operands' way from L2: 8.6 GB for 8192^3, 15.6 TB/s in
+// 551 us; a pair moves 5.0 GB.  (256 tokens would move 4.3, but two such accumulators leave tensor memory no room for scales.)
+//   warp 0        brings the operands in, seven stages of 128 columns
+//   warp 1        of the first CTA issues the products
+//   warps 2, 3    scales, four blocks of columns at a time: this CTA's rows' and all tokens'
+//   warps 4 - 7   sums to y
+struct PairShape {
+    static constexpr uint32_t kN = 192, kStages = 7, kA = kBlock * 128, kB = kN / 2 * 128, kStage = kA + kB;
+    static constexpr uint32_t kSlots = 4, kSlot = 512 + 1024, kSlotCols = 12;
+    static constexpr uint32_t kScales = kStages * kStage, kBars = kScales + kSlots * kSlot, kSmem = kBars + 512 + 1024;
+    static constexpr uint32_t kSf = 2 * kN;                              // columns of the accumulators
+    static_assert(kSf + kSlots * kSlotCols <= 512 && kSmem <= 232448);
+};
+__device__ __forceinline__ void pair_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t accumulate, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.ne.b32 q, %7, 0;\n\t"
+                 "@q tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+                 ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void pair_copy_scales(uint32_t tmem, uint32_t addr, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
+                 ::"r"(tmem), "l"(scales_desc(addr)), "r"(lead) : "memory");
+}
+// arrives at this barrier in both CTAs when what was issued before is done
+__device__ __forceinline__ void pair_commit(uint32_t bar, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\t.reg .b16 m;\n\tmov.b16 m, 3;\n\tsetp.ne.b32 q, %1, 0;\n\t"
+                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}" ::"r"(bar), "r"(lead) : "memory");
+}
+// at the first CTA's barrier
+__device__ __forceinline__ void first_arrive(uint32_t bar) {
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
+// a wait that sees what the other CTA wrote before it arrived (bar_wait_warp, acquired from the cluster)
+__device__ __forceinline__ bool pair_wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_word) {
+    bool ok = false;
+#pragma unroll 1
+    for (uint32_t i = 0; i < kOpSpinLimit && !ok; ++i) {
+        uint32_t r;
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
+                     : "=r"(r) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+        ok = r != 0;
+        if (!ok && (i & 63u) == 63u && ld_smem(abort_word)) break;
+    }
+    if (!ok) st_smem(abort_word, 1u);
+    return __all_sync(0xFFFFFFFFu, ok);
+}
+// a load into this CTA's memory that reports to the first CTA's barrier
+__device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, 0;\n\t"
+                 "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [a];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
+}
+
+template <class E>
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
+    matmul_pair_kernel(const __grid_constant__ MatmulParams P, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map) {
+    using G = PairShape;
+    using T = typename E::T;
+    extern __shared__ uint8_t raw[];
+    const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
+    const uint32_t rank = blockIdx.x & 1u, pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
+    const uint32_t full = base + G::kBars, empty = full + 8 * G::kStages, sfull = empty + 8 * G::kStages,
+                   sempty = sfull + 8 * G::kSlots, acc_full = sempty + 8 * G::kSlots, acc_empty = acc_full + 16, done = acc_empty + 16, slot_addr = done + 8,
+                   abort_word = slot_addr + 4;
+    if (tid == 0) {
+        for (uint32_t i = 0; i < G::kStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
+        for (uint32_t i = 0; i < G::kSlots; ++i) bar_init(sfull + 8 * i, 4), bar_init(sempty + 8 * i, 1);
+        for (uint32_t i = 0; i < 2; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 8);
+        bar_init(done, 1);
+        st_smem(abort_word, 0);
+        bar_init_done();
+    }
+    if (warp == 0) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot_addr), "r"(512u) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    tc_before();
+    __syncthreads();
+    cluster_sync();                                       // the other CTA's barriers are there
+    tc_after();
+    op_wait_for_stream();
+    const uint32_t tmem = ld_smem(slot_addr);
+    const uint32_t tiles = P.tiles_r * ((P.T + G::kN - 1u) / G::kN), nk = P.blocks;
+    uint32_t k_all = 0, c_all = 0, n = 0;                 // blocks, words of scales and tiles so far
+    bool ok = true;
+
+    if (warp == 0) {
+        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs) {
+            const uint32_t r0 = (tile % P.tiles_r) * 256u + rank * 128u, t0 = (tile / P.tiles_r) * G::kN + rank * (G::kN / 2);
+            for (uint32_t k = 0; k < nk; ++k, ++k_all) {
+                const uint32_t s = k_all % G::kStages, at = base + s * G::kStage;
+                if (k_all >= G::kStages) ok = bar_wait_warp(empty + 8 * s, (k_all / G::kStages - 1u) & 1u, abort_word);
+                if (!ok) break;
+                if (lane == 0) {
+                    if (rank == 0) bar_expect(full + 8 * s, 2 * G::kStage);       // both CTAs' halves
+                    pair_load_2d(at, &w_map, int32_t(k * 128u), int32_t(r0), full + 8 * s);
+                    pair_load_2d(at + G::kA, &x_map, int32_t(k * 128u), int32_t(t0), full + 8 * s);
+                }
+            }
+        }
+        // nothing may land after the pair's end (the second CTA's loads report to the first one, which waits for both)
+        if (ld_smem(abort_word) && lane == 0)
+            for (uint32_t j = k_all > G::kStages ? k_all - G::kStages : 0; j < k_all; ++j) bar_drain(full + 8 * (j % G::kStages), (j / G::kStages) & 1u);
+    } else if (warp == 1 && rank == 0) {
+        const uint32_t lead = elected();
+        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs, ++n) {
+            const uint32_t acc = tmem + (n & 1u) * G::kN;
+            if (n > 1u) ok = pair_wait_warp(acc_empty + 8 * (n & 1u), ((n >> 1) - 1u) & 1u, abort_word);
+            if (!ok) break;
+            tc_after();
+            for (uint32_t k = 0; k < nk; ++k, ++k_all) {
+                const uint32_t s = k_all % G::kStages, slot = c_all % G::kSlots, sa = tmem + G::kSf + slot * G::kSlotCols, sb = sa + 4;
+                if (k % 4 == 0) {
+                    ok = pair_wait_warp(sfull + 8 * slot, (c_all / G::kSlots) & 1u, abort_word);
+                    if (!ok) break;
+                    tc_after();
+                    const uint32_t at = base + G::kScales + slot * G::kSlot;
+                    pair_copy_scales(sa, at, lead);
+                    pair_copy_scales(sb, at + 512, lead);
+                    pair_copy_scales(sb + 4, at + 1024, lead);
+                }
+                ok = pair_wait_warp(full + 8 * s, (k_all / G::kStages) & 1u, abort_word);
+                if (!ok) break;
+                tc_after();
+                const uint64_t da = operand_desc(base + s * G::kStage), db = operand_desc(base + s * G::kStage + G::kA);
+                const uint32_t idesc = ((k % 4) << 4) | ((G::kN >> 3) << 17) | (1u << 23) | ((256u >> 4) << 24) | ((k % 4) << 29);
+#pragma unroll
+                for (uint32_t i = 0; i < 4; ++i) pair_mma(acc, da + 2 * i, db + 2 * i, idesc, sa, sb, (k | i) ? 1u : 0u, lead);
+                pair_commit(empty + 8 * s, lead);
+                if (k % 4 == 3 || k + 1u == nk) {
+                    pair_commit(sempty + 8 * slot, lead);
+                    ++c_all;
+                }
+            }
+            if (!ok) break;
+            pair_commit(acc_full + 8 * (n & 1u), lead);
+        }
+        pair_commit(done, lead);
+        bar_drain(done, 0);                               // nothing is in flight when the pair ends
+    } else if (warp == 1) {
+    } else if (warp < 4) {
+        // the scale words: byte i of a word is the scale of block k + i; row r of 128 lies at 16 (r % 32) + 4 (r / 32)
+        const uint32_t l = tid - 64u;
+        const bool words = (P.ldsx & 3) == 0 && (reinterpret_cast<uintptr_t>(P.sx) & 3u) == 0;
+        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs) {
+            const uint32_t rb = (tile % P.tiles_r) * 2u + rank, t0 = (tile / P.tiles_r) * G::kN;
+            for (uint32_t k = 0; k < nk; k += 4, ++c_all) {
+                const uint32_t slot = c_all % G::kSlots, at = base + G::kScales + slot * G::kSlot, left = min(4u, nk - k);
+                uint32_t word = 0x7F7F7F7Fu, xw[3];
+                if (P.sw && rb * kBlock < P.R) {
+                    const uint8_t *p = P.sw + int64_t(rb) * P.ldsw + k;
+                    word = 0;
+#pragma unroll
+                    for (uint32_t i = 0; i < 4; ++i)
+                        if (i < left) word |= uint32_t(__ldg(p + i)) << (8 * i);
+                }
+#pragma unroll
+                for (uint32_t j = 0; j < 3; ++j) {
+                    xw[j] = 0x7F7F7F7Fu;
+                    const uint32_t t = t0 + l + 64u * j;
+                    if (t < P.T) {
+                        const uint8_t *p = P.sx + int64_t(t) * P.ldsx + k;
+                        if (words && left == 4) {
+                            xw[j] = __ldg(reinterpret_cast<const uint32_t *>(p));
+                        } else {
+                            xw[j] = 0;
+#pragma unroll
+                            for (uint32_t i = 0; i < 4; ++i)
+                                if (i < left) xw[j] |= uint32_t(__ldg(p + i)) << (8 * i);
+                        }
+                    }
+                }
+                if (c_all >= G::kSlots) ok = bar_wait_warp(sempty + 8 * slot, (c_all / G::kSlots - 1u) & 1u, abort_word);
+                if (!ok) break;
+                st_smem(at + 4 * l, word);
+                st_smem(at + 4 * (l + 64u), word);
+#pragma unroll
+                for (uint32_t j = 0; j < 3; ++j) {
+                    const uint32_t t = l + 64u * j;
+                    st_smem(at + 512 + 512 * (t / 128) + 16 * (t % 32) + 4 * (t % 128 / 32), xw[j]);
+                }
+                fence_proxy_async();
+                __syncwarp();
+                if (lane == 0) first_arrive(sfull + 8 * slot);
+            }
+        }
+    } else {
+        const uint32_t quarter = warp & 3u;
+        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs, ++n) {
+            const uint32_t r = (tile % P.tiles_r) * 256u + rank * 128u + quarter * 32u + lane, t0 = (tile / P.tiles_r) * G::kN;
+            ok = bar_wait_warp(acc_full + 8 * (n & 1u), (n >> 1) & 1u, abort_word);
+            if (!ok) break;
+            tc_after();
+            const float a = P.a && r < P.R ? __ldg(P.a + r) : 1.0f;
+            T *y = static_cast<T *>(P.y) + r;
+#pragma unroll 1
+            for (uint32_t c = 0; c < G::kN; c += 32) {
+                if (t0 + c >= P.T) break;
+                uint32_t v[32];
+                tc_load32(tmem + (n & 1u) * G::kN + ((quarter * 32u) << 16) + c, v);
+                tc_loaded32(v);
+                if (r < P.R)
+#pragma unroll
+                    for (uint32_t i = 0; i < 32; ++i)
+                        if (t0 + c + i < P.T) y[int64_t(t0 + c + i) * P.ldy] = E::of(__uint_as_float(v[i]) * a);
+            }
+            tc_before();
+            __syncwarp();
+            if (lane == 0) first_arrive(acc_empty + 8 * (n & 1u));
+        }
+    }
+    tc_before();
+    __syncthreads();
+    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, 1u);
+    cluster_sync();                                       // the other CTA's memory is read and arrived at until here
+    if (warp == 0) {
+        tc_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
+    }
+}
+
+template <class E>
+int launch_pair(MatmulParams P, const void *x, int64_t ldx, const void *w, int64_t ldw, uint32_t C, cudaStream_t st) {
+    using G = PairShape;
+    static bool configured[64] = {};
+    int rc = op_configure(matmul_pair_kernel<E>, G::kSmem, configured);
+    if (rc) return rc;
+    CUtensorMap wm, xm;
+    if ((rc = byte_map(&wm, w, C, P.R, uint64_t(ldw), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+    if ((rc = byte_map(&xm, x, C, P.T, uint64_t(ldx), 128, G::kN / 2, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+    P.tiles_r = (P.R + 255u) / 256u;
+    const uint64_t tiles = uint64_t(P.tiles_r) * ((P.T + G::kN - 1u) / G::kN);
+    if (tiles > 0x7FFFFFFFu || tiles * P.blocks > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    const uint32_t pairs = uint32_t(op_sms()) / 2u, grid = 2u * uint32_t(tiles < pairs ? tiles : pairs);
+    return op_launch(matmul_pair_kernel<E>, grid, 256, G::kSmem, 1, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+}
+
 template <class E>
 int launch_matmul(const MatmulParams &P, const void *x, int64_t ldx, const void *w, int64_t ldw, uint32_t C, cudaStream_t st) {
     if (P.T <= 16) return launch_split<16, E>(P, x, ldx, w, ldw, C, st);
     if (P.T <= 32) return launch_split<32, E>(P, x, ldx, w, ldw, C, st);
     if (P.T <= 64) return launch_split<64, E>(P, x, ldx, w, ldw, C, st);
+#ifndef EP_PAIR
+#define EP_PAIR 1
+#endif
+    if (EP_PAIR) return launch_pair<E>(P, x, ldx, w, ldw, C, st);
     return launch_split<128, E>(P, x, ldx, w, ldw, C, st);
 }
 
