@@ -496,7 +496,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
                    abort_word = slot_addr + 4;
     if (tid == 0) {
         for (uint32_t i = 0; i < G::kStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (uint32_t i = 0; i < G::kSlots; ++i) bar_init(sfull + 8 * i, 4), bar_init(sempty + 8 * i, 1);
+        for (uint32_t i = 0; i < G::kSlots; ++i) bar_init(sfull + 8 * i, 2), bar_init(sempty + 8 * i, 1);
         for (uint32_t i = 0; i < 2; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 8);
         bar_init(done, 1);
         st_smem(abort_word, 0);
@@ -571,50 +571,51 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
         bar_drain(done, 0);                               // nothing is in flight when the pair ends
     } else if (warp == 1) {
     } else if (warp < 4) {
-        // the scale words: byte i of a word is the scale of block k + i; row r of 128 lies at 16 (r % 32) + 4 (r / 32)
-        const uint32_t l = tid - 64u;
+        // The scale words: byte i of a word is the scale of block k + i; row r of 128 lies at 16 (r % 32) + 4 (r / 32).  The two warps take
+        // words of four blocks in turn and ask for their next ones before they wait for room (a word's products take 0.8 us, about as
+        // long as its loads: one after the other they held the products up for half of the time).
         const bool words = (P.ldsx & 3) == 0 && (reinterpret_cast<uintptr_t>(P.sx) & 3u) == 0;
-        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs) {
-            const uint32_t rb = (tile % P.tiles_r) * 2u + rank, t0 = (tile / P.tiles_r) * G::kN;
-            for (uint32_t k = 0; k < nk; k += 4, ++c_all) {
-                const uint32_t slot = c_all % G::kSlots, at = base + G::kScales + slot * G::kSlot, left = min(4u, nk - k);
-                uint32_t word = 0x7F7F7F7Fu, xw[3];
-                if (P.sw && rb * kBlock < P.R) {
-                    const uint8_t *p = P.sw + int64_t(rb) * P.ldsw + k;
-                    word = 0;
+        const uint32_t per_tile = (nk + 3u) / 4u;
+        uint32_t tile = pair, q = 0;                      // the tile, and which of its words
+        auto step = [&](uint32_t by) {
+            for (q += by; q >= per_tile && tile < tiles; q -= per_tile) tile += pairs;
+        };
+        uint32_t word = 0, xw[6];
+        auto fetch = [&]() {
+            if (tile >= tiles) return;
+            const uint32_t k = 4u * q, left = min(4u, nk - k), rb = (tile % P.tiles_r) * 2u + rank, t0 = (tile / P.tiles_r) * G::kN;
+            auto four = [&](const uint8_t *p, bool aligned) {
+                if (aligned && left == 4) return __ldg(reinterpret_cast<const uint32_t *>(p));
+                uint32_t w = 0;
 #pragma unroll
-                    for (uint32_t i = 0; i < 4; ++i)
-                        if (i < left) word |= uint32_t(__ldg(p + i)) << (8 * i);
-                }
+                for (uint32_t i = 0; i < 4; ++i)
+                    if (i < left) w |= uint32_t(__ldg(p + i)) << (8 * i);
+                return w;
+            };
+            word = P.sw && rb * kBlock < P.R ? four(P.sw + int64_t(rb) * P.ldsw + k, false) : 0x7F7F7F7Fu;
 #pragma unroll
-                for (uint32_t j = 0; j < 3; ++j) {
-                    xw[j] = 0x7F7F7F7Fu;
-                    const uint32_t t = t0 + l + 64u * j;
-                    if (t < P.T) {
-                        const uint8_t *p = P.sx + int64_t(t) * P.ldsx + k;
-                        if (words && left == 4) {
-                            xw[j] = __ldg(reinterpret_cast<const uint32_t *>(p));
-                        } else {
-                            xw[j] = 0;
-#pragma unroll
-                            for (uint32_t i = 0; i < 4; ++i)
-                                if (i < left) xw[j] |= uint32_t(__ldg(p + i)) << (8 * i);
-                        }
-                    }
-                }
-                if (c_all >= G::kSlots) ok = bar_wait_warp(sempty + 8 * slot, (c_all / G::kSlots - 1u) & 1u, abort_word);
-                if (!ok) break;
-                st_smem(at + 4 * l, word);
-                st_smem(at + 4 * (l + 64u), word);
-#pragma unroll
-                for (uint32_t j = 0; j < 3; ++j) {
-                    const uint32_t t = l + 64u * j;
-                    st_smem(at + 512 + 512 * (t / 128) + 16 * (t % 32) + 4 * (t % 128 / 32), xw[j]);
-                }
-                fence_proxy_async();
-                __syncwarp();
-                if (lane == 0) first_arrive(sfull + 8 * slot);
+            for (uint32_t j = 0; j < 6; ++j) {
+                const uint32_t t = t0 + lane + 32u * j;
+                xw[j] = t < P.T ? four(P.sx + int64_t(t) * P.ldsx + k, words) : 0x7F7F7F7Fu;
             }
+        };
+        c_all = warp - 2u;
+        step(c_all);
+        fetch();
+        while (tile < tiles) {
+            const uint32_t slot = c_all % G::kSlots, at = base + G::kScales + slot * G::kSlot;
+            if (c_all >= G::kSlots) ok = bar_wait_warp(sempty + 8 * slot, (c_all / G::kSlots - 1u) & 1u, abort_word);
+            if (!ok) break;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) st_smem(at + 4 * (lane + 32u * j), word);
+#pragma unroll
+            for (uint32_t j = 0; j < 6; ++j) st_smem(at + 512 + 512 * (j / 4) + 16 * lane + 4 * (j % 4), xw[j]);
+            fence_proxy_async();
+            __syncwarp();
+            if (lane == 0) first_arrive(sfull + 8 * slot);
+            c_all += 2u;
+            step(2u);
+            fetch();
         }
     } else {
         const uint32_t quarter = warp & 3u;
