@@ -388,16 +388,30 @@ __global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant
             for (uint32_t i = 0; i < 16; ++i) st_smem(base + ((c + i) * 128u + tid) * 4u, v[i]);
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
-        const uint32_t c0 = BN * rank / P.split, c1 = BN * (rank + 1) / P.split;
-        for (uint32_t c = c0; c < c1 && t0 + c < P.T; ++c) {
-            float sum = 0.0f;
-            for (uint32_t p = 0; p < P.split; ++p) {
-                uint32_t at, v;
-                asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(at) : "r"(base + (c * 128u + tid) * 4u), "r"(p));
-                asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(at) : "memory");
-                sum += __uint_as_float(v);
-            }
-            if (r < P.R) y[int64_t(t0 + c) * P.ldy] = E::of(sum * a);
+        // this CTA's tokens, one to a warp, four rows to a lane; all CTAs' parts asked for at once, added in order
+        const uint32_t c0 = BN * rank / P.split, c1 = BN * (rank + 1) / P.split, r4 = r0 + 4u * lane;
+        uint32_t peer[8];
+        float a4[4];
+#pragma unroll
+        for (uint32_t p = 0; p < 8; ++p) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer[p]) : "r"(base), "r"(min(p, P.split - 1u)));
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) a4[j] = P.a && r4 + j < P.R ? __ldg(P.a + r4 + j) : 1.0f;
+#pragma unroll 2
+        for (uint32_t c = c0 + warp; c < c1; c += 4) {
+            if (t0 + c >= P.T) break;
+            float4 v[8];
+#pragma unroll
+            for (uint32_t p = 0; p < 8; ++p)
+                if (p < P.split)
+                    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v[p].x), "=f"(v[p].y), "=f"(v[p].z), "=f"(v[p].w) : "r"(peer[p] + (c * 128u + 4u * lane) * 4u) : "memory");
+            float sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+#pragma unroll
+            for (uint32_t p = 1; p < 8; ++p)
+                if (p < P.split) sum[0] += v[p].x, sum[1] += v[p].y, sum[2] += v[p].z, sum[3] += v[p].w;
+            T *dst = static_cast<T *>(P.y) + int64_t(t0 + c) * P.ldy + r4;
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j)
+                if (r4 + j < P.R) dst[j] = E::of(sum[j] * a4[j]);
         }
         asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
     }
@@ -419,9 +433,11 @@ int launch_split(MatmulParams P, const void *x, int64_t ldx, const void *w, int6
     if ((rc = byte_map(&wm, w, C, P.R, uint64_t(ldw), 128, 128, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
     if ((rc = byte_map(&xm, x, C, P.T, uint64_t(ldx), 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
     const uint64_t tiles = uint64_t(P.tiles_r) * ((P.T + BN - 1u) / BN);
-    // two CTAs fit an SM: as many as that allows share a tile, but none with fewer than two blocks of columns
+    // Two CTAs fit an SM: as many as that allows share a tile, but none has fewer than two blocks of columns.  (Five to seven are not
+    // taken: clusters of those sizes leave SMs of a GPC unused, 5120 x 17408 by one token in sevens 23.0 us, in fours 18.1.)
     P.split = 1;
-    while (P.split < 8 && tiles * P.split * 2 <= uint64_t(2 * sms) && P.split * 4 <= P.blocks) P.split *= 2;
+    for (const uint32_t n : {2u, 3u, 4u, 8u})
+        if (tiles * n <= uint64_t(2 * sms) && 2u * n <= P.blocks) P.split = n;
     if (tiles * P.split > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
     return op_launch(matmul_split_kernel<BN, E>, uint32_t(tiles * P.split), 128, G::kSmem, P.split, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
@@ -672,11 +688,17 @@ template <class E>
 int launch_matmul(const MatmulParams &P, const void *x, int64_t ldx, const void *w, int64_t ldw, uint32_t C, cudaStream_t st) {
     if (P.T <= 16) return launch_split<16, E>(P, x, ldx, w, ldw, C, st);
     if (P.T <= 32) return launch_split<32, E>(P, x, ldx, w, ldw, C, st);
-    if (P.T <= 64) return launch_split<64, E>(P, x, ldx, w, ldw, C, st);
-#ifndef EP_PAIR
-#define EP_PAIR 1
-#endif
-    if (EP_PAIR) return launch_pair<E>(P, x, ldx, w, ldw, C, st);
+    // (up to 128 tokens as two tiles of 64 where three CTAs can share each: 4096^2 8.8 us instead of 11.1, 512^2 6.3 / 8.8; without that 8192^2 21.1 / 20.0)
+    if (P.T <= 64 || (P.T <= 128 && 6ull * P.tiles_r <= 2ull * uint64_t(op_sms()))) return launch_split<64, E>(P, x, ldx, w, ldw, C, st);
+    // Estimates in units of 10 ns, fitted to 129 - 1024 tokens x 1024^2 .. 8192^2, 3000 x 1744 and 2048 x 17408: pairs take a round of all SMs
+    // after another, clusters share out blocks of columns.  us, pairs / clusters: 256 tokens x 1024^2 9.3 / 7.4, x 4096^2 15.3 / 13.4, x 8192^2
+    // 26.3 / 33.8, x 2048 x 17408 41.2 / 20.8, 1024 tokens 9.6 / 10.8, 24.7 / 23.8, 68 / 91, 42.7 / 60.4.
+    const int sms = op_sms();
+    if (sms <= 1) return EP_ERR_CUDA;
+    const uint64_t pairs = uint64_t(sms) / 2u, pair_tiles = uint64_t((P.R + 255u) / 256u) * ((P.T + PairShape::kN - 1u) / PairShape::kN),
+                   split_tiles = uint64_t(P.tiles_r) * ((P.T + 127u) / 128u);
+    const uint64_t by_pairs = 470u + (pair_tiles + pairs - 1u) / pairs * (27ull * P.blocks + 250u), by_clusters = 800u + 40ull * split_tiles * P.blocks / uint64_t(sms);
+    if (by_pairs < by_clusters) return launch_pair<E>(P, x, ldx, w, ldw, C, st);
     return launch_split<128, E>(P, x, ldx, w, ldw, C, st);
 }
 
