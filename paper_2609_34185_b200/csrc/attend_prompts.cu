@@ -16,7 +16,9 @@ __device__ unsigned int g_prompts_status = 0;
 //   warps 8 - 11         bring keys and values in and turn them into binary16, exactly, in the layout of the products' right operands; the
 //                        work for a token is shared by 256 rows.
 //   warp 12              issues the products.  While one tile's softmax runs, the other's products do.
-// (Warps 13 - 15 have nothing to do: registers go from one group of four warps to another.)
+//   warp 13              the scales of the pages.  (On the way of the warps that bring the keys in, table, scale, logarithm one after
+//                        the other, they took 700 cycles of every tile.)
+// (Warps 14 and 15 have nothing to do: registers go from one group of four warps to another.)
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
 // than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
 // t = score + log2(v_scale), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
@@ -26,7 +28,7 @@ __device__ unsigned int g_prompts_status = 0;
 // The tiles of tokens of all units form one list; every CTA takes an equal, contiguous share of it, as in kv_cache.cu, and what
 // crosses a share goes through the workspace: units are few and long, and 640 of unequal length on 148 SMs left a third of them idle.
 // ======================================================================================================================
-constexpr uint32_t kUnitRows = 256, kKeys = 128, kThreads = 32 * 16, kNanUnits = 8;
+constexpr uint32_t kUnitRows = 256, kKeys = 128, kHalfKeys = 64, kThreads = 32 * 16, kNanUnits = 8;
 constexpr float kSlack = 8.0f, kShift = 7.0f;
 // a piece of a unit in the workspace: O, then m and l of each row
 template <uint32_t D>
@@ -113,14 +115,16 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     uint8_t *gen = raw + (base - smem_u32(raw));
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     uint32_t *prefix = reinterpret_cast<uint32_t *>(gen + S::kPrefix), *nan_at = reinterpret_cast<uint32_t *>(gen + S::kNan);
-    const uint32_t bars = base + S::kBars, k_full = bars, k_free = bars + 16, v_full = bars + 32, v_free = bars + 48, s_full = bars + 64, p_ready = bars + 80,
-                   q_ready = bars + 96, o_full = bars + 112, drained = bars + 128, rows_out = bars + 136, slot_addr = bars + 144, abort_word = bars + 148;
+    const uint32_t bars = base + S::kBars, k_full = bars, k_free = bars + 16, v_full = bars + 32, v_free = bars + 48, s_full = bars + 64, p_ready = bars + 96,
+                   q_ready = bars + 128, o_full = bars + 144, o_moved = bars + 160, drained = bars + 176, rows_out = bars + 184, slot_addr = bars + 192,
+                   abort_word = bars + 196;
     if (tid == 0) {
         for (uint32_t i = 0; i < 2; ++i) {
-            bar_init(k_full + 8 * i, 128), bar_init(v_full + 8 * i, 128);
-            bar_init(k_free + 8 * i, 1), bar_init(v_free + 8 * i, 1), bar_init(s_full + 8 * i, 1), bar_init(o_full + 8 * i, 1);
-            bar_init(p_ready + 8 * i, 128), bar_init(q_ready + 8 * i, 128);
+            bar_init(k_full + 8 * i, 129), bar_init(v_full + 8 * i, 128);
+            bar_init(k_free + 8 * i, 1), bar_init(v_free + 8 * i, 1), bar_init(o_full + 8 * i, 1), bar_init(o_moved + 8 * i, 1);
+            bar_init(q_ready + 8 * i, 128);
         }
+        for (uint32_t i = 0; i < 4; ++i) bar_init(s_full + 8 * i, 1), bar_init(p_ready + 8 * i, 128);       // of tile t and buffer i: 2 t + i
         bar_init(drained, 1);
         bar_init(rows_out, 128);
         st_smem(abort_word, 0);
@@ -187,8 +191,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     uint32_t *desc = P.workspace ? reinterpret_cast<uint32_t *>(P.workspace) + blockIdx.x * 8u : nullptr;
     if (desc && tid == 0) desc[3] = 0;
     __syncthreads();
-    // tensor memory: scores (and weights) of the two tiles, then their accumulators
-    const uint32_t s_col[2] = {tmem, tmem + 128u}, o_col[2] = {tmem + 256u, tmem + 384u};
+    // tensor memory: two buffers of scores (and weights) of each tile, 64 columns each, then the accumulators
+    const uint32_t o_col[2] = {tmem + 256u, tmem + 384u};
     uint32_t it = 0, n_unit = 0;                          // tiles of tokens and units so far
     bool ok = true;
 
@@ -198,75 +202,122 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         // ---- products -----------------------------------------------------------------------------------------------------
         if (warp == 12) {
             const uint32_t lead = elected();
-            constexpr uint32_t kScores = f16_idesc(kKeys, 0), kValues = f16_idesc(D, 1);
-            auto scores = [&](uint32_t t, uint32_t stage) {
+            constexpr uint32_t kScores = f16_idesc(kHalfKeys, 0), kValues = f16_idesc(D, 1);
+            // half n of a unit's tokens: 64 of them, buffer n mod 2; `stage`: where its 128 tokens lie
+            auto scores = [&](uint32_t t, uint32_t n, uint32_t stage) {
                 // (descriptors differ in their address, 16 bytes a step of it: 32 bytes further along the swizzled rows, then the next 64 columns)
-                const uint64_t a = operand_desc(base + S::kQ + t * S::kTile), b = operand_desc(base + S::kK + stage * S::kTile);
+                const uint64_t a = operand_desc(base + S::kQ + t * S::kTile), b = operand_desc(base + S::kK + stage * S::kTile + (n & 1u) * kHalfKeys * 128u);
 #pragma unroll
                 for (uint32_t k = 0; k < D / 16; ++k) {
                     const uint32_t at = (k / 4 * S::kHalf + k % 4 * 32) >> 4;
-                    mma_f16_ss(t ? s_col[1] : s_col[0], a + at, b + at, kScores, k ? 1u : 0u, lead);
+                    mma_f16_ss(tmem + t * 128u + (n & 1u) * 64u, a + at, b + at, kScores, k ? 1u : 0u, lead);
                 }
+                tc_commit(s_full + 8 * (2 * t + (n & 1u)), lead);
             };
-            auto values = [&](uint32_t t, uint32_t stage, uint32_t accumulate) {
-                const uint64_t b = operand_desc(base + S::kV + stage * S::kTile, S::kHalf);
+            auto values = [&](uint32_t t, uint32_t n, uint32_t stage) {
+                const uint64_t b = operand_desc(base + S::kV + stage * S::kTile + (n & 1u) * kHalfKeys * 128u, S::kHalf);
 #pragma unroll
-                for (uint32_t k = 0; k < kKeys / 16; ++k)
-                    mma_f16_ts(t ? o_col[1] : o_col[0], (t ? s_col[1] : s_col[0]) + 8 * k, b + k * (2048 >> 4), kValues, accumulate | (k ? 1u : 0u), lead);
+                for (uint32_t k = 0; k < kHalfKeys / 16; ++k)
+                    mma_f16_ts(t ? o_col[1] : o_col[0], tmem + t * 128u + (n & 1u) * 64u + 8 * k, b + k * (2048 >> 4), kValues, n | k ? 1u : 0u, lead);
+                tc_commit(o_moved + 8 * t, lead);
             };
+            // Scores run two halves ahead of the weights, so that a tile's softmax finds its next scores ready.  (Scores of 128 tokens at
+            // a time in one buffer: softmax, second product, first product one after the other for each tile of rows, 340 us.)
             uint32_t it1 = 0, n_unit1 = 0;                // of the second tile of rows
             for (Cursor x(P, begin); x.more() && ok; x.next()) {
-                const uint32_t tiles = x.products();
+                const uint32_t tiles = x.products(), halves = 2u * tiles;
                 const bool both = x.both();
                 if (tiles == 0) continue;
                 // Units of one tile of rows: the second tile's warps take no part in them, and must have done with the unit before (its
                 // record of NaN is cleared some units later).
                 if (!both && n_unit1) ok = bar_wait_warp(rows_out, (n_unit1 - 1u) & 1u, abort_word);
-                for (uint32_t i = 0; i < tiles && ok; ++i, ++it) {
-                    const uint32_t stage = it & 1u, turn = (it >> 1) & 1u;
-                    ok = bar_wait_warp(k_full + 8 * stage, turn, abort_word) && (i || bar_wait_warp(q_ready, n_unit & 1u, abort_word));
+                ok = ok && bar_wait_warp(k_full + 8 * (it & 1u), (it >> 1) & 1u, abort_word) && bar_wait_warp(q_ready, n_unit & 1u, abort_word);
+                if (!ok) break;
+                tc_after();
+                scores(0, 0, it & 1u);
+                if (both) {
+                    ok = bar_wait_warp(q_ready + 8, n_unit1 & 1u, abort_word);
                     if (!ok) break;
                     tc_after();
-                    scores(0, stage);
-                    tc_commit(s_full, lead);
-                    if (both) {
-                        if (i) {
-                            ok = bar_wait_warp(p_ready + 8, (it1 - 1u) & 1u, abort_word);
-                            if (!ok) break;
-                            tc_after();
-                            values(1, stage ^ 1u, i > 1u);
-                            tc_commit(v_free + 8 * (stage ^ 1u), lead);
-                        } else {
-                            ok = bar_wait_warp(q_ready + 8, n_unit1 & 1u, abort_word);
-                            if (!ok) break;
-                            tc_after();
-                        }
-                        scores(1, stage);
-                        tc_commit(s_full + 8, lead);
-                        ++it1;
+                    scores(1, 0, it & 1u);
+                }
+                scores(0, 1, it & 1u);
+                if (both) scores(1, 1, it & 1u);
+                tc_commit(k_free + 8 * (it & 1u), lead);
+#pragma unroll 1
+                for (uint32_t n = 0; n < halves; ++n) {
+                    const uint32_t now = it + n / 2u, stage = now & 1u, later = now + 1u, ahead = later & 1u;
+                    const bool more = n + 2u < halves;
+                    if (!(n & 1u)) ok = bar_wait_warp(v_full + 8 * stage, (now >> 1) & 1u, abort_word);
+                    ok = ok && bar_wait_warp(p_ready + 8 * (n & 1u), now & 1u, abort_word);
+                    if (!ok) break;
+                    tc_after();
+                    values(0, n, stage);
+                    if (more) {
+                        if (!(n & 1u)) ok = bar_wait_warp(k_full + 8 * ahead, (later >> 1) & 1u, abort_word);
+                        if (!ok) break;
+                        tc_after();
+                        scores(0, n + 2u, ahead);
                     }
-                    tc_commit(k_free + 8 * stage, lead);
-                    ok = bar_wait_warp(v_full + 8 * stage, turn, abort_word) && bar_wait_warp(p_ready, it & 1u, abort_word);
-                    if (!ok) break;
-                    tc_after();
-                    values(0, stage, i ? 1u : 0u);
-                    if (!both) tc_commit(v_free + 8 * stage, lead);
-                    if (i + 1u == tiles) tc_commit(o_full, lead);
+                    if (both) {
+                        ok = bar_wait_warp(p_ready + 8 * (2u + (n & 1u)), (it1 + n / 2u) & 1u, abort_word);
+                        if (!ok) break;
+                        tc_after();
+                        values(1, n, stage);
+                        if (more) scores(1, n + 2u, ahead);
+                    }
+                    if (n & 1u) {
+                        tc_commit(v_free + 8 * stage, lead);
+                        if (more) tc_commit(k_free + 8 * ahead, lead);
+                    }
                 }
                 if (!ok) break;
+                tc_commit(o_full, lead);
                 if (both) {
-                    ok = bar_wait_warp(p_ready + 8, (it1 - 1u) & 1u, abort_word);
-                    if (!ok) break;
-                    tc_after();
-                    values(1, (it - 1u) & 1u, tiles > 1u);
-                    tc_commit(v_free + 8 * ((it - 1u) & 1u), lead);
                     tc_commit(o_full + 8, lead);
                     ++n_unit1;
+                    it1 += tiles;
                 }
+                it += tiles;
                 ++n_unit;
             }
             tc_commit(drained, lead);
             bar_drain(drained, 0);                        // nothing is in flight when tensor memory is given back
+        }
+        if (warp == 13) {
+            // ---- scales ---------------------------------------------------------------------------------------------------
+            // of groups of 16 tokens, lane = group: the page of tile i + 2 and the scales of tile i + 1 are on their way while tile i's are written
+            for (Cursor x(P, begin); x.more() && ok; x.next()) {
+                const uint32_t tiles = x.products(), t_first = x.first * kKeys;
+                if (tiles == 0) continue;
+                const int32_t *table = P.q.table + int64_t(x.p.b) * P.q.ldt;
+                auto page_at = [&](uint32_t i) {          // -1: no token, or (reported by the warps that bring it in) no page
+                    const uint32_t t = t_first + i * kKeys + 16u * lane;
+                    const int32_t id = lane < 8 && i < tiles && t < x.r.len ? __ldg(table + (t >> P.q.shift)) : -1;
+                    return uint32_t(id) < P.q.pages ? id : -1;
+                };
+                auto scales_at = [&](int32_t page, float &ks, float &vs) {
+                    const size_t block = size_t(uint32_t(max(page, 0))) * P.q.H + x.p.h;
+                    ks = page >= 0 ? __ldg(P.ks + block) : -1.0f;
+                    vs = page >= 0 ? __ldg(P.vs + block) : 1.0f;
+                };
+                float ks, vs, ks_next, vs_next;
+                scales_at(page_at(0), ks, vs);
+                int32_t page = page_at(1);
+#pragma unroll 1
+                for (uint32_t i = 0; i < tiles; ++i, ++it) {
+                    scales_at(page, ks_next, vs_next);
+                    page = page_at(i + 2u);
+                    const uint32_t stage = it & 1u;
+                    if (it > 1u) ok = bar_wait_warp(k_free + 8 * stage, (it >> 1 & 1u) ^ 1u, abort_word);
+                    if (!ok) break;
+                    const float some = fmaxf(vs, 1e-30f);
+                    if (lane < 8) *reinterpret_cast<float4 *>(gen + S::kMeta + ((it & 3u) * 8u + lane) * 16u) = make_float4(ks, log2f(some), __fdiv_rn(1.0f, some), 0.0f);
+                    __syncwarp();
+                    if (lane == 0) bar_arrive(k_full + 8 * stage);
+                    ks = ks_next, vs = vs_next;
+                }
+            }
         }
     } else if (warp >= 8) {
         asm volatile("setmaxnreg.dec.sync.aligned.u32 104;");
@@ -354,22 +405,10 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     }
                 }
             };
-            // a group's scales (threads 0 - 7), a tile ahead
-            float ks = -1.0f, vs = 1.0f;
-            auto scales_of = [&](uint32_t t0) {
-                if (l >= 8) return;
-                const int32_t page = page_at(t0 + 16u * l);
-                ks = -1.0f, vs = 1.0f;
-                if (page >= 0) {
-                    const size_t block = size_t(uint32_t(page)) * P.q.H + x.p.h;
-                    ks = __ldg(P.ks + block), vs = __ldg(P.vs + block);
-                }
-            };
             uint4 kv[kLoads], vv[kLoads];
             int32_t id0 = page_at(t_first + w * 32u), id1 = page_at(t_first + w * 32u + 16u);
             load(P.k, t_first, id0, id1, kv);
             load(P.v, t_first, id0, id1, vv);
-            scales_of(t_first);
             if (tiles > 1) id0 = page_at(t_first + kKeys + w * 32u), id1 = page_at(t_first + kKeys + w * 32u + 16u);
 #pragma unroll 1
             for (uint32_t i = 0; i < tiles; ++i, ++it) {
@@ -378,14 +417,9 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (!ok) break;
                 store(base + S::kK + stage * S::kTile, kv);
                 fence_proxy_async();
-                if (l < 8) {
-                    const float some = fmaxf(vs, 1e-30f);
-                    *reinterpret_cast<float4 *>(gen + S::kMeta + ((it & 3u) * 8u + l) * 16u) = make_float4(ks, log2f(some), __fdiv_rn(1.0f, some), 0.0f);
-                }
                 bar_arrive(k_full + 8 * stage);
                 if (i + 1u < tiles) {
                     load(P.k, t0 + kKeys, id0, id1, kv);
-                    scales_of(t0 + kKeys);
                 }
                 if (it > 1u) ok = __all_sync(0xFFFFFFFFu, bar_wait(v_free + 8 * stage, turn ^ 1u, abort_word));
                 if (!ok) break;
@@ -404,7 +438,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         asm volatile("setmaxnreg.inc.sync.aligned.u32 168;");
         // ---- softmax --------------------------------------------------------------------------------------------------------
         const uint32_t t = warp >> 2, l = tid & 127u, quarter = (warp & 3u) * 32u;
-        const uint32_t s_mine = (t ? s_col[1] : s_col[0]) + (quarter << 16), o_mine = (t ? o_col[1] : o_col[0]) + (quarter << 16);
+        const uint32_t s_mine = tmem + t * 128u + (quarter << 16), o_mine = (t ? o_col[1] : o_col[0]) + (quarter << 16);
         // Rows of a unit's tile as binary16, times a power of two that puts a row's largest magnitude in [2^13, 2^14) (see kv_cache.cu),
         // with the sign of the scale; returns the factor of the row's scores.  They go in as soon as the scores of the unit before are done.
         auto rows_in = [&](const Cursor &y) {
@@ -455,110 +489,95 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (!rows_there) fac_next = rows_in(x);
                 const float fac = fac_next;
                 rows_there = false;
-                for (uint32_t i = 0; i < tiles; ++i, ++it, ++done) {
-                    ok = bar_wait(s_full + 8 * t, done & 1u, abort_word);
-                    if (!__all_sync(0xFFFFFFFFu, ok)) { ok = false; break; }
+#pragma unroll 1
+                for (uint32_t n = 0; n < 2u * tiles; ++n) {
+                    const uint32_t buffer = n & 1u, turn = done + n / 2u;
+                    ok = bar_wait_warp(s_full + 8 * (2 * t + buffer), turn & 1u, abort_word);
+                    if (!ok) break;
                     tc_after();
-                    const uint32_t t0 = (x.first + i) * kKeys;
-                    const float4 *meta = reinterpret_cast<const float4 *>(gen + S::kMeta) + (it & 3u) * 8u;
+                    const uint32_t t0 = x.first * kKeys + n * kHalfKeys, s_at = s_mine + buffer * 64u;
+                    const float4 *meta = reinterpret_cast<const float4 *>(gen + S::kMeta) + ((it + n / 2u) & 3u) * 8u + buffer * 4u;
                     if (any_real) {
-                        float low = 0.0f;
+                        float4 scale[4];
 #pragma unroll
-                        for (uint32_t k = 0; k < 8; ++k) low = fminf(low, meta[k].x);
+                        for (uint32_t k = 0; k < 4; ++k) scale[k] = meta[k];
+                        const bool out = fminf(fminf(scale[0].x, scale[1].x), fminf(scale[2].x, scale[3].x)) < 0.0f;
                         auto tile = [&](auto edge_tag) {
                             constexpr bool kEdge = decltype(edge_tag)::value;
-                            float top = -INFINITY;
                             uint32_t v[2][32];
-                            auto highest = [&](const uint32_t (&v)[32], uint32_t c) {
+                            tc_load32(s_at, v[0]);
+                            tc_load32(s_at + 32, v[1]);
+                            tc_loaded32(v[0]);
+                            tc_loaded32(v[1]);
+                            float top = -INFINITY;
 #pragma unroll
-                                for (uint32_t k = 0; k < 2; ++k) {
-                                    const float4 s = meta[2 * c + k];
-                                    float best = -INFINITY;
+                            for (uint32_t k = 0; k < 4; ++k) {
+                                float best = -INFINITY;
 #pragma unroll
-                                    for (uint32_t e = 0; e < 16; e += 2) {
-                                        float f[2];
+                                for (uint32_t e = 0; e < 16; e += 2) {
+                                    float f[2];
 #pragma unroll
-                                        for (uint32_t z = 0; z < 2; ++z) {
-                                            f[z] = __uint_as_float(v[16 * k + e + z]);
-                                            if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) f[z] = -INFINITY;
-                                        }
-                                        best = max3(best, f[0], f[1]);
+                                    for (uint32_t z = 0; z < 2; ++z) {
+                                        uint32_t &w = v[k / 2][16 * (k % 2) + e + z];
+                                        if (kEdge && (t0 + 16 * k + e + z >= lim || scale[k].x < 0.0f)) w = 0xFF800000u;        // -infinity
+                                        f[z] = __uint_as_float(w);
                                     }
-                                    const float here = fmaf(best, fac * s.x, s.y);
-                                    top = fmaxf(top, kEdge && best == -INFINITY ? -INFINITY : here);
+                                    best = max3(best, f[0], f[1]);
                                 }
-                            };
-                            tc_load32(s_mine, v[0]);
-#pragma unroll 1
-                            for (uint32_t c = 0; c < 4; c += 2) {
-                                tc_loaded32(v[0]);
-                                tc_load32(s_mine + 32 * (c + 1), v[1]);
-                                highest(v[0], c);
-                                tc_loaded32(v[1]);
-                                tc_load32(s_mine + 32 * ((c + 2) & 3u), v[0]);           // (at the end the first ones again, for the second pass)
-                                highest(v[1], c + 1);
+                                const float here = fmaf(best, fac * scale[k].x, scale[k].y);
+                                top = fmaxf(top, kEdge && best == -INFINITY ? -INFINITY : here);
                             }
                             const bool move = top > m + kSlack;                          // (also from -infinity)
                             if (__any_sync(0xFFFFFFFFu, move)) {
                                 const float f = move ? exp2_fast(m - top) : 1.0f;
                                 if (move) m = top;
                                 sum *= f;
-                                if (i) {
-                                    tc_loaded32(v[0]);
+                                if (n) {
+                                    ok = bar_wait_warp(o_moved + 8 * t, (2u * done + n - 1u) & 1u, abort_word);       // (the half before is in the accumulator)
+                                    tc_after();
 #pragma unroll 1
-                                    for (uint32_t c = 0; c < D / 32; ++c) {
-                                        tc_load32(o_mine + 32 * c, v[1]);
-                                        tc_loaded32(v[1]);
+                                    for (uint32_t c = 0; c < D; c += 16) {
+                                        uint32_t a[16];
+                                        tc_load16(o_mine + c, a);
+                                        tc_loaded16(a);
 #pragma unroll
-                                        for (uint32_t e = 0; e < 32; ++e) v[1][e] = __float_as_uint(__uint_as_float(v[1][e]) * f);
-                                        tc_store32(o_mine + 32 * c, v[1]);
+                                        for (uint32_t e = 0; e < 16; ++e) a[e] = __float_as_uint(__uint_as_float(a[e]) * f);
+                                        tc_store16(o_mine + c, a);
                                     }
                                 }
                             }
                             const float sub = m == -INFINITY ? 0.0f : m - kShift;
-                            auto weigh = [&](const uint32_t (&v)[32], uint32_t c) {
-                                uint32_t p[16];
+                            uint32_t p[32];
 #pragma unroll
-                                for (uint32_t k = 0; k < 2; ++k) {
-                                    const float4 s = meta[2 * c + k];
-                                    const float by = fac * s.x, off = s.y - sub;
-                                    const uint64_t by2 = pair_of(by, by), off2 = pair_of(off, off);
-                                    uint64_t part = 0;
+                            for (uint32_t k = 0; k < 4; ++k) {
+                                const float by = fac * scale[k].x, off = scale[k].y - sub;
+                                const uint64_t by2 = pair_of(by, by), off2 = pair_of(off, off);
+                                uint64_t part = 0;
 #pragma unroll
-                                    for (uint32_t e = 0; e < 16; e += 2) {
-                                        float f[2];
-                                        pair_to(fma2(pair_of(__uint_as_float(v[16 * k + e]), __uint_as_float(v[16 * k + e + 1])), by2, off2), f[0], f[1]);
-#pragma unroll
-                                        for (uint32_t z = 0; z < 2; ++z) {
-                                            if (kEdge && (t0 + 32 * c + 16 * k + e + z >= lim || s.x < 0.0f)) f[z] = -INFINITY;
-                                            f[z] = exp2_fast(f[z]);
-                                        }
-                                        part = add2(part, pair_of(f[0], f[1]));
-                                        p[8 * k + e / 2] = Fp16::two(f[0], f[1]);
-                                    }
-                                    float odd, even;
-                                    pair_to(part, even, odd);
-                                    sum = fmaf(even + odd, s.z, sum);
+                                for (uint32_t e = 0; e < 16; e += 2) {
+                                    const uint32_t w0 = v[k / 2][16 * (k % 2) + e], w1 = v[k / 2][16 * (k % 2) + e + 1];
+                                    float f[2];
+                                    pair_to(fma2(pair_of(__uint_as_float(w0), __uint_as_float(w1)), by2, off2), f[0], f[1]);
+                                    if (kEdge) f[0] = w0 == 0xFF800000u ? -INFINITY : f[0], f[1] = w1 == 0xFF800000u ? -INFINITY : f[1];       // (by may be 0 or negative)
+                                    f[0] = exp2_fast(f[0]), f[1] = exp2_fast(f[1]);
+                                    part = add2(part, pair_of(f[0], f[1]));
+                                    p[8 * k + e / 2] = Fp16::two(f[0], f[1]);
                                 }
-                                tc_store16(s_mine + 16 * c, p);
-                            };
-#pragma unroll 1
-                            for (uint32_t c = 0; c < 4; c += 2) {                        // (weights of columns 32 c .. go over scores 16 c .., which have been read)
-                                tc_loaded32(v[0]);
-                                tc_load32(s_mine + 32 * (c + 1), v[1]);
-                                weigh(v[0], c);
-                                tc_loaded32(v[1]);
-                                if (c == 0) tc_load32(s_mine + 64, v[0]);
-                                weigh(v[1], c + 1);
+                                float odd, even;
+                                pair_to(part, even, odd);
+                                sum = fmaf(even + odd, scale[k].z, sum);
                             }
+                            tc_store32(s_at, p);                                         // over the scores, which have been read
                             tc_stored();
                         };
-                        if (t0 + kKeys > lim_least || low < 0.0f) tile(std::true_type{});
+                        if (t0 + kHalfKeys > lim_least || out) tile(std::true_type{});
                         else tile(std::false_type{});
                     }
                     tc_before();
-                    bar_arrive(p_ready + 8 * t);
+                    bar_arrive(p_ready + 8 * (2 * t + buffer));
                 }
+                it += tiles;
+                done += tiles;
                 if (!ok) break;
                 if (y.more() && y.products() && (!t || y.both())) {
                     fac_next = rows_in(y);

@@ -169,6 +169,7 @@ __device__ __forceinline__ void tc_load32(uint32_t tmem, uint32_t (&v)[32]) {
 __device__ __forceinline__ void tc_loaded32(uint32_t (&v)[32]) {
     asm volatile("tcgen05.wait::ld.sync.aligned;" : EP_U8(v, 0), EP_U8(v, 8), EP_U8(v, 16), EP_U8(v, 24)::"memory");
 }
+__device__ __forceinline__ void tc_loaded16(uint32_t (&v)[16]) { asm volatile("tcgen05.wait::ld.sync.aligned;" : EP_U8(v, 0), EP_U8(v, 8)::"memory"); }
 __device__ __forceinline__ void tc_loaded() { asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ void tc_store16(uint32_t tmem, const uint32_t (&v)[16]) {
     asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};"
