@@ -696,7 +696,7 @@ int launch(const AttendParams &P, cudaStream_t st) {
     const int rc = op_configure(prompts_kernel<E, D>, PromptShape<D>::kSmem, configured);
     if (rc) return rc;
     if (op_launch(prompts_kernel<E, D>, P.grid, kThreads, PromptShape<D>::kSmem, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
-    if (P.workspace && op_launch(prompts_join_kernel<E, D>, dim3(P.grid, 8), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    if (P.workspace && op_launch(prompts_join_kernel<E, D>, dim3(P.grid, kUnitRows * D / 4u / 256u), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
     return EP_OK;
 }
 

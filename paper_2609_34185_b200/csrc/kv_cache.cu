@@ -2,6 +2,8 @@
 // reads the pages.
 #include "kv_cache.hpp"
 
+#include <algorithm>
+
 using namespace ep;
 
 namespace {
@@ -12,8 +14,9 @@ __device__ unsigned int g_cache_status = 0;
 // Append.  For a page and head with scale s and older tokens q: s' = max(s, the smallest power of two that holds the new tokens), the
 // older tokens become e4m3(q s / s') if it grew, the new ones e4m3(x / s').  Powers of two: moving to a larger scale is exact but
 // for values that fall below E4M3's normal range, so a token is not rounded again each time its page's scale grows.  A page without
-// older tokens forgets what it held.  One warp (or CTA) per page, head and cache; a single new token that fits the scale costs one
-// read and write of its row.
+// older tokens forgets what it held.  One warp (or CTA) per page and head, for keys and values together: what bounds a page
+// is one chain of reads, lengths, table, rows (with keys and values apart 5 prompts of up to 4096 tokens took 26.4 us); a single new token that fits the scale
+// costs one read and write of its row.
 // ======================================================================================================================
 struct AppendParams {
     Requests q;
@@ -22,28 +25,26 @@ struct AppendParams {
     uint8_t *cache[2];
     float *scales[2];
     uint32_t D;
-    uint32_t spans;               // grid: spans pages side by side, x heads x 2 x requests
+    uint32_t spans;               // grid: spans pages side by side, x heads x requests
 };
 constexpr uint32_t kLeastScale = 127 - 100;      // of a page of zeros: 2^-100, which any value outgrows
 
 template <class E, uint32_t WARPS>
 __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ AppendParams P) {
     using T = typename E::T;
-    constexpr uint32_t kThreads = 32 * WARPS, kHeld = WARPS == 1 ? 2 : 8;
-    __shared__ float largest_of[4];
+    // rows of a lane that are held in registers, of keys and values each, and then read once: by a CTA 64 tokens of 128 dimensions, by a warp 16
+    constexpr uint32_t kThreads = 32 * WARPS, kHeld = 8;
+    __shared__ float largest_of[2][4];
     op_wait_for_stream();
     const uint32_t tid = WARPS == 1 ? threadIdx.x & 31u : threadIdx.x, lane = tid & 31u;
-    const uint64_t unit = WARPS == 1 ? uint64_t(blockIdx.x) * 4u + (threadIdx.x >> 5) : blockIdx.x;
-    uint64_t rest = unit;
+    uint64_t rest = WARPS == 1 ? uint64_t(blockIdx.x) * 4u + (threadIdx.x >> 5) : blockIdx.x;
     const uint32_t span = uint32_t(rest % P.spans); rest /= P.spans;
-    const uint32_t h = uint32_t(rest % P.q.H); rest /= P.q.H;
-    const uint32_t which = uint32_t(rest & 1u), b = uint32_t(rest >> 1);
+    const uint32_t h = uint32_t(rest % P.q.H), b = uint32_t(rest / P.q.H);
     if (b >= P.q.B) return;
     const Extent r = extent_of(P.q, b);
     const uint32_t rows = min(r.rows, r.len);             // (more rows than tokens: the first ones have no place)
     if (rows == 0) return;
     const uint32_t first = r.len - rows, lanes = P.D / 8u, at = tid % lanes * 8u, sub = tid / lanes, step = kThreads / lanes;
-    const T *x = static_cast<const T *>(P.x[which]) + int64_t(h) * P.ldh[which] + at;
     for (uint32_t j = (first >> P.q.shift) + span; j <= (r.len - 1u) >> P.q.shift; j += P.spans) {
         const int32_t id = __ldg(P.q.table + int64_t(b) * P.q.ldt + j);
         if (id < 0 || uint32_t(id) >= P.q.pages) {
@@ -52,39 +53,45 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
         }
         const uint32_t p0 = j << P.q.shift, lo = max(first, p0), hi = min(r.len, p0 + P.q.page);        // new tokens of this page
         const uint64_t block = uint64_t(uint32_t(id)) * P.q.H + h;
-        uint8_t *dst = P.cache[which] + (block << P.q.shift) * P.D + at;
-        auto row_of = [&](uint32_t pos) { return x + int64_t(r.row + (r.rows - rows) + pos - first) * P.ldx[which]; };
-        // kHeld rows of a lane at a time; a page of up to 64 tokens of 128 dimensions (by a CTA) is held whole and read once
-        float a = 0.0f;
-        uint4 held[kHeld];
-        for (uint32_t from = lo + sub; from < hi; from += kHeld * step) {
+        const bool once = hi - lo <= kHeld * step, older = lo > p0;
+        uint4 held[2][kHeld];
+        float had[2] = {0.0f, 0.0f}, a[2] = {0.0f, 0.0f};
+        if (older) had[0] = P.scales[0][block], had[1] = P.scales[1][block];
+        auto source = [&](uint32_t which) { return static_cast<const T *>(P.x[which]) + int64_t(r.row + (r.rows - rows) + lo - first) * P.ldx[which] + int64_t(h) * P.ldh[which] + at; };
+        for (uint32_t from = sub; from < hi - lo; from += kHeld * step) {
 #pragma unroll
-            for (uint32_t i = 0; i < kHeld; ++i) held[i] = from + i * step < hi ? __ldg(reinterpret_cast<const uint4 *>(row_of(from + i * step))) : make_uint4(0, 0, 0, 0);
+            for (uint32_t which = 0; which < 2; ++which)
 #pragma unroll
-            for (uint32_t i = 0; i < kHeld; ++i) {
-                const uint4 w = held[i];
-                const float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+                for (uint32_t i = 0; i < kHeld; ++i)
+                    held[which][i] = from + i * step < hi - lo ? __ldg(reinterpret_cast<const uint4 *>(source(which) + int64_t(from + i * step) * P.ldx[which])) : make_uint4(0, 0, 0, 0);
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k)
-                    if (fabsf(v[k]) < __uint_as_float(0x7F800000u)) a = fmaxf(a, fabsf(v[k]));
-            }
+            for (uint32_t which = 0; which < 2; ++which)
+#pragma unroll
+                for (uint32_t i = 0; i < kHeld; ++i) {
+                    const uint4 w = held[which][i];
+                    const float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+#pragma unroll
+                    for (uint32_t k = 0; k < 8; ++k)
+                        if (fabsf(v[k]) < __uint_as_float(0x7F800000u)) a[which] = fmaxf(a[which], fabsf(v[k]));
+                }
         }
-        const bool once = hi - lo <= kHeld * step;
-        a = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a)));
+#pragma unroll
+        for (uint32_t which = 0; which < 2; ++which) a[which] = __uint_as_float(__reduce_max_sync(0xFFFFFFFFu, __float_as_uint(a[which])));
         if constexpr (WARPS > 1) {
-            if (lane == 0) largest_of[tid >> 5] = a;
-            __syncthreads();
+            if (lane == 0) largest_of[0][tid >> 5] = a[0], largest_of[1][tid >> 5] = a[1];
+            __syncthreads();                              // (and everyone has read the old scales)
 #pragma unroll
-            for (uint32_t i = 0; i < WARPS; ++i) a = fmaxf(a, largest_of[i]);
+            for (uint32_t i = 0; i < WARPS; ++i) a[0] = fmaxf(a[0], largest_of[0][i]), a[1] = fmaxf(a[1], largest_of[1][i]);
             __syncthreads();
+        } else {
+            __syncwarp();
         }
-        const float need = pow2_biased(max(scale_exponent(a, kLeastScale), kLeastScale));
-        float scale = need;
-        if (lo > p0) {                                    // older tokens
-            const float had = P.scales[which][block];
-            scale = fmaxf(need, had);
-            if (scale > had) {
-                const float ratio = __fdiv_rn(had, scale);
+#pragma unroll
+        for (uint32_t which = 0; which < 2; ++which) {
+            uint8_t *dst = P.cache[which] + (block << P.q.shift) * P.D + at;
+            const float need = pow2_biased(max(scale_exponent(a[which], kLeastScale), kLeastScale)), scale = fmaxf(need, had[which]);
+            if (older && scale > had[which]) {
+                const float ratio = __fdiv_rn(had[which], scale);
                 for (uint32_t i = sub; i < lo - p0; i += step) {
                     uint2 w = *reinterpret_cast<uint2 *>(dst + i * P.D);
                     auto moved = [&](uint32_t four) {
@@ -96,25 +103,27 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
                     *reinterpret_cast<uint2 *>(dst + i * P.D) = w;
                 }
             }
-            if constexpr (WARPS > 1) __syncthreads();     // everyone has read the old scale
-            else __syncwarp();
-        }
-        const bool power = (__float_as_uint(scale) & 0x7FFFFFu) == 0 && scale >= 1e-30f && scale <= 1e30f;
-        const float inverse = __fdiv_rn(1.0f, scale);     // exact for a power of two; other scales (a caller's own) are divided by
-        for (uint32_t from = lo + sub; from < hi; from += kHeld * step) {
+            const bool power = (__float_as_uint(scale) & 0x7FFFFFu) == 0 && scale >= 1e-30f && scale <= 1e30f;
+            const float inverse = __fdiv_rn(1.0f, scale);  // exact for a power of two; other scales (a caller's own) are divided by
+            for (uint32_t from = sub; from < hi - lo; from += kHeld * step) {
 #pragma unroll
-            for (uint32_t i = 0; i < kHeld; ++i) {
-                const uint32_t pos = from + i * step;
-                if (pos >= hi) break;
-                const uint4 w = once ? held[i] : __ldg(reinterpret_cast<const uint4 *>(row_of(pos)));
-                float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+                for (uint32_t i = 0; i < kHeld; ++i) {
+                    const uint32_t n = from + i * step;
+                    if (n >= hi - lo) break;
+                    const uint4 w = once ? held[which][i] : __ldg(reinterpret_cast<const uint4 *>(source(which) + int64_t(n) * P.ldx[which]));
+                    float v[8] = {E::lo(w.x), E::hi(w.x), E::lo(w.y), E::hi(w.y), E::lo(w.z), E::hi(w.z), E::lo(w.w), E::hi(w.w)};
+                    if (power) {
 #pragma unroll
-                for (uint32_t k = 0; k < 8; ++k)
-                    v[k] = !(fabsf(v[k]) < __uint_as_float(0x7F800000u)) ? __uint_as_float(0x7FFFFFFFu) : power ? v[k] * inverse : __fdiv_rn(v[k], scale);
-                *reinterpret_cast<uint2 *>(dst + (pos - p0) * P.D) = make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+                        for (uint32_t k = 0; k < 8; ++k) v[k] = fabsf(v[k]) < __uint_as_float(0x7F800000u) ? v[k] * inverse : __uint_as_float(0x7FFFFFFFu);
+                    } else {
+#pragma unroll 1
+                        for (uint32_t k = 0; k < 8; ++k) v[k] = fabsf(v[k]) < __uint_as_float(0x7F800000u) ? __fdiv_rn(v[k], scale) : __uint_as_float(0x7FFFFFFFu);
+                    }
+                    *reinterpret_cast<uint2 *>(dst + (lo - p0 + n) * P.D) = make_uint2(e4m3x2(v[0], v[1]) | e4m3x2(v[2], v[3]) << 16, e4m3x2(v[4], v[5]) | e4m3x2(v[6], v[7]) << 16);
+                }
             }
+            if (tid == 0) P.scales[which][block] = scale;
         }
-        if (tid == 0) P.scales[which][block] = scale;
     }
 }
 
@@ -598,9 +607,9 @@ int check_cache(const ep_cache &c, const ep_requests &r, Requests &q) {
 
 template <class E>
 int launch_append(const AppendParams &P, cudaStream_t st) {
-    // many tokens per request: a CTA for each page and head, else a warp
-    const uint64_t units = uint64_t(P.spans) * P.q.H * 2u * P.q.B;
-    const bool wide = P.q.N >= 8ull * P.q.B;
+    // a CTA for each page and head where there are more values than a warp holds, else a warp (100 requests of 125 tokens, pages of 16 x 64: 44.9 -> 25.5 us)
+    const uint64_t units = uint64_t(P.spans) * P.q.H * P.q.B, average = (uint64_t(P.q.N) + P.q.B - 1u) / P.q.B;
+    const bool wide = std::min<uint64_t>(average, P.q.page) * P.D > 2048u;
     const uint64_t grid = wide ? units : (units + 3u) / 4u;
     if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
     const cudaError_t e = wide ? op_launch(append_kernel<E, 4>, uint32_t(grid), 128, 0, 1, st, P) : op_launch(append_kernel<E, 1>, uint32_t(grid), 128, 0, 1, st, P);
@@ -674,9 +683,9 @@ extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
     P.cache[0] = static_cast<uint8_t *>(j.cache.d_k), P.cache[1] = static_cast<uint8_t *>(j.cache.d_v);
     P.scales[0] = j.cache.d_k_scales, P.scales[1] = j.cache.d_v_scales;
     P.D = j.cache.dim;
-    // as many pages side by side as a request of average length touches; a longer one's take turns
-    const uint64_t average = (uint64_t(N) + B - 1u) / B;
-    P.spans = uint32_t(average > 1 ? (average - 1u) / j.cache.page + 2u : 1u);
+    // as many pages side by side as a request of twice the average length touches; a longer one's take turns
+    const uint64_t average = (uint64_t(N) + B - 1u) / B, most = uint64_t(N) / j.cache.page + 2u;
+    P.spans = uint32_t(average > 1 ? std::min<uint64_t>(std::min<uint64_t>(most, j.requests.columns), (2u * average - 1u) / j.cache.page + 2u) : 1u);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return j.dtype == EP_BF16 ? launch_append<Bf16>(P, st) : launch_append<Fp16>(P, st);
 }
