@@ -542,40 +542,59 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0u; j < issued; ++j) bar_drain(bars + 8 * (j % S::kStages), (j / S::kStages) & 1u);
 }
 
-// The segments that cross a share: CTA k takes the one that CTA k of the first launch began.  Its pieces are the first ones of the
-// CTAs after it, in order.
+// The segments that cross a share: CTA column k takes the one that CTA k of the first launch began, a CTA for each row.  Its other pieces are
+// the first ones of the CTAs after it.  A long request's segment is 40 pieces: their maxima and sums are taken by a thread each, their
+// values by two or four threads for each column (a thread per column, piece after piece: 13 us of the 53 that one request of 200 000 tokens took).
+constexpr uint32_t kJoinThreads = 256, kMostPieces = 256;
 template <class E, uint32_t NT, uint32_t D>
-__global__ void __launch_bounds__(256) join_kernel(const __grid_constant__ AttendParams P) {
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constant__ AttendParams P) {
     using T = typename E::T;
-    constexpr uint32_t kRows = 8 * NT;
+    constexpr uint32_t kRows = 8 * NT, kParts = kJoinThreads / D;
+    __shared__ float weight[kMostPieces], warp_top[kJoinThreads / 32], warp_sum[kJoinThreads / 32], part_of[kJoinThreads];
     op_wait_for_stream();
     const uint32_t *desc = reinterpret_cast<const uint32_t *>(P.workspace) + blockIdx.x * kDescWords;
     const uint32_t end = desc[3];
     if (end == 0) return;
+    const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, n = end - blockIdx.x;       // pieces; at most one per CTA of the first launch
     const uint32_t b = desc[0], tile = desc[1], h = desc[2];
     const Extent r = extent_of(P.q, b);
     const float *all = P.workspace + size_t(P.grid) * kDescWords;
-    const float *own = all + (size_t(blockIdx.x) * 2u + desc[4]) * kPiece<NT, D>;
-    const uint32_t e = blockIdx.y * blockDim.x + threadIdx.x, row = e / D, d = e % D, at = tile * kRows + row, i = at / P.G, g = at % P.G;
+    const uint32_t own = desc[4];
+    auto piece = [&](uint32_t c) { return all + (size_t(blockIdx.x + c) * 2u + (c ? 0u : own)) * kPiece<NT, D>; };
+    const uint32_t row = blockIdx.y;
+    const uint32_t at = tile * kRows + row, i = at / P.G, g = at % P.G;
     if (at >= r.rows * P.G) return;
-    const float *first = all + size_t(blockIdx.x + 1u) * 2u * kPiece<NT, D>;
-    const uint32_t n = end - blockIdx.x - 1u;
-    const float own_top = own[kRows * D + row];
-    float top = own_top;
+    const float m = tid < n ? piece(tid)[kRows * D + row] : -INFINITY, l = tid < n ? piece(tid)[kRows * D + kRows + row] : 0.0f;
+    float top = m;
+#pragma unroll
+    for (uint32_t k = 1; k < 32; k <<= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, k));
+    if (lane == 0) warp_top[warp] = top;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t k = 0; k < kJoinThreads / 32; ++k) top = fmaxf(top, warp_top[k]);
+    const float f = tid < n ? exp2_fast(m - (top == -INFINITY ? 0.0f : top)) : 0.0f;
+    weight[tid] = f;
+    float sum = tid < n ? l * f : 0.0f;
+#pragma unroll
+    for (uint32_t k = 1; k < 32; k <<= 1) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, k);
+    if (lane == 0) warp_sum[warp] = sum;
+    __syncthreads();
+    const uint32_t d = tid % D, part = tid / D;
+    float acc = 0.0f;
 #pragma unroll 8
-    for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPiece<NT, D> + kRows * D + row]);
-    const float ref = top == -INFINITY ? 0.0f : top, f0 = exp2_fast(own_top - ref);
-    float sum = own[kRows * D + kRows + row] * f0, acc = own[row * D + d] * f0;
-#pragma unroll 8
-    for (uint32_t c = 0; c < n; ++c) {
-        const float *p = first + size_t(c) * 2u * kPiece<NT, D>;
-        const float f = exp2_fast(p[kRows * D + row] - ref);
-        sum += p[kRows * D + kRows + row] * f;
-        acc += p[row * D + d] * f;
+    for (uint32_t c = part; c < n; c += kParts) acc = fmaf(weight[c], piece(c)[row * D + d], acc);
+    part_of[tid] = acc;
+    __syncthreads();
+    if (part == 0) {
+        sum = 0.0f;
+#pragma unroll
+        for (uint32_t k = 0; k < kJoinThreads / 32; ++k) sum += warp_sum[k];
+#pragma unroll
+        for (uint32_t k = 1; k < kParts; ++k) acc += part_of[k * D + d];
+        const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+        static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+        if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
     }
-    const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
-    static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
-    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
 }
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
@@ -616,15 +635,13 @@ int launch_append(const AppendParams &P, cudaStream_t st) {
     return e == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
-// tiles of eight rows that a warp takes together: as many as a request of average size has, at most four
-uint32_t row_tiles(uint32_t N, uint32_t G, uint32_t B) { return uint64_t(N) * G <= 8ull * B ? 1u : uint64_t(N) * G <= 16ull * B ? 2u : 4u; }
+// tiles of eight rows that a warp takes together: one, or two where requests of average size have more rows than that
+uint32_t row_tiles(uint32_t N, uint32_t G, uint32_t B) { return uint64_t(N) * G <= 8ull * B ? 1u : 2u; }
 
 template <class E, uint32_t NT, uint32_t D>
 int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
-#ifndef EP_W
-#define EP_W 12
-#endif
-    constexpr uint32_t W = NT == 1 ? EP_W : 8;
+    // what registers allow: twelve warps with eight rows (64 requests 211 us, with eight warps 235), eight with sixteen
+    constexpr uint32_t W = NT == 1 ? 12 : 8;
     using S = AttendShape<NT, D, W>;
     static bool configured[64] = {};
     int rc = op_configure(attend_kernel<E, NT, D, W>, S::kSmem, configured);
@@ -642,17 +659,15 @@ int launch_attend(AttendParams P, const ep_cache &c, size_t workspace_bytes, cud
         P.workspace = nullptr;
     }
     if (op_launch(attend_kernel<E, NT, D, W>, P.grid, 32 * W, S::kSmem, 1, st, P, km, vm) != cudaSuccess) return EP_ERR_CUDA;
-    if (joined && op_launch(join_kernel<E, NT, D>, dim3(P.grid, (8 * NT * D + 255) / 256), 256, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
+    if (joined && op_launch(join_kernel<E, NT, D>, dim3(P.grid, 8 * NT), kJoinThreads, 0, 1, st, P) != cudaSuccess) return EP_ERR_CUDA;
     return EP_OK;
 }
 
 template <class E>
 int launch_attend(const AttendParams &P, const ep_cache &c, size_t workspace_bytes, cudaStream_t st) {
-    switch (row_tiles(P.q.N, P.G, P.q.B)) {
-    case 1: return c.dim == 64 ? launch_attend<E, 1, 64>(P, c, workspace_bytes, st) : launch_attend<E, 1, 128>(P, c, workspace_bytes, st);
-    case 2: return c.dim == 64 ? launch_attend<E, 2, 64>(P, c, workspace_bytes, st) : launch_attend<E, 2, 128>(P, c, workspace_bytes, st);
-    default: return c.dim == 64 ? launch_attend<E, 4, 64>(P, c, workspace_bytes, st) : launch_attend<E, 4, 128>(P, c, workspace_bytes, st);
-    }
+    if (row_tiles(P.q.N, P.G, P.q.B) == 1)
+        return c.dim == 64 ? launch_attend<E, 1, 64>(P, c, workspace_bytes, st) : launch_attend<E, 1, 128>(P, c, workspace_bytes, st);
+    return c.dim == 64 ? launch_attend<E, 2, 64>(P, c, workspace_bytes, st) : launch_attend<E, 2, 128>(P, c, workspace_bytes, st);
 }
 
 }  // namespace
@@ -691,9 +706,10 @@ extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
 }
 
 extern "C" size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim) {
-    const int sms = op_sms();
-    if (sms <= 0 || heads == 0 || B == 0) return 0;
-    if (prompts_serve(N, B, q_heads / heads)) return prompts_workspace_bytes(uint32_t(sms), dim);
+    const int n_sms = op_sms();
+    if (n_sms <= 0 || heads == 0 || B == 0) return 0;
+    const uint32_t sms = std::min(uint32_t(n_sms), kMostPieces);
+    if (prompts_serve(N, B, q_heads / heads)) return prompts_workspace_bytes(sms, dim);
     const uint32_t rows = 8u * row_tiles(N, q_heads / heads, B);
     return size_t(sms) * (kDescWords + 2u * rows * (size_t(dim) + 2u)) * 4u;
 }
@@ -730,7 +746,7 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     if (units >= (1ull << 30) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
-    P.grid = uint32_t(sms);
+    P.grid = std::min(uint32_t(sms), kMostPieces);
     P.k = static_cast<const uint8_t *>(c.d_k);
     P.v = static_cast<const uint8_t *>(c.d_v);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
