@@ -328,7 +328,9 @@ int ep_fp8_matmul(const ep_matmul_job *job, void *stream);
 /* Keys and values of many requests in pages of E4M3, one scale for each page and head.  All pointers are device pointers. */
 typedef struct {
     void *d_k, *d_v;                    /* [pages][heads][page][dim] E4M3; 16-byte aligned */
-    float *d_k_scales, *d_v_scales;     /* [pages][heads]; finite and >= 0 wherever a token lies */
+    float *d_k_scales, *d_v_scales;     /* [pages][heads]; finite and >= 0 wherever a token lies; value scales of a request's
+                                           pages at most 2^40 times its first page's (but for a first page of
+                                           zeros), those below 2^-60 of it count as that */
     uint32_t pages, heads, page, dim;   /* page: tokens of a page, 16, 32, 64, 128 or 256; dim: 64 or 128;
                                            pages * heads * page < 2^31 - 256 */
 } ep_cache;
@@ -364,7 +366,8 @@ int ep_cache_append(const ep_append_job *job, void *stream);
 /* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row
  * i of its n.  Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token gives 0 (and -infinity
  * in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values;
- * a token's values count only for rows that see it.  B <= 4096, else EP_ERR_UNSUPPORTED. */
+ * a token's values count only for rows that see it.  EP_ERR_UNSUPPORTED for B > 4096, and for calls that could come to 2^30
+ * pieces of work: ceil(columns * page / 256) * (N * q_heads / heads / 8 + B) * heads. */
 typedef struct {
     ep_cache cache;
     ep_requests requests;

@@ -483,6 +483,15 @@ def _enqueue(f, name, job, dev, stream):
         raise EntroPackError(rc, name)
 
 
+def _empty(shape, dtype, device, stream):
+    """Memory of the stream that the call runs on: what the allocator hands out for another one may still be in use there."""
+    torch = _types[0]
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
 def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") -> KVCache:
     """An empty cache: `pages` pages of `page` tokens."""
     torch = _torch()
@@ -516,7 +525,7 @@ def quantize_blocks(x, block_rows: int = 1, out=None, stream=None):
     T, Cc = shape
     blocks = (-(-T // block_rows), -(-Cc // 128))
     if out is None:
-        out = (torch.empty(shape, dtype=e4m3, device=x.device), torch.empty(blocks, dtype=e8m0, device=x.device))
+        out = (_empty(shape, e4m3, x.device, stream), _empty(blocks, e8m0, x.device, stream))
     q, s = out
     job = QUANTIZE_JOB.pack(x.data_ptr(), q.data_ptr(), s.data_ptr(), _matrix(x, dtype, shape, dev, "x"), _matrix(q, e4m3, shape, dev, "out[0]"),
                             _matrix(s, e8m0, blocks, dev, "out[1]"), T, Cc, block_rows, code)
@@ -536,7 +545,7 @@ def fp8_matmul(x, x_scales, w, w_scales=None, row_scale=None, out_dtype: int = B
     if out is None:
         if out_dtype not in (BF16, FP16, FP32):
             raise ValueError("out_dtype must be BF16, FP16 or FP32")
-        out = torch.empty((T, R), dtype=_out_torch_dtype(out_dtype), device=x.device)
+        out = _empty((T, R), _out_torch_dtype(out_dtype), x.device, stream)
     dtype = out.dtype
     code = codes.get(dtype)
     if code is None:
@@ -615,7 +624,7 @@ def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool 
     if code is None or code == FP32 or len(shape) != 3 or shape[2] != dim or shape[1] == 0 or shape[1] % heads:
         raise ValueError("q must be bfloat16 or float16 [N, q_heads, dim], its heads a multiple of the cache's")
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=q.device)
+        out = _empty(shape, dtype, q.device, stream)
     at = 0
     if lse is not None:
         if lse.dtype != torch.float32 or lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != dev:
@@ -628,9 +637,7 @@ def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool 
         room, size = workspace.data_ptr(), workspace.numel() * workspace.element_size()
     elif columns * page > 256:
         with torch.cuda.device(dev):
-            workspace = torch.empty(cache_attention_workspace_bytes(shape[0], B, shape[1], heads, dim), dtype=torch.uint8, device=q.device)
-        if stream is not None:
-            workspace.record_stream(stream)
+            workspace = _empty(cache_attention_workspace_bytes(shape[0], B, shape[1], heads, dim), torch.uint8, q.device, stream)
         room, size = workspace.data_ptr(), workspace.numel()
     job = ATTENTION_JOB.pack(*fields, q.data_ptr(), out.data_ptr(), at, room, size, *_heads(q, dtype, shape, dev, "q"), *_heads(out, dtype, shape, dev, "out"),
                              dim ** -0.5 if scale is None else scale, shape[1], code, 1 if causal else 0)

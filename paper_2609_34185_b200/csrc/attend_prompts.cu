@@ -21,7 +21,7 @@ __device__ unsigned int g_prompts_status = 0;
 // (Warps 14 and 15 have nothing to do: registers go from one group of four warps to another.)
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
 // than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
-// t = score + log2(v_scale), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
+// t = score + log2(v_scale / the request's first), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
 // instead of the maximum first: 379 -> 462 us.)
 // The loops are short on purpose: three roles run side by side, and what they execute over and over has to fit the SM's instruction
 // cache (with everything unrolled, 170 KB, six of ten fetches hit it and a tile took 13 700 cycles).
@@ -38,7 +38,7 @@ template <uint32_t D>
 struct PromptShape {
     static constexpr uint32_t kHalves = D / 64, kHalf = 128 * 128, kTile = kHalves * kHalf;     // 128 rows x D binary16: blocks of 64 columns, 128-byte rows
     static constexpr uint32_t kQ = 0, kK = 2 * kTile, kV = kK + 2 * kTile;
-    static constexpr uint32_t kMeta = kV + 2 * kTile;                  // four slots of eight groups of 16 tokens: key scale, log2 value scale, its inverse
+    static constexpr uint32_t kMeta = kV + 2 * kTile;                  // four slots of eight groups of 16 tokens: key scale, log2 of the value scale's ratio, its inverse, the first value scale
     static constexpr uint32_t kNan = kMeta + 4 * 8 * 16;               // some units' first NaN token of each column, then their flags
     static constexpr uint32_t kBars = kNan + kNanUnits * (D + 1) * 4;
     static constexpr uint32_t kPart = kBars + 256, kPrefix = kPart + 128;      // (64 bytes for the sums' parts, then the share's first place)
@@ -291,6 +291,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 const uint32_t tiles = x.products(), t_first = x.first * kKeys;
                 if (tiles == 0) continue;
                 const int32_t *table = P.q.table + int64_t(x.p.b) * P.q.ldt;
+                const float vs_first = first_scale(P.q, P.vs, x.p.b, x.p.h), per_first = __frcp_rn(vs_first);
                 auto page_at = [&](uint32_t i) {          // -1: no token, or (reported by the warps that bring it in) no page
                     const uint32_t t = t_first + i * kKeys + 16u * lane;
                     const int32_t id = lane < 8 && i < tiles && t < x.r.len ? __ldg(table + (t >> P.q.shift)) : -1;
@@ -311,8 +312,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     const uint32_t stage = it & 1u;
                     if (it > 1u) ok = bar_wait_warp(k_free + 8 * stage, (it >> 1 & 1u) ^ 1u, abort_word);
                     if (!ok) break;
-                    const float some = fmaxf(vs, 1e-30f);
-                    if (lane < 8) *reinterpret_cast<float4 *>(gen + S::kMeta + ((it & 3u) * 8u + lane) * 16u) = make_float4(ks, log2f(some), __fdiv_rn(1.0f, some), 0.0f);
+                    const float some = fmaxf(vs * per_first, kLeastRatio);
+                    if (lane < 8) *reinterpret_cast<float4 *>(gen + S::kMeta + ((it & 3u) * 8u + lane) * 16u) = make_float4(ks, log2f(some), __fdiv_rn(1.0f, some), vs_first);
                     __syncwarp();
                     if (lane == 0) bar_arrive(k_full + 8 * stage);
                     ks = ks_next, vs = vs_next;
@@ -484,7 +485,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             const uint32_t lim = real ? sees(P, x.r, i_row) : most_of(P, x.r, x.p.j);
             const uint32_t lim_least = __reduce_min_sync(0xFFFFFFFFu, lim);
             const int64_t head = int64_t(x.p.h * P.G + g);
-            float m = -INFINITY, sum = 0.0f;
+            float m = -INFINITY, sum = 0.0f, vs_first = 1.0f;
             if (tiles) {
                 if (!rows_there) fac_next = rows_in(x);
                 const float fac = fac_next;
@@ -501,6 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                         float4 scale[4];
 #pragma unroll
                         for (uint32_t k = 0; k < 4; ++k) scale[k] = meta[k];
+                        vs_first = scale[0].w;
                         const bool out = fminf(fminf(scale[0].x, scale[1].x), fminf(scale[2].x, scale[3].x)) < 0.0f;
                         auto tile = [&](auto edge_tag) {
                             constexpr bool kEdge = decltype(edge_tag)::value;
@@ -590,7 +592,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             // ---- the unit's rows, or a piece of them --------------------------------------------------------------------------
             if (x.count == 0) continue;                   // (a share that ends before the unit's first tile)
             const bool whole = x.count == x.total;
-            const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+            const float inverse = sum == 0.0f ? 0.0f : whole ? __fdiv_rn(vs_first, sum) : vs_first;
             T *dst = static_cast<T *>(P.o) + int64_t(x.r.row + i_row) * P.ldo + head * P.ldoh;
             float *piece = whole ? nullptr : P.workspace + size_t(P.grid) * 8u + (size_t(blockIdx.x) * 2u + (x.first ? 0u : 1u)) * kPromptPiece<D>;
             const uint32_t *first_nan = nan_at + n_unit % kNanUnits * D;
@@ -605,7 +607,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     }
 #pragma unroll
                     for (uint32_t e = 0; e < 32; ++e) {
-                        float f = tiles && sum != 0.0f ? __uint_as_float(v[e]) * (whole ? inverse : 1.0f) : 0.0f;
+                        float f = tiles && sum != 0.0f ? __uint_as_float(v[e]) * inverse : 0.0f;
                         if (has_nan && first_nan[32 * c + e] < lim) f = __uint_as_float(0x7FFFFFFFu);
                         v[e] = __float_as_uint(f);
                     }

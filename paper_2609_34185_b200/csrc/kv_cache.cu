@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // handful of rows fills N = 8, where along M they would be half padding, with twice the scores, accumulators and instructions.
 // A row of q becomes binary16 times a power of two that puts its largest magnitude at 2^13: exact for binary16 and bfloat16 alike but for elements 2^-27 and
 // more below the row's largest, whose rounding is below fp32's own.  A page's value scale is taken into the exponent, t = score +
-// log2(v_scale), and out of the row's sum again.  The reference m of a row moves, and its accumulators with it, only when some t exceeds it by
+// log2(v_scale / the request's first), and out of the row's sum again.  The reference m of a row moves, and its accumulators with it, only when some t exceeds it by
 // more than 8; weights are 2^(t - m + 7): at most 2^15, and down to 2^-21 of what m stands for with 11 bits.
 // ======================================================================================================================
 constexpr uint32_t kTile = 32, kUnit = 256;
@@ -285,6 +285,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
             __syncwarp();
             ++issued;
         };
+        const float vs_first = first_scale(P.q, P.vs, b, h), per_first = __frcp_rn(vs_first);
         int32_t next_page = page_of(0);
         uint32_t asked = 0;
 #pragma unroll 1
@@ -355,7 +356,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
 #pragma unroll
                 for (uint32_t p = 0; p < 2; ++p) {
                     ks[p] = __uint_as_float(ld_smem(meta + s * 16 + 8 * p));
-                    vs[p] = fmaxf(__uint_as_float(ld_smem(meta + s * 16 + 8 * p + 4)), 1e-30f);
+                    vs[p] = fmaxf(__uint_as_float(ld_smem(meta + s * 16 + 8 * p + 4)) * per_first, kLeastRatio);
                 }
                 const bool edge = t0 + kTile > lim_min || ks[0] < 0.0f || ks[1] < 0.0f;
                 // ---- scores: c0, c1 of m tile x are token t0 + 16 x + oct against rows 8 n + 2 quad, + 1; c2, c3 token + 8 -------
@@ -383,7 +384,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
                         for (uint32_t n = 0; n < NT; ++n) mma16816(sc[x][n], a0, a1, a2, a3, qb[n][st][0], qb[n][st][1]);
                     }
                 }
-                // ---- t = score + log2(v_scale), the reference, weights -------------------------------------------------------------
+                // ---- t = score + log2(v_scale ratio), the reference, weights -------------------------------------------------------------
                 const float lift[2] = {log2_fast(vs[0]), log2_fast(vs[1])}, sink[2] = {__frcp_rn(vs[0]), __frcp_rn(vs[1])};
                 bool move = false;
 #pragma unroll
@@ -515,11 +516,11 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
             if (first_nan[d] < seen_by(P, r, i)) acc = __uint_as_float(0x7FFFFFFFu);
             if (whole) {
                 const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
-                static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum));
+                static_cast<T *>(P.o)[t * P.ldo + head * P.ldoh + d] = E::of(sum == 0.0f ? 0.0f : __fdiv_rn(acc, sum) * vs_first);
                 if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
             } else {
                 float *piece = pieces + (u == u_begin ? 0u : kPiece<NT, D>);
-                piece[row * D + d] = acc;
+                piece[row * D + d] = acc * vs_first;
                 if (d == 0) piece[kRows * D + row] = top, piece[kRows * D + kRows + row] = sum;
             }
         }

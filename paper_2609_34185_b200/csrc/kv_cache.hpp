@@ -23,6 +23,18 @@ __device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
     return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(__ldg(q.seq_lens + b), 0))), room))};
 }
 
+// The softmax's weights carry the pages' value scales, as ratios to that of the request's first page: t = score + log2(ratio), and a row's sum
+// takes them out again.  What such a weight would lose below fp32's range is lost to the sum, so ratios stop at 2^-60: the values
+// of a page further below (zeros, as append leaves them with 2^-100) then count as up to 2^-51 of the first page's largest, less than
+// fp32 resolves, and weights keep 2^-30 of the largest for pages of up to 2^40 times the first one's scale.
+constexpr float kLeastRatio = 0x1p-60f;
+// the value scale of the request's first page; 1 where there is none
+__device__ __forceinline__ float first_scale(const Requests &q, const float *vs, uint32_t b, uint32_t h) {
+    const int32_t id = __ldg(q.table + int64_t(b) * q.ldt);
+    const float v = uint32_t(id) < q.pages ? __ldg(vs + size_t(uint32_t(id)) * q.H + h) : 1.0f;
+    return v > 0x1p-120f && v < 0x1p120f ? v : 1.0f;
+}
+
 // ---- softmax in powers of two -------------------------------------------------------------------------------------------
 __device__ __forceinline__ float exp2_fast(float x) {
     float r;

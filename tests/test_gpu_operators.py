@@ -175,6 +175,20 @@ def test_matmul(T, R, C, out):
 
 
 @gpu
+@pytest.mark.parametrize("T,R,C", [(3, 10240, 784), (100, 300, 1040), (128, 2000, 256), (1500, 600, 2064), (2000, 5000, 272), (4100, 2600, 128), (193, 8200, 1936), (513, 257, 16)])
+def test_matmul_shapes_of_the_ways_it_is_shared_out(T, R, C):
+    # three CTAs per tile; two tiles of 64 tokens; pairs of CTAs with several tiles each, one block of columns, odd numbers of blocks, ragged edges
+    xq, xs, wq, ws = operands(T, R, C, T + R + C)
+    a = torch.rand(R, generator=cuda(R), device="cuda") + 0.5
+    for out in (ep.BF16, ep.FP32):
+        y = ep.fp8_matmul(xq, xs, wq, ws, a, out)
+        want, S = product(xq, xs, wq, ws, a)
+        check_product(y, want, S, C)
+    assert torch.equal(ep.fp8_matmul(xq, xs, wq, ws, a, ep.FP32), y)
+    assert ep.last_device_status() == 0
+
+
+@gpu
 @pytest.mark.parametrize("T", [2, 40, 200])
 def test_matmul_without_scales_and_with_strides(T):
     R, C = 330, 912
@@ -588,6 +602,90 @@ def test_lengths_and_starts_outside_are_cut():
     check_attention(out, want, bound)
     ep.cache_append(cache, q[:, :1], q[:, :1], ints(table), ints([2 ** 31 - 1, -7]), ints([-5, 2, 10 ** 6]))
     assert ep.last_device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("new", [1, 100])
+def test_a_cache_beyond_32_bits_of_bytes(new):
+    # 4.5 GB of keys and of values, the requests' pages at its end; against the same pages in a small cache
+    H, D, page, pages = 8, 128, 128, 36000
+    big, small = ep.kv_cache(pages, H, D, page), ep.kv_cache(8, H, D, page)
+    lens, starts = [300, 500], [0, new, 2 * new]
+    near, far = [[0, 1, 2, 0], [3, 4, 5, 6]], [[pages - 1, pages - 2, pages - 3, 0], [pages - 4, pages - 5, pages - 6, pages - 7]]
+    g = cuda(50)
+    k, v = (torch.randn(800, H, D, generator=g, device="cuda").to(torch.bfloat16) for _ in range(2))
+    q = torch.randn(2 * new, 4 * H, D, generator=g, device="cuda").to(torch.bfloat16)
+    out = []
+    for cache, table in ((small, near), (big, far)):
+        ep.cache_append(cache, k, v, ints(table), ints(lens), ints([0, 300, 800]))
+        out.append(ep.cache_attention(q, cache, ints(table), ints(lens), ints(starts)))
+    assert torch.equal(out[0], out[1]) and ep.last_device_status() == 0
+    for a, b in zip(small, big):
+        assert torch.equal(a.view(torch.uint8)[[0, 1, 2, 3, 4, 5, 6]], b.view(torch.uint8)[[pages - 1 - i for i in range(7)]])
+
+
+@gpu
+def test_requests_that_share_full_pages():
+    # a common prefix of two pages, each request's own tokens behind it
+    H, D, page = 2, 64, 32
+    cache, table = filled([64, 90, 70], H, D, page, seed=77)
+    shared = [table[0][:2] + table[1][2:3], table[0][:2] + table[2][2:3]]
+    k = torch.randn(2, H, D, generator=cuda(4), device="cuda").to(torch.bfloat16)
+    plain = Plain(cache)
+    lens = [91, 71]
+    ep.cache_append(cache, k, k, ints(shared), ints(lens), ints([0, 1, 2]))
+    plain.append(k, k, shared, lens, [0, 1, 2])
+    assert same(cache.k, plain.k) and same(cache.v_scales, plain.vs)
+    q = torch.randn(2, 4 * H, D, generator=cuda(6), device="cuda").to(torch.bfloat16)
+    out = ep.cache_attention(q, cache, ints(shared), ints(lens), ints([0, 1, 2]))
+    want, bound, _ = attended(q, cache, shared, lens, [0, 1, 2], 0.125, True)
+    check_attention(out, want, bound)
+
+
+@gpu
+@pytest.mark.parametrize("news", [[1, 1], [70, 90]])
+def test_attention_scales_at_their_limits(news):
+    # value scales far apart, a page of zeros as append leaves it, keys of scale 0, a scale of 0 or below
+    G, H, lens, starts = 4, 1, [300, 130], offsets(news)
+    cache, table = filled(lens, H, 128, 32, seed=19)
+    cache.v_scales[table[0][1]], cache.v_scales[table[0][3]], cache.v_scales[table[1][0]] = 2.0 ** 40, 2.0 ** -60, 2.0 ** -30
+    cache.v_scales[table[0][4]] = 2.0 ** -100
+    cache.v.view(torch.uint8)[table[0][4]] = 0
+    cache.k_scales[table[0][2]] = 0.0
+    q = torch.randn(starts[-1], G, 128, generator=cuda(3), device="cuda").to(torch.bfloat16)
+    for scale in (0.1, 0.0, -0.3):
+        out = ep.cache_attention(q, cache, ints(table), ints(lens), ints(starts), scale=scale)
+        want, bound, _ = attended(q, cache, table, lens, starts, scale, True)
+        check_attention(out, want, bound + 1e-7 * bound.amax(2, keepdim=True))
+    tiny = ep.KVCache(cache.k, cache.v, cache.k_scales, torch.full_like(cache.v_scales, 2.0 ** -100))
+    out = ep.cache_attention(q.half(), tiny, ints(table), ints(lens), ints(starts))
+    assert bool((out == 0).all())                         # (below binary16's range)
+
+
+@gpu
+def test_two_graphs_at_once_with_their_own_workspaces():
+    lens = [2000, 700]
+    cache, table = filled(lens, 4, 128, 64, seed=5)
+    t, sl = ints(table), ints(lens)
+    graphs, outs, want, keep = [], [], [], []
+    for n in (1, 60):
+        st = ints([0, n, 2 * n])
+        q = torch.randn(2 * n, 16, 128, generator=cuda(n), device="cuda").to(torch.bfloat16)
+        ws = torch.empty(ep.cache_attention_workspace_bytes(2 * n, 2, 16, 4, 128), dtype=torch.uint8, device="cuda")
+        want.append(ep.cache_attention(q, cache, t, sl, st))
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(ep.cache_attention(q, cache, t, sl, st, workspace=ws))
+        graphs.append(graph)
+        keep.append((q, st, ws))
+    streams = [torch.cuda.Stream() for _ in graphs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for s, graph in zip(streams, graphs):
+            with torch.cuda.stream(s):
+                graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(outs, want))
 
 
 @gpu
