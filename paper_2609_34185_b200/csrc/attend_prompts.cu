@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (t >= x.r.len) return -1;
                 const int32_t id = __ldg(table + (t >> P.q.shift));
                 if (id >= 0 && uint32_t(id) < P.q.pages) return id;
-                atomicOr(&g_prompts_status, 2u);
+                atomicOr(&g_prompts_status, unsigned(kStatusPage));
                 return -1;
             };
             // a warp's 32 tokens lie in one page or two, 16 in each
@@ -646,7 +646,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
     }
     tc_before();
     __syncthreads();
-    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_prompts_status, 1u);
+    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_prompts_status, unsigned(kStatusWait));
     if (warp == 12) {
         tc_after();
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512u) : "memory");
@@ -702,6 +702,8 @@ int launch(const AttendParams &P, cudaStream_t st) {
     return EP_OK;
 }
 
+const bool registered = ep::add_status_word([] { return op_status(g_prompts_status); });
+
 }  // namespace
 
 // Rows enough to fill the products' 256: the other kernel takes 32 at a time and reads the cache again for each 32.
@@ -714,11 +716,4 @@ int ep::launch_prompts(AttendParams P, size_t workspace_bytes, bool cut, uint32_
     else if (!P.workspace || workspace_bytes < prompts_workspace_bytes(P.grid, dim) || (reinterpret_cast<uintptr_t>(P.workspace) & 15u)) return EP_ERR_SCRATCH;
     if (dtype == EP_BF16) return dim == 64 ? launch<Bf16, 64>(P, st) : launch<Bf16, 128>(P, st);
     return dim == 64 ? launch<Fp16, 64>(P, st) : launch<Fp16, 128>(P, st);
-}
-
-int ep::op8_status_prompts() {
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_prompts_status, sizeof(v)) != cudaSuccess) return -1;
-    if (v && cudaMemcpyToSymbol(g_prompts_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
-    return int(v);
 }

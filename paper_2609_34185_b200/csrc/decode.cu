@@ -26,7 +26,6 @@
 #include <cstdint>
 #include <cstring>
 
-#include "op8.hpp"
 #include "stream.hpp"
 
 namespace {
@@ -2595,9 +2594,9 @@ extern "C" int ep_last_device_status(void *stream) {
     unsigned int v = 0, zero = 0;
     if (cudaMemcpyFromSymbol(&v, g_ep_status, sizeof(v)) != cudaSuccess) return EP_ERR_CUDA;
     if (v && cudaMemcpyToSymbol(g_ep_status, &zero, sizeof(zero)) != cudaSuccess) return EP_ERR_CUDA;
-    const int m = ep::op8_status_matmul(), c = ep::op8_status_cache();       // the operators' own words
-    if (m < 0 || c < 0) return EP_ERR_CUDA;
-    return v || ((m | c) & 1) ? EP_ERR_BAD_STREAM : c ? EP_ERR_BAD_PAGE : EP_OK;
+    const int ops = ep::read_status_words();                                 // the operators' own words
+    if (ops < 0) return EP_ERR_CUDA;
+    return v || (ops & ep::kStatusWait) ? EP_ERR_BAD_STREAM : ops ? EP_ERR_BAD_PAGE : EP_OK;
 }
 
 // ---- decode without a caller-provided scratch buffer ----------------------------------------------------

@@ -417,7 +417,7 @@ __global__ void __launch_bounds__(128) matmul_split_kernel(const __grid_constant
     }
     tc_before();
     __syncthreads();
-    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, 1u);
+    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, unsigned(kStatusWait));
     if (warp == 0) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(G::kCols) : "memory");
 }
 
@@ -660,7 +660,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
     }
     tc_before();
     __syncthreads();
-    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, 1u);
+    if (tid == 0 && ld_smem(abort_word)) atomicOr(&g_matmul_status, unsigned(kStatusWait));
     cluster_sync();                                       // the other CTA's memory is read and arrived at until here
     if (warp == 0) {
         tc_after();
@@ -702,16 +702,11 @@ int launch_matmul(const MatmulParams &P, const void *x, int64_t ldx, const void 
     return launch_split<128, E>(P, x, ldx, w, ldw, C, st);
 }
 
+const bool registered = ep::add_status_word([] { return op_status(g_matmul_status); });
+
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
 
 }  // namespace
-
-int ep::op8_status_matmul() {
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_matmul_status, sizeof(v)) != cudaSuccess) return -1;
-    if (v && cudaMemcpyToSymbol(g_matmul_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
-    return int(v);
-}
 
 extern "C" int ep_quantize_blocks(const ep_quantize_job *job, void *stream) {
     if (!job) return EP_ERR_BAD_ARG;

@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
     for (uint32_t j = (first >> P.q.shift) + span; j <= (r.len - 1u) >> P.q.shift; j += P.spans) {
         const int32_t id = __ldg(P.q.table + int64_t(b) * P.q.ldt + j);
         if (id < 0 || uint32_t(id) >= P.q.pages) {
-            if (tid == 0) atomicOr(&g_cache_status, 2u);
+            if (tid == 0) atomicOr(&g_cache_status, unsigned(kStatusPage));
             continue;
         }
         const uint32_t p0 = j << P.q.shift, lo = max(first, p0), hi = min(r.len, p0 + P.q.page);        // new tokens of this page
@@ -253,7 +253,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
             if (i < n_tiles && lane < per_tile && t < r.len) {
                 id = __ldg(table + (t >> P.q.shift));
                 if (id < 0 || uint32_t(id) >= P.q.pages) {
-                    atomicOr(&g_cache_status, 2u);
+                    atomicOr(&g_cache_status, unsigned(kStatusPage));
                     id = -1;
                 }
             }
@@ -538,7 +538,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
         if (u + last_unit - first_unit < u_end) __syncthreads();
         u += last_unit - first_unit;
     }
-    if (tid == 0 && ld_smem(abort_at)) atomicOr(&g_cache_status, 1u);
+    if (tid == 0 && ld_smem(abort_at)) atomicOr(&g_cache_status, unsigned(kStatusWait));
     if (ld_smem(abort_at) && lane == 0)                   // (a wait ran out: what is still under way gets its time)
         for (uint32_t j = issued > S::kStages ? issued - S::kStages : 0u; j < issued; ++j) bar_drain(bars + 8 * (j % S::kStages), (j / S::kStages) & 1u);
 }
@@ -597,6 +597,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const __grid_constan
         if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
     }
 }
+
+const bool registered = ep::add_status_word([] { return op_status(g_cache_status); });
 
 bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
 
@@ -672,15 +674,6 @@ int launch_attend(const AttendParams &P, const ep_cache &c, size_t workspace_byt
 }
 
 }  // namespace
-
-int ep::op8_status_cache() {
-    const int more = op8_status_prompts();
-    if (more < 0) return more;
-    unsigned int v = 0, zero = 0;
-    if (cudaMemcpyFromSymbol(&v, g_cache_status, sizeof(v)) != cudaSuccess) return -1;
-    if (v && cudaMemcpyToSymbol(g_cache_status, &zero, sizeof(zero)) != cudaSuccess) return -1;
-    return int(v) | more;
-}
 
 extern "C" int ep_cache_append(const ep_append_job *job, void *stream) {
     if (!job) return EP_ERR_BAD_ARG;

@@ -123,7 +123,6 @@ struct AttendParams {
 bool prompts_serve(uint32_t N, uint32_t B, uint32_t G);
 size_t prompts_workspace_bytes(uint32_t grid, uint32_t dim);
 int launch_prompts(AttendParams P, size_t workspace_bytes, bool cut, uint32_t dim, int32_t dtype, cudaStream_t st);
-int op8_status_prompts();
 
 #endif  // __CUDACC__
 

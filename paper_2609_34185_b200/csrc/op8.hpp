@@ -11,13 +11,9 @@
 #include <type_traits>
 
 #include "entropack.h"
+#include "stream.hpp"
 
 namespace ep {
-
-// The operators' integrity words (bits: 1 = a wait ran out, 2 = a page number outside the cache): read and, if any is set,
-// cleared by ep_last_device_status.  Negative on a CUDA error.
-int op8_status_matmul();
-int op8_status_cache();
 
 #ifdef __CUDACC__
 
@@ -218,6 +214,15 @@ inline int op_configure(K kernel, uint32_t smem, bool (&done)[64]) {
     if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, int(smem)) != cudaSuccess) return EP_ERR_CUDA;
     if (dev >= 0 && dev < 64) done[dev] = true;
     return EP_OK;
+}
+
+// the value of a translation unit's integrity word, cleared if it is set; negative on a CUDA error
+template <class W>
+inline int op_status(W &word) {
+    unsigned int v = 0, zero = 0;
+    if (cudaMemcpyFromSymbol(&v, word, sizeof(v)) != cudaSuccess) return -1;
+    if (v && cudaMemcpyToSymbol(word, &zero, sizeof(zero)) != cudaSuccess) return -1;
+    return int(v);
 }
 
 inline int op_sms() {

@@ -97,6 +97,26 @@ extern "C" int ep_validate(const void *blob_v, size_t n) {
     return EP_OK;
 }
 
+namespace {
+int (*g_status_words[8])() = {};
+int g_status_count = 0;
+}  // namespace
+
+bool ep::add_status_word(int (*read)()) {
+    if (g_status_count < 8) g_status_words[g_status_count++] = read;
+    return true;
+}
+
+int ep::read_status_words() {
+    int all = 0;
+    for (int i = 0; i < g_status_count; ++i) {
+        const int v = g_status_words[i]();
+        if (v < 0) return v;
+        all |= v;
+    }
+    return all;
+}
+
 extern "C" const char *ep_strerror(int status) {
     switch (status) {
     case EP_OK: return "ok";

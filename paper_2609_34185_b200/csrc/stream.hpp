@@ -16,6 +16,12 @@ constexpr uint32_t kTileRecordBytes = 4 * kStates + 4;
 constexpr uint32_t kStateLow = 1u << 15;  // states live in [2^15, 2^31)
 constexpr uint32_t kDecodeTilesPerCta = 32;  // tiles one CTA of the decode kernel works on at a time (one per warp)
 
+// Device-side integrity words of the operators' translation units: each gives a function that reads its word (bits below),
+// clears it if it is set and returns it, negative on a CUDA error.  ep_last_device_status asks all of them.
+enum { kStatusWait = 1, kStatusPage = 2 };       // a wait ran out; a page number outside the cache
+bool add_status_word(int (*read)());
+int read_status_words();
+
 template <class T>
 inline T load_le(const uint8_t *p) {
     T v;
