@@ -57,7 +57,7 @@ typedef enum {
     EP_ERR_NOMEM = -6,       /* host allocation failed */
     EP_ERR_SCRATCH = -7,     /* scratch buffer missing, misaligned or too small */
     EP_ERR_STATIC_LIMIT = -8, /* ep_decode_tensor_static: the stream's tables exceed the built-in area */
-    EP_ERR_BAD_PAGE = -9     /* a kernel met a page number outside the cache (ep_last_device_status) */
+    EP_ERR_BAD_PAGE = -9     /* a kernel met a page number outside the cache, or rows that several requests claim (ep_last_device_status) */
 } ep_status;
 
 /* Output element types of the decoder: snap_tau of Eq. 19. */
@@ -290,7 +290,8 @@ int ep_decode_gemm(const ep_info *info, const void *d_stream, const void *d_tile
  * stand for s q; the scales s made here are powers of two, the smallest with which the largest finite magnitude of a block
  * fits 448 (at least 2^-126), so that scaling never rounds.  All calls are asynchronous on `stream`, allocate nothing, keep
  * nothing between calls (ep_cache_append aside, whose cache it is) and can be recorded in a stream capture; the first
- * call of a kind on a device also sets a kernel attribute.  Leading dimensions (`ld*`) are in elements. */
+ * call of a kind on a device also sets a kernel attribute.  What a call writes overlaps nothing that it reads.  There are no
+ * gradients: these are operators of a program that answers.  Leading dimensions (`ld*`) are in elements. */
 
 /* q[i, j] = e4m3(x[i, j] / s), round to nearest even, one scale s per block of block_rows x 128 (block_rows 1: activations,
  * 128: weights; blocks at the edges are smaller).  What is not finite becomes NaN and has no part in the scale; a block without
@@ -340,7 +341,9 @@ typedef struct {
  * them token d_seq_lens[b] - 1.  The arrays are read on the device, so a captured call serves requests of any lengths.  Rows outside
  * the requests are left alone.  Whatever the arrays hold, nothing outside the buffers is read or written: a page number outside
  * the cache is passed over (the tokens are not written, and are left out of the attention) and raises EP_ERR_BAD_PAGE in the
- * integrity word; lengths are cut to columns * page, starts to 0 .. N. */
+ * integrity word; lengths are cut to columns * page, starts to 0 .. N.  Starts do not descend; where they do, so that rows belong to
+ * several requests, those rows may come from any of them, and an attention with more work than the call's N rows can make does nothing
+ * and raises EP_ERR_BAD_PAGE. */
 typedef struct {
     const int32_t *d_table, *d_seq_lens, *d_starts;   /* device: B x columns, B, B + 1 */
     int64_t ldt;                                      /* between the table's rows */
@@ -352,7 +355,7 @@ typedef struct {
  * that holds the new tokens); where it grows the older tokens become e4m3(q s / s').  A page without older tokens gets the new
  * tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request
  * that has fewer tokens than rows is passed over, from the first on.
- * A page that a call writes must belong to one request only; pages that are full may be shared. */
+ * A page that a call writes must belong to one request only and stand in its table once; pages that are full may be shared. */
 typedef struct {
     ep_cache cache;
     ep_requests requests;
@@ -364,8 +367,8 @@ typedef struct {
 int ep_cache_append(const ep_append_job *job, void *stream);
 
 /* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row
- * i of its n.  Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token gives 0 (and -infinity
- * in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values;
+ * i of its n.  Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token, or only scores of -infinity,
+ * gives 0 (and -infinity in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values;
  * a token's values count only for rows that see it.  EP_ERR_UNSUPPORTED for B > 4096, and for calls that could come to 2^30
  * pieces of work: ceil(columns * page / 256) * (N * q_heads / heads / 8 + B) * heads. */
 typedef struct {

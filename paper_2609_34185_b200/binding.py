@@ -621,7 +621,7 @@ def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool 
     torch, dtype = _types[0], q.dtype
     code = _types[3].get(dtype)
     heads, page, dim, columns, B = fields[5], fields[6], fields[7], fields[12], fields[13]
-    if code is None or code == FP32 or len(shape) != 3 or shape[2] != dim or shape[1] == 0 or shape[1] % heads:
+    if code is None or code == FP32 or len(shape) != 3 or shape[2] != dim or shape[1] == 0 or heads == 0 or shape[1] % heads:
         raise ValueError("q must be bfloat16 or float16 [N, q_heads, dim], its heads a multiple of the cache's")
     if out is None:
         out = _empty(shape, dtype, q.device, stream)

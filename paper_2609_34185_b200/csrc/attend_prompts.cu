@@ -149,7 +149,8 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         if (lane == 0) prefix[b] = n * P.q.H;
     }
     __syncthreads();
-    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t b) { return prefix[b]; }, prefix, reinterpret_cast<uint32_t *>(gen + S::kPart));
+    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t b) { return prefix[b]; }, P.most, prefix, reinterpret_cast<uint32_t *>(gen + S::kPart));
+    if (all == 0 && blockIdx.x == 0 && tid == 0 && prefix[P.q.B]) atomicOr(&g_prompts_status, unsigned(kStatusPage));
     const uint32_t ctas = min(P.grid, all), u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
                    u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
     Place *start = reinterpret_cast<Place *>(gen + S::kPart + 64);

@@ -201,7 +201,7 @@ int launch_quantize(const QuantParams &P, uint32_t block_rows, cudaStream_t st) 
         if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
         e = few ? op_launch(quantize_rows_kernel<E, 1>, uint32_t(grid), 128, 0, 1, st, P) : op_launch(quantize_rows_kernel<E, 4>, uint32_t(grid), 128, 0, 1, st, P);
     } else {
-        const uint64_t grid = uint64_t((P.T + kBlock - 1u) / kBlock) * P.blocks;
+        const uint64_t grid = (uint64_t(P.T) + kBlock - 1u) / kBlock * P.blocks;
         if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
         e = op_launch(quantize_blocks_kernel<E>, uint32_t(grid), 256, 0, 1, st, P);
     }

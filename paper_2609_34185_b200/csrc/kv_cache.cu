@@ -223,7 +223,8 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
     if (tid == 0) st_smem(abort_at, 0);
     for (uint32_t i = tid; i < D; i += 32 * W) first_nan[i] = 0xFFFFFFFFu;
     op_wait_for_stream();
-    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t i) { return units_of(extent_of(P.q, i), P.G, P.q.H, kRows); }, prefix, reinterpret_cast<uint32_t *>(join));
+    const uint32_t all = prefix_sums(P.q.B, [&](uint32_t i) { return units_of(extent_of(P.q, i), P.G, P.q.H, kRows); }, P.most, prefix, reinterpret_cast<uint32_t *>(join));
+    if (all == 0 && blockIdx.x == 0 && tid == 0 && prefix[P.q.B]) atomicOr(&g_cache_status, unsigned(kStatusPage));
     const uint32_t ctas = min(P.grid, all);               // those with a share: none of theirs is empty
     const uint32_t u_begin = blockIdx.x < ctas ? uint32_t(uint64_t(all) * blockIdx.x / ctas) : 0u,
                    u_end = blockIdx.x < ctas ? uint32_t(uint64_t(all) * (blockIdx.x + 1u) / ctas) : 0u;
@@ -741,6 +742,8 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
     P.grid = std::min(uint32_t(sms), kMostPieces);
+    // of prompts: row tiles of 256, in each at most three places more than tiles of 128 tokens; below 2^32, as N * G > 16 B there
+    P.most = prompts_serve(N, B, P.G) ? uint32_t(((uint64_t(P.q.columns) * c.page + 127u) / 128u + 3u) * (uint64_t(N) * P.G / 256u + B) * c.heads) : uint32_t(units);
     P.k = static_cast<const uint8_t *>(c.d_k);
     P.v = static_cast<const uint8_t *>(c.d_v);
     cudaStream_t st = static_cast<cudaStream_t>(stream);

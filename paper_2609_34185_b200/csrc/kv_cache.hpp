@@ -42,25 +42,27 @@ __device__ __forceinline__ float exp2_fast(float x) {
     return r;
 }
 
-// prefix[b] = the sum of units(b') over b' < b, prefix[B] = all; by a whole CTA of at most 32 warps.  Returns all.
+// prefix[b] = the sum of units(b') over b' < b, prefix[B] = all; by a whole CTA of at most 32 warps.  Returns all, and 0 if that is
+// more than `most`, which no call can come to whose requests' rows are its own: sums stop at 2^32 - 1 on the way.
+__device__ __forceinline__ uint32_t add_capped(uint32_t a, uint32_t b) { return a + b < a ? 0xFFFFFFFFu : a + b; }
 template <class F>
-__device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t *prefix, uint32_t *part) {
+__device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t most, uint32_t *prefix, uint32_t *part) {
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, per = (B + blockDim.x - 1u) / blockDim.x;
     const uint32_t b0 = min(tid * per, B), b1 = min(b0 + per, B);
     uint32_t sum = 0;
-    for (uint32_t b = b0; b < b1; ++b) sum += units(b);
+    for (uint32_t b = b0; b < b1; ++b) sum = add_capped(sum, units(b));
     uint32_t inc = sum;
 #pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
         const uint32_t o = __shfl_up_sync(0xFFFFFFFFu, inc, d);
-        if (lane >= d) inc += o;
+        if (lane >= d) inc = add_capped(inc, o);
     }
     if (lane == 31) part[warp] = inc;
     __syncthreads();
     uint32_t at = inc - sum, all = 0;
     for (uint32_t w = 0; w < (blockDim.x >> 5); ++w) {
         if (w < warp) at += part[w];
-        all += part[w];
+        all = add_capped(all, part[w]);
     }
     for (uint32_t b = b0; b < b1; ++b) {
         prefix[b] = at;
@@ -68,7 +70,7 @@ __device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t *prefix, uint32_t 
     }
     if (tid == 0) prefix[B] = all;
     __syncthreads();
-    return all;
+    return all <= most ? all : 0u;
 }
 // the last b in [lo, B) with prefix[b] <= u (prefix[lo] <= u < prefix[B]): its units hold u
 __device__ __forceinline__ uint32_t request_of(const uint32_t *prefix, uint32_t lo, uint32_t B, uint32_t u) {
@@ -117,6 +119,7 @@ struct AttendParams {
     uint32_t causal;
     float *workspace;             // null: no segment can cross a share
     uint32_t grid;
+    uint32_t most;                // units (places) that a call of this size can come to
 };
 
 // many rows per request (attend_prompts.cu): whether a call's shape is for it; `cut`: segments may be cut (a workspace is there)

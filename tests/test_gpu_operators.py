@@ -12,6 +12,9 @@ error d (in powers of two) changes it by a factor 2^d: d is D 2^-23 A for A = su
 above, and twice 2^-22 for the exponential and the products around it.  Numerator and denominator both have the second kind.  Bound: (2^-11 + 4 ln 2
 (D 2^-23 A + 2^-21)) sum p |v|, and half a step of the result's type."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -867,3 +870,53 @@ def test_attention_of_prompts_many_units_and_captured():
             check_attention(out[:rows[-1], at], want[:rows[-1]], bound[:rows[-1]])
         if now is lens:
             assert torch.equal(out, first)
+
+
+@gpu
+@pytest.mark.parametrize("N,G", [(4096, 8), (4096, 32)])
+def test_rows_that_several_requests_claim_are_refused(N, G):
+    # starts that go up and down between 0 and N: 2048 requests each claim all rows, more than 2^32 pieces of work
+    B, H, page, columns = 4096, 8, 256, 64
+    cache = ep.kv_cache(1, H, 64, page)
+    table, lens = torch.zeros(B, columns, dtype=torch.int32, device="cuda"), torch.full((B,), columns * page, dtype=torch.int32, device="cuda")
+    starts = ints([0, N] * (B // 2) + [0])
+    q = torch.zeros(N, H * G, 64, dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(q, 4.0)
+    ep.cache_attention(q, cache, table, lens, starts, out=out)
+    assert ep.last_device_status() == -9 and ep.last_device_status() == 0
+    assert bool((out == 4.0).all())
+
+
+FIRST_CALLS = """
+import torch, {name} as ep
+x = torch.randn(3, 256, device="cuda").to(torch.bfloat16)
+w = torch.randn(384, 256, device="cuda")
+cache = ep.kv_cache(8, 1, 64, 64)
+ints = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+table, lens, starts = ints([[0, 1, 2, 3, 4, 5]]), ints([3]), ints([0, 3])
+
+def layer(rows):
+    xq, xs = ep.quantize_blocks(x)
+    wq, ws = ep.quantize_blocks(w, 128)
+    y = ep.fp8_matmul(xq, xs, wq, ws).unflatten(1, (6, 64))
+    ep.cache_append(cache, y[:, :1], y[:, 1:2], table, lens, starts)
+    return ep.cache_attention(y[:rows, 2:], cache, table, lens, ints_of[rows])
+
+ints_of = {{1: ints([0, 1]), 3: starts}}
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    a, b = layer(1), layer(3)
+graph.replay()
+torch.cuda.synchronize()
+assert torch.equal(a, layer(1)) and torch.equal(b, layer(3)) and bool(a.isfinite().all()) and float(b.float().abs().sum()) > 0
+assert ep.last_device_status() == 0
+print("captured")
+"""
+
+
+@gpu
+def test_first_calls_of_a_process_can_be_captured():
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(name=ep.__name__)], capture_output=True, text=True, timeout=300,
+                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0 and done.stdout.split() == ["captured"], done.stderr[-2000:]
