@@ -30,7 +30,8 @@ __device__ unsigned int g_prompts_status = 0;
 // ======================================================================================================================
 constexpr uint32_t kUnitRows = 256, kKeys = 128, kHalfKeys = 64, kThreads = 32 * 16, kNanUnits = 8;
 constexpr float kSlack = 8.0f, kShift = 7.0f;
-// a piece of a unit in the workspace: O, then m and l of each row
+// A piece of a unit in the workspace: O, four columns of all rows after another (a thread has a row, so a warp's store of four columns is 512
+// bytes side by side), then m and l of each row.
 template <uint32_t D>
 constexpr uint32_t kPromptPiece = kUnitRows * (D + 2);
 
@@ -46,6 +47,11 @@ struct PromptShape {
     static_assert(kSmem <= 232448);
 };
 
+// the power of two that puts a row's largest magnitude in [2^13, 2^14); 0 for a row of zeros or with an infinity
+__device__ __forceinline__ int32_t lifted(float largest) {
+    const int32_t e = int32_t(__float_as_uint(largest) >> 23);
+    return e == 0 || e == 255 ? 0 : min(140 - e, 100);
+}
 __device__ __forceinline__ void mma_f16_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate, uint32_t lead) {
     asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.b32 p, %4, 0;\n\tsetp.ne.b32 q, %5, 0;\n\t@q tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}"
                  ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate), "r"(lead) : "memory");
@@ -444,29 +450,33 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         // Rows of a unit's tile as binary16, times a power of two that puts a row's largest magnitude in [2^13, 2^14) (see kv_cache.cu),
         // with the sign of the scale; returns the factor of the row's scores.  They go in as soon as the scores of the unit before are done.
         auto rows_in = [&](const Cursor &y) {
-            const uint32_t row = y.row0() + t * 128u + l, i_row = row / P.G;
-            const bool real = row < y.r.rows * P.G;
+            // a warp's 32 rows, 16 bytes to a lane: D / 8 lanes side by side have a row (a row to a lane: 32 places 256 bytes apart in every load)
+            constexpr uint32_t kLanes = D / 8, kPer = 32 / kLanes;
+            const uint32_t row = y.row0() + t * 128u + l, i_row = row / P.G, n_rows = y.r.rows * P.G, sub = lane / kLanes, c = lane % kLanes;
             const T *src = static_cast<const T *>(P.x) + int64_t(y.r.row + i_row) * P.ldq + int64_t(y.p.h * P.G + row % P.G) * P.ldqh;
-            uint4 w[D / 8];
+            uint4 w[kLanes];
 #pragma unroll
-            for (uint32_t c = 0; c < D / 8; ++c) w[c] = real ? __ldg(reinterpret_cast<const uint4 *>(src) + c) : make_uint4(0, 0, 0, 0);
-            float a = 0.0f;
-#pragma unroll
-            for (uint32_t c = 0; c < D / 8; ++c) {
-                a = max3(a, max3(fabsf(E::lo(w[c].x)), fabsf(E::hi(w[c].x)), fabsf(E::lo(w[c].y))), fabsf(E::hi(w[c].y)));
-                a = max3(a, max3(fabsf(E::lo(w[c].z)), fabsf(E::hi(w[c].z)), fabsf(E::lo(w[c].w))), fabsf(E::hi(w[c].w)));
+            for (uint32_t k = 0; k < kLanes; ++k) {
+                const T *from = reinterpret_cast<const T *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(src), k * kPer + sub));
+                w[k] = row - lane + k * kPer + sub < n_rows ? __ldg(reinterpret_cast<const uint4 *>(from) + c) : make_uint4(0, 0, 0, 0);
             }
-            const int32_t ea = int32_t(__float_as_uint(a) >> 23), up = ea == 0 || ea == 255 ? 0 : min(140 - ea, 100);
-            const float mul = copysignf(pow2_biased(uint32_t(127 + up)), P.scale_log2);
+            float largest = 0.0f;                         // of this lane's row
 #pragma unroll
-            for (uint32_t c = 0; c < D / 8; ++c) {
-                const uint32_t at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + l * 128u + (((c & 7u) ^ (l & 7u)) << 4);
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w[c].x) * mul, E::hi(w[c].x) * mul)), "r"(Fp16::two(E::lo(w[c].y) * mul, E::hi(w[c].y) * mul)),
-                             "r"(Fp16::two(E::lo(w[c].z) * mul, E::hi(w[c].z) * mul)), "r"(Fp16::two(E::lo(w[c].w) * mul, E::hi(w[c].w) * mul)) : "memory");
+            for (uint32_t k = 0; k < kLanes; ++k) {
+                float a = max3(max3(fabsf(E::lo(w[k].x)), fabsf(E::hi(w[k].x)), fabsf(E::lo(w[k].y))), fabsf(E::hi(w[k].y)), fabsf(E::lo(w[k].z)));
+                a = max3(a, max3(fabsf(E::hi(w[k].z)), fabsf(E::lo(w[k].w)), fabsf(E::hi(w[k].w))), 0.0f);
+#pragma unroll
+                for (uint32_t x = 1; x < kLanes; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, x));
+                const float mine = __shfl_sync(0xFFFFFFFFu, a, lane % kPer * kLanes);
+                if (lane / kPer == k) largest = mine;
+                const float mul = copysignf(pow2_biased(uint32_t(127 + lifted(a))), P.scale_log2);
+                const uint32_t in_tile = (warp & 3u) * 32u + k * kPer + sub, at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + in_tile * 128u + (((c & 7u) ^ (in_tile & 7u)) << 4);
+                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w[k].x) * mul, E::hi(w[k].x) * mul)), "r"(Fp16::two(E::lo(w[k].y) * mul, E::hi(w[k].y) * mul)),
+                             "r"(Fp16::two(E::lo(w[k].z) * mul, E::hi(w[k].z) * mul)), "r"(Fp16::two(E::lo(w[k].w) * mul, E::hi(w[k].w) * mul)) : "memory");
             }
             fence_proxy_async();
             bar_arrive(q_ready + 8 * t);
-            return fabsf(P.scale_log2) * pow2_biased(uint32_t(127 - up));
+            return fabsf(P.scale_log2) * pow2_biased(uint32_t(127 - lifted(largest)));
         };
         float fac_next = 0.0f;
         bool rows_there = false;                          // of the unit that comes
@@ -615,13 +625,24 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     if (!whole) {
 #pragma unroll
                         for (uint32_t e = 0; e < 32; e += 4)
-                            *reinterpret_cast<uint4 *>(piece + (t * 128u + l) * D + 32 * c + e) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
-                    } else if (real) {
+                            *reinterpret_cast<uint4 *>(piece + ((8 * c + e / 4) * kUnitRows + t * 128u + l) * 4u) = make_uint4(v[e], v[e + 1], v[e + 2], v[e + 3]);
+                    } else {
+                        // 32 columns of the warp's rows, turned in shared memory so that four lanes write a row's 64 bytes
+                        const uint32_t mine = base + S::kPrefix + warp * 2048u;
 #pragma unroll
                         for (uint32_t e = 0; e < 32; e += 8)
-                            *reinterpret_cast<uint4 *>(dst + 32 * c + e) =
-                                make_uint4(E::two(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), E::two(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])),
-                                           E::two(__uint_as_float(v[e + 4]), __uint_as_float(v[e + 5])), E::two(__uint_as_float(v[e + 6]), __uint_as_float(v[e + 7])));
+                            asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(mine + lane * 64u + ((e / 8 ^ (lane >> 1 & 3u)) << 4)), "r"(E::two(__uint_as_float(v[e]), __uint_as_float(v[e + 1]))),
+                                         "r"(E::two(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3]))), "r"(E::two(__uint_as_float(v[e + 4]), __uint_as_float(v[e + 5]))),
+                                         "r"(E::two(__uint_as_float(v[e + 6]), __uint_as_float(v[e + 7]))) : "memory");
+                        __syncwarp();
+#pragma unroll
+                        for (uint32_t k = 0; k < 4; ++k) {
+                            const uint32_t other = 8 * k + (lane >> 2);
+                            T *to = reinterpret_cast<T *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(dst), other));
+                            const uint4 w = ld_smem16(mine + other * 64u + (((lane & 3u) ^ (other >> 1 & 3u)) << 4));
+                            if (row - lane + other < n_rows) *reinterpret_cast<uint4 *>(to + 32 * c + 8 * (lane & 3u)) = w;
+                        }
+                        __syncwarp();
                     }
                 }
                 if (!whole) {
@@ -667,30 +688,30 @@ __global__ void __launch_bounds__(256) prompts_join_kernel(const __grid_constant
     const Extent r = extent_of(P.q, b);
     const float *pieces = P.workspace + size_t(P.grid) * 8u;
     const float *own = pieces + (size_t(blockIdx.x) * 2u + 1u) * kPromptPiece<D>, *first = pieces + size_t(blockIdx.x + 1u) * 2u * kPromptPiece<D>;
-    for (uint32_t e = blockIdx.y * blockDim.x + threadIdx.x; e < kUnitRows * D / 4u; e += gridDim.y * blockDim.x) {
-        const uint32_t row = e / (D / 4u), d = e % (D / 4u) * 4u, at = j * kUnitRows + row, i = at / P.G, g = at % P.G;
-        if (at >= r.rows * P.G) return;
-        const float own_top = own[kUnitRows * D + row];
-        float top = own_top;
+    // eight lanes have eight rows of the same columns, as they lie in the pieces; four such groups write 32 bytes of each row
+    const uint32_t group = threadIdx.x >> 3, d = group % (D / 4u) * 4u, row = blockIdx.y * (1024u / D) + group / (D / 4u) * 8u + (threadIdx.x & 7u), place = (d * kUnitRows) + row * 4u;
+    const uint32_t at = j * kUnitRows + row, i = at / P.G, g = at % P.G;
+    if (at >= r.rows * P.G) return;
+    const float own_top = own[kUnitRows * D + row];
+    float top = own_top;
 #pragma unroll 4
-        for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPromptPiece<D> + kUnitRows * D + row]);
-        const float ref = top == -INFINITY ? 0.0f : top;
-        float f = exp2_fast(own_top - ref), sum = own[kUnitRows * (D + 1) + row] * f;
-        float4 acc = *reinterpret_cast<const float4 *>(own + row * D + d);
-        acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
+    for (uint32_t c = 0; c < n; ++c) top = fmaxf(top, first[size_t(c) * 2u * kPromptPiece<D> + kUnitRows * D + row]);
+    const float ref = top == -INFINITY ? 0.0f : top;
+    float f = exp2_fast(own_top - ref), sum = own[kUnitRows * (D + 1) + row] * f;
+    float4 acc = *reinterpret_cast<const float4 *>(own + place);
+    acc.x *= f, acc.y *= f, acc.z *= f, acc.w *= f;
 #pragma unroll 4
-        for (uint32_t c = 0; c < n; ++c) {
-            const float *p = first + size_t(c) * 2u * kPromptPiece<D>;
-            f = exp2_fast(p[kUnitRows * D + row] - ref);
-            sum += p[kUnitRows * (D + 1) + row] * f;
-            const float4 v = *reinterpret_cast<const float4 *>(p + row * D + d);
-            acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
-        }
-        const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
-        const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
-        *reinterpret_cast<uint2 *>(static_cast<T *>(P.o) + t * P.ldo + head * P.ldoh + d) = make_uint2(E::two(acc.x * inverse, acc.y * inverse), E::two(acc.z * inverse, acc.w * inverse));
-        if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
+    for (uint32_t c = 0; c < n; ++c) {
+        const float *p = first + size_t(c) * 2u * kPromptPiece<D>;
+        f = exp2_fast(p[kUnitRows * D + row] - ref);
+        sum += p[kUnitRows * (D + 1) + row] * f;
+        const float4 v = *reinterpret_cast<const float4 *>(p + place);
+        acc.x += v.x * f, acc.y += v.y * f, acc.z += v.z * f, acc.w += v.w * f;
     }
+    const float inverse = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+    const int64_t t = int64_t(r.row + i), head = int64_t(h * P.G + g);
+    *reinterpret_cast<uint2 *>(static_cast<T *>(P.o) + t * P.ldo + head * P.ldoh + d) = make_uint2(E::two(acc.x * inverse, acc.y * inverse), E::two(acc.z * inverse, acc.w * inverse));
+    if (P.lse && d == 0) P.lse[t * P.Hq + head] = sum == 0.0f ? -INFINITY : (top - kShift + log2f(sum)) * 0.69314718055994531f;
 }
 
 template <class E, uint32_t D>
