@@ -450,29 +450,49 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
         // Rows of a unit's tile as binary16, times a power of two that puts a row's largest magnitude in [2^13, 2^14) (see kv_cache.cu),
         // with the sign of the scale; returns the factor of the row's scores.  They go in as soon as the scores of the unit before are done.
         auto rows_in = [&](const Cursor &y) {
-            // a warp's 32 rows, 16 bytes to a lane: D / 8 lanes side by side have a row (a row to a lane: 32 places 256 bytes apart in every load)
+            // A warp's 32 rows, 16 bytes to a lane: D / 8 lanes side by side have a row (a row to a lane: 32 places 256 bytes apart in every load).
+            // In loops, by way of shared memory: the first unit's rows come while nothing of this code is in the instruction cache.
             constexpr uint32_t kLanes = D / 8, kPer = 32 / kLanes;
             const uint32_t row = y.row0() + t * 128u + l, i_row = row / P.G, n_rows = y.r.rows * P.G, sub = lane / kLanes, c = lane % kLanes;
             const T *src = static_cast<const T *>(P.x) + int64_t(y.r.row + i_row) * P.ldq + int64_t(y.p.h * P.G + row % P.G) * P.ldqh;
-            uint4 w[kLanes];
-#pragma unroll
+            auto place = [&](uint32_t k) {
+                const uint32_t in_tile = (warp & 3u) * 32u + k * kPer + sub;
+                return base + S::kQ + t * S::kTile + c / 8 * S::kHalf + in_tile * 128u + (((c & 7u) ^ (in_tile & 7u)) << 4);
+            };
+#pragma unroll 4
             for (uint32_t k = 0; k < kLanes; ++k) {
                 const T *from = reinterpret_cast<const T *>(__shfl_sync(0xFFFFFFFFu, reinterpret_cast<unsigned long long>(src), k * kPer + sub));
-                w[k] = row - lane + k * kPer + sub < n_rows ? __ldg(reinterpret_cast<const uint4 *>(from) + c) : make_uint4(0, 0, 0, 0);
+                const bool there = row - lane + k * kPer + sub < n_rows;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place(k)), "l"(there ? from + c * 8u : static_cast<const T *>(P.x)), "r"(there ? 16u : 0u) : "memory");
             }
+            asm volatile("cp.async.wait_all;" ::: "memory");
             float largest = 0.0f;                         // of this lane's row
+#pragma unroll 1
+            for (uint32_t k0 = 0; k0 < kLanes; k0 += 4) { // (what this lane has brought, four rows' chains side by side)
+                uint4 w[4];
+                float a[4];
 #pragma unroll
-            for (uint32_t k = 0; k < kLanes; ++k) {
-                float a = max3(max3(fabsf(E::lo(w[k].x)), fabsf(E::hi(w[k].x)), fabsf(E::lo(w[k].y))), fabsf(E::hi(w[k].y)), fabsf(E::lo(w[k].z)));
-                a = max3(a, max3(fabsf(E::hi(w[k].z)), fabsf(E::lo(w[k].w)), fabsf(E::hi(w[k].w))), 0.0f);
+                for (uint32_t k = 0; k < 4; ++k) w[k] = ld_smem16(place(k0 + k));
 #pragma unroll
-                for (uint32_t x = 1; x < kLanes; x <<= 1) a = fmaxf(a, __shfl_xor_sync(0xFFFFFFFFu, a, x));
-                const float mine = __shfl_sync(0xFFFFFFFFu, a, lane % kPer * kLanes);
-                if (lane / kPer == k) largest = mine;
-                const float mul = copysignf(pow2_biased(uint32_t(127 + lifted(a))), P.scale_log2);
-                const uint32_t in_tile = (warp & 3u) * 32u + k * kPer + sub, at = base + S::kQ + t * S::kTile + c / 8 * S::kHalf + in_tile * 128u + (((c & 7u) ^ (in_tile & 7u)) << 4);
-                asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(at), "r"(Fp16::two(E::lo(w[k].x) * mul, E::hi(w[k].x) * mul)), "r"(Fp16::two(E::lo(w[k].y) * mul, E::hi(w[k].y) * mul)),
-                             "r"(Fp16::two(E::lo(w[k].z) * mul, E::hi(w[k].z) * mul)), "r"(Fp16::two(E::lo(w[k].w) * mul, E::hi(w[k].w) * mul)) : "memory");
+                for (uint32_t k = 0; k < 4; ++k) {
+                    a[k] = max3(max3(fabsf(E::lo(w[k].x)), fabsf(E::hi(w[k].x)), fabsf(E::lo(w[k].y))), fabsf(E::hi(w[k].y)), fabsf(E::lo(w[k].z)));
+                    a[k] = max3(a[k], max3(fabsf(E::hi(w[k].z)), fabsf(E::lo(w[k].w)), fabsf(E::hi(w[k].w))), 0.0f);
+                }
+#pragma unroll
+                for (uint32_t x = 1; x < kLanes; x <<= 1)
+#pragma unroll
+                    for (uint32_t k = 0; k < 4; ++k) a[k] = fmaxf(a[k], __shfl_xor_sync(0xFFFFFFFFu, a[k], x));
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const float mine = __shfl_sync(0xFFFFFFFFu, a[k], lane % kPer * kLanes);
+                    if (lane / kPer == k0 + k) largest = mine;
+                }
+#pragma unroll
+                for (uint32_t k = 0; k < 4; ++k) {
+                    const float mul = copysignf(pow2_biased(uint32_t(127 + lifted(a[k]))), P.scale_log2);
+                    asm volatile("st.shared.v4.u32 [%0], {%1, %2, %3, %4};" ::"r"(place(k0 + k)), "r"(Fp16::two(E::lo(w[k].x) * mul, E::hi(w[k].x) * mul)), "r"(Fp16::two(E::lo(w[k].y) * mul, E::hi(w[k].y) * mul)),
+                                 "r"(Fp16::two(E::lo(w[k].z) * mul, E::hi(w[k].z) * mul)), "r"(Fp16::two(E::lo(w[k].w) * mul, E::hi(w[k].w) * mul)) : "memory");
+                }
             }
             fence_proxy_async();
             bar_arrive(q_ready + 8 * t);
