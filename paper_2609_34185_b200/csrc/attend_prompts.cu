@@ -9,8 +9,11 @@ __device__ unsigned int g_prompts_status = 0;
 
 // ======================================================================================================================
 // A unit is 256 rows (a row = a query and one of the query heads that share a head of the cache) of one request and head, as two tiles
-// of 128, against the request's tokens, 128 at a time.  Bound by the tensor cores: 2 * 2 * 256 * 128 * D operations for each 128 tokens, in
-// binary16, and next to them by the 256 * 128 exponentials (at 16 per cycle and SM as long as the products with D = 128).
+// of 128, against the request's tokens, 128 at a time.  For each 128 tokens the tensor cores need 2 * 2 * 256 * 128 * D operations in binary16, 2048
+// cycles with D = 128, and the 256 * 128 exponentials at 16 per cycle and SM as many; a tile takes 4200.  What bounds it is the softmax
+// of a row, one instruction after another: two warps to a scheduler, which spend half of their time at the exponentials and half at
+// all that comes before and after (scores in, maximum, weights out), and registers leave no room for more warps.  Two prompts of up to
+// 2048 rows x 40 heads on up to 4096 tokens 311 us, 838 TFLOP/s.
 //   warps 0 - 3, 4 - 7   a tile's softmax: a thread has a row.  Scores come from tensor memory, the weights go back there (binary16, over
 //                        the scores) as the second product's left operand.
 //   warps 8 - 11         bring keys and values in and turn them into binary16, exactly, in the layout of the products' right operands; the
@@ -22,7 +25,8 @@ __device__ unsigned int g_prompts_status = 0;
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
 // than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
 // t = score + log2(v_scale / the request's first), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
-// instead of the maximum first: 379 -> 462 us.)
+// instead of the maximum first: 379 -> 462 us.  The two warps of a scheduler taking turns at the exponentials: 336 -> 360.  The next scores asked
+// for before the weights are out: 311 -> 325.  A quarter of the exponentials as polynomials beside the unit: 311 -> 314, half: 335.)
 // The loops are short on purpose: three roles run side by side, and what they execute over and over has to fit the SM's instruction
 // cache (with everything unrolled, 170 KB, six of ten fetches hit it and a tile took 13 700 cycles).
 // The tiles of tokens of all units form one list; every CTA takes an equal, contiguous share of it, as in kv_cache.cu, and what
