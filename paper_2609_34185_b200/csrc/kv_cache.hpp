@@ -44,13 +44,27 @@ __device__ __forceinline__ float exp2_fast(float x) {
 
 // prefix[b] = the sum of units(b') over b' < b, prefix[B] = all; by a whole CTA of at most 32 warps.  Returns all, and 0 if that is
 // more than `most`, which no call can come to whose requests' rows are its own: sums stop at 2^32 - 1 on the way.
-__device__ __forceinline__ uint32_t add_capped(uint32_t a, uint32_t b) { return a + b < a ? 0xFFFFFFFFu : a + b; }
+__host__ __device__ __forceinline__ uint32_t add_capped(uint32_t a, uint32_t b) { return a + b < a ? 0xFFFFFFFFu : a + b; }
+// A thread's requests b0 .. b1 - 1: the sum of their units, then, with what lies before them, their entries.
+template <class F>
+__host__ __device__ __forceinline__ uint32_t sum_units(uint32_t b0, uint32_t b1, F units) {
+    uint32_t sum = 0;
+    for (uint32_t b = b0; b < b1; ++b) sum = add_capped(sum, units(b));
+    return sum;
+}
+template <class F>
+__host__ __device__ __forceinline__ void lay_prefix(uint32_t b0, uint32_t b1, uint32_t at, F units, uint32_t *prefix) {
+    for (uint32_t b = b0; b < b1; ++b) {
+        const uint32_t n = units(b);                      // (the count may stand in prefix[b])
+        prefix[b] = at;
+        at += n;
+    }
+}
 template <class F>
 __device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t most, uint32_t *prefix, uint32_t *part) {
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = tid >> 5, per = (B + blockDim.x - 1u) / blockDim.x;
     const uint32_t b0 = min(tid * per, B), b1 = min(b0 + per, B);
-    uint32_t sum = 0;
-    for (uint32_t b = b0; b < b1; ++b) sum = add_capped(sum, units(b));
+    const uint32_t sum = sum_units(b0, b1, units);
     uint32_t inc = sum;
 #pragma unroll
     for (uint32_t d = 1; d < 32; d <<= 1) {
@@ -64,10 +78,7 @@ __device__ uint32_t prefix_sums(uint32_t B, F units, uint32_t most, uint32_t *pr
         if (w < warp) at += part[w];
         all = add_capped(all, part[w]);
     }
-    for (uint32_t b = b0; b < b1; ++b) {
-        prefix[b] = at;
-        at += units(b);
-    }
+    lay_prefix(b0, b1, at, units, prefix);
     if (tid == 0) prefix[B] = all;
     __syncthreads();
     return all <= most ? all : 0u;

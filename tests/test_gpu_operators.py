@@ -887,6 +887,51 @@ def test_rows_that_several_requests_claim_are_refused(N, G):
     assert bool((out == 4.0).all())
 
 
+def many_requests(B, kind):
+    """Rows and tokens of B requests, some without rows or tokens."""
+    r = np.random.default_rng(B)
+    lens = r.integers(0, 200, B)
+    lens[r.random(B) < 0.1] = 0
+    if kind == "few":                                     # three rows each, or none
+        news = np.where(r.random(B) < 0.05, 0, 3)
+    elif kind in ("first", "middle", "last"):             # a prompt among single tokens
+        news, at = np.ones(B, int), {"first": 0, "middle": B // 2, "last": B - 1}[kind]
+        news[at], lens[at] = B + 100, B + 150
+    elif kind == "alone":                                 # most requests have no rows
+        news = np.zeros(B, int)
+        news[0], lens[0], news[1], lens[1], news[B - 1], lens[B - 1] = 3 * B + 200, 3 * B + 210, 1, 1, 2, 90
+    else:
+        news = np.full(B, int(kind))
+        lens[B // 3::97] = 700                            # (of two to four units: cut between CTAs now and then)
+    return news.tolist(), lens.tolist()
+
+
+@gpu
+@pytest.mark.parametrize("B,kind,G,D,page", [
+    # prompts' kernel: 512 requests are one to a thread, more are several
+    (512, "few", 8, 64, 64), (513, "few", 8, 64, 64), (513, "few", 8, 128, 256), (600, "few", 8, 128, 16), (1025, "few", 8, 64, 32), (4096, "few", 8, 64, 64), (600, "alone", 5, 64, 64),
+    (600, "first", 8, 64, 32), (600, "middle", 8, 128, 64), (600, "last", 8, 64, 64), (1025, "middle", 8, 64, 64), (700, "1", 20, 64, 64), (600, "4", 5, 128, 64),
+    # single tokens: twelve warps with up to eight rows a request, eight with up to sixteen
+    (385, "1", 5, 64, 64), (1000, "1", 8, 128, 256), (4096, "1", 5, 64, 32), (257, "2", 7, 64, 64), (1025, "2", 7, 128, 16), (4096, "2", 7, 64, 64)])
+def test_attention_of_many_requests(B, kind, G, D, page):
+    news, lens = many_requests(B, kind)
+    starts = [2 + s for s in offsets(news)]
+    N = starts[-1] + 3                                    # rows of nobody before and after
+    cache, table = filled(lens, 1, D, page, seed=B + D)
+    q = torch.randn(N, G, D, generator=cuda(B), device="cuda").mul_(1.5).to(torch.bfloat16)
+    out, lse = torch.full_like(q, 9.0), torch.full((N, G), 7.0, device="cuda")
+    ep.cache_attention(q, cache, ints(table), ints(lens), ints(starts), scale=0.2, out=out, lse=lse)
+    want, bound, want_lse = attended(q, cache, table, lens, starts, 0.2, True)
+    mine = slice(starts[0], starts[-1])
+    check_attention(out[mine], want[mine], bound[mine])
+    seen = want_lse[mine] > -math.inf
+    assert torch.equal(lse[mine].cpu() > -math.inf, seen)
+    assert bool(((lse[mine].double().cpu() - want_lse[mine])[seen].abs() <= 1e-3).all())
+    for t, value in ((out, 9.0), (lse, 7.0)):
+        assert bool((t[:2] == value).all()) and bool((t[-3:] == value).all())
+    assert ep.last_device_status() == 0
+
+
 FIRST_CALLS = """
 import torch, {name} as ep
 x = torch.randn(3, 256, device="cuda").to(torch.bfloat16)
