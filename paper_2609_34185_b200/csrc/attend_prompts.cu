@@ -67,13 +67,13 @@ __device__ __forceinline__ void mma_f16_ts(uint32_t d, uint32_t a, uint64_t b, u
 // binary16 x binary16 to fp32, M = 128, N = n; `mn` = the right operand is MN-major
 __host__ __device__ constexpr uint32_t f16_idesc(uint32_t n, uint32_t mn) { return (1u << 4) | (mn << 16) | ((n >> 3) << 17) | ((128u >> 4) << 24); }
 
-__device__ __forceinline__ uint32_t sees(const AttendParams &P, const Extent &r, uint32_t query) {
+__host__ __device__ __forceinline__ uint32_t sees(const AttendParams &P, const Extent &r, uint32_t query) {
     return !P.causal ? r.len : r.len + query + 1u > r.rows ? min(r.len, r.len + query + 1u - r.rows) : 0u;
 }
 // row tile j of a request: tokens that its last row sees; tiles of tokens, at least one, so that rows that see nothing are written too
-__device__ __forceinline__ uint32_t most_of(const AttendParams &P, const Extent &r, uint32_t j) { return sees(P, r, (min((j + 1u) * kUnitRows, r.rows * P.G) - 1u) / P.G); }
-__device__ __forceinline__ uint32_t tiles_of(const AttendParams &P, const Extent &r, uint32_t j) { return max(1u, (most_of(P, r, j) + kKeys - 1u) / kKeys); }
-__device__ __forceinline__ uint32_t row_tiles_of(const AttendParams &P, const Extent &r) { return (r.rows * P.G + kUnitRows - 1u) / kUnitRows; }
+__host__ __device__ __forceinline__ uint32_t most_of(const AttendParams &P, const Extent &r, uint32_t j) { return sees(P, r, (min((j + 1u) * kUnitRows, r.rows * P.G) - 1u) / P.G); }
+__host__ __device__ __forceinline__ uint32_t tiles_of(const AttendParams &P, const Extent &r, uint32_t j) { return max(1u, (most_of(P, r, j) + kKeys - 1u) / kKeys); }
+__host__ __device__ __forceinline__ uint32_t row_tiles_of(const AttendParams &P, const Extent &r) { return (r.rows * P.G + kUnitRows - 1u) / kUnitRows; }
 
 // A unit's place in the list is its tiles and kStart before them, which is about what its start and end cost (rows in, the first
 // tile and those at the diagonal the careful way, rows out).
@@ -88,20 +88,20 @@ struct Cursor {
     Extent r;
     uint32_t total;               // tiles of the unit
     uint32_t first, count, taken; // taken: places of the share
-    __device__ __forceinline__ Cursor(const AttendParams &P_, const Place &start) : P(P_), p(start) { enter(); }
-    __device__ __forceinline__ void enter() {
+    __host__ __device__ __forceinline__ Cursor(const AttendParams &P_, const Place &start) : P(P_), p(start) { enter(); }
+    __host__ __device__ __forceinline__ void enter() {
         if (!p.left) return;
-        for (;; ++p.b, p.j = 0) {                         // (p.left: there is one)
-            r = extent_of(P.q, p.b);
-            if (p.j < row_tiles_of(P, r)) break;
+        for (;; ++p.b, p.j = 0) {                         // (p.left: there is one, unless somebody writes the lengths during the call: then a unit
+            r = extent_of(P.q, p.b);                      // without rows at the last request, which the warp of the scales reports)
+            if (p.j < row_tiles_of(P, r) || p.b + 1u >= P.q.B) break;
         }
         total = tiles_of(P, r, p.j);
         taken = P.workspace ? min(total + kStart - p.off, p.left) : total + kStart;
         first = max(p.off, kStart) - kStart;
         count = max(p.off + taken, kStart) - kStart - first;
     }
-    __device__ __forceinline__ bool more() const { return p.left != 0; }
-    __device__ __forceinline__ void next() {
+    __host__ __device__ __forceinline__ bool more() const { return p.left != 0; }
+    __host__ __device__ __forceinline__ void next() {
         p.left -= min(p.left, taken);
         p.at += taken;
         p.off = 0;
@@ -109,11 +109,11 @@ struct Cursor {
         enter();
     }
     // tiles that take part in products (none where no row sees a token)
-    __device__ __forceinline__ uint32_t products() const { return most_of(P, r, p.j) ? count : 0u; }
-    __device__ __forceinline__ uint32_t row0() const { return p.j * kUnitRows; }
+    __host__ __device__ __forceinline__ uint32_t products() const { return most_of(P, r, p.j) ? count : 0u; }
+    __host__ __device__ __forceinline__ uint32_t row0() const { return p.j * kUnitRows; }
     // a unit of up to 128 rows has one tile of rows: nothing is done for the other
-    __device__ __forceinline__ bool both() const { return row0() + kUnitRows / 2u < r.rows * P.G; }
-    __device__ __forceinline__ uint32_t least() const { return sees(P, r, row0() / P.G); }
+    __host__ __device__ __forceinline__ bool both() const { return row0() + kUnitRows / 2u < r.rows * P.G; }
+    __host__ __device__ __forceinline__ uint32_t least() const { return sees(P, r, row0() / P.G); }
 };
 
 template <class E, uint32_t D>
@@ -192,7 +192,11 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                     break;
                 }
                 before += __shfl_sync(0xFFFFFFFFu, inc, 31);
-                if (j0 >= row_tiles_of(P, r)) { p.left = 0; break; }         // (never)
+                if (j0 >= row_tiles_of(P, r)) {           // (see Cursor::enter)
+                    p.left = 0;
+                    if (lane == 0) atomicOr(&g_prompts_status, unsigned(kStatusPage));
+                    break;
+                }
             }
         }
         if (lane == 0) *start = p;
@@ -300,6 +304,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
             // of groups of 16 tokens, lane = group: the page of tile i + 2 and the scales of tile i + 1 are on their way while tile i's are written
             for (Cursor x(P, begin); x.more() && ok; x.next()) {
                 const uint32_t tiles = x.products(), t_first = x.first * kKeys;
+                if (lane == 0 && x.row0() >= x.r.rows * P.G) atomicOr(&g_prompts_status, unsigned(kStatusPage));       // (see Cursor::enter)
                 if (tiles == 0) continue;
                 const int32_t *table = P.q.table + int64_t(x.p.b) * P.q.ldt;
                 const float vs_first = first_scale(P.q, P.vs, x.p.b, x.p.h), per_first = __frcp_rn(vs_first);

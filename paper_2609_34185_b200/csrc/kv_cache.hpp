@@ -17,10 +17,17 @@ struct Requests {
 };
 // rows and tokens of request b; whatever the arrays hold, rows lie inside the call's and tokens inside the table
 struct Extent { uint32_t row, rows, len; };
-__device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
-    const uint32_t lo = uint32_t(min(max(__ldg(q.starts + b), 0), int32_t(q.N))), hi = uint32_t(min(max(__ldg(q.starts + b + 1), int32_t(lo)), int32_t(q.N)));
+__host__ __device__ __forceinline__ int32_t entry_of(const int32_t *p) {
+#ifdef __CUDA_ARCH__
+    return __ldg(p);
+#else
+    return *p;
+#endif
+}
+__host__ __device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t b) {
+    const uint32_t lo = uint32_t(min(max(entry_of(q.starts + b), 0), int32_t(q.N))), hi = uint32_t(min(max(entry_of(q.starts + b + 1), int32_t(lo)), int32_t(q.N)));
     const uint64_t room = uint64_t(q.columns) << q.shift;
-    return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(__ldg(q.seq_lens + b), 0))), room))};
+    return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(entry_of(q.seq_lens + b), 0))), room))};
 }
 
 // The softmax's weights carry the pages' value scales, as ratios to that of the request's first page: t = score + log2(ratio), and a row's sum
