@@ -330,8 +330,8 @@ int ep_fp8_matmul(const ep_matmul_job *job, void *stream);
 typedef struct {
     void *d_k, *d_v;                    /* [pages][heads][page][dim] E4M3; 16-byte aligned */
     float *d_k_scales, *d_v_scales;     /* [pages][heads]; finite and >= 0 wherever a token lies; value scales of a request's
-                                           pages at most 2^40 times its first page's (but for a first page of
-                                           zeros), those below 2^-60 of it count as that */
+                                           pages at most 2^40 times that of its first page above 2^-100 (pages
+                                           of zeros are not), those below 2^-60 of it count as that */
     uint32_t pages, heads, page, dim;   /* page: tokens of a page, 16, 32, 64, 128 or 256; dim: 64 or 128;
                                            pages * heads * page < 2^31 - 256 */
 } ep_cache;

@@ -24,7 +24,7 @@ __device__ unsigned int g_prompts_status = 0;
 // (Warps 14 and 15 have nothing to do: registers go from one group of four warps to another.)
 // The running maximum is a reference m: it moves, and the accumulator in tensor memory is scaled, only when a score exceeds it by more
 // than 2^8; weights are 2^(t - m + 7), so at most 2^15, inside binary16.  A page's value scale is taken into the exponent,
-// t = score + log2(v_scale / the request's first), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
+// t = score + log2(v_scale / one page's of the request), and out of the row's sum again.  (Weights made in one pass, in registers, with a check of their sums
 // instead of the maximum first: 379 -> 462 us.  The two warps of a scheduler taking turns at the exponentials: 336 -> 360.  The next scores asked
 // for before the weights are out: 311 -> 325.  A quarter of the exponentials as polynomials beside the unit: 311 -> 314, half: 335.)
 // The loops are short on purpose: three roles run side by side, and what they execute over and over has to fit the SM's instruction
@@ -307,7 +307,7 @@ __global__ void __launch_bounds__(kThreads, 1) prompts_kernel(const __grid_const
                 if (lane == 0 && x.row0() >= x.r.rows * P.G) atomicOr(&g_prompts_status, unsigned(kStatusPage));       // (see Cursor::enter)
                 if (tiles == 0) continue;
                 const int32_t *table = P.q.table + int64_t(x.p.b) * P.q.ldt;
-                const float vs_first = first_scale(P.q, P.vs, x.p.b, x.p.h), per_first = __frcp_rn(vs_first);
+                const float vs_first = first_scale(P.q, P.vs, x.p.b, x.p.h, x.r.len), per_first = __frcp_rn(vs_first);
                 auto page_at = [&](uint32_t i) {          // -1: no token, or (reported by the warps that bring it in) no page
                     const uint32_t t = t_first + i * kKeys + 16u * lane;
                     const int32_t id = lane < 8 && i < tiles && t < x.r.len ? __ldg(table + (t >> P.q.shift)) : -1;

@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(128) append_kernel(const __grid_constant__ App
 // handful of rows fills N = 8, where along M they would be half padding, with twice the scores, accumulators and instructions.
 // A row of q becomes binary16 times a power of two that puts its largest magnitude at 2^13: exact for binary16 and bfloat16 alike but for elements 2^-27 and
 // more below the row's largest, whose rounding is below fp32's own.  A page's value scale is taken into the exponent, t = score +
-// log2(v_scale / the request's first), and out of the row's sum again.  The reference m of a row moves, and its accumulators with it, only when some t exceeds it by
+// log2(v_scale / one page's of the request), and out of the row's sum again.  The reference m of a row moves, and its accumulators with it, only when some t exceeds it by
 // more than 8; weights are 2^(t - m + 7): at most 2^15, and down to 2^-21 of what m stands for with 11 bits.
 // ======================================================================================================================
 constexpr uint32_t kTile = 32, kUnit = 256;
@@ -286,7 +286,7 @@ __global__ void __launch_bounds__(32 * W, 1) attend_kernel(const __grid_constant
             __syncwarp();
             ++issued;
         };
-        const float vs_first = first_scale(P.q, P.vs, b, h), per_first = __frcp_rn(vs_first);
+        const float vs_first = first_scale(P.q, P.vs, b, h, r.len), per_first = __frcp_rn(vs_first);
         int32_t next_page = page_of(0);
         uint32_t asked = 0;
 #pragma unroll 1

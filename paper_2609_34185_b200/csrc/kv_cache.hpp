@@ -30,16 +30,30 @@ __host__ __device__ __forceinline__ Extent extent_of(const Requests &q, uint32_t
     return {lo, hi - lo, uint32_t(min(uint64_t(uint32_t(max(entry_of(q.seq_lens + b), 0))), room))};
 }
 
-// The softmax's weights carry the pages' value scales, as ratios to that of the request's first page: t = score + log2(ratio), and a row's sum
-// takes them out again.  What such a weight would lose below fp32's range is lost to the sum, so ratios stop at 2^-60: the values
-// of a page further below (zeros, as append leaves them with 2^-100) then count as up to 2^-51 of the first page's largest, less than
-// fp32 resolves, and weights keep 2^-30 of the largest for pages of up to 2^40 times the first one's scale.
+// The softmax's weights carry the pages' value scales, as ratios to one page's of the request: t = score + log2(ratio), and a row's sum
+// takes them out again.  That page is the first one that is more than zeros (append leaves those with 2^-100, and a ratio to that would leave fp32's
+// range).  What a weight would lose below fp32's range is lost to the sum, so ratios stop at 2^-60: the values of a page further below (zeros
+// again) then count as up to 2^-51 of that page's largest, less than fp32 resolves, and weights keep 2^-30 of the largest for pages of
+// up to 2^40 times that one's scale.
 constexpr float kLeastRatio = 0x1p-60f;
-// the value scale of the request's first page; 1 where there is none
-__device__ __forceinline__ float first_scale(const Requests &q, const float *vs, uint32_t b, uint32_t h) {
-    const int32_t id = __ldg(q.table + int64_t(b) * q.ldt);
-    const float v = uint32_t(id) < q.pages ? __ldg(vs + size_t(uint32_t(id)) * q.H + h) : 1.0f;
-    return v > 0x1p-120f && v < 0x1p120f ? v : 1.0f;
+// the value scale that ratios refer to: of the first page above 2^-100 (and below 2^120), else of the first page, else 1; by a whole warp
+__device__ __forceinline__ float first_scale(const Requests &q, const float *vs, uint32_t b, uint32_t h, uint32_t len) {
+    const int32_t *row = q.table + int64_t(b) * q.ldt;
+    auto scale_at = [&](uint32_t j) {
+        const int32_t id = __ldg(row + j);
+        return uint32_t(id) < q.pages ? __ldg(vs + size_t(uint32_t(id)) * q.H + h) : 0.0f;
+    };
+    auto serves = [](float v, float least) { return v > least && v < 0x1p120f; };
+    const float v = scale_at(0);
+    if (serves(v, 0x1p-100f)) return v;
+    const uint32_t lane = threadIdx.x & 31u, n = (len + q.page - 1u) >> q.shift;
+#pragma unroll 1
+    for (uint32_t j = 0; j < n; j += 32u) {
+        const float other = j + lane < n ? scale_at(j + lane) : 0.0f;
+        const uint32_t found = __ballot_sync(0xFFFFFFFFu, serves(other, 0x1p-100f));
+        if (found) return __shfl_sync(0xFFFFFFFFu, other, __ffs(int(found)) - 1);
+    }
+    return serves(v, 0x1p-120f) ? v : 1.0f;
 }
 
 // ---- softmax in powers of two -------------------------------------------------------------------------------------------

@@ -666,6 +666,27 @@ def test_attention_scales_at_their_limits(news):
 
 
 @gpu
+@pytest.mark.parametrize("news", [[1, 1, 1], [70, 90, 3]])
+@pytest.mark.parametrize("zeros,large", [(1, 2.0 ** 20), (1, 2.0 ** 60), (3, 2.0 ** 100), (35, 2.0 ** 60), (1, 2.0 ** -70)])
+def test_attention_first_pages_of_zeros(news, zeros, large):
+    # pages of zeros as append leaves them, then values that their scale of 2^-100 is no measure for; a long request whose work CTAs share; one of zeros alone
+    G, H, page, lens, starts = 4, 2, 16, [16 * zeros + 150, 9000, 130], offsets(news)
+    cache, table = filled(lens, H, 128, page, seed=29)
+    for b, n in enumerate((zeros, zeros, len(table[2]))):
+        for i in table[b][:n]:
+            cache.v_scales[i] = 2.0 ** -100
+            cache.v.view(torch.uint8)[i] = 0
+        for j, i in enumerate(table[b][n:-(-lens[b] // page)]):
+            cache.v_scales[i] = min(large * 2.0 ** ((0, 7, -30, 40)[j % 4]), 2.0 ** 110)
+    q = torch.randn(starts[-1], G * H, 128, generator=cuda(3), device="cuda").to(torch.bfloat16)
+    out = ep.cache_attention(q, cache, ints(table), ints(lens), ints(starts))
+    want, bound, _ = attended(q, cache, table, lens, starts, 128 ** -0.5, True)
+    up = max(1.0, 1 / large)                              # (the bound's last term is an absolute one)
+    check_attention(out * up, want * up, (bound + 1e-7 * bound.amax(2, keepdim=True)) * up)
+    assert bool((out[starts[2]:] == 0).all()) and ep.last_device_status() == 0
+
+
+@gpu
 def test_two_graphs_at_once_with_their_own_workspaces():
     lens = [2000, 700]
     cache, table = filled(lens, 4, 128, 64, seed=5)
