@@ -502,13 +502,13 @@ def kv_cache(pages: int, heads: int, dim: int, page: int = 64, device="cuda") ->
 
 def _matrix(t, dtype, shape, dev, what):
     """Distance between the rows of a [T, C] tensor on device `dev` with contiguous rows; of a single row, whose stride means
-    nothing, at least its length."""
+    nothing, its length as a multiple of 16 (which the copy engine asks for)."""
     if t.dtype != dtype or t.shape != shape or t.get_device() != dev:
         raise ValueError(f"{what} must be {dtype} {list(shape)} on the operands' CUDA device")
     ld, one = t.stride()
     if one != 1 and shape[1] > 1:
         raise ValueError(f"rows of {what} must be contiguous")
-    return ld if shape[0] > 1 or ld > shape[1] else shape[1]
+    return ld if shape[0] > 1 else shape[1] + 15 & ~15
 
 
 def quantize_blocks(x, block_rows: int = 1, out=None, stream=None):
@@ -585,13 +585,14 @@ def _cache_and_requests(cache, table, seq_lens, starts, N):
 
 
 def _heads(t, dtype, shape, dev, what):
-    """Distances between rows and between heads of [N, heads, dim] whose heads are contiguous."""
+    """Distances between rows and between heads of [N, heads, dim] whose heads are contiguous; 0 where there is only one, whose stride
+    means nothing."""
     if t.dtype != dtype or t.shape != shape or t.get_device() != dev:
         raise ValueError(f"{what} must be {dtype} {list(shape)} on the cache's CUDA device")
     row, head, one = t.stride()
     if one != 1:
         raise ValueError(f"heads of {what} must be contiguous")
-    return row, head
+    return row if shape[0] > 1 else 0, head if shape[1] > 1 else 0
 
 
 def cache_append(cache, k, v, table, seq_lens, starts, stream=None) -> None:

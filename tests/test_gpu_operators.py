@@ -687,6 +687,37 @@ def test_attention_first_pages_of_zeros(news, zeros, large):
 
 
 @gpu
+def test_one_token_with_strides_that_mean_nothing():
+    # a row of something turned round, and of buffers with odd rows
+    H, G, D, C = 2, 4, 64, 256
+    turned = lambda n, seed: torch.randn(n * D, generator=cuda(seed), device="cuda").to(torch.bfloat16).as_strided((1, n, D), (1, D, 1))  # noqa: E731
+    k, v, q = turned(H, 1), turned(H, 2), turned(H * G, 3)
+    assert k.stride(0) == 1
+    caches = [filled([70], H, D, 32, seed=6) for _ in range(2)]
+    got = []
+    for (cache, table), copy in zip(caches, (lambda t: t, lambda t: t.flatten().clone().view(t.shape))):
+        t, sl, st = ints(table), ints([70]), ints([0, 1])
+        ep.cache_append(cache, copy(k), copy(v), t, sl, st)
+        out = torch.empty(H * G * D, dtype=torch.bfloat16, device="cuda").as_strided((1, H * G, D), (1, D, 1))
+        got.append((cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scales, ep.cache_attention(copy(q), cache, t, sl, st, out=out)))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    one = torch.randn(3, D, generator=cuda(4), device="cuda").to(torch.bfloat16)                      # one head: its stride means nothing either
+    cache, table = filled([70], 1, D, 32, seed=7)
+    odd = torch.zeros(3, 1, D + 8, dtype=torch.bfloat16, device="cuda").as_strided((3, 1, D), (D + 8, 3, 1))
+    odd.copy_(one[:, None])
+    a = ep.cache_attention(odd, cache, ints(table), ints([70]), ints([0, 3]))
+    assert torch.equal(a, ep.cache_attention(one[:, None], cache, ints(table), ints([70]), ints([0, 3])))
+    xb, wq = torch.randn(4, C + 24, generator=cuda(5), device="cuda"), ep.quantize_blocks(torch.randn(50, C, generator=cuda(6), device="cuda"), 128)
+    xq = torch.zeros(4, C + 24, dtype=torch.uint8, device="cuda").view(E4M3)[:1, :C]
+    xs = torch.zeros(2, 1, dtype=torch.uint8, device="cuda").view(E8M0).t()
+    ep.quantize_blocks(xb[:1, :C], out=(xq, xs))
+    y = torch.zeros(50, 1, device="cuda").t()
+    ep.fp8_matmul(xq, xs, *wq, out=y)
+    check_product(y, *product(xq, xs, *wq), C)
+    assert ep.last_device_status() == 0
+
+
+@gpu
 def test_two_graphs_at_once_with_their_own_workspaces():
     lens = [2000, 700]
     cache, table = filled(lens, 4, 128, 64, seed=5)

@@ -2,6 +2,10 @@
 import os
 import subprocess
 
+import torch
+
+import paper_2609_34185_b200 as ep
+
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 CSRC = os.path.join(ROOT, "paper_2609_34185_b200", "csrc")
 
@@ -22,3 +26,15 @@ def test_the_list_of_requests_is_their_running_sum(tmp_path):
 def test_shares_of_prompts_take_every_tile_once_and_end_with_the_requests(tmp_path):
     program = _program(tmp_path, "prompt_shares.cu", os.path.join(CSRC, "stream.cpp"))
     assert subprocess.run([program], check=True, capture_output=True, text=True, timeout=300).stdout.split() == ["96", "0", "0", "0"]
+
+
+def test_strides_of_a_single_row_or_head_mean_nothing():
+    # a step of one token comes out of products and slices with whatever stride: only what lies between rows that exist counts
+    heads, matrix, bf = ep.binding._heads, ep.binding._matrix, torch.bfloat16
+    one = torch.zeros(128, dtype=bf).as_strided((1, 2, 64), (1, 64, 1))
+    assert one.stride() == (1, 64, 1) and heads(one, bf, one.shape, -1, "k") == (0, 64)
+    single = torch.zeros(9, 67, dtype=bf)[:, None, :64]
+    assert single.stride() == (67, 67, 1) and heads(single, bf, single.shape, -1, "k") == (67, 0)
+    assert heads(torch.zeros(3, 2, 72, dtype=bf)[:, :, :64], bf, (3, 2, 64), -1, "k") == (144, 72)
+    for t, ld in ((torch.zeros(5, 264)[:1, :256], 256), (torch.zeros(256, 1).t(), 256), (torch.zeros(1, 100), 112), (torch.zeros(0, 48), 48), (torch.zeros(5, 264)[:2, :256], 264)):
+        assert matrix(t, torch.float32, t.shape, -1, "x") == ld
