@@ -127,7 +127,7 @@ extern "C" const char *ep_strerror(int status) {
     case EP_ERR_NOMEM: return "out of host memory";
     case EP_ERR_SCRATCH: return "scratch buffer missing, misaligned or too small";
     case EP_ERR_STATIC_LIMIT: return "stream needs lookup tables larger than the built-in area (b above EP_STATIC_MAX_B)";
-    case EP_ERR_BAD_PAGE: return "page number outside the cache";
+    case EP_ERR_BAD_PAGE: return "page number outside the cache, or rows that several requests claim";
     default: return "unknown status";
     }
 }

@@ -18,7 +18,7 @@ constexpr uint32_t kDecodeTilesPerCta = 32;  // tiles one CTA of the decode kern
 
 // Device-side integrity words of the operators' translation units: each gives a function that reads its word (bits below),
 // clears it if it is set and returns it, negative on a CUDA error.  ep_last_device_status asks all of them.
-enum { kStatusWait = 1, kStatusPage = 2 };       // a wait ran out; a page number outside the cache
+enum { kStatusWait = 1, kStatusPage = 2 };       // a wait ran out; a page number outside the cache, or rows that several requests claim
 bool add_status_word(int (*read)());
 int read_status_words();
 

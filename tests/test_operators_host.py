@@ -38,3 +38,7 @@ def test_strides_of_a_single_row_or_head_mean_nothing():
     assert heads(torch.zeros(3, 2, 72, dtype=bf)[:, :, :64], bf, (3, 2, 64), -1, "k") == (144, 72)
     for t, ld in ((torch.zeros(5, 264)[:1, :256], 256), (torch.zeros(256, 1).t(), 256), (torch.zeros(1, 100), 112), (torch.zeros(0, 48), 48), (torch.zeros(5, 264)[:2, :256], 264)):
         assert matrix(t, torch.float32, t.shape, -1, "x") == ld
+
+
+def test_the_status_of_bad_pages_names_both_its_causes():
+    assert "page number outside the cache" in ep.strerror(-9) and "several requests" in ep.strerror(-9)
