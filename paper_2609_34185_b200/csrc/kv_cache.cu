@@ -735,10 +735,10 @@ extern "C" int ep_cache_attention(const ep_attention_job *job, void *stream) {
     P.scale_log2 = j.scale * 1.4426950408889634f;
     P.causal = j.causal ? 1u : 0u;
     P.workspace = static_cast<float *>(j.d_workspace);
-    // units (of 256 tokens here, of 128 for prompts) are counted in 32 bits
-    const uint64_t rows = 8u * row_tiles(N, P.G, B),
-                   units = ((uint64_t(P.q.columns) * c.page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B) * c.heads;
-    if (units >= (1ull << 30) || uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
+    // units (of 256 tokens here, of 128 for prompts) are counted in 32 bits; their number can pass 64 on the way
+    if (uint64_t(N) * P.G >= (1ull << 31)) return EP_ERR_UNSUPPORTED;
+    const uint64_t rows = 8u * row_tiles(N, P.G, B), per_head = ((uint64_t(P.q.columns) * c.page + kUnit - 1u) / kUnit) * ((uint64_t(N) * P.G + rows - 1u) / rows + B), units = per_head * c.heads;
+    if (per_head >= (1ull << 30) || units >= (1ull << 30)) return EP_ERR_UNSUPPORTED;
     const int sms = op_sms();
     if (sms <= 0) return EP_ERR_CUDA;
     P.grid = std::min(uint32_t(sms), kMostPieces);

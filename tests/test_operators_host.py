@@ -42,3 +42,12 @@ def test_strides_of_a_single_row_or_head_mean_nothing():
 
 def test_the_status_of_bad_pages_names_both_its_causes():
     assert "page number outside the cache" in ep.strerror(-9) and "several requests" in ep.strerror(-9)
+
+
+def test_work_beyond_64_bits_is_refused():
+    # 2^22 units of tokens x 2^27 tiles of rows x 2^15 heads are 2^64 pieces of work, which 64 bits hold as none
+    p = 1 << 20                                           # an address that is never read
+    job = lambda N, heads, columns: ep.binding.ATTENTION_JOB.pack(p, p, p, p, 1, heads, 16, 64, p, p, p, columns, columns, 1, N, p, p, 0, p, 1 << 40, 64, 64, 64, 64, 1.0, heads, ep.BF16, 1)  # noqa: E731
+    assert ep.load().ep_cache_attention(job(2 ** 31 - 16, 2 ** 15, 2 ** 26), None) == -3
+    assert ep.load().ep_cache_attention(job(2 ** 31 - 1, 2 ** 15, 2 ** 26), None) == -3
+    assert ep.load().ep_cache_attention(job(2 ** 31 - 1, 1, 2 ** 8), None) == -3
