@@ -718,6 +718,30 @@ def test_one_token_with_strides_that_mean_nothing():
 
 
 @gpu
+@pytest.mark.parametrize("B,H,G,D,page,steps,new", [(150, 8, 1, 64, 16, 40, 1), (16, 8, 4, 128, 32, 30, 7)])
+def test_steps_one_behind_another_need_no_wait(B, H, G, D, page, steps, new):
+    # each call may come up while the one before still runs: pages and scales that one step writes are read by the next on other SMs
+    table, pages = paged([steps * new] * B, page, seed=B)
+    t, st, g = ints(table), ints([i * new for i in range(B + 1)]), cuda(B)
+    lens = [ints([(i + 1) * new] * B) for i in range(steps)]
+    x = [(torch.randn(B * new, H, D, generator=g, device="cuda") * 2.0 ** (i / 6)).to(torch.bfloat16) for i in range(steps)]       # (so that scales grow)
+    q = torch.randn(B * new, G * H, D, generator=g, device="cuda").to(torch.bfloat16)
+    got = []
+    for wait in (True, False):
+        cache, outs = ep.kv_cache(pages, H, D, page), []
+        for i in range(steps):
+            ep.cache_append(cache, x[i], x[i], t, lens[i], st)
+            if wait:
+                torch.cuda.synchronize()
+            outs.append(ep.cache_attention(q, cache, t, lens[i], st))
+            if wait:
+                torch.cuda.synchronize()
+        got.append(outs + [cache.k.view(torch.uint8), cache.v.view(torch.uint8), cache.k_scales, cache.v_scales])
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(*got)) and ep.last_device_status() == 0
+
+
+@gpu
 def test_two_graphs_at_once_with_their_own_workspaces():
     lens = [2000, 700]
     cache, table = filled(lens, 4, 128, 64, seed=5)
