@@ -352,8 +352,8 @@ typedef struct {
 } ep_requests;
 
 /* Writes the call's rows to the cache.  A page's scale only grows while the page fills: s' = max(s, the smallest power of two
- * that holds the new tokens); where it grows the older tokens become e4m3(q s / s').  A page without older tokens gets the new
- * tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request
+ * that holds the new tokens, at least 2^-100); where it grows the older tokens become e4m3(q s / s').  A page without older tokens
+ * gets the new tokens' scale (2^-100 if they are all 0).  What is not finite becomes NaN and has no part in the scale.  A row of a request
  * that has fewer tokens than rows is passed over, from the first on.
  * A page that a call writes must belong to one request only and stand in its table once; pages that are full may be shared. */
 typedef struct {
@@ -368,9 +368,11 @@ int ep_cache_append(const ep_append_job *job, void *stream);
 
 /* o = softmax(scale q K^T) V, the softmax over all tokens of the row's request or (causal) over tokens 0 .. len - n + i for row
  * i of its n.  Query head g belongs to head g / (q_heads / heads) of the cache.  A row that sees no token, or only scores of -infinity,
- * gives 0 (and -infinity in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values;
- * a token's values count only for rows that see it.  EP_ERR_UNSUPPORTED for B > 4096, and for calls that could come to 2^30
- * pieces of work: ceil(columns * page / 256) * (N * q_heads / heads / 8 + B) * heads. */
+ * gives 0 (and -infinity in d_lse).  Scores, sums and outputs are kept in fp32, the softmax's weights are rounded to 11 bits before they multiply the values
+ * (which moves an output by some 1.4e-4 of itself, a twelfth of what rounding it to bfloat16 does); a token's values count only
+ * for rows that see it.  EP_ERR_UNSUPPORTED for B > 4096, for N * q_heads / heads >= 2^31, and for calls that could come to 2^30 pieces of
+ * work: ceil(columns * page / 256) * (ceil(N * q_heads / heads / n) + B) * heads, n = 8 up to 8 rows (N * q_heads / heads / B) per request and
+ * head, else 16. */
 typedef struct {
     ep_cache cache;
     ep_requests requests;
