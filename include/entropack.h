@@ -391,6 +391,96 @@ typedef struct {
 size_t ep_cache_attention_workspace_bytes(uint32_t N, uint32_t B, uint32_t q_heads, uint32_t heads, uint32_t dim);
 int ep_cache_attention(const ep_attention_job *job, void *stream);
 
+/* The INT8 route.  A row x of T x C becomes whole numbers q and one scale s: m = max(max_j |x[j]|, 2^-119), s = m / 127,
+ * q[j] = x[j] * (127 / m) rounded to the nearest whole number, ties to even, each operation in fp32 (so |q| <= 127).  A row of zeros has s = 1;
+ * a row with a value that is not finite has q = 0 and s = NaN, so that its products are NaN.  Rows are the tokens of activations, or
+ * the channels of a weight. */
+typedef struct {
+    const void *d_x;            /* device: T x C of x_dtype, ldx >= C; aligned to its element (rows that begin on 16 bytes are read fastest) */
+    void *d_q;                  /* device: T x C int8, ldq >= C */
+    float *d_scales;            /* device: T floats */
+    int64_t ldx, ldq;
+    uint32_t T, C;
+    int32_t x_dtype;            /* EP_BF16, EP_FP16 or EP_FP32 */
+} ep_quantize_rows_job;
+int ep_quantize_rows(const ep_quantize_rows_job *job, void *stream);
+
+/* y[t, r] = a[r] (s[t] sum_k xq[t, k] wq[r, k]) + bias[r]: the sum over whole numbers in 32 bits on the tensor cores, exact, then rounded to fp32;
+ * scales and bias in fp32; one rounding to out_dtype (EP_FP16 overflows to infinity).  The operands may hold all of -128 .. 127.
+ * The copy engine reads the operands: d_x and d_w on 16 bytes, C, ldx and ldw multiples of 16, and C < 2^17 (128 * 128 * C < 2^31), else
+ * EP_ERR_UNSUPPORTED.  A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
+typedef struct {
+    const void *d_x;                /* device: T x C int8, as ep_quantize_rows leaves them */
+    const float *d_x_scales;        /* device: T floats s[t] */
+    const void *d_w;                /* device: R x C int8: a weight decoded to EP_INT8, or one of ep_quantize_rows */
+    const float *d_row_scales;      /* device: R floats a[r], or NULL: ones */
+    const float *d_bias;            /* device: R floats, or NULL: zeros */
+    void *d_y;                      /* device: T x R of out_dtype, aligned to its element, ldy >= R */
+    int64_t ldx, ldw, ldy;
+    uint32_t T, R, C;
+    int32_t out_dtype;              /* EP_BF16, EP_FP16 or EP_FP32 */
+} ep_int8_matmul_job;
+int ep_int8_matmul(const ep_int8_matmul_job *job, void *stream);
+
+/* A vector of C values that rows are multiplied by or to which they are added: one for all rows (groups = 1), or one for each of `groups`
+ * groups of T / groups rows that follow one another (the gate, scale and shift of each sample of a batch; groups = T: of each row). */
+typedef struct {
+    const void *d;                  /* device: groups x C of dtype, aligned to its element; NULL: not there */
+    int64_t ld;                     /* between the groups' vectors */
+    uint32_t groups;                /* divides T */
+    int32_t dtype;                  /* EP_BF16, EP_FP16 or EP_FP32 */
+} ep_vector;
+
+/* What stands between two blocks of a model: the norm of the block that ended, its gate, the residual, the norm of the block that begins.
+ *     b = norm(x) * (o + post_weight)     with a post weight, else x
+ *     r = residual_scale * residual + gate * b     (without a residual: gate * b; without a gate: b)
+ *     z = norm(r) * (o + weight) + bias
+ * norm(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps), the mean taken as 0 unless `center`; o = weight_offset, 0 or 1 as the weights are
+ * stored (o + weight is 1 where there is no weight).  Everything is held in fp32, r too: it is rounded where it is written, not before z is computed.  z is
+ * rounded once: to a 16- or 32-bit type, to E4M3 with the scales of ep_quantize_blocks (block_rows 1), or to INT8 with the scale of ep_quantize_rows.
+ * C up to 32768, else EP_ERR_UNSUPPORTED.  d_residual_out may be d_residual, and d_z may be d_x
+ * (with the same type and ld): a row is read before it is written. */
+typedef struct {
+    const void *d_x;                /* device: T x C of x_dtype */
+    const void *d_residual;         /* device: T x C of residual_dtype, or NULL */
+    void *d_residual_out;           /* device: T x C of residual_dtype, r; or NULL: r is not written */
+    void *d_z;                      /* device: T x C of z_dtype */
+    void *d_z_scales;               /* device: EP_FP8_E4M3: T x ceil(C / 128) E8M0 bytes, ldz_scales apart; EP_INT8: T floats; else not used */
+    int64_t ldx, ld_residual, ld_residual_out, ldz, ldz_scales;
+    ep_vector weight, bias, gate, post_weight;
+    float residual_scale, weight_offset, eps;
+    uint32_t T, C;
+    int32_t x_dtype, residual_dtype;    /* EP_BF16, EP_FP16 or EP_FP32 */
+    int32_t z_dtype;                    /* one of these, EP_FP8_E4M3 or EP_INT8 */
+    int32_t center;
+} ep_norm_job;
+int ep_norm(const ep_norm_job *job, void *stream);
+
+/* Rotary positions: of each head's first 2 * pairs values, value i and value i + pairs (or, interleaved, 2 i and 2 i + 1) are a pair (u, v), which
+ * becomes factor * (u cos a - v sin a, v cos a + u sin a) for a = position * frequency[i]; the other values of the head stay.  The angle is kept as a
+ * fraction of a turn in 64 bits, so that it is as exact for the farthest position as the frequencies are; everything else is fp32, rounded once.  d_out may
+ * be d_x (with the same strides): the rotation is then in place. */
+typedef struct {
+    const void *d_x;                /* device: T x heads x dim of dtype */
+    void *d_out;                    /* device: the same */
+    const void *d_positions;        /* device: T whole numbers of 32 or 64 bits */
+    const double *d_frequencies;    /* device: `pairs` frequencies in radians per position, finite */
+    int64_t ldx, ldx_head, ldo, ldo_head;   /* between rows, between heads */
+    uint32_t T, heads, dim, pairs;  /* 1 <= pairs, 2 * pairs <= dim <= 1024, heads <= 65535 */
+    float factor;
+    int32_t dtype;                  /* EP_BF16, EP_FP16 or EP_FP32 */
+    int32_t position_bits;          /* 32 or 64 */
+    int32_t interleaved;
+} ep_rotary_job;
+int ep_rotary(const ep_rotary_job *job, void *stream);
+
+/* The frequencies of `pairs` pairs, out[i] = base^(-i / pairs) radians per position (host memory, no GPU needed), for a context that is `stretch` >= 1 times
+ * as long as the one of `original` positions that the model was trained on: a frequency that makes fewer than `slow` turns in that context is divided by
+ * stretch, one that makes more than `fast` stays, and between the two
+ *     out[i] = f (k + (1 - k) / stretch),   k = (original f / 2 pi - slow) / (fast - slow)
+ * With original = 0 every frequency is divided by stretch.  (Models stretched like this are usually run with factor = 0.1 ln(stretch) + 1.) */
+int ep_rotary_frequencies(uint32_t pairs, double base, double stretch, double original, double fast, double slow, double *out);
+
 /* Device-side integrity word (no counterpart in the paper; it uses the fact that the encoder of Eq. 17 starts
  * every state at 2^15, so a correct decode of Eq. 18 must end there).  The kernel ORs in a flag when a tile does
  * not end with every state at 2^15 and its word pointer at the next tile's offset (a damaged stream).  There is ONE

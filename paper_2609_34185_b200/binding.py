@@ -110,8 +110,9 @@ def load():
                                           C.c_void_p]
     L.ep_decode_gemm.argtypes = [C.POINTER(Info), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_uint32,
                                  C.c_void_p, C.c_void_p]
-    for f in (L.ep_quantize_blocks, L.ep_fp8_matmul, L.ep_cache_append, L.ep_cache_attention):
+    for f in (L.ep_quantize_blocks, L.ep_fp8_matmul, L.ep_cache_append, L.ep_cache_attention, L.ep_quantize_rows, L.ep_int8_matmul, L.ep_norm, L.ep_rotary):
         f.argtypes = [C.c_char_p, C.c_void_p]      # a job's bytes (see the *_JOB layouts), the stream
+    L.ep_rotary_frequencies.argtypes = [C.c_uint32] + [C.c_double] * 5 + [C.c_void_p]
     L.ep_cache_attention_workspace_bytes.restype = C.c_size_t
     L.ep_cache_attention_workspace_bytes.argtypes = [C.c_uint32] * 5
     L.ep_decode_batch.argtypes = [C.POINTER(DecodeJob), C.c_int32, C.c_void_p]
@@ -458,6 +459,10 @@ QUANTIZE_JOB = struct.Struct("@PPPqqqIIIi")
 MATMUL_JOB = struct.Struct("@PPPPPPqqqqqIIIi")
 APPEND_JOB = struct.Struct("@" + _CACHE + _REQUESTS + "PPqqqqixxxx")
 ATTENTION_JOB = struct.Struct("@" + _CACHE + _REQUESTS + "PPPPNqqqqfIii")
+QUANTIZE_ROWS_JOB = struct.Struct("@PPPqqIIixxxx")
+INT8_MATMUL_JOB = struct.Struct("@PPPPPPqqqIIIi")
+NORM_JOB = struct.Struct("@PPPPPqqqqq" + 4 * "PqIi" + "fffIIiiiixxxx")
+ROTARY_JOB = struct.Struct("@PPPPqqqqIIIIfiii")
 
 _types = None
 
@@ -643,4 +648,171 @@ def cache_attention(q, cache, table, seq_lens, starts, scale=None, causal: bool 
     job = ATTENTION_JOB.pack(*fields, q.data_ptr(), out.data_ptr(), at, room, size, *_heads(q, dtype, shape, dev, "q"), *_heads(out, dtype, shape, dev, "out"),
                              dim ** -0.5 if scale is None else scale, shape[1], code, 1 if causal else 0)
     _enqueue(load().ep_cache_attention, "ep_cache_attention", job, dev, stream)
+    return out
+
+
+def _floats(t, n, dev, what):
+    """Address of a contiguous float32 [n] on device `dev`; 0 for None."""
+    if t is None:
+        return 0
+    if t.dtype != _types[0].float32 or t.shape != (n,) or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{what} must be contiguous float32 [{n}] on the operands' CUDA device")
+    return t.data_ptr()
+
+
+def quantize_rows(x, out=None, stream=None):
+    """x [T, C] (bfloat16, float16 or float32) as INT8 values and one scale for each row - a token of activations, a channel of a weight:
+    (int8 [T, C], float32 [T]).  `out`: such a pair to fill.  See ep_quantize_rows."""
+    torch, _, _, codes, _ = _float8()
+    dtype, shape, dev = x.dtype, x.shape, x.get_device()
+    code = codes.get(dtype)
+    if code is None or len(shape) != 2 or dev < 0:
+        raise ValueError("x must be a CUDA matrix of bfloat16, float16 or float32")
+    T, Cc = shape
+    if out is None:
+        out = (_empty(shape, torch.int8, x.device, stream), _empty((T,), torch.float32, x.device, stream))
+    q, s = out
+    if s is None:
+        raise ValueError("out must be a pair of tensors")
+    job = QUANTIZE_ROWS_JOB.pack(x.data_ptr(), q.data_ptr(), _floats(s, T, dev, "out[1]"), _matrix(x, dtype, shape, dev, "x"), _matrix(q, torch.int8, shape, dev, "out[0]"),
+                                 T, Cc, code)
+    _enqueue(load().ep_quantize_rows, "ep_quantize_rows", job, dev, stream)
+    return out
+
+
+def int8_matmul(x, x_scales, w, row_scale=None, bias=None, out_dtype: int = BF16, out=None, stream=None):
+    """x [T, C] times w [R, C] transposed, both INT8, row t of x times x_scales[t], row r of w times row_scale[r] (None: ones), plus bias[r]
+    (None: zeros), all float32: [T, R] of out_dtype (BF16, FP16 or FP32), or `out`.  See ep_int8_matmul."""
+    torch, _, _, codes, _ = _float8()
+    xs, wsh, dev = x.shape, w.shape, x.get_device()
+    if len(xs) != 2 or len(wsh) != 2 or xs[1] != wsh[1] or dev < 0:
+        raise ValueError("x and w must be CUDA matrices of as many columns")
+    (T, Cc), R = xs, wsh[0]
+    if out is None:
+        if out_dtype not in (BF16, FP16, FP32):
+            raise ValueError("out_dtype must be BF16, FP16 or FP32")
+        out = _empty((T, R), _out_torch_dtype(out_dtype), x.device, stream)
+    dtype = out.dtype
+    code = codes.get(dtype)
+    if code is None:
+        raise ValueError("out must be bfloat16, float16 or float32")
+    if x_scales is None:
+        raise ValueError("x_scales must be float32 [T]")
+    i8 = torch.int8
+    job = INT8_MATMUL_JOB.pack(x.data_ptr(), _floats(x_scales, T, dev, "x_scales"), w.data_ptr(), _floats(row_scale, R, dev, "row_scale"), _floats(bias, R, dev, "bias"),
+                               out.data_ptr(), _matrix(x, i8, xs, dev, "x"), _matrix(w, i8, wsh, dev, "w"), _matrix(out, dtype, (T, R), dev, "out"), T, R, Cc, code)
+    _enqueue(load().ep_int8_matmul, "ep_int8_matmul", job, dev, stream)
+    return out
+
+
+def _vector(v, T, Cc, dev, what):
+    """The fields of an ep_vector: one vector of Cc values, or one for each of v.shape[0] groups of rows."""
+    if v is None:
+        return 0, 0, 0, 0
+    code, shape = _types[3].get(v.dtype), v.shape
+    if code is None or v.get_device() != dev or (shape != (Cc,) and (len(shape) != 2 or shape[1] != Cc or shape[0] == 0 or T % shape[0])):
+        raise ValueError(f"{what} must be bfloat16, float16 or float32 [{Cc}], or [groups, {Cc}] with groups that divide the {T} rows, on x's CUDA device")
+    if v.stride(-1) != 1 and Cc > 1:
+        raise ValueError(f"{what} must be contiguous along its values")
+    return v.data_ptr(), v.stride(0) if len(shape) == 2 and shape[0] > 1 else 0, shape[0] if len(shape) == 2 else 1, code
+
+
+def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, gate=None, post_weight=None, weight_offset: float = 0.0, eps: float = 1e-6,
+         center: bool = False, out_dtype: int | None = None, out=None, residual_out=None, stream=None):
+    """What stands between two blocks, for x [T, C], the output of the block that ended:
+
+        b = norm(x) * (weight_offset + post_weight)        (without a post_weight: x)
+        r = residual_scale * residual + gate * b           (without a residual: gate * b)
+        z = norm(r) * (weight_offset + weight) + bias      norm: by the root of the mean square, or (center) by mean and variance
+
+    weight, bias, gate, post_weight: [C], or [groups, C] for groups of T / groups rows that follow one another.  x, residual and the vectors
+    are of bfloat16, float16 or float32, each its own.  z is of x's type or of out_dtype (BF16, FP16, FP32; FP8_E4M3: the pair that quantize_blocks returns; INT8:
+    the pair of quantize_rows), or `out`.  Returns z, with a residual (z, r); residual_out: the tensor that r goes to, which may be `residual` itself;
+    False: r is not written, and z returned.  See ep_norm."""
+    torch, e4m3, e8m0, codes, _ = _float8()
+    dtype, shape, dev = x.dtype, x.shape, x.get_device()
+    code = codes.get(dtype)
+    if code is None or len(shape) != 2 or dev < 0:
+        raise ValueError("x must be a CUDA matrix of bfloat16, float16 or float32")
+    T, Cc = shape
+    if out is None:
+        if out_dtype is None:
+            out = _empty(shape, dtype, x.device, stream)
+        elif out_dtype == FP8_E4M3:
+            out = (_empty(shape, e4m3, x.device, stream), _empty((T, -(-Cc // 128)), e8m0, x.device, stream))
+        elif out_dtype == INT8:
+            out = (_empty(shape, torch.int8, x.device, stream), _empty((T,), torch.float32, x.device, stream))
+        elif out_dtype in (BF16, FP16, FP32):
+            out = _empty(shape, _out_torch_dtype(out_dtype), x.device, stream)
+        else:
+            raise ValueError("out_dtype must be BF16, FP16, FP32, FP8_E4M3 or INT8")
+    z, scales, ld_scales = out, 0, 0
+    if isinstance(out, (tuple, list)):
+        z, s = out
+        if z.dtype == e4m3:
+            scales, ld_scales = s.data_ptr(), _matrix(s, e8m0, (T, -(-Cc // 128)), dev, "out[1]")
+        elif s is not None:
+            scales = _floats(s, T, dev, "out[1]")
+        z_code = FP8_E4M3 if z.dtype == e4m3 else INT8 if z.dtype == torch.int8 and scales else None
+    else:
+        z_code = codes.get(z.dtype)
+    if z_code is None:
+        raise ValueError("out must be bfloat16, float16 or float32, or a pair of E4M3 or INT8 values and their scales")
+    h = ldh = r = ldr = r_code = 0
+    if residual is not None:
+        r_code = codes.get(residual.dtype)
+        if r_code is None:
+            raise ValueError("residual must be bfloat16, float16 or float32")
+        h, ldh = residual.data_ptr(), _matrix(residual, residual.dtype, shape, dev, "residual")
+        if residual_out is None:
+            residual_out = _empty(shape, residual.dtype, x.device, stream)
+    wanted = residual_out is not None and residual_out is not False
+    if wanted:
+        if residual is None:
+            r_code = codes.get(residual_out.dtype)
+            if r_code is None:
+                raise ValueError("residual_out must be bfloat16, float16 or float32")
+        r, ldr = residual_out.data_ptr(), _matrix(residual_out, residual_out.dtype if residual is None else residual.dtype, shape, dev, "residual_out")
+    job = NORM_JOB.pack(x.data_ptr(), h, r, z.data_ptr(), scales, _matrix(x, dtype, shape, dev, "x"), ldh, ldr, _matrix(z, z.dtype, shape, dev, "out"), ld_scales,
+                        *_vector(weight, T, Cc, dev, "weight"), *_vector(bias, T, Cc, dev, "bias"), *_vector(gate, T, Cc, dev, "gate"),
+                        *_vector(post_weight, T, Cc, dev, "post_weight"), residual_scale, weight_offset, eps, T, Cc, code, r_code, z_code, 1 if center else 0)
+    _enqueue(load().ep_norm, "ep_norm", job, dev, stream)
+    return (out, residual_out) if wanted else out
+
+
+def rotary_frequencies(dim: int, base: float = 10000.0, stretch: float = 1.0, original: float = 0.0, fast: float = 32.0, slow: float = 1.0, device="cuda"):
+    """The dim / 2 frequencies base^(-2 i / dim) in radians per position, float64 on `device`, for a context `stretch` times as long as the model was
+    trained for: with `original`, the length of that one, those that turn fewer than `slow` times in it are divided by stretch, those that turn more than `fast`
+    times stay, and it is shared out between; without, all are divided.  See ep_rotary_frequencies."""
+    torch = _torch()
+    if dim < 2 or dim % 2:
+        raise ValueError("dim must be even")
+    out = np.empty(dim // 2)
+    _check(load().ep_rotary_frequencies(dim // 2, float(base), float(stretch), float(original), float(fast), float(slow), out.ctypes.data), "ep_rotary_frequencies")
+    return torch.from_numpy(out).to(device)
+
+
+def rotary(x, positions, frequencies, interleaved: bool = False, factor: float = 1.0, out=None, stream=None):
+    """x [T, heads, dim] (bfloat16, float16 or float32) with pairs of each head's first 2 * len(frequencies) values turned by positions[t] *
+    frequencies[i]: values i and i + len(frequencies), or 2 i and 2 i + 1 if interleaved.  positions: int32 or int64 [T]; frequencies: float64, radians per
+    position (rotary_frequencies).  out: the same shape; x itself turns it in place.  See ep_rotary."""
+    torch, _, _, codes, i32 = _float8()
+    dtype, shape, dev = x.dtype, x.shape, x.get_device()
+    code = codes.get(dtype)
+    if code is None or len(shape) != 3 or dev < 0:
+        raise ValueError("x must be CUDA bfloat16, float16 or float32 [T, heads, dim]")
+    T, heads, dim = shape
+    bits = 32 if positions.dtype == i32 else 64 if positions.dtype == torch.int64 else 0
+    if not bits or positions.shape != (T,) or not positions.is_contiguous() or positions.get_device() != dev:
+        raise ValueError("positions must be contiguous int32 or int64 [T] on x's CUDA device")
+    if frequencies.dtype != torch.float64 or frequencies.dim() != 1 or not frequencies.is_contiguous() or frequencies.get_device() != dev:
+        raise ValueError("frequencies must be contiguous float64 on x's CUDA device")
+    pairs = frequencies.shape[0]
+    if pairs == 0 or 2 * pairs > dim:
+        raise ValueError("frequencies must be one for each pair of values that turns, at most half of dim")
+    if out is None:
+        out = _empty(shape, dtype, x.device, stream)
+    job = ROTARY_JOB.pack(x.data_ptr(), out.data_ptr(), positions.data_ptr(), frequencies.data_ptr(), *_heads(x, dtype, shape, dev, "x"), *_heads(out, dtype, shape, dev, "out"),
+                          T, heads, dim, pairs, factor, code, bits, 1 if interleaved else 0)
+    _enqueue(load().ep_rotary, "ep_rotary", job, dev, stream)
     return out

@@ -467,36 +467,6 @@ __device__ __forceinline__ void pair_copy_scales(uint32_t tmem, uint32_t addr, u
     asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;\n\t}"
                  ::"r"(tmem), "l"(scales_desc(addr)), "r"(lead) : "memory");
 }
-// arrives at this barrier in both CTAs when what was issued before is done
-__device__ __forceinline__ void pair_commit(uint32_t bar, uint32_t lead) {
-    asm volatile("{\n\t.reg .pred q;\n\t.reg .b16 m;\n\tmov.b16 m, 3;\n\tsetp.ne.b32 q, %1, 0;\n\t"
-                 "@q tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], m;\n\t}" ::"r"(bar), "r"(lead) : "memory");
-}
-// at the first CTA's barrier
-__device__ __forceinline__ void first_arrive(uint32_t bar) {
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, 0;\n\tmbarrier.arrive.release.cluster.shared::cluster.b64 _, [a];\n\t}" ::"r"(bar) : "memory");
-}
-__device__ __forceinline__ void cluster_sync() { asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory"); }
-// a wait that sees what the other CTA wrote before it arrived (bar_wait_warp, acquired from the cluster)
-__device__ __forceinline__ bool pair_wait_warp(uint32_t bar, uint32_t parity, uint32_t abort_word) {
-    bool ok = false;
-#pragma unroll 1
-    for (uint32_t i = 0; i < kOpSpinLimit && !ok; ++i) {
-        uint32_t r;
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\tselp.u32 %0, 1, 0, p;\n\t}"
-                     : "=r"(r) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
-        ok = r != 0;
-        if (!ok && (i & 63u) == 63u && ld_smem(abort_word)) break;
-    }
-    if (!ok) st_smem(abort_word, 1u);
-    return __all_sync(0xFFFFFFFFu, ok);
-}
-// a load into this CTA's memory that reports to the first CTA's barrier
-__device__ __forceinline__ void pair_load_2d(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar) {
-    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %4, 0;\n\t"
-                 "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [a];\n\t}"
-                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
-}
 
 template <class E>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)

@@ -1,0 +1,243 @@
+// Rotary positions.
+#include <cmath>
+
+#include "op8.hpp"
+
+using namespace ep;
+
+namespace {
+
+constexpr uint32_t kTable = 1024;                // cosines and sines that a CTA holds
+
+// ======================================================================================================================
+// (u, v) -> f (u cos a - v sin a, v cos a + u sin a),   a = position * frequency[i]
+//
+// A far position times a frequency has more turns than 32 bits can hold beside the fraction that counts (200 000 radians in fp32 are
+// off by 0.008).  So a frequency is a fraction of a turn in 64 bits, whole numbers multiply it, and what passes 64 bits are whole turns, which fall
+// away by themselves: no reduction, and exact for positions of any size.  The fraction's first 32 bits then go to sincospi.
+// Bound by memory: a CTA works out its tokens' cosines and sines once, for all heads.
+// ======================================================================================================================
+struct RotaryParams {
+    const uint8_t *x;
+    uint8_t *o;
+    const void *positions;
+    const double *frequencies;
+    int64_t ldx, ldx_head, ldo, ldo_head;        // bytes
+    uint32_t T, heads, dim, pairs;
+    uint32_t tokens, parts;                      // tokens of a CTA; CTAs that share these tokens' heads
+    uint32_t per_head;                           // units of a head: pieces that turn (half layout: pairs of pieces), then pieces that stay
+    uint32_t turning;
+    uint32_t wide_positions;
+    float factor;
+};
+
+__device__ __forceinline__ uint64_t turn_fraction(double radians) {
+    double t = radians * 0.15915494309189533577;                                 // 1 / (2 pi)
+    t -= rint(t);
+    return uint64_t(__double2ll_rn(t * 18446744073709551616.0));
+}
+__device__ __forceinline__ float2 cosine_sine(int64_t position, uint64_t step, float factor) {
+    const int32_t fraction = int32_t(uint32_t((uint64_t(position) * step) >> 32));     // of a turn, in 2^-32, -1/2 .. 1/2
+    float s, c;
+    sincospif(float(fraction) * 4.656612873077393e-10f, &s, &c);                       // 2^-31: half turns
+    return make_float2(c * factor, s * factor);
+}
+
+// a piece of V values of type E: V * sizeof a power of two up to 16 bytes, read and written as one
+template <class E, uint32_t V>
+struct Piece {
+    using T = typename E::T;
+    static constexpr uint32_t kBytes = V * sizeof(T);
+    uint32_t w[kBytes < 4 ? 1 : kBytes / 4];
+    __device__ __forceinline__ void load(const uint8_t *p) {
+        if constexpr (kBytes == 16) {
+            const uint4 a = *reinterpret_cast<const uint4 *>(p);
+            w[0] = a.x, w[1] = a.y, w[2] = a.z, w[3] = a.w;
+        } else if constexpr (kBytes == 8) {
+            const uint2 a = *reinterpret_cast<const uint2 *>(p);
+            w[0] = a.x, w[1] = a.y;
+        } else if constexpr (kBytes == 4) w[0] = *reinterpret_cast<const uint32_t *>(p);
+        else w[0] = *reinterpret_cast<const uint16_t *>(p);
+    }
+    __device__ __forceinline__ void store(uint8_t *p) const {
+        if constexpr (kBytes == 16) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+        else if constexpr (kBytes == 8) *reinterpret_cast<uint2 *>(p) = make_uint2(w[0], w[1]);
+        else if constexpr (kBytes == 4) *reinterpret_cast<uint32_t *>(p) = w[0];
+        else *reinterpret_cast<uint16_t *>(p) = uint16_t(w[0]);
+    }
+    __device__ __forceinline__ float get(uint32_t i) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+        else return i % 2 ? E::hi(w[i / 2]) : E::lo(w[i / 2]);
+    }
+    __device__ __forceinline__ void set(const float (&v)[V]) {
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (uint32_t i = 0; i < V; ++i) w[i] = __float_as_uint(v[i]);
+        } else if constexpr (V == 1) w[0] = E::bits(E::of(v[0]));
+        else {
+#pragma unroll
+            for (uint32_t i = 0; i < V; i += 2) w[i / 2] = E::two(v[i], v[i + 1]);
+        }
+    }
+};
+
+// V: values of a piece; NEXT: pairs side by side (V = 1: a unit is the two pieces of one pair in either layout)
+template <class E, uint32_t V, bool NEXT>
+__global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryParams P) {
+    constexpr uint32_t kSize = sizeof(typename E::T), kAtOnce = 4;
+    constexpr bool kTwo = !NEXT || V == 1;                                      // a unit that turns is two pieces
+    __shared__ float2 table[kTable];
+    op_wait_for_stream();
+    const uint32_t t0 = (blockIdx.x / P.parts) * P.tokens, part = blockIdx.x % P.parts, tokens = min(P.tokens, P.T - t0);
+    for (uint32_t i = threadIdx.x; i < tokens * P.pairs; i += blockDim.x) {
+        const uint32_t t = i / P.pairs, k = i - t * P.pairs;
+        const int64_t position = P.wide_positions ? static_cast<const int64_t *>(P.positions)[t0 + t] : int64_t(static_cast<const int32_t *>(P.positions)[t0 + t]);
+        table[i] = cosine_sine(position, turn_fraction(P.frequencies[k]), P.factor);
+    }
+    __syncthreads();
+    const uint32_t h0 = uint32_t(uint64_t(P.heads) * part / P.parts), heads = uint32_t(uint64_t(P.heads) * (part + 1) / P.parts) - h0;
+    const uint32_t units = tokens * heads * P.per_head;
+    for (uint32_t first = threadIdx.x; first < units; first += blockDim.x * kAtOnce) {
+        Piece<E, V> a[kAtOnce], b[kAtOnce];
+        int64_t to[kAtOnce];
+        uint32_t at[kAtOnce], apart[kAtOnce];
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            const uint32_t unit = first + k * blockDim.x;
+            if (unit >= units) break;
+            const uint32_t th = unit / P.per_head, j = unit - th * P.per_head, t = th / heads, h = h0 + th - t * heads;
+            uint32_t c;                                                         // the unit's first value
+            if (j < P.turning) {
+                c = NEXT && V == 1 ? 2 * j : j * V;
+                at[k] = t * P.pairs + (NEXT ? c / 2 : c);
+                apart[k] = kTwo ? (NEXT ? kSize : P.pairs * kSize) : 0;
+            } else {
+                c = 2 * P.pairs + (j - P.turning) * V;
+                at[k] = ~0u;
+                apart[k] = 0;
+            }
+            const uint8_t *src = P.x + int64_t(t0 + t) * P.ldx + int64_t(h) * P.ldx_head + c * kSize;
+            to[k] = int64_t(t0 + t) * P.ldo + int64_t(h) * P.ldo_head + c * kSize;
+            a[k].load(src);
+            if (kTwo && apart[k]) b[k].load(src + apart[k]);
+        }
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            if (first + k * blockDim.x >= units) break;
+            if (at[k] != ~0u) {
+                float u[V], v[V];
+                if constexpr (kTwo) {
+#pragma unroll
+                    for (uint32_t i = 0; i < V; ++i) {
+                        const float2 cs = table[at[k] + i];
+                        const float p = a[k].get(i), q = b[k].get(i);
+                        u[i] = p * cs.x - q * cs.y;
+                        v[i] = q * cs.x + p * cs.y;
+                    }
+                    b[k].set(v);
+                } else {
+#pragma unroll
+                    for (uint32_t i = 0; i < V; i += 2) {
+                        const float2 cs = table[at[k] + i / 2];
+                        const float p = a[k].get(i), q = a[k].get(i + 1);
+                        u[i] = p * cs.x - q * cs.y;
+                        u[i + 1] = q * cs.x + p * cs.y;
+                    }
+                }
+                a[k].set(u);
+            }
+            a[k].store(P.o + to[k]);
+            if (kTwo && apart[k]) b[k].store(P.o + to[k] + apart[k]);
+        }
+    }
+}
+
+template <class E>
+int launch_rotary(RotaryParams P, bool next, bool in_place, cudaStream_t st) {
+    // the largest piece of which heads, halves and addresses are whole multiples
+    constexpr uint32_t kSize = sizeof(typename E::T);
+    const uint64_t unit = (reinterpret_cast<uintptr_t>(P.x) | reinterpret_cast<uintptr_t>(P.o) | uint64_t(P.ldx) | uint64_t(P.ldx_head) | uint64_t(P.ldo) | uint64_t(P.ldo_head) |
+                           uint64_t(P.dim) * kSize | uint64_t(next ? 2 * P.pairs : P.pairs) * kSize);
+    const uint32_t bytes = unit % 16 == 0 ? 16u : unit % 8 == 0 ? 8u : kSize, V = bytes / kSize;
+    P.turning = next && V > 1 ? 2 * P.pairs / V : P.pairs / V;
+    P.per_head = P.turning + (in_place ? 0u : (P.dim - 2 * P.pairs) / V);
+    // As many tokens to a CTA as make four rounds of its threads, or fewer where the GPU has room for more CTAs
+    const uint32_t sms = uint32_t(op_sms());
+    if (!sms) return EP_ERR_CUDA;
+    const uint64_t per_token = uint64_t(P.heads) * P.per_head;
+    uint64_t tokens = (1024 + per_token - 1) / per_token;
+    if (tokens > kTable / P.pairs) tokens = kTable / P.pairs;
+    const uint64_t spread = (uint64_t(P.T) + 2 * sms - 1) / (2 * sms);
+    if (tokens > spread) tokens = spread;
+    if (tokens < 1) tokens = 1;
+    P.tokens = uint32_t(tokens);
+    const uint64_t ctas = (uint64_t(P.T) + tokens - 1) / tokens;
+    P.parts = 1;
+    while (P.parts < 8 && ctas * P.parts < sms && per_token * tokens > 256u * P.parts && 2 * P.parts <= P.heads) P.parts *= 2;
+    if (ctas * P.parts > 0x7FFFFFFFu || per_token * tokens > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    auto launch = [&](auto kernel) { return op_launch(kernel, uint32_t(ctas * P.parts), 256, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA; };
+    if constexpr (kSize == 4) {
+        if (V == 4) return next ? launch(rotary_kernel<E, 4, true>) : launch(rotary_kernel<E, 4, false>);
+        if (V == 2) return next ? launch(rotary_kernel<E, 2, true>) : launch(rotary_kernel<E, 2, false>);
+    } else {
+        if (V == 8) return next ? launch(rotary_kernel<E, 8, true>) : launch(rotary_kernel<E, 8, false>);
+        if (V == 4) return next ? launch(rotary_kernel<E, 4, true>) : launch(rotary_kernel<E, 4, false>);
+    }
+    return next ? launch(rotary_kernel<E, 1, true>) : launch(rotary_kernel<E, 1, false>);
+}
+
+bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1u)) == 0; }
+
+}  // namespace
+
+extern "C" int ep_rotary(const ep_rotary_job *job, void *stream) {
+    if (!job) return EP_ERR_BAD_ARG;
+    const ep_rotary_job &j = *job;
+    if (j.T == 0) return EP_OK;
+    const uint32_t size = j.dtype == EP_FP32 ? 4 : j.dtype == EP_BF16 || j.dtype == EP_FP16 ? 2 : 0;
+    if (!j.d_x || !j.d_out || !j.d_positions || !j.d_frequencies || !size || j.heads == 0 || j.heads > 65535 || j.pairs == 0 || j.dim > 1024 || 2 * uint64_t(j.pairs) > j.dim ||
+        j.T > 0x7FFFFF00u || (j.position_bits != 32 && j.position_bits != 64) || !aligned(j.d_x, size) || !aligned(j.d_out, size) ||
+        !aligned(j.d_positions, uintptr_t(j.position_bits / 8)) || !aligned(j.d_frequencies, 8))
+        return EP_ERR_BAD_ARG;
+    const int64_t most = int64_t(1) << 40;
+    for (const int64_t ld : {j.ldx, j.ldx_head, j.ldo, j.ldo_head})
+        if (ld < 0 || ld >= most) return EP_ERR_BAD_ARG;
+    const bool in_place = j.d_x == j.d_out;
+    if (in_place && (j.ldx != j.ldo || j.ldx_head != j.ldo_head)) return EP_ERR_BAD_ARG;
+    RotaryParams P;
+    std::memset(&P, 0, sizeof(P));
+    P.x = static_cast<const uint8_t *>(j.d_x);
+    P.o = static_cast<uint8_t *>(j.d_out);
+    P.positions = j.d_positions;
+    P.frequencies = j.d_frequencies;
+    P.ldx = j.ldx * size;
+    P.ldx_head = j.ldx_head * size;
+    P.ldo = j.ldo * size;
+    P.ldo_head = j.ldo_head * size;
+    P.T = j.T;
+    P.heads = j.heads;
+    P.dim = j.dim;
+    P.pairs = j.pairs;
+    P.wide_positions = j.position_bits == 64;
+    P.factor = j.factor;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    if (j.dtype == EP_BF16) return launch_rotary<Bf16>(P, j.interleaved != 0, in_place, st);
+    if (j.dtype == EP_FP16) return launch_rotary<Fp16>(P, j.interleaved != 0, in_place, st);
+    return launch_rotary<Fp32>(P, j.interleaved != 0, in_place, st);
+}
+
+extern "C" int ep_rotary_frequencies(uint32_t pairs, double base, double stretch, double original, double fast, double slow, double *out) {
+    if (!out || pairs == 0 || !(base > 0) || !(stretch >= 1) || !(original >= 0) || (original > 0 && !(fast > slow)) || !std::isfinite(base) || !std::isfinite(stretch) ||
+        !std::isfinite(original))
+        return EP_ERR_BAD_ARG;
+    for (uint32_t i = 0; i < pairs; ++i) {
+        const double f = std::pow(base, -double(i) / double(pairs));
+        double k = 0.0;
+        if (original > 0) {
+            k = (original * f / 6.283185307179586 - slow) / (fast - slow);
+            k = k < 0.0 ? 0.0 : k > 1.0 ? 1.0 : k;
+        }
+        out[i] = f * (k + (1.0 - k) / stretch);
+    }
+    return EP_OK;
+}
