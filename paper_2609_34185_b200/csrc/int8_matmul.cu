@@ -39,12 +39,13 @@ __device__ __forceinline__ uint32_t largest_bits(const Eight<BITS> &e, bool half
     }
 }
 template <uint32_t BITS>
-__device__ __forceinline__ void store_int8(const Eight<BITS> &e, bool half, float inverse, uint8_t *row, uint32_t c, uint32_t n, bool vec) {
-    float v[8];
-    to_floats<BITS>(e, half, v);
-#pragma unroll
-    for (uint32_t j = 0; j < 8; ++j) v[j] = inverse == 0.0f ? 0.0f : __fmul_rn(v[j], inverse);
-    store_bytes(row, c, n, vec, int8x4(v[0], v[1], v[2], v[3]), int8x4(v[4], v[5], v[6], v[7]));
+__device__ __forceinline__ void store_int8(const Eight<BITS> &e, bool half, const Int8Scale &s, uint8_t *row, uint32_t c, uint32_t n, bool vec) {
+    Pair v[4];
+    to_pairs<BITS>(e, half, v);
+    uint32_t lo, hi;
+    to_int8(v, s.inverse, lo, hi);
+    if (s.s != s.s) lo = hi = 0;
+    store_bytes(row, c, n, vec, lo, hi);
 }
 
 template <uint32_t BITS, uint32_t N>
@@ -53,7 +54,7 @@ __global__ void __launch_bounds__(512) quantize_rows_kernel(const __grid_constan
     op_wait_for_stream();
     const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, of = warp / P.warps;
     const uint32_t row = blockIdx.x * P.rows + of, l = (warp - of * P.warps) * 32u + lane;
-    RowGroup group{room, P.warps, of * P.warps, 0};
+    RowGroup group{room, P.warps, of * P.warps, 1u + of, 0};
     const uint8_t *x = P.x + int64_t(row) * P.ldx;
     Eight<BITS> e[N];
     uint32_t top = 0;
@@ -69,7 +70,7 @@ __global__ void __launch_bounds__(512) quantize_rows_kernel(const __grid_constan
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i) {
         const uint32_t c = (i * P.warps * 32u + l) * 8u;
-        store_int8<BITS>(e[i], P.half, s.inverse, P.q + int64_t(row) * P.ldq, c, inside(c, P.C), P.q_vec);
+        store_int8<BITS>(e[i], P.half, s, P.q + int64_t(row) * P.ldq, c, inside(c, P.C), P.q_vec);
     }
     if (l == 0) P.s[row] = s.s;
 }
@@ -77,7 +78,7 @@ template <uint32_t BITS>
 __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const __grid_constant__ RowsParams P) {
     __shared__ uint32_t room[64];
     op_wait_for_stream();
-    RowGroup group{room, P.warps, 0, 0};
+    RowGroup group{room, P.warps, 0, 1, 0};
     const uint8_t *x = P.x + int64_t(blockIdx.x) * P.ldx;
     uint32_t top = 0;
     Eight<BITS> e;
@@ -90,7 +91,7 @@ __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const __grid_co
 #pragma unroll 4
     for (uint32_t c = threadIdx.x * 8u; c < P.C; c += blockDim.x * 8u) {
         load_eight<BITS>(x, c, inside(c, P.C), P.x_vec, e);
-        store_int8<BITS>(e, P.half, s.inverse, P.q + int64_t(blockIdx.x) * P.ldq, c, inside(c, P.C), P.q_vec);
+        store_int8<BITS>(e, P.half, s, P.q + int64_t(blockIdx.x) * P.ldq, c, inside(c, P.C), P.q_vec);
     }
     if (threadIdx.x == 0) P.s[blockIdx.x] = s.s;
 }

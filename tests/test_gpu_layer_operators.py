@@ -281,6 +281,45 @@ def test_norm_groups(T, groups):
 
 
 @gpu
+@pytest.mark.parametrize("T,groups,more", [(6000, 2, 2), (6000, 3, 6), (6000, 12, 4), (6000, 4, 6), (5000, 50, 1), (4000, 1, 1000), (2000, 2000, 2), (1500, 1, 3), (296 * 5, 296, 148)])
+@pytest.mark.parametrize("C", [72, 1000, 3848])
+def test_norm_groups_of_many_rows(T, C, groups, more):
+    x, v = norm_inputs(T, C, torch.float16, torch.float32, groups, T + C)
+    v["gate"] = norm_inputs(T, C, torch.float16, torch.float32, more, C)[1]["gate"]
+    for left in ((), ("weight",), ("gate", "bias")):
+        given = {k: t for k, t in v.items() if k not in left}
+        z, r = ep.norm(x, weight_offset=1.0, center=True, **given)
+        want, r_want = normed(x, weight_offset=1.0, center=True, **given)
+        assert near(z, want) and near(r, r_want)
+    assert ep.last_device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,wide", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float32, torch.bfloat16), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("T,C", [(1201, 8), (1203, 64), (5000, 256), (3001, 264), (1205, 520), (1500, 1000), (2501, 2048), (1301, 5120), (1200, 8200), (1190, 17408), (1184, 32768), (1900, 136), (2000, 12000), (1200, 1028)])
+@pytest.mark.parametrize("center", [False, True])
+def test_norm_of_many_rows(T, C, dtype, wide, center):
+    x, v = norm_inputs(T, C, dtype, wide, 1, T * 3 + C)
+    for left in ((), ("post_weight", "gate"), ("residual", "bias")):
+        given = {k: t for k, t in v.items() if k not in left}
+        z, r = ep.norm(x, residual_scale=0.7, center=center, residual_out=None if "residual" in given else torch.empty_like(x), **given)
+        want, r_want = normed(x, residual_scale=0.7, center=center, **given)
+        assert near(z, want) and near(r, r_want)
+        if C < 10000:
+            z, _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.FP32, **given)
+            (q, s), _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.FP8_E4M3, **given)
+            (q8, s8), _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.INT8, **given)
+            same = lambda a, b: torch.equal(a.view(torch.uint8), b.view(torch.uint8))  # noqa: E731
+            assert all(map(same, (q, s, q8, s8), ep.quantize_blocks(z) + ep.quantize_rows(z)))
+    if "residual" in v:                                    # in place: the residual, and z over x
+        h, x2 = v["residual"].clone(), x.clone()
+        z, r = ep.norm(x, **v)
+        z2, r2 = ep.norm(x2, **{**v, "residual": h}, out=x2, residual_out=h)
+        assert z2 is x2 and r2 is h and torch.equal(z, z2) and torch.equal(r, r2)
+    assert ep.last_device_status() == 0
+
+
+@gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,C", SIZES + [(70, 640)])
 def test_norm_into_the_containers(T, C, dtype):
