@@ -1,13 +1,14 @@
 // Rotary positions.
 #include <cmath>
 
-#include "op8.hpp"
+#include "op_rows.hpp"
 
 using namespace ep;
 
 namespace {
 
-constexpr uint32_t kTable = 1024;                // cosines and sines that a CTA holds
+constexpr uint32_t kTable = 4096;                // cosines and sines that a CTA holds at most
+constexpr uint32_t kThreads = 256, kAtOnce = 4;  // units that a thread has under way
 
 // ======================================================================================================================
 // (u, v) -> f (u cos a - v sin a, v cos a + u sin a),   a = position * frequency[i]
@@ -27,9 +28,19 @@ struct RotaryParams {
     uint32_t tokens, parts;                      // tokens of a CTA; CTAs that share these tokens' heads
     uint32_t per_head;                           // units of a head: pieces that turn (half layout: pairs of pieces), then pieces that stay
     uint32_t turning;
+    uint32_t apart;                              // bytes between the two pieces of a unit that stays (0: it is one)
+    uint32_t heads_of_part;
+    uint32_t step_j, step_h, step_t;             // kThreads units further: units of a head, heads, tokens
+    uint32_t lines;                              // tokens whose cosines the threads work out at a time
+    uint64_t by_units, by_heads, by_columns;     // 2^32 / n, rounded up: n / per_head, n / heads_of_part, n / min(pairs, kThreads)
     uint32_t wide_positions;
     float factor;
 };
+
+// n / d for n < 256 and d < 2^24, of 2^32 / d rounded up (a division takes the threads longer than their first loads need to be put together)
+__device__ __forceinline__ uint32_t quotient(uint32_t n, uint64_t inverse) { return uint32_t((n * inverse) >> 32); }
+inline uint64_t inverse_of(uint32_t d) { return ((uint64_t(1) << 32) + d - 1u) / d; }
+
 
 __device__ __forceinline__ uint64_t turn_fraction(double radians) {
     double t = radians * 0.15915494309189533577;                                 // 1 / (2 pi)
@@ -83,72 +94,115 @@ struct Piece {
 
 // V: values of a piece; NEXT: pairs side by side (V = 1: a unit is the two pieces of one pair in either layout)
 template <class E, uint32_t V, bool NEXT>
-__global__ void __launch_bounds__(256) rotary_kernel(const __grid_constant__ RotaryParams P) {
-    constexpr uint32_t kSize = sizeof(typename E::T), kAtOnce = 4;
+__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryParams P) {
+    constexpr uint32_t kSize = sizeof(typename E::T);
     constexpr bool kTwo = !NEXT || V == 1;                                      // a unit that turns is two pieces
-    __shared__ float2 table[kTable];
+    // A unit's cosines and sines two pairs at a time, {c, c', s, s'}, in planes: units that lie side by side read 16 bytes side by side.
+    constexpr uint32_t kPairs = NEXT ? (V > 1 ? V / 2 : 1) : V;                 // of a unit
+    extern __shared__ __align__(16) float table[];
+    auto place = [&](uint32_t token, uint32_t i) {
+        if constexpr (kPairs == 1) return 2u * (token * P.pairs + i);
+        return 2u * token * P.pairs + 4u * ((i % kPairs) / 2u * P.turning + i / kPairs) + i % 2u;
+    };
     op_wait_for_stream();
     const uint32_t t0 = (blockIdx.x / P.parts) * P.tokens, part = blockIdx.x % P.parts, tokens = min(P.tokens, P.T - t0);
-    for (uint32_t i = threadIdx.x; i < tokens * P.pairs; i += blockDim.x) {
-        const uint32_t t = i / P.pairs, k = i - t * P.pairs;
-        const int64_t position = P.wide_positions ? static_cast<const int64_t *>(P.positions)[t0 + t] : int64_t(static_cast<const int32_t *>(P.positions)[t0 + t]);
-        table[i] = cosine_sine(position, turn_fraction(P.frequencies[k]), P.factor);
+    const uint32_t h0 = part * P.heads_of_part, heads = P.heads_of_part;
+    Piece<E, V> a[kAtOnce], b[kAtOnce];
+    int64_t to[kAtOnce];
+    uint32_t at[kAtOnce], apart[kAtOnce];
+    // Units are counted through the heads and the tokens; a thread's next one is kThreads further.
+    uint32_t h = quotient(threadIdx.x, P.by_units), j = threadIdx.x - h * P.per_head, t = quotient(h, P.by_heads);
+    h -= t * heads;
+    auto load = [&]() {
+#pragma unroll
+        for (uint32_t k = 0; k < kAtOnce; ++k) {
+            at[k] = ~0u;
+            apart[k] = 0;
+            to[k] = -1;
+            if (t < tokens) {
+                uint32_t c;                                                     // the unit's first value
+                if (j < P.turning) {
+                    c = NEXT && V == 1 ? 2 * j : j * V;
+                    at[k] = 2u * t * P.pairs + (kPairs == 1 ? 2u : 4u) * j;
+                    apart[k] = kTwo ? (NEXT ? kSize : P.pairs * kSize) : 0;
+                } else {
+                    c = 2 * P.pairs + (j - P.turning) * V;
+                    apart[k] = kTwo ? P.apart : 0;
+                }
+                const uint8_t *src = P.x + int64_t(t0 + t) * P.ldx + int64_t(h0 + h) * P.ldx_head + c * kSize;
+                to[k] = int64_t(t0 + t) * P.ldo + int64_t(h0 + h) * P.ldo_head + c * kSize;
+                a[k].load(src);
+                if (kTwo && apart[k]) b[k].load(src + apart[k]);
+            }
+            j += P.step_j, h += P.step_h, t += P.step_t;
+            if (j >= P.per_head) j -= P.per_head, ++h;
+            if (h >= heads) h -= heads, ++t;
+        }
+    };
+    load();                                                                     // (under way while the cosines are worked out)
+    const uint32_t columns = min(P.pairs, kThreads), lines = P.lines, line = quotient(threadIdx.x, P.by_columns);
+    auto position_of = [&](uint32_t n) {
+        return P.wide_positions ? static_cast<const int64_t *>(P.positions)[t0 + n] : int64_t(static_cast<const int32_t *>(P.positions)[t0 + n]);
+    };
+    if (line < lines && line < tokens) {
+        const int64_t first = position_of(line);                                // (asked for together with the frequency)
+        for (uint32_t i = threadIdx.x - line * columns; i < P.pairs; i += kThreads) {
+            const uint64_t step = turn_fraction(P.frequencies[i]);
+            float2 cs = cosine_sine(first, step, P.factor);
+            uint32_t p = place(line, i);
+            table[p] = cs.x, table[p + (kPairs == 1 ? 1 : 2)] = cs.y;
+#pragma unroll 4
+            for (uint32_t n = line + lines; n < tokens; n += lines) {
+                cs = cosine_sine(position_of(n), step, P.factor);
+                p = place(n, i);
+                table[p] = cs.x, table[p + (kPairs == 1 ? 1 : 2)] = cs.y;
+            }
+        }
     }
     __syncthreads();
-    const uint32_t h0 = uint32_t(uint64_t(P.heads) * part / P.parts), heads = uint32_t(uint64_t(P.heads) * (part + 1) / P.parts) - h0;
-    const uint32_t units = tokens * heads * P.per_head;
-    for (uint32_t first = threadIdx.x; first < units; first += blockDim.x * kAtOnce) {
-        Piece<E, V> a[kAtOnce], b[kAtOnce];
-        int64_t to[kAtOnce];
-        uint32_t at[kAtOnce], apart[kAtOnce];
+    while (true) {
 #pragma unroll
         for (uint32_t k = 0; k < kAtOnce; ++k) {
-            const uint32_t unit = first + k * blockDim.x;
-            if (unit >= units) break;
-            const uint32_t th = unit / P.per_head, j = unit - th * P.per_head, t = th / heads, h = h0 + th - t * heads;
-            uint32_t c;                                                         // the unit's first value
-            if (j < P.turning) {
-                c = NEXT && V == 1 ? 2 * j : j * V;
-                at[k] = t * P.pairs + (NEXT ? c / 2 : c);
-                apart[k] = kTwo ? (NEXT ? kSize : P.pairs * kSize) : 0;
-            } else {
-                c = 2 * P.pairs + (j - P.turning) * V;
-                at[k] = ~0u;
-                apart[k] = 0;
-            }
-            const uint8_t *src = P.x + int64_t(t0 + t) * P.ldx + int64_t(h) * P.ldx_head + c * kSize;
-            to[k] = int64_t(t0 + t) * P.ldo + int64_t(h) * P.ldo_head + c * kSize;
-            a[k].load(src);
-            if (kTwo && apart[k]) b[k].load(src + apart[k]);
-        }
-#pragma unroll
-        for (uint32_t k = 0; k < kAtOnce; ++k) {
-            if (first + k * blockDim.x >= units) break;
+            if (to[k] < 0) break;
             if (at[k] != ~0u) {
-                float u[V], v[V];
-                if constexpr (kTwo) {
-#pragma unroll
-                    for (uint32_t i = 0; i < V; ++i) {
-                        const float2 cs = table[at[k] + i];
-                        const float p = a[k].get(i), q = b[k].get(i);
-                        u[i] = p * cs.x - q * cs.y;
-                        v[i] = q * cs.x + p * cs.y;
+                if constexpr (kPairs == 1) {
+                    const float c = table[at[k]], s = table[at[k] + 1];
+                    if constexpr (kTwo) {
+                        const float p = a[k].get(0), q = b[k].get(0);
+                        float u[1] = {p * c - q * s}, v[1] = {q * c + p * s};
+                        a[k].set(u), b[k].set(v);
+                    } else {
+                        const float p = a[k].get(0), q = a[k].get(1);
+                        float u[2] = {p * c - q * s, q * c + p * s};
+                        a[k].set(u);
                     }
-                    b[k].set(v);
                 } else {
+                    float u[V], v[V];
 #pragma unroll
-                    for (uint32_t i = 0; i < V; i += 2) {
-                        const float2 cs = table[at[k] + i / 2];
-                        const float p = a[k].get(i), q = a[k].get(i + 1);
-                        u[i] = p * cs.x - q * cs.y;
-                        u[i + 1] = q * cs.x + p * cs.y;
+                    for (uint32_t i = 0; i < kPairs; i += 2) {
+                        const float4 cs = *reinterpret_cast<const float4 *>(table + at[k] + 2u * i * P.turning);
+                        if constexpr (NEXT) {
+#pragma unroll
+                            for (uint32_t m = 0; m < 2; ++m) {
+                                const float p = a[k].get(2 * (i + m)), q = a[k].get(2 * (i + m) + 1), c = m ? cs.y : cs.x, s = m ? cs.w : cs.z;
+                                u[2 * (i + m)] = p * c - q * s;
+                                u[2 * (i + m) + 1] = q * c + p * s;
+                            }
+                        } else {
+                            const Pair c(cs.x, cs.y), s(cs.z, cs.w), p(a[k].get(i), a[k].get(i + 1)), q(b[k].get(i), b[k].get(i + 1));
+                            const float2 x = fma2(p, c, q * s * Pair(-1.0f)).two(), y = fma2(q, c, p * s).two();
+                            u[i] = x.x, u[i + 1] = x.y, v[i] = y.x, v[i + 1] = y.y;
+                        }
                     }
+                    a[k].set(u);
+                    if constexpr (!NEXT) b[k].set(v);
                 }
-                a[k].set(u);
             }
             a[k].store(P.o + to[k]);
             if (kTwo && apart[k]) b[k].store(P.o + to[k] + apart[k]);
         }
+        if (t >= tokens) break;
+        load();
     }
 }
 
@@ -160,12 +214,16 @@ int launch_rotary(RotaryParams P, bool next, bool in_place, cudaStream_t st) {
                            uint64_t(P.dim) * kSize | uint64_t(next ? 2 * P.pairs : P.pairs) * kSize);
     const uint32_t bytes = unit % 16 == 0 ? 16u : unit % 8 == 0 ? 8u : kSize, V = bytes / kSize;
     P.turning = next && V > 1 ? 2 * P.pairs / V : P.pairs / V;
-    P.per_head = P.turning + (in_place ? 0u : (P.dim - 2 * P.pairs) / V);
-    // As many tokens to a CTA as make four rounds of its threads, or fewer where the GPU has room for more CTAs
+    // what stays: two pieces to a unit as well, where there is an even number of them
+    const uint32_t stay = in_place ? 0u : (P.dim - 2 * P.pairs) / V;
+    const bool two = (!next || V == 1) && stay % 2 == 0 && stay;
+    P.per_head = P.turning + (two ? stay / 2 : stay);
+    P.apart = two ? stay / 2 * V * kSize : 0u;
+    // As many tokens to a CTA as give its threads what they load at once, or fewer where the GPU has room for more CTAs
     const uint32_t sms = uint32_t(op_sms());
     if (!sms) return EP_ERR_CUDA;
     const uint64_t per_token = uint64_t(P.heads) * P.per_head;
-    uint64_t tokens = (1024 + per_token - 1) / per_token;
+    uint64_t tokens = kThreads * kAtOnce / per_token;
     if (tokens > kTable / P.pairs) tokens = kTable / P.pairs;
     const uint64_t spread = (uint64_t(P.T) + 2 * sms - 1) / (2 * sms);
     if (tokens > spread) tokens = spread;
@@ -173,9 +231,18 @@ int launch_rotary(RotaryParams P, bool next, bool in_place, cudaStream_t st) {
     P.tokens = uint32_t(tokens);
     const uint64_t ctas = (uint64_t(P.T) + tokens - 1) / tokens;
     P.parts = 1;
-    while (P.parts < 8 && ctas * P.parts < sms && per_token * tokens > 256u * P.parts && 2 * P.parts <= P.heads) P.parts *= 2;
+    while (P.parts < 8 && ctas * P.parts < sms && per_token * tokens > kThreads * P.parts && P.heads % (2 * P.parts) == 0) P.parts *= 2;
+    P.heads_of_part = P.heads / P.parts;
+    P.step_j = kThreads % P.per_head;
+    P.step_t = kThreads / P.per_head / P.heads_of_part;
+    P.step_h = kThreads / P.per_head - P.step_t * P.heads_of_part;
+    const uint32_t columns = P.pairs < kThreads ? P.pairs : kThreads;
+    P.lines = kThreads / columns;
+    P.by_units = inverse_of(P.per_head);
+    P.by_heads = inverse_of(P.heads_of_part);
+    P.by_columns = inverse_of(columns);
     if (ctas * P.parts > 0x7FFFFFFFu || per_token * tokens > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
-    auto launch = [&](auto kernel) { return op_launch(kernel, uint32_t(ctas * P.parts), 256, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA; };
+    auto launch = [&](auto kernel) { return op_launch(kernel, uint32_t(ctas * P.parts), kThreads, P.tokens * P.pairs * 8u, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA; };
     if constexpr (kSize == 4) {
         if (V == 4) return next ? launch(rotary_kernel<E, 4, true>) : launch(rotary_kernel<E, 4, false>);
         if (V == 2) return next ? launch(rotary_kernel<E, 2, true>) : launch(rotary_kernel<E, 2, false>);
