@@ -125,9 +125,12 @@ struct ProductParams {
     void *y;
     int64_t ldy;
     uint32_t T, R, blocks;        // blocks = ceil(C / 128)
-    uint32_t rows, strips;        // rows of the weight to a strip, strips: a grid walks them first
+    uint32_t strips;              // of rows of the weight: a grid walks them first
     uint32_t split;               // CTAs (one cluster) that share a strip's columns
     uint32_t stages, stage;       // in shared memory; bytes of one
+    uint32_t whole, chunk;        // whole blocks of 128 columns; how many of them a stage holds
+    uint32_t m;                   // rows of the instruction: 64 or 128
+    uint32_t x_block, w_block;    // bytes of a block: rows in whole eights
 };
 
 // the epilogue, the same in every kernel so that results do not depend on which one is taken
@@ -151,23 +154,42 @@ __device__ __forceinline__ void pair_mma_i8(uint32_t d, uint64_t a, uint64_t b, 
 // columns of a higher strip; at the end they lay their sums down in shared memory and each adds up its share of the tokens over the cluster.
 template <uint32_t BN>
 struct StripShape {
-    static constexpr uint32_t kB = BN * 128, kMaxStages = 16, kRoom = 96 * 1024;      // bytes of stages: two CTAs fit an SM
-    static constexpr uint32_t kTail = 128 * 128;                                       // what the last stage's instructions may read beyond it
-    static constexpr uint32_t kBars = kRoom + kTail - 8 * 128, kScales = kBars + 16 * kMaxStages + 32, kSmem = kScales + 4 * BN + 1024;
-    static_assert(2 * (kSmem + 1024) <= 228 * 1024);
+    static constexpr uint32_t kB = BN * 128, kMaxStages = 32, kTail = 128 * 128;       // kTail: what the last stage's instructions may read beyond it
+    static constexpr uint32_t kBars = 0, kScales = 16 * kMaxStages + 16, kStages = 2048;
+    static constexpr uint32_t kSmem(uint32_t stages, uint32_t stage) { return kStages + stages * stage + kTail + 1024; }
+    static constexpr uint32_t kMost = 226 * 1024;
     static constexpr uint32_t kCols = BN < 32 ? 32 : BN;
+    static_assert(kScales + 4 * BN <= kStages && BN <= 128);
 };
 
+// Sixteen tokens' sums from tensor memory to y, a row of the weight to each lane; the first n tokens are there.  Token i's scale lies at scales + 4 i.
+template <class E>
+__device__ __forceinline__ void put_sixteen(uint32_t tmem, uint32_t scales, typename E::T *y, int64_t ldy, uint32_t n, float a, float bias) {
+    uint32_t v[16];
+    uint4 f[4];
+    tc_load16(tmem, v);
+#pragma unroll
+    for (uint32_t i = 0; i < 4; ++i) f[i] = ld_smem16(scales + 16 * i);
+    tc_loaded16(v);
+#pragma unroll
+    for (uint32_t i = 0; i < 16; ++i, y += ldy) {
+        const uint4 g = f[i / 4];
+        const uint32_t s = i % 4 == 0 ? g.x : i % 4 == 1 ? g.y : i % 4 == 2 ? g.z : g.w;
+        if (i < n) *y = E::of(scaled(v[i], __uint_as_float(s), a, bias));
+    }
+}
+
 template <uint32_t BN, class E>
-__global__ void __launch_bounds__(128) product_strip_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ CUtensorMap w_map,
-                                                            const __grid_constant__ CUtensorMap x_map) {
+__global__ void __launch_bounds__(128)
+    product_strip_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map,
+                         const __grid_constant__ CUtensorMap w_tail, const __grid_constant__ CUtensorMap x_tail) {
     using G = StripShape<BN>;
     using T = typename E::T;
     extern __shared__ uint8_t raw[];
     const uint32_t base = (smem_u32(raw) + 1023u) & ~1023u;
     const uint32_t tid = threadIdx.x, lane = tid & 31u, warp = __shfl_sync(0xFFFFFFFFu, tid >> 5, 0);
     const uint32_t full = base + G::kBars, empty = full + 8 * G::kMaxStages, done = empty + 8 * G::kMaxStages, slot_addr = done + 8, abort_word = slot_addr + 4,
-                   scales = base + G::kScales;
+                   scales = base + G::kScales, ring = base + G::kStages;
     if (tid == 0) {
         for (uint32_t i = 0; i < P.stages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
         bar_init(done, 1);
@@ -187,34 +209,45 @@ __global__ void __launch_bounds__(128) product_strip_kernel(const __grid_constan
     const uint32_t strip = tile % P.strips, t0 = (tile / P.strips) * BN;
     // strips of equal height, but for one row
     const uint32_t r0 = uint32_t(uint64_t(P.R) * strip / P.strips), r1 = uint32_t(uint64_t(P.R) * (strip + 1) / P.strips);
-    const uint32_t kb0 = P.blocks * rank / P.split, kb1 = P.blocks * (rank + 1) / P.split, nk = kb1 - kb0;
-    const uint32_t r = r0 + tid;
+    // chunks of whole blocks, and what is left of the columns as one of its own
+    const uint32_t chunks = (P.whole + P.chunk - 1u) / P.chunk + (P.blocks - P.whole);
+    const uint32_t k0 = chunks * rank / P.split, nk = chunks * (rank + 1) / P.split - k0;
+    // this thread's row of the sums: of 64 rows, tensor memory has 16 in each quarter
+    const uint32_t mine = P.m == 64 ? lane < 16 ? warp * 16u + lane : 128u : tid, r = r0 + mine;
     float a = 1.0f, bias = 0.0f;
 
     if (warp == 0) {
-        if (lane == 0) {
-            uint32_t k = 0, s = 0, phase = 1;
-            for (; k < nk; ++k) {
-                const uint32_t at = base + s * P.stage;
-                if (k >= P.stages && !bar_wait(empty + 8 * s, phase, abort_word)) break;
-                bar_expect(full + 8 * s, P.rows * 128 + G::kB);
-                tma_load_2d(at + G::kB, &w_map, int32_t((kb0 + k) * 128u), int32_t(r0), full + 8 * s);
-                tma_load_2d(at, &x_map, int32_t((kb0 + k) * 128u), int32_t(t0), full + 8 * s);
-                if (++s == P.stages) s = 0, phase ^= 1u;
-            }
-            if (ld_smem(abort_word))                     // nothing may land after the CTA's end
-                for (uint32_t j = k > P.stages ? k - P.stages : 0; j < k; ++j) bar_drain(full + 8 * (j % P.stages), (j / P.stages) & 1u);
-        }
-    } else if (warp == 1) {
         const uint32_t lead = elected();
-        uint32_t s = 0, phase = 0;
+        uint32_t k = 0, s = 0, phase = 1;
+        for (; k < nk; ++k) {
+            const uint32_t at = ring + s * P.stage, bar = full + 8 * s, first = (k0 + k) * P.chunk;
+            if (k >= P.stages && !bar_wait_warp(empty + 8 * s, phase, abort_word)) break;
+            if (first < P.whole) {
+                bar_expect_by(bar, P.stage, lead);
+                tma_load_3d_by(at + P.chunk * P.x_block, &w_map, 0, int32_t(r0), int32_t(first), bar, lead);
+                tma_load_3d_by(at, &x_map, 0, int32_t(t0), int32_t(first), bar, lead);
+            } else {
+                bar_expect_by(bar, P.w_block + P.x_block, lead);
+                tma_load_2d_by(at + P.chunk * P.x_block, &w_tail, int32_t(P.whole * 128u), int32_t(r0), bar, lead);
+                tma_load_2d_by(at, &x_tail, int32_t(P.whole * 128u), int32_t(t0), bar, lead);
+            }
+            if (++s == P.stages) s = 0, phase ^= 1u;
+        }
+        if (ld_smem(abort_word))                         // nothing may land after the CTA's end
+            for (uint32_t j = k > P.stages ? k - P.stages : 0; j < k; ++j) bar_drain(full + 8 * (j % P.stages), (j / P.stages) & 1u);
+    } else if (warp == 1) {
+        const uint32_t lead = elected(), idesc = i8_idesc(P.m, BN);
+        uint32_t s = 0, phase = 0, any = 0;
         for (uint32_t k = 0; k < nk; ++k) {
             if (!bar_wait_warp(full + 8 * s, phase, abort_word)) break;
             tc_after();
-            const uint32_t at = base + s * P.stage;
-            const uint64_t da = operand_desc(at + G::kB), db = operand_desc(at);
+            const uint32_t at = ring + s * P.stage, first = (k0 + k) * P.chunk, blocks = first < P.whole ? min(P.chunk, P.whole - first) : 1u;
+            uint64_t da = operand_desc(at + P.chunk * P.x_block), db = operand_desc(at);
+            for (uint32_t n = 0; n < blocks; ++n, da += P.w_block >> 4, db += P.x_block >> 4) {
 #pragma unroll
-            for (uint32_t i = 0; i < 4; ++i) mma_i8(tmem, da + 2 * i, db + 2 * i, i8_idesc(128, BN), (k | i) ? 1u : 0u, lead);
+                for (uint32_t i = 0; i < 4; ++i) mma_i8(tmem, da + 2 * i, db + 2 * i, idesc, any | i, lead);
+                any = 1;
+            }
             tc_commit(empty + 8 * s, lead);
             if (++s == P.stages) s = 0, phase ^= 1u;
         }
@@ -233,7 +266,12 @@ __global__ void __launch_bounds__(128) product_strip_kernel(const __grid_constan
 
     // lane = row of the weight, register = token
     if (P.split == 1) {
-        T *y = static_cast<T *>(P.y) + r;
+        T *y = static_cast<T *>(P.y) + int64_t(t0) * P.ldy + r;
+#pragma unroll 2
+        for (uint32_t c = 0; c < BN && t0 + c < P.T; c += 16)
+            put_sixteen<E>(tmem + ((warp * 32u) << 16) + c, scales + 4 * c, y + int64_t(c) * P.ldy, P.ldy, r < r1 ? min(16u, P.T - t0 - c) : 0u, a, bias);
+    } else {
+        __syncthreads();                                 // (the stages are read no more: every thread has passed `done`)
 #pragma unroll
         for (uint32_t c = 0; c < BN; c += 16) {
             if (t0 + c >= P.T) break;
@@ -242,46 +280,43 @@ __global__ void __launch_bounds__(128) product_strip_kernel(const __grid_constan
             tc_loaded16(v);
 #pragma unroll
             for (uint32_t i = 0; i < 16; ++i)
-                if (r < r1 && t0 + c + i < P.T) y[int64_t(t0 + c + i) * P.ldy] = E::of(scaled(v[i], __uint_as_float(ld_smem(scales + 4 * (c + i))), a, bias));
-        }
-    } else {
-#pragma unroll
-        for (uint32_t c = 0; c < BN; c += 16) {
-            uint32_t v[16];
-            tc_load16(tmem + ((warp * 32u) << 16) + c, v);
-            tc_loaded16(v);
-#pragma unroll
-            for (uint32_t i = 0; i < 16; ++i) st_smem(base + ((c + i) * 128u + tid) * 4u, v[i]);
+                if (mine < 128) st_smem(ring + ((c + i) * 128u + mine) * 4u, v[i]);
         }
         cluster_sync();
-        // this CTA's tokens, one to a warp, four rows to a lane; all CTAs' parts asked for at once
-        const uint32_t c0 = BN * rank / P.split, c1 = BN * (rank + 1) / P.split, r4 = r0 + 4u * lane;
+        // This CTA's tokens, four rows to a lane, two tokens to a warp at a time; all CTAs' parts asked for at once, then added up.
+        const uint32_t tokens = min(BN, P.T - t0), c0 = tokens * rank / P.split, c1 = tokens * (rank + 1) / P.split, r4 = r0 + 4u * lane;
         uint32_t peer[8];
         float a4[4], b4[4];
 #pragma unroll
-        for (uint32_t p = 0; p < 8; ++p) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer[p]) : "r"(base), "r"(min(p, P.split - 1u)));
+        for (uint32_t p = 0; p < 8; ++p) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer[p]) : "r"(ring), "r"(min(p, P.split - 1u)));
 #pragma unroll
         for (uint32_t j = 0; j < 4; ++j) {
             a4[j] = P.a && r4 + j < r1 ? __ldg(P.a + r4 + j) : 1.0f;
             b4[j] = P.bias && r4 + j < r1 ? __ldg(P.bias + r4 + j) : 0.0f;
         }
-#pragma unroll 2
-        for (uint32_t c = c0 + warp; c < c1; c += 4) {
-            if (t0 + c >= P.T) break;
-            int4 v[8];
+        for (uint32_t c = c0 + warp; c < c1; c += 8) {
+            const bool two = c + 4 < c1;
+            int4 v[8], w[8];
 #pragma unroll
             for (uint32_t p = 0; p < 8; ++p)
-                if (p < P.split)
+                if (p < P.split && r4 < r1) {
                     asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v[p].x), "=r"(v[p].y), "=r"(v[p].z), "=r"(v[p].w) : "r"(peer[p] + (c * 128u + 4u * lane) * 4u) : "memory");
-            int32_t sum[4] = {v[0].x, v[0].y, v[0].z, v[0].w};
+                    if (two)
+                        asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(peer[p] + ((c + 4) * 128u + 4u * lane) * 4u) : "memory");
+                }
+            auto finish = [&](const int4 (&q)[8], uint32_t token) {
+                int32_t sum[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
 #pragma unroll
-            for (uint32_t p = 1; p < 8; ++p)
-                if (p < P.split) sum[0] += v[p].x, sum[1] += v[p].y, sum[2] += v[p].z, sum[3] += v[p].w;
-            const float s = __uint_as_float(ld_smem(scales + 4 * c));
-            T *dst = static_cast<T *>(P.y) + int64_t(t0 + c) * P.ldy + r4;
+                for (uint32_t p = 1; p < 8; ++p)
+                    if (p < P.split) sum[0] += q[p].x, sum[1] += q[p].y, sum[2] += q[p].z, sum[3] += q[p].w;
+                const float s = __uint_as_float(ld_smem(scales + 4 * token));
+                T *dst = static_cast<T *>(P.y) + int64_t(t0 + token) * P.ldy + r4;
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j)
-                if (r4 + j < r1) dst[j] = E::of(scaled(uint32_t(sum[j]), s, a4[j], b4[j]));
+                for (uint32_t j = 0; j < 4; ++j)
+                    if (r4 + j < r1) dst[j] = E::of(scaled(uint32_t(sum[j]), s, a4[j], b4[j]));
+            };
+            finish(v, c);
+            if (two) finish(w, c + 4);
         }
         cluster_sync();
     }
@@ -297,32 +332,68 @@ struct Operands {
     uint32_t C;
 };
 
-template <uint32_t BN, class E>
-int launch_strip(ProductParams P, const Operands &o, uint32_t split, cudaStream_t st) {
-    using G = StripShape<BN>;
-    static bool configured[64] = {};
-    int rc = op_configure(product_strip_kernel<BN, E>, G::kSmem, configured);
-    if (rc) return rc;
-    const uint32_t sms = uint32_t(op_sms());
-    if (!sms) return EP_ERR_CUDA;
-    const uint64_t tiles_t = (P.T + BN - 1u) / BN;
-    P.split = split;
+// How strips would share out the work, `split` CTAs to a strip, and an estimate of the time in ns.
+struct StripPlan {
+    uint32_t split, strips, rows, tokens;        // rows and tokens of a block, in whole eights
+    uint64_t grid, ns;
+};
+StripPlan strip_plan(const ProductParams &P, uint32_t C, uint32_t bn, uint32_t split, uint32_t sms) {
+    StripPlan p;
+    const uint64_t tiles_t = (P.T + bn - 1u) / bn;
+    p.split = split;
     // as many strips as make one CTA on each SM, or a whole number of them where strips of 128 rows are more
     const uint64_t least = (uint64_t(P.R) + 127u) / 128u, round = sms / split / tiles_t;
     uint64_t strips = round ? (least + round - 1u) / round * round : least;
     if (strips > P.R) strips = P.R;
-    P.strips = uint32_t(strips);
-    P.rows = (P.R + P.strips - 1u) / P.strips;
-    if (P.rows > 128) return EP_ERR_UNSUPPORTED;
-    P.stage = (P.rows + 7u) / 8u * 1024u + G::kB;
-    P.stages = G::kRoom / P.stage;
+    p.strips = uint32_t(strips);
+    p.rows = (uint32_t((P.R + strips - 1u) / strips) + 7u) / 8u * 8u;
+    p.tokens = P.T < bn ? (P.T + 7u) / 8u * 8u : bn;
+    p.grid = strips * tiles_t * split;
+    // A block of columns takes its operands' way from L2, 100 bytes/ns for an SM, or the instructions', (rows + tokens) of 0.8 ns; the weight
+    // comes from memory at 6200 bytes/ns; a cluster's join takes 1 us and 22 ns for each token (measured between 1 and 128 tokens x 1024 x 8192 and 17408 x 5120).
+    const uint64_t block = 8u * ((p.rows <= 64 ? 64u : 128u) + bn) / 10u, way = (p.rows + p.tokens) * 128u / 100u, each = block > way ? block : way;
+    const uint64_t rounds = 1u + (p.grid - 1u) / sms, busy = rounds * ((P.blocks + split - 1u) / split) * each;
+    const uint64_t memory = uint64_t(P.R) * C / 6200u;
+    p.ns = 3300u + (busy > memory ? busy : memory) + (split > 1 ? 1000u + 22u * P.T : 0u);
+    return p;
+}
+
+template <uint32_t BN, class E>
+int launch_strip(ProductParams P, const Operands &o, const StripPlan &plan, uint32_t sms, cudaStream_t st) {
+    using G = StripShape<BN>;
+    static bool configured[64] = {};
+    int rc = op_configure(product_strip_kernel<BN, E>, G::kMost, configured);
+    if (rc) return rc;
+    if (plan.grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    P.split = plan.split;
+    P.strips = plan.strips;
+    P.m = plan.rows <= 64 ? 64 : 128;
+    P.w_block = plan.rows * 128u;
+    P.x_block = plan.tokens * 128u;
+    const uint32_t block = P.w_block + P.x_block;
+    P.whole = o.C / 128u;
+    // One CTA to an SM with all of its memory; or two that share it, the next one beginning while the last one ends, where there are more CTAs than SMs or
+    // a CTA's share is not much more than fits (4096 x 4096, 1 token: 5.8 us, 6.4 with all memory; 5120 x 17408 19.9, 17.8).
+    const uint32_t room = (plan.grid > sms || plan.split > 2 || uint64_t(block) * P.blocks / plan.split <= 310u * 1024u ? 92u : 204u) * 1024u;
+    // Four blocks to a stage where three stages of them fit: a stage costs the issuing warps some 250 cycles, a block's instructions 130
+    P.chunk = 4;
+    while (P.chunk > 1 && 3 * P.chunk * block > room) P.chunk /= 2;
+    P.stage = P.chunk * block;
+    P.stages = room / P.stage;
     if (P.stages > G::kMaxStages) P.stages = G::kMaxStages;
-    CUtensorMap wm, xm;
-    if ((rc = byte_map(&wm, o.w, o.C, P.R, uint64_t(o.ldw), 128, P.rows, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
-    if ((rc = byte_map(&xm, o.x, o.C, P.T, uint64_t(o.ldx), 128, BN, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
-    const uint64_t grid = uint64_t(P.strips) * tiles_t * split;
-    if (grid > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
-    return op_launch(product_strip_kernel<BN, E>, uint32_t(grid), 128, G::kSmem, split, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+    const uint32_t join = plan.split > 1 ? 512u * BN : 0u;                       // the sums' place
+    uint32_t smem = G::kSmem(P.stages, P.stage);
+    if (smem < G::kSmem(0, 0) + join) smem = G::kSmem(0, 0) + join;
+    CUtensorMap wm, xm, wt, xt;
+    if (P.whole && ((rc = block_map(&wm, o.w, P.whole, P.R, uint64_t(o.ldw), plan.rows, P.chunk)) ||
+                    (rc = block_map(&xm, o.x, P.whole, P.T, uint64_t(o.ldx), plan.tokens, P.chunk))))
+        return rc;
+    if (P.blocks > P.whole) {
+        if ((rc = byte_map(&wt, o.w, o.C, P.R, uint64_t(o.ldw), 128, plan.rows, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+        if ((rc = byte_map(&xt, o.x, o.C, P.T, uint64_t(o.ldx), 128, plan.tokens, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
+        if (!P.whole) wm = wt, xm = xt;
+    } else wt = wm, xt = xm;                             // (not used)
+    return op_launch(product_strip_kernel<BN, E>, uint32_t(plan.grid), 128, smem, plan.split, st, P, wm, xm, wt, xt) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
 // ---- many tokens: a pair of CTAs per tile -----------------------------------------------------------------------------------
@@ -331,16 +402,16 @@ int launch_strip(ProductParams P, const Operands &o, uint32_t split, cudaStream_
 // is summed.
 //   warp 0        brings the operands in
 //   warp 1        of the first CTA issues the products
-//   warps 4 - 7   sums to y
+//   warps 2 - 9   sums to y: two warps to each quarter of the rows, half of the tokens each
 template <uint32_t N>
 struct PairShape {
-    static constexpr uint32_t kA = kBlock * 128, kB = N / 2 * 128, kStage = kA + kB, kStages = N == 256 ? 7 : 9;
-    static constexpr uint32_t kBars = kStages * kStage, kSmem = kBars + 512 + 1024, kCols = 2 * N;
+    static constexpr uint32_t kA = kBlock * 128, kB = N / 2 * 128, kStage = kA + kB, kStages = N == 256 ? 6 : 9;
+    static constexpr uint32_t kBars = kStages * kStage, kScales = kBars + 512, kSmem = kScales + 2 * 4 * N + 1024, kCols = 2 * N, kThreads = 320;
     static_assert(kSmem <= 232448 && kCols <= 512);
 };
 
 template <uint32_t N, class E>
-__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(PairShape<N>::kThreads, 1)
     product_pair_kernel(const __grid_constant__ ProductParams P, const __grid_constant__ CUtensorMap w_map, const __grid_constant__ CUtensorMap x_map) {
     using G = PairShape<N>;
     using T = typename E::T;
@@ -352,7 +423,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
                    slot_addr = done + 8, abort_word = slot_addr + 4;
     if (tid == 0) {
         for (uint32_t i = 0; i < G::kStages; ++i) bar_init(full + 8 * i, 1), bar_init(empty + 8 * i, 1);
-        for (uint32_t i = 0; i < 2; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 8);
+        for (uint32_t i = 0; i < 2; ++i) bar_init(acc_full + 8 * i, 1), bar_init(acc_empty + 8 * i, 16);
         bar_init(done, 1);
         st_smem(abort_word, 0);
         bar_init_done();
@@ -410,30 +481,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(256, 1)
         }
         pair_commit(done, lead);
         bar_drain(done, 0);                               // nothing is in flight when the pair ends
-    } else if (warp >= 4) {
-        const uint32_t quarter = warp & 3u;
-        for (uint32_t tile = pair; tile < tiles && ok; tile += pairs, ++n) {
-            const uint32_t r = (tile % P.strips) * 256u + rank * 128u + quarter * 32u + lane, t0 = (tile / P.strips) * N;
+    } else if (warp >= 2) {
+        const uint32_t quarter = warp & 3u, c0 = warp >= 6 ? N / 2 : 0;
+        // (after a wait that ran out the warps still meet at the barrier, tile by tile, and store nothing)
+        for (uint32_t tile = pair; tile < tiles; tile += pairs, ++n) {
+            const uint32_t r = (tile % P.strips) * 256u + rank * 128u + quarter * 32u + lane, t0 = (tile / P.strips) * N, scales = base + G::kScales + (n & 1u) * 4u * N;
             const float a = P.a && r < P.R ? __ldg(P.a + r) : 1.0f, bias = P.bias && r < P.R ? __ldg(P.bias + r) : 0.0f;
-            float s[N / 32];                              // of token t0 + 32 i + lane
-#pragma unroll
-            for (uint32_t i = 0; i < N / 32; ++i) s[i] = t0 + 32 * i + lane < P.T ? __ldg(P.s + t0 + 32 * i + lane) : 0.0f;
-            ok = bar_wait_warp(acc_full + 8 * (n & 1u), (n >> 1) & 1u, abort_word);
-            if (!ok) break;
+            // (the buffer's last tile but one has been read by all: they have been through the barrier of the last one)
+            if (tid - 64u < N) st_smem(scales + 4 * (tid - 64u), __float_as_uint(t0 + tid - 64u < P.T ? __ldg(P.s + t0 + tid - 64u) : 0.0f));
+            asm volatile("barrier.sync.aligned 1, 256;" ::: "memory");
+            ok = ok && bar_wait_warp(acc_full + 8 * (n & 1u), (n >> 1) & 1u, abort_word);
+            if (!ok) continue;
             tc_after();
-            T *y = static_cast<T *>(P.y) + r;
-#pragma unroll
-            for (uint32_t c = 0; c < N; c += 32) {
-                if (t0 + c >= P.T) break;
-                uint32_t v[32];
-                tc_load32(tmem + (n & 1u) * N + ((quarter * 32u) << 16) + c, v);
-                tc_loaded32(v);
-#pragma unroll
-                for (uint32_t i = 0; i < 32; ++i) {
-                    const float f = scaled(v[i], __shfl_sync(0xFFFFFFFFu, s[c / 32], i), a, bias);
-                    if (r < P.R && t0 + c + i < P.T) y[int64_t(t0 + c + i) * P.ldy] = E::of(f);
-                }
-            }
+            T *y = static_cast<T *>(P.y) + int64_t(t0) * P.ldy + r;
+#pragma unroll 2
+            for (uint32_t c = c0; c < c0 + N / 2 && t0 + c < P.T; c += 16)
+                put_sixteen<E>(tmem + (n & 1u) * N + ((quarter * 32u) << 16) + c, scales + 4 * c, y + int64_t(c) * P.ldy, P.ldy, r < P.R ? min(16u, P.T - t0 - c) : 0u, a, bias);
             tc_before();
             __syncwarp();
             if (lane == 0) first_arrive(acc_empty + 8 * (n & 1u));
@@ -462,16 +525,38 @@ int launch_pair(ProductParams P, const Operands &o, cudaStream_t st) {
     const uint64_t tiles = uint64_t(P.strips) * ((P.T + N - 1u) / N);
     if (tiles > 0x7FFFFFFFu || tiles * P.blocks > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
     const uint32_t pairs = uint32_t(op_sms()) / 2u, grid = 2u * uint32_t(tiles < pairs ? tiles : pairs);
-    return op_launch(product_pair_kernel<N, E>, grid, 256, G::kSmem, 1, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+    return op_launch(product_pair_kernel<N, E>, grid, G::kThreads, G::kSmem, 1, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
+// Which kernel: the least of the estimates.  Pairs take a round of tiles after another, each a time for a block of columns that grows with the SMs at work as L2
+// becomes what bounds it, and a last read-out.  us, strips of 64 / pairs of 128 / of 256 tokens: 128 tokens x 4096^2 8.1 / 9.1 / 12.9, x 10240 x 3840 13.0 / 11.5 /
+// 14.5, 200 x 10240 x 3840 23.2 / 16.2 / 15.2, 512 x 1024 x 8192 12.8 / 15.3 / 23.3, x 8192^2 47.7 / 33.0 / 26.3, 777 x 3000 x 1744 - / 11.7 / 11.2.
 template <class E>
 int launch_product(const ProductParams &P, const Operands &o, cudaStream_t st) {
-    if (P.T <= 16) return launch_strip<16, E>(P, o, 1, st);
-    if (P.T <= 32) return launch_strip<32, E>(P, o, 1, st);
-    if (P.T <= 64) return launch_strip<64, E>(P, o, 1, st);
-    if (P.T <= 128) return launch_strip<128, E>(P, o, 1, st);
-    return launch_pair<256, E>(P, o, st);
+    const uint32_t sms = uint32_t(op_sms()), pairs = sms / 2u;
+    if (!pairs) return EP_ERR_CUDA;
+    const uint32_t bn = P.T <= 16 ? 16u : P.T <= 32 ? 32u : 64u;
+    StripPlan best = strip_plan(P, o.C, bn, 1, sms);
+    if (P.T <= 64)                                       // a cluster for each strip; not fewer than four blocks to a CTA
+        for (const uint32_t split : {2u, 8u})
+            if (P.blocks >= 4u * split) {
+                const StripPlan p = strip_plan(P, o.C, bn, split, sms);
+                if (p.ns < best.ns && p.grid <= sms) best = p;
+            }
+    if (P.T > 64) {
+        const auto pair_ns = [&](uint32_t n, uint64_t block, uint64_t more, uint64_t end) {
+            const uint64_t tiles = uint64_t((P.R + 255u) / 256u) * ((P.T + n - 1u) / n), rounds = (tiles + pairs - 1u) / pairs;
+            const uint64_t one = P.blocks * (block + more * (tiles < pairs ? tiles : pairs) / pairs), busy = rounds * (one > end ? one : end);
+            const uint64_t memory = uint64_t(P.R) * o.C / 6200u;
+            return 3300u + end + (busy > memory ? busy : memory);
+        };
+        const uint64_t of128 = pair_ns(128, 170, 65, 600), of256 = pair_ns(256, 275, 55, 1900);
+        if (of256 < best.ns && of256 <= of128) return launch_pair<256, E>(P, o, st);
+        if (of128 < best.ns) return launch_pair<128, E>(P, o, st);
+    }
+    if (bn == 16) return launch_strip<16, E>(P, o, best, sms, st);
+    if (bn == 32) return launch_strip<32, E>(P, o, best, sms, st);
+    return launch_strip<64, E>(P, o, best, sms, st);
 }
 
 const bool registered = ep::add_status_word([] { return op_status(g_int8_status); });

@@ -125,7 +125,20 @@ __device__ __forceinline__ void tma_load_2d(uint32_t dst, const CUtensorMap *map
     asm volatile("cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
                  ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar) : "memory");
 }
-
+// by a whole warp, one lane of which (`lead`) issues
+__device__ __forceinline__ void bar_expect_by(uint32_t bar, uint32_t bytes, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %2, 0;\n\t@q mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;\n\t}" ::"r"(bar), "r"(bytes), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void tma_load_2d_by(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, uint32_t bar, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %5, 0;\n\t"
+                 "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(bar), "r"(lead) : "memory");
+}
+__device__ __forceinline__ void tma_load_3d_by(uint32_t dst, const CUtensorMap *map, int32_t x, int32_t y, int32_t z, uint32_t bar, uint32_t lead) {
+    asm volatile("{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+                 "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+                 ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar), "r"(lead) : "memory");
+}
 
 // ---- tensor cores ------------------------------------------------------------------------------------------------------
 __device__ __forceinline__ void tc_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -292,6 +305,17 @@ inline int byte_map(CUtensorMap *map, const void *base, uint64_t cols, uint64_t 
     const cuuint32_t box[2] = {box_cols, box_rows}, estr[2] = {1u, 1u};
     return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
               swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+               ? EP_OK : EP_ERR_CUDA;
+}
+// The same bytes as [blocks][rows][128], the blocks being 128 columns each that follow one another in a row: boxes of box_blocks x box_rows x 128 with
+// 128-byte swizzle.  What is left of a row beyond its last whole block is not part of it.
+inline int block_map(CUtensorMap *map, const void *base, uint64_t blocks, uint64_t rows, uint64_t pitch, uint32_t box_rows, uint32_t box_blocks) {
+    const TensorMapFn fn = tensor_map_fn();
+    if (!fn) return EP_ERR_CUDA;
+    const cuuint64_t dims[3] = {128, rows, blocks}, strides[2] = {pitch, 128};
+    const cuuint32_t box[3] = {128, box_rows, box_blocks}, estr[3] = {1u, 1u, 1u};
+    return fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, 3, const_cast<void *>(base), dims, strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE,
+              CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
                ? EP_OK : EP_ERR_CUDA;
 }
 
