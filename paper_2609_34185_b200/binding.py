@@ -464,7 +464,7 @@ INT8_MATMUL_JOB = struct.Struct("@PPPPPPqqqIIIi")
 NORM_JOB = struct.Struct("@PPPPPqqqqq" + 4 * "PqIi" + "fffIIiiiixxxx")
 ROTARY_JOB = struct.Struct("@PPPPqqqqIIIIfiii")
 
-_types = None
+_types = _device_and_stream = None
 
 
 def _float8():
@@ -478,11 +478,16 @@ def _float8():
 
 def _enqueue(f, name, job, dev, stream):
     """f(job, the stream's handle) with device `dev` current."""
-    torch = _types[0]
-    if dev == torch.cuda.current_device():
-        rc = f(job, _stream_handle(stream) or None)
+    global _device_and_stream
+    if _device_and_stream is None:                        # both without the objects that torch.cuda makes of them (0.6 us a call)
+        torch = _types[0]
+        _device_and_stream = (getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device),
+                              getattr(torch._C, "_cuda_getCurrentRawStream", lambda dev: torch.cuda.current_stream(dev).cuda_stream))
+    device, raw = _device_and_stream
+    if dev == device():
+        rc = f(job, (raw(dev) if stream is None else stream.cuda_stream) or None)
     else:
-        with torch.cuda.device(dev):
+        with _types[0].cuda.device(dev):
             rc = f(job, _stream_handle(stream) or None)
     if rc:
         raise EntroPackError(rc, name)
@@ -705,16 +710,20 @@ def int8_matmul(x, x_scales, w, row_scale=None, bias=None, out_dtype: int = BF16
     return out
 
 
+_NO_VECTOR = (0, 0, 0, 0)
+
+
 def _vector(v, T, Cc, dev, what):
     """The fields of an ep_vector: one vector of Cc values, or one for each of v.shape[0] groups of rows."""
     if v is None:
-        return 0, 0, 0, 0
-    code, shape = _types[3].get(v.dtype), v.shape
-    if code is None or v.get_device() != dev or (shape != (Cc,) and (len(shape) != 2 or shape[1] != Cc or shape[0] == 0 or T % shape[0])):
+        return _NO_VECTOR
+    code, shape, stride = _types[3].get(v.dtype), v.shape, v.stride()
+    groups = shape[0] if len(shape) == 2 else 1
+    if code is None or v.get_device() != dev or len(shape) not in (1, 2) or shape[-1] != Cc or groups == 0 or T % groups:
         raise ValueError(f"{what} must be bfloat16, float16 or float32 [{Cc}], or [groups, {Cc}] with groups that divide the {T} rows, on x's CUDA device")
-    if v.stride(-1) != 1 and Cc > 1:
+    if stride[-1] != 1 and Cc > 1:
         raise ValueError(f"{what} must be contiguous along its values")
-    return v.data_ptr(), v.stride(0) if len(shape) == 2 and shape[0] > 1 else 0, shape[0] if len(shape) == 2 else 1, code
+    return v.data_ptr(), stride[0] if groups > 1 else 0, groups, code
 
 
 def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, gate=None, post_weight=None, weight_offset: float = 0.0, eps: float = 1e-6,
