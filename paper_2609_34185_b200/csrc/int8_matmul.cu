@@ -130,6 +130,7 @@ struct ProductParams {
     uint32_t stages, stage;       // in shared memory; bytes of one
     uint32_t whole, chunk;        // whole blocks of 128 columns; how many of them a stage holds
     uint32_t m;                   // rows of the instruction: 64 or 128
+    uint32_t sums;                // where a cluster's sums go, behind the stages
     uint32_t x_block, w_block;    // bytes of a block: rows in whole eights
 };
 
@@ -151,7 +152,7 @@ __device__ __forceinline__ void pair_mma_i8(uint32_t d, uint64_t a, uint64_t b, 
 // The weight's bytes bound it, so every SM has to have an equal share of them and some tens of KB in flight.  A CTA takes a strip of up to 128 rows, however
 // many make the shares equal (the instruction's other lanes are computed from whatever follows in shared memory and never read).  Where a
 // strip would be so low that the tokens' bytes, which every CTA reads, outgrow the weight's, a cluster of CTAs shares the
-// columns of a higher strip; at the end they lay their sums down in shared memory and each adds up its share of the tokens over the cluster.
+// columns of a higher strip; at the end they send one another their sums, and each adds up its share of the tokens.
 template <uint32_t BN>
 struct StripShape {
     static constexpr uint32_t kB = BN * 128, kMaxStages = 32, kTail = 128 * 128;       // kTail: what the last stage's instructions may read beyond it
@@ -203,6 +204,7 @@ __global__ void __launch_bounds__(128)
     tc_before();
     __syncthreads();
     tc_after();
+    if (P.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // (this CTA has begun)
     op_wait_for_stream();
     const uint32_t tmem = ld_smem(slot_addr);
     const uint32_t tile = blockIdx.x / P.split, rank = blockIdx.x % P.split;
@@ -271,54 +273,48 @@ __global__ void __launch_bounds__(128)
         for (uint32_t c = 0; c < BN && t0 + c < P.T; c += 16)
             put_sixteen<E>(tmem + ((warp * 32u) << 16) + c, scales + 4 * c, y + int64_t(c) * P.ldy, P.ldy, r < r1 ? min(16u, P.T - t0 - c) : 0u, a, bias);
     } else {
-        __syncthreads();                                 // (the stages are read no more: every thread has passed `done`)
-#pragma unroll
-        for (uint32_t c = 0; c < BN; c += 16) {
-            if (t0 + c >= P.T) break;
+        // CTA p finishes tokens p each .. (p + 1) each, of which all send it their sums: a place for each CTA, beside the stages, which others may still be
+        // using, four tokens of a row in 16 bytes.  Nobody reads another's memory, so that one barrier is all.
+        const uint32_t tokens = min(BN, P.T - t0), each = ((tokens + P.split - 1u) / P.split + 3u) / 4u * 4u, sums = ring + P.sums;
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");                            // (all have begun)
+        uint32_t owner = 0, local = 0;
+        for (uint32_t c = 0; c < tokens; c += 16) {
             uint32_t v[16];
             tc_load16(tmem + ((warp * 32u) << 16) + c, v);
             tc_loaded16(v);
 #pragma unroll
-            for (uint32_t i = 0; i < 16; ++i)
-                if (mine < 128) st_smem(ring + ((c + i) * 128u + mine) * 4u, v[i]);
+            for (uint32_t i = 0; i < 16; i += 4) {
+                if (mine < 128 && c + i < tokens)
+                    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %0, %1;\n\tst.shared::cluster.v4.u32 [a], {%2, %3, %4, %5};\n\t}"
+                                 ::"r"(sums + ((rank * 128u + mine) * each + local) * 4u), "r"(owner), "r"(v[i]), "r"(v[i + 1]), "r"(v[i + 2]), "r"(v[i + 3]) : "memory");
+                local += 4;
+                if (local == each) local = 0, ++owner;
+            }
         }
         cluster_sync();
-        // This CTA's tokens, four rows to a lane, two tokens to a warp at a time; all CTAs' parts asked for at once, then added up.
-        const uint32_t tokens = min(BN, P.T - t0), c0 = tokens * rank / P.split, c1 = tokens * (rank + 1) / P.split, r4 = r0 + 4u * lane;
-        uint32_t peer[8];
-        float a4[4], b4[4];
+        const uint32_t row = r0 + tid, first = rank * each;
+        if (row < r1) {
+            if (P.a) a = __ldg(P.a + row);
+            if (P.bias) bias = __ldg(P.bias + row);
+            T *y = static_cast<T *>(P.y) + int64_t(t0 + first) * P.ldy + row;
+#pragma unroll 2
+            for (uint32_t q = 0; q < each && first + q < tokens; q += 4) {
+                uint4 sum = make_uint4(0, 0, 0, 0);
 #pragma unroll
-        for (uint32_t p = 0; p < 8; ++p) asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(peer[p]) : "r"(ring), "r"(min(p, P.split - 1u)));
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            a4[j] = P.a && r4 + j < r1 ? __ldg(P.a + r4 + j) : 1.0f;
-            b4[j] = P.bias && r4 + j < r1 ? __ldg(P.bias + r4 + j) : 0.0f;
+                for (uint32_t p = 0; p < 8; ++p)
+                    if (p < P.split) {
+                        const uint4 v = ld_smem16(sums + ((p * 128u + tid) * each + q) * 4u);
+                        sum.x += v.x, sum.y += v.y, sum.z += v.z, sum.w += v.w;
+                    }
+                const uint4 s = ld_smem16(scales + 4 * (first + q));
+                const uint32_t n = tokens - first - q;
+                y[0] = E::of(scaled(sum.x, __uint_as_float(s.x), a, bias));
+                if (n > 1) y[P.ldy] = E::of(scaled(sum.y, __uint_as_float(s.y), a, bias));
+                if (n > 2) y[2 * P.ldy] = E::of(scaled(sum.z, __uint_as_float(s.z), a, bias));
+                if (n > 3) y[3 * P.ldy] = E::of(scaled(sum.w, __uint_as_float(s.w), a, bias));
+                y += 4 * P.ldy;
+            }
         }
-        for (uint32_t c = c0 + warp; c < c1; c += 8) {
-            const bool two = c + 4 < c1;
-            int4 v[8], w[8];
-#pragma unroll
-            for (uint32_t p = 0; p < 8; ++p)
-                if (p < P.split && r4 < r1) {
-                    asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(v[p].x), "=r"(v[p].y), "=r"(v[p].z), "=r"(v[p].w) : "r"(peer[p] + (c * 128u + 4u * lane) * 4u) : "memory");
-                    if (two)
-                        asm volatile("ld.shared::cluster.v4.s32 {%0, %1, %2, %3}, [%4];" : "=r"(w[p].x), "=r"(w[p].y), "=r"(w[p].z), "=r"(w[p].w) : "r"(peer[p] + ((c + 4) * 128u + 4u * lane) * 4u) : "memory");
-                }
-            auto finish = [&](const int4 (&q)[8], uint32_t token) {
-                int32_t sum[4] = {q[0].x, q[0].y, q[0].z, q[0].w};
-#pragma unroll
-                for (uint32_t p = 1; p < 8; ++p)
-                    if (p < P.split) sum[0] += q[p].x, sum[1] += q[p].y, sum[2] += q[p].z, sum[3] += q[p].w;
-                const float s = __uint_as_float(ld_smem(scales + 4 * token));
-                T *dst = static_cast<T *>(P.y) + int64_t(t0 + token) * P.ldy + r4;
-#pragma unroll
-                for (uint32_t j = 0; j < 4; ++j)
-                    if (r4 + j < r1) dst[j] = E::of(scaled(uint32_t(sum[j]), s, a4[j], b4[j]));
-            };
-            finish(v, c);
-            if (two) finish(w, c + 4);
-        }
-        cluster_sync();
     }
     tc_before();
     __syncthreads();
@@ -350,11 +346,12 @@ StripPlan strip_plan(const ProductParams &P, uint32_t C, uint32_t bn, uint32_t s
     p.tokens = P.T < bn ? (P.T + 7u) / 8u * 8u : bn;
     p.grid = strips * tiles_t * split;
     // A block of columns takes its operands' way from L2, 100 bytes/ns for an SM, or the instructions', (rows + tokens) of 0.8 ns; the weight
-    // comes from memory at 6200 bytes/ns; a cluster's join takes 1 us and 22 ns for each token (measured between 1 and 128 tokens x 1024 x 8192 and 17408 x 5120).
+    // comes from memory at 6200 bytes/ns; a cluster's join takes 0.9 us and 0.6 ns for each sum of a strip (fitted to 1 - 64 tokens x 64 x 8192 .. 5120 x 17408:
+    // 1024 x 8192 with clusters of eight and without 4.6 / 8.4 us for one token, 5.3 / 10.5 for 32, 7.9 / 10.5 for 64).
     const uint64_t block = 8u * ((p.rows <= 64 ? 64u : 128u) + bn) / 10u, way = (p.rows + p.tokens) * 128u / 100u, each = block > way ? block : way;
     const uint64_t rounds = 1u + (p.grid - 1u) / sms, busy = rounds * ((P.blocks + split - 1u) / split) * each;
     const uint64_t memory = uint64_t(P.R) * C / 6200u;
-    p.ns = 3300u + (busy > memory ? busy : memory) + (split > 1 ? 1000u + 22u * P.T : 0u);
+    p.ns = 3300u + (busy > memory ? busy : memory) + (split > 1 ? 900u + uint64_t(p.rows) * P.T * 10u / 17u : 0u);
     return p;
 }
 
@@ -374,16 +371,17 @@ int launch_strip(ProductParams P, const Operands &o, const StripPlan &plan, uint
     P.whole = o.C / 128u;
     // One CTA to an SM with all of its memory; or two that share it, the next one beginning while the last one ends, where there are more CTAs than SMs or
     // a CTA's share is not much more than fits (4096 x 4096, 1 token: 5.8 us, 6.4 with all memory; 5120 x 17408 19.9, 17.8).
-    const uint32_t room = (plan.grid > sms || plan.split > 2 || uint64_t(block) * P.blocks / plan.split <= 310u * 1024u ? 92u : 204u) * 1024u;
+    // (The place of a cluster's sums comes off it.)
+    const uint32_t join = plan.split > 1 ? 512u * plan.split * (((plan.tokens + plan.split - 1u) / plan.split + 3u) / 4u * 4u) : 0u, room = (plan.grid > sms || plan.split > 2 || uint64_t(block) * P.blocks / plan.split <= 310u * 1024u ? 92u : 204u) * 1024u - join;
     // Four blocks to a stage where three stages of them fit: a stage costs the issuing warps some 250 cycles, a block's instructions 130
     P.chunk = 4;
     while (P.chunk > 1 && 3 * P.chunk * block > room) P.chunk /= 2;
     P.stage = P.chunk * block;
     P.stages = room / P.stage;
     if (P.stages > G::kMaxStages) P.stages = G::kMaxStages;
-    const uint32_t join = plan.split > 1 ? 512u * BN : 0u;                       // the sums' place
-    uint32_t smem = G::kSmem(P.stages, P.stage);
-    if (smem < G::kSmem(0, 0) + join) smem = G::kSmem(0, 0) + join;
+    // (the last stage's instructions may read beyond it, into the sums' place or the tail)
+    P.sums = P.stages * P.stage + G::kTail;
+    const uint32_t smem = G::kSmem(P.stages, P.stage) + join;
     CUtensorMap wm, xm, wt, xt;
     if (P.whole && ((rc = block_map(&wm, o.w, P.whole, P.R, uint64_t(o.ldw), plan.rows, P.chunk)) ||
                     (rc = block_map(&xm, o.x, P.whole, P.T, uint64_t(o.ldx), plan.tokens, P.chunk))))
