@@ -205,8 +205,6 @@ __global__ void __launch_bounds__(128)
     __syncthreads();
     tc_after();
     if (P.split > 1) asm volatile("barrier.cluster.arrive.relaxed.aligned;" ::: "memory");        // (this CTA has begun)
-    op_wait_for_stream();
-    const uint32_t tmem = ld_smem(slot_addr);
     const uint32_t tile = blockIdx.x / P.split, rank = blockIdx.x % P.split;
     const uint32_t strip = tile % P.strips, t0 = (tile / P.strips) * BN;
     // strips of equal height, but for one row
@@ -214,6 +212,8 @@ __global__ void __launch_bounds__(128)
     // chunks of whole blocks, and what is left of the columns as one of its own
     const uint32_t chunks = (P.whole + P.chunk - 1u) / P.chunk + (P.blocks - P.whole);
     const uint32_t k0 = chunks * rank / P.split, nk = chunks * (rank + 1) / P.split - k0;
+    op_wait_for_stream();
+    const uint32_t tmem = ld_smem(slot_addr);
     // this thread's row of the sums: of 64 rows, tensor memory has 16 in each quarter
     const uint32_t mine = P.m == 64 ? lane < 16 ? warp * 16u + lane : 128u : tid, r = r0 + mine;
     float a = 1.0f, bias = 0.0f;
@@ -403,9 +403,9 @@ int launch_strip(ProductParams P, const Operands &o, const StripPlan &plan, uint
 //   warps 2 - 9   sums to y: two warps to each quarter of the rows, half of the tokens each
 template <uint32_t N>
 struct PairShape {
-    static constexpr uint32_t kA = kBlock * 128, kB = N / 2 * 128, kStage = kA + kB, kStages = N == 256 ? 6 : 9;
-    static constexpr uint32_t kBars = kStages * kStage, kScales = kBars + 512, kSmem = kScales + 2 * 4 * N + 1024, kCols = 2 * N, kThreads = 320;
-    static_assert(kSmem <= 232448 && kCols <= 512);
+    static constexpr uint32_t kA = kBlock * 128, kB = N / 2 * 128, kStage = kA + kB, kStages = N == 256 ? 6 : N == 192 ? 7 : 9;
+    static constexpr uint32_t kBars = kStages * kStage, kScales = kBars + 512, kSmem = kScales + 2 * 4 * N + 1024, kCols = N > 128 ? 512 : 256, kThreads = 320;
+    static_assert(kSmem <= 232448 && 2 * N <= kCols && kB % 1024 == 0 && N % 32 == 0);
 };
 
 template <uint32_t N, class E>
@@ -527,8 +527,9 @@ int launch_pair(ProductParams P, const Operands &o, cudaStream_t st) {
 }
 
 // Which kernel: the least of the estimates.  Pairs take a round of tiles after another, each a time for a block of columns that grows with the SMs at work as L2
-// becomes what bounds it, and a last read-out.  us, strips of 64 / pairs of 128 / of 256 tokens: 128 tokens x 4096^2 8.1 / 9.1 / 12.9, x 10240 x 3840 13.0 / 11.5 /
-// 14.5, 200 x 10240 x 3840 23.2 / 16.2 / 15.2, 512 x 1024 x 8192 12.8 / 15.3 / 23.3, x 8192^2 47.7 / 33.0 / 26.3, 777 x 3000 x 1744 - / 11.7 / 11.2.
+// becomes what bounds it, and a last read-out.  us, strips of 64 / pairs of 128 / 192 / 256 tokens: 128 tokens x 4096^2 8.1 / 9.1 / - / 12.9, 192 x 10240 x 3840 23.2 /
+// 16.1 / 13.3 / 14.9, 512 x 1024 x 8192 10.5 / 14.7 / 17.4 / 22.2, x 5120 x 17408 84.6 / 54.1 / 38.5 / 45.6, x 8192^2 47.7 / 32.7 / 34.4 / 26.5, 777 x 3000 x 1744 - /
+// 11.7 / 9.7 / 10.7, 8192^3 - / 468 / 389 / 355.
 template <class E>
 int launch_product(const ProductParams &P, const Operands &o, cudaStream_t st) {
     const uint32_t sms = uint32_t(op_sms()), pairs = sms / 2u;
@@ -548,8 +549,9 @@ int launch_product(const ProductParams &P, const Operands &o, cudaStream_t st) {
             const uint64_t memory = uint64_t(P.R) * o.C / 6200u;
             return 3300u + end + (busy > memory ? busy : memory);
         };
-        const uint64_t of128 = pair_ns(128, 170, 65, 600), of256 = pair_ns(256, 275, 55, 1900);
-        if (of256 < best.ns && of256 <= of128) return launch_pair<256, E>(P, o, st);
+        const uint64_t of128 = pair_ns(128, 170, 65, 600), of192 = pair_ns(192, 222, 60, 1200), of256 = pair_ns(256, 275, 55, 1900);
+        if (of256 < best.ns && of256 <= of192 && of256 <= of128) return launch_pair<256, E>(P, o, st);
+        if (of192 < best.ns && of192 < of128) return launch_pair<192, E>(P, o, st);
         if (of128 < best.ns) return launch_pair<128, E>(P, o, st);
     }
     if (bn == 16) return launch_strip<16, E>(P, o, best, sms, st);
