@@ -408,7 +408,7 @@ int ep_quantize_rows(const ep_quantize_rows_job *job, void *stream);
 /* y[t, r] = a[r] (s[t] sum_k xq[t, k] wq[r, k]) + bias[r]: the sum over whole numbers in 32 bits on the tensor cores, exact, then rounded to fp32;
  * scales and bias in fp32; one rounding to out_dtype (EP_FP16 overflows to infinity).  The operands may hold all of -128 .. 127.
  * The copy engine reads the operands: d_x and d_w on 16 bytes, C, ldx and ldw multiples of 16, and C < 2^17 (128 * 128 * C < 2^31), else
- * EP_ERR_UNSUPPORTED.  A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
+ * EP_ERR_UNSUPPORTED, as for products of more than about 2^54 operations.  A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
 typedef struct {
     const void *d_x;                /* device: T x C int8, as ep_quantize_rows leaves them */
     const float *d_x_scales;        /* device: T floats s[t] */
@@ -465,7 +465,7 @@ typedef struct {
     void *d_out;                    /* device: the same */
     const void *d_positions;        /* device: T whole numbers of 32 or 64 bits */
     const double *d_frequencies;    /* device: `pairs` frequencies in radians per position, finite */
-    int64_t ldx, ldx_head, ldo, ldo_head;   /* between rows, between heads */
+    int64_t ldx, ldx_head, ldo, ldo_head;   /* between rows, between heads; of d_out (where there are several) >= dim */
     uint32_t T, heads, dim, pairs;  /* 1 <= pairs, 2 * pairs <= dim <= 1024, heads <= 65535 */
     float factor;
     int32_t dtype;                  /* EP_BF16, EP_FP16 or EP_FP32 */

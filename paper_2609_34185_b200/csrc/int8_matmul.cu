@@ -521,8 +521,10 @@ int launch_pair(ProductParams P, const Operands &o, cudaStream_t st) {
     if ((rc = byte_map(&xm, o.x, o.C, P.T, uint64_t(o.ldx), 128, N / 2, CU_TENSOR_MAP_SWIZZLE_128B))) return rc;
     P.strips = (P.R + 255u) / 256u;
     const uint64_t tiles = uint64_t(P.strips) * ((P.T + N - 1u) / N);
-    if (tiles > 0x7FFFFFFFu || tiles * P.blocks > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
-    const uint32_t pairs = uint32_t(op_sms()) / 2u, grid = 2u * uint32_t(tiles < pairs ? tiles : pairs);
+    const uint32_t pairs = uint32_t(op_sms()) / 2u;
+    if (!pairs) return EP_ERR_CUDA;
+    if (tiles > 0x7FFFFFFFu || (tiles / pairs + 1u) * P.blocks > 0x7FFFFFFFu) return EP_ERR_UNSUPPORTED;
+    const uint32_t grid = 2u * uint32_t(tiles < pairs ? tiles : pairs);
     return op_launch(product_pair_kernel<N, E>, grid, G::kThreads, G::kSmem, 1, st, P, wm, xm) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 

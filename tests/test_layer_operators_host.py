@@ -41,7 +41,7 @@ def rotary_job(x=P, o=2 * P, at=P, f=P, ldx=64, ldxh=64, ldo=64, ldoh=64, T=4, H
                 dict(zdtype=ep.FP8_E4M3, s=P, lds=0), dict(zdtype=ep.INT8, s=P + 1), dict(h=P, ldh=63), dict(r=P, ldr=10), dict(h=P, hdtype=ep.INT8), dict(h=P, r=P, ldh=64, ldr=72),
                 dict(w=vector(P, 64, 3)), dict(w=vector(P, 64, 0)), dict(d=vector(P, 60, 2)), dict(g=vector(P, 64, 1, ep.INT8)), dict(p=vector(P + 1, 64, 1))]),
     (rotary_job, [dict(x=0), dict(o=0), dict(at=0), dict(f=0), dict(H=0), dict(H=65536), dict(pairs=0), dict(pairs=33), dict(D=1025), dict(dtype=ep.INT8), dict(bits=16), dict(at=P + 2),
-                  dict(at=P + 4, bits=64), dict(f=P + 4), dict(ldx=-1), dict(x=P, o=P, ldo=72), dict(x=P + 1)]),
+                  dict(at=P + 4, bits=64), dict(f=P + 4), dict(ldx=-1), dict(x=P, o=P, ldo=72), dict(x=P + 1), dict(ldo=32), dict(H=2, ldoh=0), dict(H=2, ldo=128, ldoh=63)]),
 ])
 def test_bad_arguments(job, wrong):
     assert job(T=0) == 0
