@@ -205,6 +205,76 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
     }
 }
 
+// ---- many short rows: a part of a warp each, one after another ----------------------------------------------------------------------
+// Rows of up to 256 values (the heads of queries and keys): a CTA for four of them spends its time on starting.  Here a lane keeps its
+// piece of the vectors in registers and has the next row's piece under way.
+template <class X, class H>
+__global__ void __launch_bounds__(256) norm_short_kernel(const __grid_constant__ NormParams P) {
+    constexpr uint32_t XB = sizeof(typename X::T), HB = sizeof(typename H::T);
+    op_wait_for_stream();
+    const uint32_t of = threadIdx.x / P.lanes, l = threadIdx.x - of * P.lanes, step = gridDim.x * P.rows;
+    const bool mine = l * 8u < P.C;
+    RowGroup group{nullptr, 1, 0, 0, 0, P.lanes};
+    Pair p[4], g[4], w[4], d[4];
+    auto keep = [&](const NormVector &V, float offset, Pair (&to)[4]) {
+        if (V.d) load_vector(V, 0, l * 8u, mine ? 8u : 0u, offset, to);
+    };
+    keep(P.p, P.offset, p), keep(P.g, 0.0f, g), keep(P.w, P.offset, w), keep(P.d, 0.0f, d);
+    Eight<8 * XB> x;
+    Eight<8 * HB> h;
+    auto ask = [&](uint64_t row) {
+        const uint32_t n = mine && row < P.T ? 8u : 0u;
+        load_eight<8 * XB>(P.x + int64_t(row) * P.ldx, l * 8u, n, true, x);
+        if (P.h) load_eight<8 * HB>(P.h + int64_t(row) * P.ldh, l * 8u, n, true, h);
+    };
+    ask(uint64_t(blockIdx.x) * P.rows + of);
+    for (uint64_t base = uint64_t(blockIdx.x) * P.rows; base < P.T; base += step) {
+        const uint64_t row = base + of;
+        const bool there = mine && row < P.T;
+        const uint32_t n[1] = {mine ? 8u : 0u};
+        Pair v[1][4], old[4];
+        to_pairs<X>(x, v[0]);
+        if (P.h) to_pairs<H>(h, old);
+        ask(row + step);
+        auto times = [&](const Pair (&by)[4]) {
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[0][j] = v[0][j] * by[j];
+        };
+        if (P.p.d) {
+            normed<1>(P, group, n, v);
+            times(p);
+        }
+        if (P.g.d) times(g);
+        if (P.h)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[0][j] = fma2(Pair(P.c), old[j], v[0][j]);
+        if (P.r && there) store_eight<H>(P.r + int64_t(row) * P.ldr + l * 8u * HB, v[0]);
+        normed<1>(P, group, n, v);
+        if (P.w.d) times(w);
+        if (P.d.d)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) v[0][j] = v[0][j] + d[j];
+        uint8_t *z = P.z + int64_t(row) * P.ldz;
+        if (P.z_dtype == EP_INT8) {
+            const Int8Scale q = int8_pieces<1>(group, v, [&](uint32_t, uint32_t lo, uint32_t hi) {
+                if (there) *reinterpret_cast<uint2 *>(z + l * 8u) = make_uint2(lo, hi);
+            });
+            if (l == 0 && there) reinterpret_cast<float *>(P.s)[row] = q.s;
+        } else if (P.z_dtype == EP_FP8_E4M3) {
+            e4m3_pieces<1>(group, v, [&](uint32_t, uint32_t lo, uint32_t hi, uint8_t e) {
+                if (there) {
+                    *reinterpret_cast<uint2 *>(z + l * 8u) = make_uint2(lo, hi);
+                    if ((l & 15u) == 0) P.s[int64_t(row) * P.lds + l / 16u] = e;
+                }
+            });
+        } else if (there) {
+            if (P.z_dtype == EP_FP32) store_eight<Fp32>(z + l * 32u, v[0]);
+            else if (P.z_dtype == EP_FP16) store_eight<Fp16>(z + l * 16u, v[0]);
+            else store_eight<Bf16>(z + l * 16u, v[0]);
+        }
+    }
+}
+
 // ---- many rows: brought into shared memory ahead ----------------------------------------------------------------------------------
 // A row's exchanges between its warps take longer than its bytes, so an SM works on several rows at a time, a group of warps to each, and bulk
 // copies bring in the next ones meanwhile.  Vectors wait in shared memory as floats: read from L1
@@ -413,8 +483,18 @@ bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem) {
 
 template <class X, class H>
 int try_stream(NormParams P, cudaStream_t st, bool &done) {
-    const uint32_t sms = uint32_t(op_sms());
+    const uint32_t sms = uint32_t(op_sms()), pieces = P.C / 8u;
     uint32_t smem = 0;
+    if (sms && P.C % 8 == 0 && pieces <= 32 && !P.p.rows && !P.g.rows && !P.w.rows && !P.d.rows) {
+        P.lanes = 32;
+        while (P.lanes / 2 >= pieces) P.lanes /= 2;
+        P.rows = 256u / P.lanes;
+        const uint32_t ctas = (P.T - 1u) / P.rows + 1u, most = 3u * sms;         // (three CTAs fit an SM)
+        if (ctas > most) {
+            done = true;
+            return op_launch(norm_short_kernel<X, H>, most, 256, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+        }
+    }
     done = sms && stream_shape(P, P.C * uint32_t(sizeof(typename X::T) + (P.h ? sizeof(typename H::T) : 0)), sms, smem);
     return done ? launch_stream<X, H, 4>(P, smem, sms, st) : EP_OK;
 }

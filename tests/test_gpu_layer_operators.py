@@ -320,6 +320,26 @@ def test_norm_of_many_rows(T, C, dtype, wide, center):
 
 
 @gpu
+@pytest.mark.parametrize("dtype,wide", [(torch.bfloat16, torch.bfloat16), (torch.bfloat16, torch.float32), (torch.float16, torch.float16), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("T,C", [(120001, 8), (70000, 24), (30011, 64), (30000, 72), (20001, 128), (9000, 136), (10007, 256)])
+def test_norm_of_many_short_rows(T, C, dtype, wide):
+    x, v = norm_inputs(T, C, dtype, wide, 1, T + C)
+    x[5], x[T - 3, 3] = 0.0, math.inf
+    for center in (False, True):
+        for left in ((), ("post_weight", "gate", "bias")):
+            given = {k: t for k, t in v.items() if k not in left}
+            z, r = ep.norm(x, residual_scale=0.7, center=center, **given)
+            want, r_want = normed(x, residual_scale=0.7, center=center, **given)
+            fine = torch.arange(T, device="cuda") != T - 3
+            assert near(z[fine], tuple(t[fine] for t in want)) and near(r[fine], tuple(t[fine] for t in r_want))
+            z, _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.FP32, **given)
+            (q, s), _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.FP8_E4M3, **given)
+            (q8, s8), _ = ep.norm(x, residual_scale=0.7, center=center, residual_out=r, out_dtype=ep.INT8, **given)
+            same = lambda a, b: torch.equal(a.view(torch.uint8), b.view(torch.uint8))  # noqa: E731
+            assert all(map(same, (q, s, q8, s8), ep.quantize_blocks(z) + ep.quantize_rows(z)))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("T,C", SIZES + [(70, 640)])
 def test_norm_into_the_containers(T, C, dtype):
