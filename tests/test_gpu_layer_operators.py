@@ -15,6 +15,9 @@ Rotary: the angle's fraction of a turn is rounded to 24 bits of half a turn, pi 
 frequency to 2^-52 of itself twice over.  Cosine and sine are good to 2 units of 2^-24 (CUDA's bound for sincospi is 2), the factor and the two products and
 their sum add 4 of |u| + |v|.  The oracle's angles are in 80 bits."""
 import math
+import os
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -83,6 +86,15 @@ def test_quantize_rows_edges(C):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("C", [8, 300, 33000])
+def test_quantize_rows_what_is_not_finite_in_16_bits(C, dtype):
+    x = torch.randn(6, C, generator=cuda(8), device="cuda").to(dtype)
+    x[1, C - 1], x[2, 0], x[3, C // 2], x[4] = math.inf, -math.inf, math.nan, 0.0
+    assert_rows(ep.quantize_rows(x), rounded_rows(x))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [torch.float16, torch.float32])
 def test_quantize_rows_views_and_outputs(dtype):
     # rows of any distance and alignment, results into parts of larger buffers whose other bytes stay
@@ -131,6 +143,16 @@ def test_product(T, R, C, out):
     x, s, w, a, bias = operands(T, R, C, T * 31 + R + C)
     check_product(ep.int8_matmul(x, s, w, row_scale=a, bias=bias, out_dtype=CODE[out]), x, s, w, a, bias)
     check_product(ep.int8_matmul(x, s, w, out_dtype=CODE[out]), x, s, w, None, None)
+
+
+@gpu
+@pytest.mark.parametrize("T,R,C", [(1, 64, 8208), (7, 1000, 4112), (20, 1000, 8192), (33, 2049, 8208), (48, 300, 16400), (64, 1024, 8192), (64, 5120, 17424), (1, 17408, 5120), (3, 19001, 528),
+                                   (64, 30000, 128), (150, 10240, 2000), (192, 8000, 2064), (400, 4096, 512), (513, 4100, 1040), (900, 2100, 3088)])
+def test_product_shapes_of_the_ways_it_is_shared_out(T, R, C):
+    # strips alone and in clusters of two and eight, one round and several; pairs of 128, 192 and 256 tokens; with columns left over from whole blocks and without
+    x, s, w, a, bias = operands(T, R, C, T + R + C)
+    check_product(ep.int8_matmul(x, s, w, a, bias, out_dtype=ep.FP32), x, s, w, a, bias)
+    assert ep.last_device_status() == 0
 
 
 @gpu
@@ -630,6 +652,98 @@ def test_on_a_given_stream():
 
 
 @gpu
+@pytest.mark.parametrize("T", [3, 40, 1500])
+def test_two_graphs_at_once(T):
+    # the same operators on other data, on two streams side by side, many times
+    made = []
+    for seed in (11, 12):
+        calls, flat, _ = each_operator(seed, T)
+        calls()
+        torch.cuda.synchronize()
+        want = [t.clone() for t in flat()]
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            for _ in range(5):
+                calls()
+        for t in flat():
+            t.zero_()
+        made.append((graph, stream, flat, want, calls))    # (calls holds the inputs)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for graph, stream, *_ in made:
+            with torch.cuda.stream(stream):
+                graph.replay()
+    torch.cuda.synchronize()
+    for _, _, flat, want, _ in made:
+        assert all(torch.equal(g, w) for g, w in zip(flat(), want))
+    assert ep.last_device_status() == 0
+
+
+@gpu
+def test_steps_one_behind_another_need_no_wait():
+    # each operator reads what the one before it wrote, and each may come up while that one still runs: the same bits as with waits
+    x0 = torch.randn(50, 1024, generator=cuda(2), device="cuda", dtype=torch.bfloat16)
+    w, a = ep.quantize_rows(torch.randn(1024, 1024, generator=cuda(3), device="cuda") * 0.03)
+    f, at = ep.rotary_frequencies(64), torch.arange(50, device="cuda")
+
+    def steps(wait):
+        x, h = x0, x0
+        for _ in range(20):
+            (q, s), h = ep.norm(x, residual=h, out_dtype=ep.INT8)
+            wait()
+            x = ep.int8_matmul(q, s, w, row_scale=a)
+            wait()
+            heads = x.view(50, 16, 64)
+            ep.rotary(heads, at, f, out=heads)
+            wait()
+            q, s = ep.quantize_rows(x)
+            wait()
+            x = ep.int8_matmul(q, s, w, row_scale=a)
+            wait()
+        torch.cuda.synchronize()
+        return x, h
+
+    want = steps(torch.cuda.synchronize)
+    for _ in range(3):
+        assert all(torch.equal(g, w) for g, w in zip(steps(lambda: None), want))
+
+
+FIRST_CALLS = """
+import torch, {name} as ep
+torch.zeros(1, device="cuda")
+x = torch.randn(1300, 512, device="cuda", dtype=torch.bfloat16)
+w = torch.randint(-127, 128, (300, 512), device="cuda", dtype=torch.int8)
+at, f = torch.arange(1300, device="cuda"), ep.rotary_frequencies(64)
+q, s = torch.empty(1300, 512, device="cuda", dtype=torch.int8), torch.empty(1300, device="cuda")
+outs = [torch.empty(1300, 512, device="cuda", dtype=torch.bfloat16), torch.empty(1300, 300, device="cuda"), torch.empty(5, 300, device="cuda"), torch.empty(1300, 8, 64, device="cuda", dtype=torch.bfloat16)]
+torch.cuda.synchronize()
+def calls():
+    ep.norm(x, out=outs[0])
+    ep.quantize_rows(x, out=(q, s))
+    ep.int8_matmul(q, s, w, out=outs[1])
+    ep.int8_matmul(q[:5], s[:5], w, out=outs[2])
+    ep.rotary(x.view(1300, 8, 64), at, f, out=outs[3])
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    calls()
+graph.replay()
+torch.cuda.synchronize()
+got = [t.clone() for t in outs]
+calls()
+torch.cuda.synchronize()
+assert all(torch.equal(a, b) for a, b in zip(got, outs)) and outs[1].abs().sum() > 0
+print("captured")
+"""
+
+
+@gpu
+def test_first_calls_of_a_process_can_be_captured():
+    done = subprocess.run([sys.executable, "-c", FIRST_CALLS.format(name=ep.__name__)], capture_output=True, text=True, timeout=300,
+                          cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    assert done.returncode == 0 and done.stdout.split() == ["captured"], done.stderr[-2000:]
+
+
+@gpu
 def test_no_rows():
     e = lambda *shape, dtype=torch.bfloat16: torch.empty(*shape, dtype=dtype, device="cuda")  # noqa: E731
     q, s = ep.quantize_rows(e(0, 64))
@@ -653,6 +767,12 @@ def test_more_than_32_bits_of_values():
     z = ep.norm(x, out=x)                                  # (each row is read before it is written)
     assert torch.equal(z[0], z[-1])
     del q
+    a, w = (torch.randint(-127, 128, (n, 64), generator=cuda(n), device="cuda", dtype=torch.int8) for n in (T, C))
+    a[-1], s[0] = a[0], 0.01
+    s[-1] = s[0]
+    y = ep.int8_matmul(a, s, w)
+    assert torch.equal(y[0], y[-1]) and torch.equal(y[0], ((w.double() @ a[0].double()).float() * s[0]).to(torch.bfloat16))
+    del y
     heads = z.view(T, 256, 128)
     at = torch.zeros(T, dtype=torch.int32, device="cuda")
     at[0] = at[-1] = 77
