@@ -160,7 +160,7 @@ __device__ __forceinline__ void pair_mma_i8(uint32_t d, uint64_t a, uint64_t b, 
 // SM's way from L2, which brings all tokens), 1024 x 8192 by 32 in clusters of eight 5.3.
 template <uint32_t BN>
 struct StripShape {
-    static constexpr uint32_t kB = BN * 128, kMaxStages = 32, kTail = 128 * 128;       // kTail: what the last stage's instructions may read beyond it
+    static constexpr uint32_t kMaxStages = 32, kTail = 128 * 128;       // kTail: what the last stage's instructions may read beyond it
     static constexpr uint32_t kBars = 0, kScales = 16 * kMaxStages + 16, kStages = 2048;
     static constexpr uint32_t kSmem(uint32_t stages, uint32_t stage) { return kStages + stages * stage + kTail + 1024; }
     static constexpr uint32_t kMost = 226 * 1024;
