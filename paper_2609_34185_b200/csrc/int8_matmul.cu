@@ -590,8 +590,8 @@ extern "C" int ep_quantize_rows(const ep_quantize_rows_job *job, void *stream) {
     P.T = j.T;
     P.C = j.C;
     P.half = j.x_dtype == EP_FP16;
-    P.x_vec = aligned(j.d_x, 16) && P.ldx % 16 == 0;
-    P.q_vec = aligned(j.d_q, 8) && j.ldq % 8 == 0;
+    P.x_vec = aligned(j.d_x, 16) && P.ldx % 16 == 0 ? 2 : aligned(j.d_x, 8) && P.ldx % 8 == 0 ? 1 : 0;
+    P.q_vec = aligned(j.d_q, 8) && j.ldq % 8 == 0 ? 2 : aligned(j.d_q, 4) && j.ldq % 4 == 0 ? 1 : 0;
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     return size == 4 ? launch_rows<32>(P, st) : launch_rows<16>(P, st);
 }

@@ -135,7 +135,7 @@ __device__ __forceinline__ void e4m3_pieces(const RowGroup &group, Pair (&v)[N][
     }
 }
 
-// ---- few rows, or rows that do not begin on 16 bytes: straight from memory ------------------------------------------------------
+// ---- any rows: straight from memory -------------------------------------------------------------------------------------------
 template <uint32_t XBITS, uint32_t HBITS, uint32_t N, uint32_t THREADS>
 __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams P) {
     __shared__ uint32_t room[64];
@@ -206,6 +206,83 @@ __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ N
     }
 }
 
+// ---- few rows that begin on 16 bytes: the same, a piece to a lane, with types known -----------------------------------------------------
+// (Some tens of rows wait for launch and exchanges, some hundreds for instructions: 5120 columns in 7800 of a warp's the general way.)
+template <class X, class H>
+__global__ void __launch_bounds__(1024) norm_few_kernel(const __grid_constant__ NormParams P) {
+    constexpr uint32_t XB = sizeof(typename X::T), HB = sizeof(typename H::T);
+    __shared__ uint32_t room[64];
+    op_wait_for_stream();
+    const uint32_t warp = threadIdx.x >> 5, of = warp / P.warps, row = blockIdx.x * P.rows + of, l = threadIdx.x - of * P.warps * 32u;
+    const bool there = row < P.T && l * 8u < P.C;
+    RowGroup group{room, P.warps, of * P.warps, 1u + of, 0};
+    Eight<8 * XB> x;
+    Eight<8 * HB> h;
+    const uint32_t n[1] = {there ? 8u : 0u};
+    load_eight<8 * XB>(P.x + int64_t(row) * P.ldx, l * 8u, n[0], 2, x);
+    if (P.h) load_eight<8 * HB>(P.h + int64_t(row) * P.ldh, l * 8u, n[0], 2, h);
+    Pair v[1][4];
+    to_pairs<X>(x, v[0]);
+    auto vector = [&](const NormVector &V, float offset, Pair (&w)[4]) {
+        const uint8_t *at = V.d + (V.rows ? int64_t(row / V.rows) * V.pitch : 0);
+        if (V.dtype == EP_FP32) {
+            Eight<32> e;
+            load_eight<32, true>(at, l * 8u, n[0], 2, e);
+            to_pairs<Fp32>(e, w);
+        } else {
+            Eight<16> e;
+            load_eight<16, true>(at, l * 8u, n[0], 2, e);
+            to_pairs<16>(e, V.dtype == EP_FP16, w);
+        }
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
+    };
+    auto times = [&](const NormVector &V, float offset) {
+        Pair w[4];
+        vector(V, offset, w);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) v[0][j] = v[0][j] * w[j];
+    };
+    if (P.p.d) {
+        normed<1>(P, group, n, v);
+        times(P.p, P.offset);
+    }
+    if (P.g.d) times(P.g, 0.0f);
+    if (P.h) {
+        Pair old[4];
+        to_pairs<H>(h, old);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) v[0][j] = fma2(Pair(P.c), old[j], v[0][j]);
+    }
+    if (P.r && there) store_eight<H>(P.r + int64_t(row) * P.ldr + l * 8u * HB, v[0]);
+    normed<1>(P, group, n, v);
+    if (P.w.d) times(P.w, P.offset);
+    if (P.d.d) {
+        Pair d[4];
+        vector(P.d, 0.0f, d);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) v[0][j] = v[0][j] + d[j];
+    }
+    uint8_t *z = P.z + int64_t(row) * P.ldz;
+    if (P.z_dtype == EP_INT8) {
+        const Int8Scale q = int8_pieces<1>(group, v, [&](uint32_t, uint32_t lo, uint32_t hi) {
+            if (there) *reinterpret_cast<uint2 *>(z + l * 8u) = make_uint2(lo, hi);
+        });
+        if (l == 0 && there) reinterpret_cast<float *>(P.s)[row] = q.s;
+    } else if (P.z_dtype == EP_FP8_E4M3) {
+        e4m3_pieces<1>(group, v, [&](uint32_t, uint32_t lo, uint32_t hi, uint8_t e) {
+            if (there) {
+                *reinterpret_cast<uint2 *>(z + l * 8u) = make_uint2(lo, hi);
+                if ((l & 15u) == 0) P.s[int64_t(row) * P.lds + l / 16u] = e;
+            }
+        });
+    } else if (there) {
+        if (P.z_dtype == EP_FP32) store_eight<Fp32>(z + l * 32u, v[0]);
+        else if (P.z_dtype == EP_FP16) store_eight<Fp16>(z + l * 16u, v[0]);
+        else store_eight<Bf16>(z + l * 16u, v[0]);
+    }
+}
+
 // ---- many short rows: a part of a warp each, one after another ----------------------------------------------------------------------
 // Rows of up to 256 values (the heads of queries and keys): a CTA for four of them spends its time on starting (327680 x 128 82 us).  Here a lane keeps its
 // piece of the vectors in registers and has the next row's piece under way.
@@ -225,8 +302,8 @@ __global__ void __launch_bounds__(256) norm_short_kernel(const __grid_constant__
     Eight<8 * HB> h;
     auto ask = [&](uint64_t row) {
         const uint32_t n = mine && row < P.T ? 8u : 0u;
-        load_eight<8 * XB>(P.x + int64_t(row) * P.ldx, l * 8u, n, true, x);
-        if (P.h) load_eight<8 * HB>(P.h + int64_t(row) * P.ldh, l * 8u, n, true, h);
+        load_eight<8 * XB>(P.x + int64_t(row) * P.ldx, l * 8u, n, 2, x);
+        if (P.h) load_eight<8 * HB>(P.h + int64_t(row) * P.ldh, l * 8u, n, 2, h);
     };
     ask(uint64_t(blockIdx.x) * P.rows + of);
     for (uint64_t base = uint64_t(blockIdx.x) * P.rows; base < P.T; base += step) {
@@ -483,7 +560,7 @@ bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem) {
 }
 
 template <class X, class H>
-int try_stream(NormParams P, cudaStream_t st, bool &done) {
+int launch_whole(NormParams P, cudaStream_t st, bool &done) {
     const uint32_t sms = uint32_t(op_sms()), pieces = P.C / 8u;
     uint32_t smem = 0;
     if (sms && P.C % 8 == 0 && pieces <= 32 && !P.p.rows && !P.g.rows && !P.w.rows && !P.d.rows) {
@@ -497,7 +574,14 @@ int try_stream(NormParams P, cudaStream_t st, bool &done) {
         }
     }
     done = sms && stream_shape(P, P.C * uint32_t(sizeof(typename X::T) + (P.h ? sizeof(typename H::T) : 0)), sms, smem);
-    return done ? launch_stream<X, H, 4>(P, smem, sms, st) : EP_OK;
+    if (done) return launch_stream<X, H, 4>(P, smem, sms, st);
+    if (pieces > 16 && pieces <= 1024) {                 // (shorter rows share a warp the general way)
+        done = true;
+        P.warps = (pieces + 31u) / 32u;
+        P.rows = P.warps >= 4 ? 1u : 4u / P.warps;
+        return op_launch(norm_few_kernel<X, H>, (P.T - 1u) / P.rows + 1u, P.warps * P.rows * 32u, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
+    }
+    return EP_OK;
 }
 
 template <uint32_t XBITS, uint32_t HBITS>
@@ -520,6 +604,8 @@ bool aligned(const void *p, uintptr_t n) { return (reinterpret_cast<uintptr_t>(p
 // a row of `size`-byte values every ld of them: whether it is one, and whether each begins on `n` bytes
 bool rows_fit(const void *p, int64_t ld, uint32_t C, uint32_t size) { return aligned(p, size) && ld >= int64_t(C) && ld < (int64_t(1) << 40); }
 bool rows_begin_on(uint32_t n, const void *p, int64_t ld, uint32_t size) { return aligned(p, n) && ld * size % n == 0; }
+// 2 if they begin on n bytes, 1 on half of that, else 0
+uint32_t rows_vec(uint32_t n, const void *p, int64_t ld, uint32_t size) { return rows_begin_on(n, p, ld, size) ? 2u : rows_begin_on(n / 2, p, ld, size) ? 1u : 0u; }
 
 int vector_of(const ep_vector &v, uint32_t T, uint32_t C, NormVector &out) {
     std::memset(&out, 0, sizeof(out));
@@ -529,7 +615,7 @@ int vector_of(const ep_vector &v, uint32_t T, uint32_t C, NormVector &out) {
     out.d = static_cast<const uint8_t *>(v.d);
     out.dtype = v.dtype;
     if (v.groups > 1) out.pitch = v.ld * size, out.rows = T / v.groups;
-    out.vec = rows_begin_on(16, v.d, v.groups > 1 ? v.ld : 0, size);
+    out.vec = rows_vec(16, v.d, v.groups > 1 ? v.ld : 0, size);
     return EP_OK;
 }
 
@@ -577,23 +663,23 @@ extern "C" int ep_norm(const ep_norm_job *job, void *stream) {
     P.r_dtype = j.residual_dtype;
     P.z_dtype = j.z_dtype;
     P.center = j.center != 0;
-    P.x_vec = rows_begin_on(16, j.d_x, j.ldx, xs);
-    P.h_vec = j.d_residual && rows_begin_on(16, j.d_residual, j.ld_residual, hs);
-    P.r_vec = j.d_residual_out && rows_begin_on(16, j.d_residual_out, j.ld_residual_out, hs);
-    P.z_vec = rows_begin_on(zs == 1 ? 8 : 16, j.d_z, j.ldz, zs);
+    P.x_vec = rows_vec(16, j.d_x, j.ldx, xs);
+    P.h_vec = j.d_residual ? rows_vec(16, j.d_residual, j.ld_residual, hs) : 0u;
+    P.r_vec = j.d_residual_out ? rows_vec(16, j.d_residual_out, j.ld_residual_out, hs) : 0u;
+    P.z_vec = rows_vec(zs == 1 ? 8 : 16, j.d_z, j.ldz, zs);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
     // what the stream's kernel reads and writes in whole pieces: bulk copies on 16 bytes, stores of 32-bit values on 32
-    bool whole = P.x_vec && (!P.h || P.h_vec) && rows_begin_on(zs == 1 ? 8 : 8 * zs, j.d_z, j.ldz, zs) && (!P.r || rows_begin_on(8 * hs, j.d_residual_out, j.ld_residual_out, hs));
-    for (const NormVector *v : {&P.p, &P.g, &P.w, &P.d}) whole = whole && (!v->d || v->vec);
+    bool whole = P.C % 8 == 0 && P.x_vec == 2 && (!P.h || P.h_vec == 2) && rows_begin_on(zs == 1 ? 8 : 8 * zs, j.d_z, j.ldz, zs) && (!P.r || rows_begin_on(8 * hs, j.d_residual_out, j.ld_residual_out, hs));
+    for (const NormVector *v : {&P.p, &P.g, &P.w, &P.d}) whole = whole && (!v->d || v->vec == 2);
     if (whole) {
         bool done = false;
         const int32_t h = P.h || P.r ? j.residual_dtype : j.x_dtype;
         rc = EP_OK;
-        if (j.x_dtype == EP_BF16 && h == EP_BF16) rc = try_stream<Bf16, Bf16>(P, st, done);
-        if (j.x_dtype == EP_BF16 && h == EP_FP32) rc = try_stream<Bf16, Fp32>(P, st, done);
-        if (j.x_dtype == EP_FP16 && h == EP_FP16) rc = try_stream<Fp16, Fp16>(P, st, done);
-        if (j.x_dtype == EP_FP16 && h == EP_FP32) rc = try_stream<Fp16, Fp32>(P, st, done);
-        if (j.x_dtype == EP_FP32 && h == EP_FP32) rc = try_stream<Fp32, Fp32>(P, st, done);
+        if (j.x_dtype == EP_BF16 && h == EP_BF16) rc = launch_whole<Bf16, Bf16>(P, st, done);
+        if (j.x_dtype == EP_BF16 && h == EP_FP32) rc = launch_whole<Bf16, Fp32>(P, st, done);
+        if (j.x_dtype == EP_FP16 && h == EP_FP16) rc = launch_whole<Fp16, Fp16>(P, st, done);
+        if (j.x_dtype == EP_FP16 && h == EP_FP32) rc = launch_whole<Fp16, Fp32>(P, st, done);
+        if (j.x_dtype == EP_FP32 && h == EP_FP32) rc = launch_whole<Fp32, Fp32>(P, st, done);
         if (done) return rc;
     }
     if (xs == 4) return j.d_residual && hs == 4 ? launch_norm<32, 32>(P, st) : launch_norm<32, 16>(P, st);

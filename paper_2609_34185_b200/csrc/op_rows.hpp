@@ -15,17 +15,26 @@ struct Eight {
 // which of a piece's eight values lie inside the row: the first n
 __device__ __forceinline__ uint32_t inside(uint32_t c, uint32_t C) { return c < C ? min(8u, C - c) : 0u; }
 
-// Values c .. c + n of a row; `vec`: the row begins on 16 bytes.  What is outside reads as zero.  KEPT: vectors that every row needs, which
+// Values c .. c + n of a row; `vec`: 2 if rows begin on 16 bytes, 1 on 8, else 0.  What is outside reads as zero.  KEPT: vectors that every row needs, which
 // stay in L1; rows are read once.
 template <uint32_t BITS, bool KEPT = false>
-__device__ __forceinline__ void load_eight(const uint8_t *row, uint32_t c, uint32_t n, bool vec, Eight<BITS> &e) {
-    if (vec && n == 8) {
+__device__ __forceinline__ void load_eight(const uint8_t *row, uint32_t c, uint32_t n, uint32_t vec, Eight<BITS> &e) {
+    if (vec == 2 && n == 8) {
         const uint4 *p = reinterpret_cast<const uint4 *>(row + size_t(c) * (BITS / 8));
         const uint4 a = KEPT ? __ldg(p) : __ldcs(p);
         e.w[0] = a.x, e.w[1] = a.y, e.w[2] = a.z, e.w[3] = a.w;
         if constexpr (BITS == 32) {
             const uint4 b = KEPT ? __ldg(p + 1) : __ldcs(p + 1);
             e.w[4] = b.x, e.w[5] = b.y, e.w[6] = b.z, e.w[7] = b.w;
+        }
+        return;
+    }
+    if (vec == 1 && n == 8) {
+        const uint2 *p = reinterpret_cast<const uint2 *>(row + size_t(c) * (BITS / 8));
+#pragma unroll
+        for (uint32_t i = 0; i < BITS / 8; ++i) {
+            const uint2 a = KEPT ? __ldg(p + i) : __ldcs(p + i);
+            e.w[2 * i] = a.x, e.w[2 * i + 1] = a.y;
         }
         return;
     }
@@ -108,14 +117,17 @@ __device__ __forceinline__ float largest_of(const Pair (&v)[4], float top) {
     }
     return top;
 }
-// values c .. c + n of a row of `dtype`, rounded; `vec`: the row begins on 16 bytes
-__device__ __forceinline__ void store_pairs(uint8_t *row, uint32_t c, uint32_t n, int32_t dtype, bool vec, const Pair (&v)[4]) {
+// values c .. c + n of a row of `dtype`, rounded; `vec` as above
+__device__ __forceinline__ void store_pairs(uint8_t *row, uint32_t c, uint32_t n, int32_t dtype, uint32_t vec, const Pair (&v)[4]) {
     const float2 a = v[0].two(), b = v[1].two(), d = v[2].two(), e = v[3].two();
     if (dtype == EP_FP32) {
         float *p = reinterpret_cast<float *>(row) + c;
-        if (vec && n == 8) {
+        if (vec == 2 && n == 8) {
             *reinterpret_cast<float4 *>(p) = make_float4(a.x, a.y, b.x, b.y);
             *reinterpret_cast<float4 *>(p + 4) = make_float4(d.x, d.y, e.x, e.y);
+        } else if (vec == 1 && n == 8) {
+            float2 *q = reinterpret_cast<float2 *>(p);
+            q[0] = a, q[1] = b, q[2] = d, q[3] = e;
         } else {
             const float f[8] = {a.x, a.y, b.x, b.y, d.x, d.y, e.x, e.y};
 #pragma unroll
@@ -128,8 +140,11 @@ __device__ __forceinline__ void store_pairs(uint8_t *row, uint32_t c, uint32_t n
     if (dtype == EP_FP16) w[0] = Fp16::two(a.x, a.y), w[1] = Fp16::two(b.x, b.y), w[2] = Fp16::two(d.x, d.y), w[3] = Fp16::two(e.x, e.y);
     else w[0] = Bf16::two(a.x, a.y), w[1] = Bf16::two(b.x, b.y), w[2] = Bf16::two(d.x, d.y), w[3] = Bf16::two(e.x, e.y);
     uint16_t *p = reinterpret_cast<uint16_t *>(row) + c;
-    if (vec && n == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-    else
+    if (vec == 2 && n == 8) *reinterpret_cast<uint4 *>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+    else if (vec == 1 && n == 8) {
+        uint2 *q = reinterpret_cast<uint2 *>(p);
+        q[0] = make_uint2(w[0], w[1]), q[1] = make_uint2(w[2], w[3]);
+    } else
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
             if (i < n) p[i] = uint16_t(w[i / 2] >> (16 * (i % 2)));
@@ -142,10 +157,13 @@ __device__ __forceinline__ void store_eight(void *p, const Pair (&v)[4]) {
         asm volatile("st.global.v8.f32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "f"(a.x), "f"(a.y), "f"(b.x), "f"(b.y), "f"(c.x), "f"(c.y), "f"(d.x), "f"(d.y) : "memory");
     else *static_cast<uint4 *>(p) = make_uint4(E::two(a.x, a.y), E::two(b.x, b.y), E::two(c.x, c.y), E::two(d.x, d.y));
 }
-// eight one-byte values; `vec`: the row begins on 8 bytes
-__device__ __forceinline__ void store_bytes(uint8_t *row, uint32_t c, uint32_t n, bool vec, uint32_t lo, uint32_t hi) {
-    if (vec && n == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(lo, hi);
-    else
+// eight one-byte values; `vec`: 2 if rows begin on 8 bytes, 1 on 4, else 0
+__device__ __forceinline__ void store_bytes(uint8_t *row, uint32_t c, uint32_t n, uint32_t vec, uint32_t lo, uint32_t hi) {
+    if (vec == 2 && n == 8) *reinterpret_cast<uint2 *>(row + c) = make_uint2(lo, hi);
+    else if (vec == 1 && n == 8) {
+        *reinterpret_cast<uint32_t *>(row + c) = lo;
+        *reinterpret_cast<uint32_t *>(row + c + 4) = hi;
+    } else
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i)
             if (i < n) row[c + i] = uint8_t((i < 4 ? lo : hi) >> (8 * (i % 4)));
