@@ -374,7 +374,8 @@ __device__ __forceinline__ void kept_vector(uint32_t at, uint32_t piece, bool th
     to_pairs<Fp32>(e, v);
 }
 
-template <class X, class H, uint32_t N>
+// RAW: vectors of 16 bits wait as they lie in memory, where as floats they would leave no room for two rows
+template <class X, class H, uint32_t N, bool RAW>
 __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const __grid_constant__ NormParams P) {
     constexpr uint32_t XB = sizeof(typename X::T), HB = sizeof(typename H::T);
     extern __shared__ __align__(16) uint8_t stages[];
@@ -410,10 +411,16 @@ __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const 
         auto keep = [&](const NormVector &V, float offset) {
             if (!V.d || (start != r0 && V.rows == 0)) return;
             for (uint32_t i = threadIdx.x; i < pieces; i += blockDim.x) {
-                Pair v[4];
-                load_vector(V, start, i * 8u, 8, offset, v);
-                Pair *to = reinterpret_cast<Pair *>(stages + V.kept + (i >> 5) * 1024u + (i & 31u) * 16u);
-                to[0] = v[0], to[1] = v[1], to[64] = v[2], to[65] = v[3];
+                if constexpr (RAW) {
+                    Eight<16> e;
+                    load_eight<16, true>(V.d + int64_t(V.rows ? start / V.rows : 0) * V.pitch, i * 8u, 8, 2, e);
+                    *reinterpret_cast<uint4 *>(stages + V.kept + i * 16u) = make_uint4(e.w[0], e.w[1], e.w[2], e.w[3]);
+                } else {
+                    Pair v[4];
+                    load_vector(V, start, i * 8u, 8, offset, v);
+                    Pair *to = reinterpret_cast<Pair *>(stages + V.kept + (i >> 5) * 1024u + (i & 31u) * 16u);
+                    to[0] = v[0], to[1] = v[1], to[64] = v[2], to[65] = v[3];
+                }
             }
         };
         keep(P.p, P.offset);
@@ -442,20 +449,29 @@ __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const 
                 smem_eight<8 * XB>(at + (i * apart + l) * 8u * XB, there[i], x);
                 to_pairs<X>(x, v[i]);
             }
-            auto times = [&](const NormVector &V) {
+            auto vector = [&](const NormVector &V, float offset, uint32_t i, Pair (&w)[4]) {
+                if constexpr (RAW) {
+                    Eight<16> e;
+                    smem_eight<16>(shared + V.kept + (i * apart + l) * 16u, there[i], e);
+                    to_pairs<16>(e, V.dtype == EP_FP16, w);
+#pragma unroll
+                    for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
+                } else kept_vector(shared + V.kept, i * apart + l, there[i], w);
+            };
+            auto times = [&](const NormVector &V, float offset) {
 #pragma unroll
                 for (uint32_t i = 0; i < N; ++i) {
                     Pair w[4];
-                    kept_vector(shared + V.kept, i * apart + l, there[i], w);
+                    vector(V, offset, i, w);
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) v[i][j] = v[i][j] * w[j];
                 }
             };
             if (P.p.d) {
                 normed<N>(P, group, n, v);
-                times(P.p);
+                times(P.p, P.offset);
             }
-            if (P.g.d) times(P.g);
+            if (P.g.d) times(P.g, 0.0f);
             if (P.h)
 #pragma unroll
                 for (uint32_t i = 0; i < N; ++i) {
@@ -474,12 +490,12 @@ __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const 
             }
             normed<N>(P, group, n, v);
             if (l == 0 && row + P.slots < r1) bring(row + P.slots, s);           // (every warp of the row has read it: all have taken part in the exchange)
-            if (P.w.d) times(P.w);
+            if (P.w.d) times(P.w, P.offset);
             if (P.d.d)
 #pragma unroll
                 for (uint32_t i = 0; i < N; ++i) {
                     Pair d[4];
-                    kept_vector(shared + P.d.kept, i * apart + l, there[i], d);
+                    vector(P.d, 0.0f, i, d);
 #pragma unroll
                     for (uint32_t j = 0; j < 4; ++j) v[i][j] = v[i][j] + d[j];
                 }
@@ -520,23 +536,25 @@ __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const 
     }
 }
 
-template <class X, class H, uint32_t N>
+template <class X, class H, uint32_t N, bool RAW>
 int launch_stream(const NormParams &P, uint32_t smem, uint32_t sms, cudaStream_t st) {
     static bool configured[64] = {};
-    const auto kernel = norm_stream_kernel<X, H, N>;
+    const auto kernel = norm_stream_kernel<X, H, N, RAW>;
     if (const int rc = op_configure(kernel, kStreamRoom, configured)) return rc;
     return op_launch(kernel, sms, P.warps * P.rows * 32u, smem, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
 }
 
 // How the stream's kernel would work on these rows, if it would.
-bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem) {
+bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem, bool &raw) {
     const uint32_t pieces = P.C / 8u;
     if (P.C % 8 || pieces <= 32 || P.T < 8u * sms) return false;
-    P.kept = P.stretch = 0;
-    for (NormVector *v : {&P.p, &P.g, &P.w, &P.d}) {
+    uint32_t vectors = 0;
+    bool narrow = true;
+    P.stretch = 0;
+    for (const NormVector *v : {&P.p, &P.g, &P.w, &P.d}) {
         if (!v->d) continue;
-        v->kept = P.kept;
-        P.kept += (pieces + 31u) / 32u * 1024u;
+        ++vectors;
+        narrow = narrow && v->dtype != EP_FP32;
         // stretches: rows that share all their vectors (groups' lengths that are not multiples of one another are left to the other kernel)
         if (v->rows) {
             const uint32_t a = P.stretch ? P.stretch : v->rows, lo = a < v->rows ? a : v->rows, hi = a < v->rows ? v->rows : a;
@@ -544,19 +562,29 @@ bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem) {
             P.stretch = lo;
         }
     }
-    if (P.kept >= kStreamRoom) return false;
     // as many rows at a time as there are warps for with four pieces to a lane, and 100 KB on the way: 8192 x 5120 BF16, 5 rows at a time, 5 slots
     // 61 us, 9 slots 66; 4 rows, 8 slots 60; 3 rows, 9 slots 67
     P.warps = (pieces + 127u) / 128u;
     P.rows = stream_warps() / P.warps;
     if (P.warps > 1 && P.rows > 15) P.rows = 15;                                 // (named barriers: 1 .. 15)
+    if (P.rows < 1 || (P.stretch && P.stretch < 2u * P.rows)) return false;
     P.slots = kStreamFlight / row;
     if (P.slots < P.rows) P.slots = P.rows;
+    if (P.slots < 2) P.slots = 2;
     if (P.slots > kMaxSlots) P.slots = kMaxSlots;
-    if (P.slots > (kStreamRoom - P.kept) / row) P.slots = (kStreamRoom - P.kept) / row;
-    if (P.rows < 1 || P.slots < 2 || (P.stretch && P.stretch < 2u * P.rows)) return false;
-    smem = P.kept + P.slots * row;
-    return true;
+    for (const bool as_they_are : {false, true}) {
+        if (as_they_are && !narrow) return false;
+        const uint32_t each = (pieces + 31u) / 32u * (as_they_are ? 512u : 1024u);
+        if (vectors * each + 2u * row > kStreamRoom) continue;
+        P.kept = 0;
+        for (NormVector *v : {&P.p, &P.g, &P.w, &P.d})
+            if (v->d) v->kept = P.kept, P.kept += each;
+        if (P.slots > (kStreamRoom - P.kept) / row) P.slots = (kStreamRoom - P.kept) / row;
+        smem = P.kept + P.slots * row;
+        raw = as_they_are;
+        return true;
+    }
+    return false;
 }
 
 template <class X, class H>
@@ -573,8 +601,9 @@ int launch_whole(NormParams P, cudaStream_t st, bool &done) {
             return op_launch(norm_short_kernel<X, H>, most, 256, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
         }
     }
-    done = sms && stream_shape(P, P.C * uint32_t(sizeof(typename X::T) + (P.h ? sizeof(typename H::T) : 0)), sms, smem);
-    if (done) return launch_stream<X, H, 4>(P, smem, sms, st);
+    bool raw = false;
+    done = sms && stream_shape(P, P.C * uint32_t(sizeof(typename X::T) + (P.h ? sizeof(typename H::T) : 0)), sms, smem, raw);
+    if (done) return raw ? launch_stream<X, H, 4, true>(P, smem, sms, st) : launch_stream<X, H, 4, false>(P, smem, sms, st);
     if (pieces > 16 && pieces <= 1024) {                 // (shorter rows share a warp the general way)
         done = true;
         P.warps = (pieces + 31u) / 32u;

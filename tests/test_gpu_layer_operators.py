@@ -318,7 +318,7 @@ def test_norm_groups_of_many_rows(T, C, groups, more):
 
 @gpu
 @pytest.mark.parametrize("dtype,wide", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float32, torch.bfloat16), (torch.float32, torch.float32)])
-@pytest.mark.parametrize("T,C", [(1201, 8), (1203, 64), (5000, 256), (3001, 264), (1205, 520), (1500, 1000), (2501, 2048), (1301, 5120), (1200, 8200), (1190, 17408), (1184, 32768), (1900, 136), (2000, 12000), (1200, 1028)])
+@pytest.mark.parametrize("T,C", [(1201, 8), (1203, 64), (5000, 256), (3001, 264), (1205, 520), (1500, 1000), (2501, 2048), (1301, 5120), (1200, 8200), (1190, 17408), (1184, 32768), (1900, 136), (2000, 12000), (1200, 1028), (1300, 16384), (1190, 12808), (1500, 14336)])
 @pytest.mark.parametrize("center", [False, True])
 def test_norm_of_many_rows(T, C, dtype, wide, center):
     x, v = norm_inputs(T, C, dtype, wide, 1, T * 3 + C)
