@@ -736,8 +736,8 @@ def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, 
 
     weight, bias, gate, post_weight: [C], or [groups, C] for groups of T / groups rows that follow one another.  x, residual and the vectors
     are of bfloat16, float16 or float32, each its own.  z is of x's type or of out_dtype (BF16, FP16, FP32; FP8_E4M3: the pair that quantize_blocks returns; INT8:
-    the pair of quantize_rows), or `out`, which may be x.  Returns z, with a residual (z, r); residual_out: the tensor that r goes to, which may be `residual` itself;
-    False: r is not written, and z returned.  See ep_norm."""
+    the pair of quantize_rows), or `out`, which may be x.  residual_out: the tensor that r goes to, which may be `residual` itself (None: a new one
+    where there is a residual, False: r is not written).  Returns z, or (z, r) where r is written.  See ep_norm."""
     torch, e4m3, e8m0, codes, _ = _float8()
     dtype, shape, dev = x.dtype, x.shape, x.get_device()
     code = codes.get(dtype)
