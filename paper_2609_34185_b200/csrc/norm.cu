@@ -13,8 +13,8 @@ __device__ unsigned int g_norm_status = 0;
 //
 // A row stays in the registers of its warps from its first byte to its last: x and h are read once, r and z written once, whatever
 // stands between.  Deviations from the mean are summed in a second walk through the registers, so that nothing cancels.
-// Bound by memory for many rows (8192 x 5120 BF16, two norms and a residual, 60.5 us: 5.5 TB/s; 327680 x 128 33.5 us), by the launch and two to five exchanges
-// between warps for few (16 x 5120 2.9 us).
+// Bound by memory for many rows (8192 x 5120 BF16, two norms and a residual, 60.5 us: 5.5 TB/s; 327680 x 128 32.6 us), by the launch and two to five exchanges
+// between warps for few (16 x 5120 2.6 us).
 // ======================================================================================================================
 struct NormVector {
     const uint8_t *d;
@@ -29,7 +29,7 @@ struct NormParams {
     uint8_t *r, *z, *s;
     int64_t ldx, ldh, ldr, ldz, lds;      // bytes; scales: elements
     NormVector w, d, g, p;
-    float c, offset, eps, columns;
+    float c, offset, eps, columns, inverse;      // (inverse: of columns; a mean is divided, so that a row of equal values has none but zeros left)
     uint32_t T, C;
     uint32_t warps, rows;         // warps of a row, rows of a CTA
     uint32_t lanes;               // of a row that takes less than a warp (32: whole warps)
@@ -83,7 +83,7 @@ __device__ __forceinline__ void normed(const NormParams &P, RowGroup &group, con
 #pragma unroll
         for (uint32_t j = 0; j < 4; j += 2) squares = fma2(v[i][j], v[i][j], squares), more = fma2(v[i][j + 1], v[i][j + 1], more);
     const float2 two = (squares + more).two();
-    const Pair f(1.0f / sqrtf(group.sum(two.x + two.y) / P.columns + P.eps));
+    const Pair f(rsqrtf(group.sum(two.x + two.y) * P.inverse + P.eps));          // (good to 2^-22.9; a root and two quotients take 60 instructions of some 330)
 #pragma unroll
     for (uint32_t i = 0; i < N; ++i)
 #pragma unroll
@@ -685,6 +685,7 @@ extern "C" int ep_norm(const ep_norm_job *job, void *stream) {
     P.offset = j.weight_offset;
     P.eps = j.eps;
     P.columns = float(j.C);
+    P.inverse = 1.0f / P.columns;
     P.T = j.T;
     P.C = j.C;
     P.x_half = j.x_dtype == EP_FP16;
