@@ -564,7 +564,8 @@ bool stream_shape(NormParams &P, uint32_t row, uint32_t sms, uint32_t &smem, boo
     }
     // as many rows at a time as there are warps for with four pieces to a lane, and 100 KB on the way: 8192 x 5120 BF16, 5 rows at a time, 5 slots
     // 61 us, 9 slots 66; 4 rows, 8 slots 60; 3 rows, 9 slots 67
-    P.warps = (pieces + 127u) / 128u;
+    const uint32_t span = pieces <= 64 ? 64u : 128u;     // (two pieces to a lane for rows that leave half of four's lanes over)
+    P.warps = (pieces + span - 1u) / span;
     P.rows = stream_warps() / P.warps;
     if (P.warps > 1 && P.rows > 15) P.rows = 15;                                 // (named barriers: 1 .. 15)
     if (P.rows < 1 || (P.stretch && P.stretch < 2u * P.rows)) return false;
@@ -603,7 +604,7 @@ int launch_whole(NormParams P, cudaStream_t st, bool &done) {
     }
     bool raw = false;
     done = sms && stream_shape(P, P.C * uint32_t(sizeof(typename X::T) + (P.h ? sizeof(typename H::T) : 0)), sms, smem, raw);
-    if (done) return raw ? launch_stream<X, H, 4, true>(P, smem, sms, st) : launch_stream<X, H, 4, false>(P, smem, sms, st);
+    if (done) return pieces <= 64 ? launch_stream<X, H, 2, false>(P, smem, sms, st) : raw ? launch_stream<X, H, 4, true>(P, smem, sms, st) : launch_stream<X, H, 4, false>(P, smem, sms, st);
     if (pieces > 16 && pieces <= 1024) {                 // (shorter rows share a warp the general way)
         done = true;
         P.warps = (pieces + 31u) / 32u;
