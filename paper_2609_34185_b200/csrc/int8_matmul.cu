@@ -20,6 +20,7 @@ struct RowsParams {
     int64_t ldx, ldq;             // bytes
     uint32_t T, C;
     uint32_t warps, rows;         // warps of a row, rows of a CTA
+    uint32_t lanes;               // of a row that takes less than a warp (32: whole warps)
     int32_t half;
     uint32_t x_vec, q_vec;
 };
@@ -52,9 +53,9 @@ template <uint32_t BITS, uint32_t N>
 __global__ void __launch_bounds__(512) quantize_rows_kernel(const __grid_constant__ RowsParams P) {
     __shared__ uint32_t room[64];
     op_wait_for_stream();
-    const uint32_t lane = threadIdx.x & 31u, warp = threadIdx.x >> 5, of = warp / P.warps;
-    const uint32_t row = blockIdx.x * P.rows + of, l = (warp - of * P.warps) * 32u + lane;
-    RowGroup group{room, P.warps, of * P.warps, 1u + of, 0};
+    const uint32_t of = P.lanes < 32 ? threadIdx.x / P.lanes : (threadIdx.x >> 5) / P.warps;
+    const uint32_t row = blockIdx.x * P.rows + of, l = threadIdx.x - of * (P.lanes < 32 ? P.lanes : P.warps * 32u);
+    RowGroup group{room, P.warps, of * P.warps, 1u + of, 0, P.lanes};
     const uint8_t *x = P.x + int64_t(row) * P.ldx;
     Eight<BITS> e[N];
     uint32_t top = 0;
@@ -99,14 +100,19 @@ __global__ void __launch_bounds__(512) quantize_long_rows_kernel(const __grid_co
 template <uint32_t BITS>
 int launch_rows(RowsParams P, cudaStream_t st) {
     const uint32_t pieces = (P.C + 7u) / 8u;
-    const uint32_t each = pieces <= 512 ? 1u : pieces <= 1024 ? 2u : pieces <= 2048 ? 4u : 8u;
+    // Few rows are spread over many lanes; of many, a row of up to 2048 values is a warp's and one of 4096 two warps' (spread and not, us: 160000 x 128 BF16 87 / 43,
+    // 40000 x 1024 86 / 36, 8192 x 3840 32 / 25, 8192 x 5120 33 / 42).
+    const bool many = P.T >= 8u * uint32_t(op_sms());
+    const uint32_t each = many && pieces <= 512 ? (pieces <= 32 ? 1u : pieces <= 64 ? 2u : pieces <= 128 ? 4u : 8u) : pieces <= 512 ? 1u : pieces <= 1024 ? 2u : pieces <= 2048 ? 4u : 8u;
+    P.lanes = 32;
+    while (P.lanes / 2 >= pieces) P.lanes /= 2;
     if (pieces > 4096) {
         P.warps = 16, P.rows = 1;
         return op_launch(quantize_long_rows_kernel<BITS>, P.T, 512, 0, 1, st, P) == cudaSuccess ? EP_OK : EP_ERR_CUDA;
     }
     P.warps = (pieces + 32u * each - 1u) / (32u * each);
-    P.rows = P.warps >= 4 ? 1u : 4u / P.warps;
-    const uint32_t threads = P.warps * P.rows * 32u, grid = uint32_t((uint64_t(P.T) + P.rows - 1u) / P.rows);
+    P.rows = P.warps >= 4 ? 1u : 4u / P.warps * (32u / P.lanes);
+    const uint32_t threads = P.warps * P.rows * P.lanes, grid = uint32_t((uint64_t(P.T) + P.rows - 1u) / P.rows);
     const cudaError_t e = each == 1 ? op_launch(quantize_rows_kernel<BITS, 1>, grid, threads, 0, 1, st, P)
                         : each == 2 ? op_launch(quantize_rows_kernel<BITS, 2>, grid, threads, 0, 1, st, P)
                         : each == 4 ? op_launch(quantize_rows_kernel<BITS, 4>, grid, threads, 0, 1, st, P)

@@ -86,6 +86,15 @@ def test_quantize_rows_edges(C):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("T,C", [(1201, 5), (1300, 9), (1184, 60), (1211, 128), (1250, 250), (1201, 264), (1190, 700), (1203, 1500), (1187, 2056), (1185, 4096), (1184, 4104)])
+def test_quantize_rows_of_many_rows(T, C, dtype):
+    x = (torch.randn(T, C, generator=cuda(T + C), device="cuda") * torch.exp(3 * torch.randn(T, 1, generator=cuda(C), device="cuda"))).clamp(-60000, 60000).to(dtype)
+    x[7], x[T - 1, C - 1] = 0.0, math.inf
+    assert_rows(ep.quantize_rows(x), rounded_rows(x))
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 @pytest.mark.parametrize("C", [8, 300, 33000])
 def test_quantize_rows_what_is_not_finite_in_16_bits(C, dtype):
