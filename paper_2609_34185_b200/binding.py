@@ -755,14 +755,14 @@ def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, 
             out = _empty(shape, _out_torch_dtype(out_dtype), x.device, stream)
         else:
             raise ValueError("out_dtype must be BF16, FP16, FP32, FP8_E4M3 or INT8")
-    z, scales, ld_scales = out, 0, 0
+    z, s, scales, ld_scales = out, None, 0, 0
     if isinstance(out, (tuple, list)):
         z, s = out
         if z.dtype == e4m3:
             scales, ld_scales = s.data_ptr(), _matrix(s, e8m0, (T, -(-Cc // 128)), dev, "out[1]")
         elif s is not None:
             scales = _floats(s, T, dev, "out[1]")
-        z_code = FP8_E4M3 if z.dtype == e4m3 else INT8 if z.dtype == torch.int8 and scales else None
+        z_code = FP8_E4M3 if z.dtype == e4m3 else INT8 if z.dtype == torch.int8 and s is not None else None
     else:
         z_code = codes.get(z.dtype)
     if z_code is None:

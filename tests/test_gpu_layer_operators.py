@@ -764,6 +764,15 @@ def test_no_rows():
 
 
 @gpu
+def test_norm_of_no_rows_to_eight_bits():
+    x, w = torch.empty(0, 300, dtype=torch.bfloat16, device="cuda"), torch.ones(300, device="cuda")
+    q, s = ep.norm(x, w, out_dtype=ep.INT8)
+    assert q.shape == (0, 300) and q.dtype == torch.int8 and s.shape == (0,)
+    (q, s), r = ep.norm(x, w, residual=x, out_dtype=ep.FP8_E4M3)
+    assert q.shape == r.shape == (0, 300) and s.shape == (0, 3)
+
+
+@gpu
 def test_more_than_32_bits_of_values():
     # rows and outputs beyond 2^31 values and 2^32 bytes: the last row is as the first
     T, C = 70000, 32768
