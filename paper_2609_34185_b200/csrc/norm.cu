@@ -663,6 +663,8 @@ extern "C" int ep_norm(const ep_norm_job *job, void *stream) {
         (j.d_residual && !rows_fit(j.d_residual, j.ld_residual, j.C, hs)) || (j.d_residual_out && !rows_fit(j.d_residual_out, j.ld_residual_out, j.C, hs)) ||
         (j.d_residual && j.d_residual == j.d_residual_out && j.ld_residual != j.ld_residual_out))
         return EP_ERR_BAD_ARG;
+    // z in x's place: rows where they were, so that what a row's threads write is that row; z and r are two things
+    if ((j.d_z == j.d_x && (j.z_dtype != j.x_dtype || (j.T > 1 && j.ldz != j.ldx))) || j.d_z == j.d_residual_out) return EP_ERR_BAD_ARG;
     if (j.z_dtype == EP_FP8_E4M3 && (!j.d_z_scales || j.ldz_scales < int64_t((j.C + 127u) / 128u))) return EP_ERR_BAD_ARG;
     if (j.z_dtype == EP_INT8 && (!j.d_z_scales || !aligned(j.d_z_scales, 4))) return EP_ERR_BAD_ARG;
     if (j.C > kMaxColumns) return EP_ERR_UNSUPPORTED;

@@ -49,6 +49,12 @@ def test_bad_arguments(job, wrong):
         assert job(**w) == BAD, w
 
 
+@pytest.mark.parametrize("wrong", [dict(zdtype=ep.FP32), dict(zdtype=ep.FP16), dict(ldz=72), dict(zdtype=ep.INT8, s=3 * P), dict(zdtype=ep.FP8_E4M3, s=3 * P), dict(z=2 * P, r=2 * P)])
+def test_norm_over_what_it_reads(wrong):
+    """z in x's place has x's type and ld, and z and r have places of their own."""
+    assert norm_job(T=0, **wrong) == 0 and norm_job(**wrong) == BAD
+
+
 def test_unsupported():
     for w in (dict(C=56), dict(ldx=72), dict(ldw=72), dict(x=P + 8), dict(w=P + 8), dict(C=1 << 17, ldx=1 << 17, ldw=1 << 17)):
         assert matmul_job(**w) == UNSUPPORTED, w
