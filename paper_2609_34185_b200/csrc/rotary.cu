@@ -270,8 +270,9 @@ extern "C" int ep_rotary(const ep_rotary_job *job, void *stream) {
     const int64_t most = int64_t(1) << 40;
     for (const int64_t ld : {j.ldx, j.ldx_head, j.ldo, j.ldo_head})
         if (ld < 0 || ld >= most) return EP_ERR_BAD_ARG;
-    // (what is written is written once)
+    // What is written is written once: rows lie apart and heads lie apart, and all heads of a row lie before the next row, or all rows of a head before the next head.
     if ((j.T > 1 && j.ldo < int64_t(j.dim)) || (j.heads > 1 && j.ldo_head < int64_t(j.dim))) return EP_ERR_BAD_ARG;
+    if (j.T > 1 && j.heads > 1 && j.ldo < int64_t(j.heads - 1u) * j.ldo_head + int64_t(j.dim) && (j.ldo_head - int64_t(j.dim)) / j.ldo < int64_t(j.T - 1u)) return EP_ERR_BAD_ARG;
     const bool in_place = j.d_x == j.d_out;
     if (in_place && (j.ldx != j.ldo || j.ldx_head != j.ldo_head)) return EP_ERR_BAD_ARG;
     RotaryParams P;

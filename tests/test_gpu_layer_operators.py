@@ -829,3 +829,25 @@ def test_refusals():
         with pytest.raises(ep.EntroPackError) as e:
             call()
         assert e.value.status == -3
+
+
+@gpu
+@pytest.mark.parametrize("next", [False, True])
+def test_rotary_of_heads_before_rows(next):
+    # each head's rows side by side, the tightest that lie apart; one row or one head may have any distance; what overlaps is refused
+    T, H, D, f = 21, 3, 64, ep.rotary_frequencies(64)
+    x, at = torch.randn(T, H, D, generator=cuda(4), device="cuda"), torch.arange(T, device="cuda") * 7
+    out = torch.zeros(H, T, D, device="cuda").transpose(0, 1)
+    assert ep.rotary(x, at, f, interleaved=next, out=out) is out
+    check_turn(out, x, at, f, next, 1.0)
+    here = x.transpose(0, 1).contiguous().transpose(0, 1)
+    check_turn(ep.rotary(here, at, f, interleaved=next, out=here), x, at, f, next, 1.0)
+    room = torch.zeros(T * H * D, device="cuda")
+    for shape, stride in (((1, H, D), (1, D, 1)), ((T, 1, D), (D, 3, 1))):
+        rows, heads = shape[:2]
+        out = room.as_strided(shape, stride)
+        check_turn(ep.rotary(x[:rows, :heads], at[:rows], f, interleaved=next, out=out), x[:rows, :heads], at[:rows], f, next, 1.0)
+    for stride in ((D, D, 1), (2 * D + 32, D, 1), (D, T * D - 1, 1)):
+        with pytest.raises(ep.EntroPackError) as e:
+            ep.rotary(x, at, f, out=room.as_strided((T, H, D), stride))
+        assert e.value.status == -1

@@ -100,3 +100,10 @@ def test_tensors_of_the_host_are_refused():
                  lambda: ep.rotary(z(4, 2, 8), z(4, dtype=torch.int32), ep.rotary_frequencies(8, device="cpu"))):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("wrong", [dict(ldo=64, ldoh=64), dict(ldo=96, ldoh=64), dict(ldo=64, ldoh=64, T=2, H=2), dict(ldo=64, ldoh=255), dict(ldo=191, ldoh=64, H=3),
+                                   dict(o=P, ldx=64, ldxh=64, ldo=64, ldoh=64), dict(ldo=(1 << 40) - 1, ldoh=(1 << 40) - 1, T=1 << 30)])
+def test_rotary_of_outputs_that_overlap(wrong):
+    """A row's heads reach into the next row, or a head's rows into the next head: two places for one value."""
+    assert rotary_job(**{"T": 5, "H": 2, **wrong}) == BAD
