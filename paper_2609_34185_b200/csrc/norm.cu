@@ -660,11 +660,16 @@ extern "C" int ep_norm(const ep_norm_job *job, void *stream) {
     const uint32_t xs = bytes_of(j.x_dtype), hs = bytes_of(j.residual_dtype), zs = j.z_dtype == EP_FP8_E4M3 || j.z_dtype == EP_INT8 ? 1u : bytes_of(j.z_dtype);
     const bool residual = j.d_residual || j.d_residual_out;
     if (!j.d_x || !j.d_z || j.C == 0 || j.T > 0x7FFFFF00u || !xs || !zs || (residual && !hs) || !rows_fit(j.d_x, j.ldx, j.C, xs) || !rows_fit(j.d_z, j.ldz, j.C, zs) ||
-        (j.d_residual && !rows_fit(j.d_residual, j.ld_residual, j.C, hs)) || (j.d_residual_out && !rows_fit(j.d_residual_out, j.ld_residual_out, j.C, hs)) ||
-        (j.d_residual && j.d_residual == j.d_residual_out && j.ld_residual != j.ld_residual_out))
+        (j.d_residual && !rows_fit(j.d_residual, j.ld_residual, j.C, hs)) || (j.d_residual_out && !rows_fit(j.d_residual_out, j.ld_residual_out, j.C, hs)))
         return EP_ERR_BAD_ARG;
-    // z in x's place: rows where they were, so that what a row's threads write is that row; z and r are two things
-    if ((j.d_z == j.d_x && (j.z_dtype != j.x_dtype || (j.T > 1 && j.ldz != j.ldx))) || j.d_z == j.d_residual_out) return EP_ERR_BAD_ARG;
+    // What is written in the place of what is read: the same type and rows where they were, so that each thread writes what it has read itself.  z and r are two things.
+    auto in_place = [&](const void *to, int32_t to_dtype, int64_t ldto, const void *from, int32_t dtype, int64_t ld) {
+        return to != from || !to || (to_dtype == dtype && (j.T == 1 || ldto == ld));
+    };
+    if (!in_place(j.d_z, j.z_dtype, j.ldz, j.d_x, j.x_dtype, j.ldx) || !in_place(j.d_z, j.z_dtype, j.ldz, j.d_residual, j.residual_dtype, j.ld_residual) ||
+        !in_place(j.d_residual_out, j.residual_dtype, j.ld_residual_out, j.d_x, j.x_dtype, j.ldx) ||
+        !in_place(j.d_residual_out, j.residual_dtype, j.ld_residual_out, j.d_residual, j.residual_dtype, j.ld_residual) || j.d_z == j.d_residual_out)
+        return EP_ERR_BAD_ARG;
     if (j.z_dtype == EP_FP8_E4M3 && (!j.d_z_scales || j.ldz_scales < int64_t((j.C + 127u) / 128u))) return EP_ERR_BAD_ARG;
     if (j.z_dtype == EP_INT8 && (!j.d_z_scales || !aligned(j.d_z_scales, 4))) return EP_ERR_BAD_ARG;
     if (j.C > kMaxColumns) return EP_ERR_UNSUPPORTED;

@@ -851,3 +851,24 @@ def test_rotary_of_heads_before_rows(next):
         with pytest.raises(ep.EntroPackError) as e:
             ep.rotary(x, at, f, out=room.as_strided((T, H, D), stride))
         assert e.value.status == -1
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,C", [(1, 5120), (16, 5120), (9, 1001), (2, 17408), (40000, 128), (1300, 1000), (1200, 12808)])
+def test_norm_in_the_places_of_what_it_reads(T, C, dtype):
+    # z over x or over the residual, r over the other one or over x alone: the same bits as with places of their own; another type is refused
+    x, v = norm_inputs(T, C, dtype, dtype, 1, T + C)
+    want, r_want = ep.norm(x, **v)
+    for z_over, r_over in (("h", None), ("h", "x"), ("x", "h"), ("x", None), (None, "x"), (None, "h")):
+        here = {"x": x.clone(), "h": v["residual"].clone(), None: None}
+        got = ep.norm(here["x"], **{**v, "residual": here["h"]}, out=here[z_over], residual_out=here[r_over])
+        assert torch.equal(got[0], want) and torch.equal(got[1], r_want)
+        assert all(over is None or g is here[over] for g, over in zip(got, (z_over, r_over)))
+    other = torch.float16
+    for call in (lambda: ep.norm(x, **v, out=v["residual"].view(torch.int16 if dtype != torch.float32 else torch.int32).view(other)[:, :C]),
+                 lambda: ep.norm(x, out=x, residual_out=x), lambda: ep.norm(x, residual_out=x.view(other)[:, :C])):
+        with pytest.raises(ep.EntroPackError) as e:
+            call()
+        assert e.value.status == -1
+    assert ep.last_device_status() == 0

@@ -107,3 +107,11 @@ def test_tensors_of_the_host_are_refused():
 def test_rotary_of_outputs_that_overlap(wrong):
     """A row's heads reach into the next row, or a head's rows into the next head: two places for one value."""
     assert rotary_job(**{"T": 5, "H": 2, **wrong}) == BAD
+
+
+@pytest.mark.parametrize("wrong", [dict(h=2 * P, z=2 * P, hdtype=ep.FP32), dict(h=2 * P, z=2 * P, zdtype=ep.FP16), dict(h=2 * P, z=2 * P, ldz=72), dict(h=2 * P, z=2 * P, zdtype=ep.INT8, s=3 * P),
+                                   dict(h=2 * P, z=2 * P, r=3 * P, zdtype=ep.FP8_E4M3, s=4 * P), dict(r=P, z=2 * P, hdtype=ep.FP32), dict(r=P, z=2 * P, dtype=ep.FP32, ldx=64),
+                                   dict(r=P, z=2 * P, ldr=72), dict(h=3 * P, r=P, z=2 * P, ldh=72, ldr=72), dict(x=P, h=P, z=2 * P, r=P, hdtype=ep.FP16)])
+def test_norm_over_a_residual_or_with_r_over_x(wrong):
+    """z in the residual's place and r in x's place have the type and ld of what was there."""
+    assert norm_job(T=0, **wrong) == 0 and norm_job(**wrong) == BAD
