@@ -394,7 +394,7 @@ int ep_cache_attention(const ep_attention_job *job, void *stream);
 /* The INT8 route.  A row x of T x C becomes whole numbers q and one scale s: m = max(max_j |x[j]|, 2^-119), s = m / 127,
  * q[j] = x[j] * (127 / m) rounded to the nearest whole number, ties to even, each operation in fp32 (so |q| <= 127).  A row of zeros has s = 1;
  * a row with a value that is not finite has q = 0 and s = NaN, so that its products are NaN.  Rows are the tokens of activations, or
- * the channels of a weight. */
+ * the channels of a weight.  The results have places of their own (d_q = d_x is EP_ERR_BAD_ARG). */
 typedef struct {
     const void *d_x;            /* device: T x C of x_dtype, ldx >= C; aligned to its element (rows that begin on 16 bytes are read fastest) */
     void *d_q;                  /* device: T x C int8, ldq >= C */
@@ -408,7 +408,7 @@ int ep_quantize_rows(const ep_quantize_rows_job *job, void *stream);
 /* y[t, r] = a[r] (s[t] sum_k xq[t, k] wq[r, k]) + bias[r]: the sum over whole numbers in 32 bits on the tensor cores, exact, then rounded to fp32;
  * scales and bias in fp32; one rounding to out_dtype (EP_FP16 overflows to infinity).  The operands may hold all of -128 .. 127.
  * The copy engine reads the operands: d_x and d_w on 16 bytes, C, ldx and ldw multiples of 16, and C < 2^17 (128 * 128 * C < 2^31), else
- * EP_ERR_UNSUPPORTED, as for products of more than about 2^54 operations.  A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
+ * EP_ERR_UNSUPPORTED, as for products of more than about 2^54 operations.  d_y has a place of its own (d_x or d_w there is EP_ERR_BAD_ARG).  A wait inside the kernel that does not end raises the integrity word below instead of hanging. */
 typedef struct {
     const void *d_x;                /* device: T x C int8, as ep_quantize_rows leaves them */
     const float *d_x_scales;        /* device: T floats s[t] */

@@ -586,6 +586,7 @@ extern "C" int ep_quantize_rows(const ep_quantize_rows_job *job, void *stream) {
     if (!j.d_x || !j.d_q || !j.d_scales || j.C == 0 || j.C > 0x7FFFFF00u || j.T > 0x7FFFFF00u || !size || !aligned(j.d_x, size) || !aligned(j.d_scales, 4) ||
         j.ldx < int64_t(j.C) || j.ldq < int64_t(j.C) || j.ldx >= (int64_t(1) << 40) || j.ldq >= (int64_t(1) << 40))
         return EP_ERR_BAD_ARG;
+    if (j.d_x == static_cast<const void *>(j.d_q)) return EP_ERR_BAD_ARG;        // (q's rows lie where other rows still have to be read)
     RowsParams P;
     std::memset(&P, 0, sizeof(P));
     P.x = static_cast<const uint8_t *>(j.d_x);
@@ -614,6 +615,7 @@ extern "C" int ep_int8_matmul(const ep_int8_matmul_job *job, void *stream) {
     // the copy engine's rows begin on 16 bytes; sums of 128 * 128 * C stay below 2^31
     if (j.C % 16 || j.C >= (1u << 17) || j.ldx % 16 || j.ldw % 16 || !aligned(j.d_x, 16) || !aligned(j.d_w, 16) || j.ldx >= (int64_t(1) << 40) || j.ldw >= (int64_t(1) << 40))
         return EP_ERR_UNSUPPORTED;
+    if (j.d_y == j.d_x || j.d_y == j.d_w) return EP_ERR_BAD_ARG;                 // (every tile reads operands that other tiles' results would lie on)
     ProductParams P;
     std::memset(&P, 0, sizeof(P));
     P.s = j.d_x_scales;

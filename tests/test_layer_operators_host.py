@@ -115,3 +115,11 @@ def test_rotary_of_outputs_that_overlap(wrong):
 def test_norm_over_a_residual_or_with_r_over_x(wrong):
     """z in the residual's place and r in x's place have the type and ld of what was there."""
     assert norm_job(T=0, **wrong) == 0 and norm_job(**wrong) == BAD
+
+
+def test_results_in_the_place_of_operands():
+    """Other rows, or other tiles, still have to be read there."""
+    for w in (dict(q=P), dict(q=P, dtype=ep.FP32), dict(q=P, ldq=128)):
+        assert rows_job(T=0, **w) == 0 and rows_job(x=P, **w) == BAD, w
+    for w in (dict(x=P, w=2 * P), dict(x=2 * P, w=P), dict(x=P, w=2 * P, dtype=ep.FP32)):
+        assert matmul_job(T=0, y=P, **w) == 0 and matmul_job(y=P, **w) == BAD, w
