@@ -872,3 +872,31 @@ def test_norm_in_the_places_of_what_it_reads(T, C, dtype):
             call()
         assert e.value.status == -1
     assert ep.last_device_status() == 0
+
+
+def angles(at, f):
+    """position * frequency as fractions of a turn, exactly, nearest to 0, in doubles: 1 / 2 pi to 80 digits, whole numbers."""
+    from fractions import Fraction
+    inverse = Fraction(15915494309189533576888376337251436203445964574045644874766734405889679763422653509, 10 ** 83)
+    one = lambda p, w: (p * Fraction(w) * inverse + Fraction(1, 2)) % 1 - Fraction(1, 2)  # noqa: E731
+    return torch.tensor([[float(one(p, w)) for w in f.tolist()] for p in at.tolist()], dtype=torch.float64, device="cuda") * (2 * math.pi)
+
+
+FAR = [1, -5, 200000, (1 << 31) - 1, 1 << 40, (1 << 45) + 1, 1 << 50, -(1 << 56) - 12345, (1 << 60) + 3, (1 << 63) - 1, -(1 << 63)]
+
+
+@gpu
+@pytest.mark.parametrize("next", [False, True])
+def test_rotary_as_far_as_64_bits_reach(next):
+    # Pairs (1, 0) show the cosine and sine themselves: 2 units for CUDA's sincospi; pi 2^-25 for the angle in a float, 2 pi 2^-32 for what is cut off before that; and what the
+    # position makes of its step's rounding, to 2^-64 of a turn (half a turn: to one less) and 2^-52 of itself.
+    at = torch.tensor(FAR, device="cuda")
+    for f in (ep.rotary_frequencies(64, 1e6, 8.0, 8192.0), torch.tensor([1.0, 0.5, 3.6e-6, 1e-9, 1e-12, 2.5, -1.0, math.pi], dtype=torch.float64, device="cuda")):
+        n = len(f)
+        x = torch.zeros(len(at), 1, 2 * n, device="cuda")
+        (x[..., 0::2] if next else x[..., :n]).fill_(1)
+        y = ep.rotary(x, at, f, interleaved=next).double()[:, 0]
+        cos, sin = (y[:, 0::2], y[:, 1::2]) if next else (y[:, :n], y[:, n:])
+        a = angles(at, f)
+        bound = 2 * U + math.pi * 2.0 ** -25 + 2 * math.pi * 2.0 ** -32 + at.double().abs()[:, None] * (f.abs() * 2.0 ** -52 + 2.0 ** -61)
+        assert ((cos - a.cos()).abs() <= bound).all() and ((sin - a.sin()).abs() <= bound).all()
