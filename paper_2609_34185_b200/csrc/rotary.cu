@@ -16,7 +16,7 @@ constexpr uint32_t kThreads = 256, kAtOnce = 4;  // units that a thread has unde
 // A far position times a frequency has more turns than 32 bits can hold beside the fraction that counts (200 000 radians in fp32 are
 // off by 0.008).  So a frequency is a fraction of a turn in 64 bits, whole numbers multiply it, and what passes 64 bits are whole turns, which fall
 // away by themselves: no reduction.  The step is off by 2^-64 of a turn and by 2^-52 of itself (the product and the reciprocal of 2 pi are doubles, as the
-// frequency is: its own last bit makes half as much), which a position multiplies: the first by 2^-32 of a turn at 2^32, 2^-24 at 2^40.  The product's first 32 bits go to sincospi.
+// frequency is: its own last bit makes half as much), which a position multiplies: the first by 2^-32 of a turn at 2^32, 2^-24 at 2^40.  The product's first bits go to sincospi, for 32-bit values all of them count.
 // (96 bits, by a second double and a longer product, took 8192 tokens of a single head from 4.1 to 4.4 us, for positions that no context has.)
 // Bound by memory: a CTA works out its tokens' cosines and sines once, for all heads (48 heads of 128 of 8192 tokens BF16 in 33.7 us, 6.0 TB/s; with
 // cosines read 8 bytes at a time, 64 bytes apart, 43.7).
@@ -50,11 +50,22 @@ __device__ __forceinline__ uint64_t turn_fraction(double radians) {
     t -= rint(t);
     return uint64_t(__double2ll_rn(t * 18446744073709551616.0));
 }
+template <class E>
 __device__ __forceinline__ float2 cosine_sine(int64_t position, uint64_t step, float factor) {
-    const int32_t fraction = int32_t(uint32_t((uint64_t(position) * step) >> 32));     // of a turn, in 2^-32, -1/2 .. 1/2
+    const uint64_t angle = uint64_t(position) * step;                                  // of a turn, in 2^-64
+    const uint32_t high = uint32_t(angle >> 32);
     float s, c;
-    sincospif(float(fraction) * 4.656612873077393e-10f, &s, &c);                       // 2^-31: half turns
-    return make_float2(c * factor, s * factor);
+    if constexpr (sizeof(typename E::T) == 4) {
+        // The first 24 bits, the nearest, go to sincospi, exactly; what that leaves, d radians, turns the result on: 1 - d^2 / 2 is 1.  (A single
+        // head of 8192 tokens 4.45 -> 4.70 us, 48 of 4096 32.3 -> 32.5.)
+        const float d = float(int32_t(__funnelshift_r(uint32_t(angle), high, 8))) * 8.719671245021580e-17f;    // 2 pi / 2^56
+        sincospif(float(int32_t((high + 128u) & ~255u)) * 4.656612873077393e-10f, &s, &c);                     // 2^-31: half turns
+        return make_float2(fmaf(-s, d, c) * factor, fmaf(c, d, s) * factor);
+    } else {
+        // (32 bits, of which the float keeps 24: pi 2^-25 in a result that is rounded to 2^-11 or 2^-8.  The rest costs a single head of 200 000 tokens 8 %.)
+        sincospif(float(int32_t(high)) * 4.656612873077393e-10f, &s, &c);
+        return make_float2(c * factor, s * factor);
+    }
 }
 
 // a piece of V values of type E: V * sizeof a power of two up to 16 bytes, read and written as one
@@ -95,9 +106,12 @@ struct Piece {
     }
 };
 
+// CTAs of an SM that the registers leave room for (what a thread has under way takes 8 to 32 of them)
+constexpr uint32_t ctas_of_sm(uint32_t piece, bool next) { return piece == 16 ? (next ? 4u : 3u) : piece == 8 && !next ? 4u : 5u; }
+
 // V: values of a piece; NEXT: pairs side by side (V = 1: a unit is the two pieces of one pair in either layout)
 template <class E, uint32_t V, bool NEXT>
-__global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant__ RotaryParams P) {
+__global__ void __launch_bounds__(kThreads, ctas_of_sm(Piece<E, V>::kBytes, NEXT)) rotary_kernel(const __grid_constant__ RotaryParams P) {
     constexpr uint32_t kSize = sizeof(typename E::T);
     constexpr bool kTwo = !NEXT || V == 1;                                      // a unit that turns is two pieces
     // A unit's cosines and sines two pairs at a time, {c, c', s, s'}, in planes: units that lie side by side read 16 bytes side by side.
@@ -151,12 +165,12 @@ __global__ void __launch_bounds__(kThreads) rotary_kernel(const __grid_constant_
         const int64_t first = position_of(line);                                // (asked for together with the frequency)
         for (uint32_t i = threadIdx.x - line * columns; i < P.pairs; i += kThreads) {
             const uint64_t step = turn_fraction(P.frequencies[i]);
-            float2 cs = cosine_sine(first, step, P.factor);
+            float2 cs = cosine_sine<E>(first, step, P.factor);
             uint32_t p = place(line, i);
             table[p] = cs.x, table[p + (kPairs == 1 ? 1 : 2)] = cs.y;
 #pragma unroll 4
             for (uint32_t n = line + lines; n < tokens; n += lines) {
-                cs = cosine_sine(position_of(n), step, P.factor);
+                cs = cosine_sine<E>(position_of(n), step, P.factor);
                 p = place(n, i);
                 table[p] = cs.x, table[p + (kPairs == 1 ? 1 : 2)] = cs.y;
             }

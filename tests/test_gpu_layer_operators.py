@@ -900,3 +900,21 @@ def test_rotary_as_far_as_64_bits_reach(next):
         a = angles(at, f)
         bound = 2 * U + math.pi * 2.0 ** -25 + 2 * math.pi * 2.0 ** -32 + at.double().abs()[:, None] * (f.abs() * 2.0 ** -52 + 2.0 ** -61)
         assert ((cos - a.cos()).abs() <= bound).all() and ((sin - a.sin()).abs() <= bound).all()
+
+
+@gpu
+@pytest.mark.parametrize("next", [False, True])
+def test_rotary_in_32_bits_keeps_the_bits_of_an_angle(next):
+    # Near half a turn the sine is small and shows the angle: 4 units of it for sincospi, which takes from half of it to one and a half, 1 for the sum with the rest; the rest d
+    # (below pi 2^-24) is good to 3 units of itself and to one of 2^-56 of a turn that is cut off.  And the position's share, as above.
+    f = torch.tensor([math.pi + d for d in (1e-3, -1e-3, 3.1e-4, 7e-5, -2.2e-5, 1e-5)] + [2 * math.pi + 1e-4, 1e-4], dtype=torch.float64, device="cuda")
+    at = torch.tensor([1, -1, 3, -17, 251, -249, 901], device="cuda")
+    n = len(f)
+    x = torch.zeros(len(at), 1, 2 * n, device="cuda")
+    (x[..., 0::2] if next else x[..., :n]).fill_(1)
+    y = ep.rotary(x, at, f, interleaved=next).double()[:, 0]
+    cos, sin = (y[:, 0::2], y[:, 1::2]) if next else (y[:, :n], y[:, n:])
+    a = angles(at, f)
+    share = at.double().abs()[:, None] * (f.abs() * 2.0 ** -52 + 2.0 ** -61) + 2 * math.pi * 2.0 ** -56 + 3 * U * math.pi * 2.0 ** -24
+    assert ((sin - a.sin()).abs() <= 8 * U * a.sin().abs() + share).all()
+    assert ((cos - a.cos()).abs() <= 2.6 * U + share).all()
