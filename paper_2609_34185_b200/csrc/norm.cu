@@ -234,8 +234,9 @@ __global__ void __launch_bounds__(1024) norm_few_kernel(const __grid_constant__ 
             load_eight<16, true>(at, l * 8u, n[0], 2, e);
             to_pairs<16>(e, V.dtype == EP_FP16, w);
         }
+        if (offset != 0.0f)                               // (as load_vector does: a zero keeps its sign)
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
+            for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
     };
     auto times = [&](const NormVector &V, float offset) {
         Pair w[4];
@@ -454,8 +455,9 @@ __global__ void __launch_bounds__(stream_warps() * 32) norm_stream_kernel(const 
                     Eight<16> e;
                     smem_eight<16>(shared + V.kept + (i * apart + l) * 16u, there[i], e);
                     to_pairs<16>(e, V.dtype == EP_FP16, w);
+                    if (offset != 0.0f)
 #pragma unroll
-                    for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
+                        for (uint32_t j = 0; j < 4; ++j) w[j] = w[j] + Pair(offset);
                 } else kept_vector(shared + V.kept, i * apart + l, there[i], w);
             };
             auto times = [&](const NormVector &V, float offset) {

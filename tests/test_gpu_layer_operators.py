@@ -918,3 +918,18 @@ def test_rotary_in_32_bits_keeps_the_bits_of_an_angle(next):
     share = at.double().abs()[:, None] * (f.abs() * 2.0 ** -52 + 2.0 ** -61) + 2 * math.pi * 2.0 ** -56 + 3 * U * math.pi * 2.0 ** -24
     assert ((sin - a.sin()).abs() <= 8 * U * a.sin().abs() + share).all()
     assert ((cos - a.cos()).abs() <= 2.6 * U + share).all()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("T,C", [(4, 64), (16, 512), (7, 1001), (40000, 128), (1300, 1000), (1190, 12808)])
+def test_norm_keeps_the_sign_of_a_zero(T, C, dtype):
+    # without an offset nothing is added to a vector: a weight or gate of -0 turns the sign of what it multiplies, whichever kernel takes the rows
+    x = (torch.rand(T, C, generator=cuda(C), device="cuda") + 0.5).to(dtype)
+    w = torch.full((C,), -0.0, dtype=dtype, device="cuda")
+    p, one = torch.where(torch.arange(C, device="cuda") % 3 == 0, w, torch.ones_like(w)), torch.ones_like(w)
+    z = ep.norm(x, w)
+    assert (z == 0).all() and z.signbit().all()
+    r = torch.empty_like(x)
+    z = ep.norm(x, one, one * -0.0, gate=p, post_weight=one, residual_out=r)[0]
+    assert torch.equal(r.signbit(), r == 0) and torch.equal(z.signbit(), z == 0) and torch.equal(z == 0, (p == 0).expand(T, C))
