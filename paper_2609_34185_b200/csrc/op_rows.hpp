@@ -15,8 +15,8 @@ struct Eight {
 // which of a piece's eight values lie inside the row: the first n
 __device__ __forceinline__ uint32_t inside(uint32_t c, uint32_t C) { return c < C ? min(8u, C - c) : 0u; }
 
-// Values c .. c + n of a row; `vec`: 2 if rows begin on 16 bytes, 1 on 8, else 0.  What is outside reads as zero.  KEPT: vectors that every row needs, which
-// stay in L1; rows are read once.
+// Values c .. c + n of a row; `vec`: 2 if rows begin on 16 bytes, 1 on 8, else 0.  What is outside reads as zero.  KEPT: vectors that every row needs, or a row that is
+// read again, which stay in L1; rows are read once.  (Value by value the next seven loads want the same sectors, so that rows stay there as well.)
 template <uint32_t BITS, bool KEPT = false>
 __device__ __forceinline__ void load_eight(const uint8_t *row, uint32_t c, uint32_t n, uint32_t vec, Eight<BITS> &e) {
     if (vec == 2 && n == 8) {
@@ -43,8 +43,13 @@ __device__ __forceinline__ void load_eight(const uint8_t *row, uint32_t c, uint3
 #pragma unroll
     for (uint32_t i = 0; i < 8; ++i)
         if (i < n) {
-            if constexpr (BITS == 32) e.w[i] = __ldcs(reinterpret_cast<const uint32_t *>(row) + c + i);
-            else e.w[i / 2] |= uint32_t(__ldcs(reinterpret_cast<const uint16_t *>(row) + c + i)) << (16 * (i % 2));
+            if constexpr (BITS == 32) {
+                const uint32_t *p = reinterpret_cast<const uint32_t *>(row) + c + i;
+                e.w[i] = KEPT ? __ldg(p) : *p;
+            } else {
+                const uint16_t *p = reinterpret_cast<const uint16_t *>(row) + c + i;
+                e.w[i / 2] |= uint32_t(KEPT ? __ldg(p) : *p) << (16 * (i % 2));
+            }
         }
 }
 // the same from shared memory, all eight values or none
