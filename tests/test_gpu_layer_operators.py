@@ -933,3 +933,68 @@ def test_norm_keeps_the_sign_of_a_zero(T, C, dtype):
     r = torch.empty_like(x)
     z = ep.norm(x, one, one * -0.0, gate=p, post_weight=one, residual_out=r)[0]
     assert torch.equal(r.signbit(), r == 0) and torch.equal(z.signbit(), z == 0) and torch.equal(z == 0, (p == 0).expand(T, C))
+
+
+@gpu
+def test_on_a_given_stream_while_the_current_one_is_busy():
+    # What the given stream holds when it has ended, looked at from itself, while a wait of a second or two still stands before everything on the current stream.  (Once
+    # before that, since the first launch of a kernel waits for the device.)
+    calls, flat, (x, qx, heads) = each_operator(9)
+    ones, at, f = torch.ones(len(qx), device="cuda"), torch.arange(len(heads), device="cuda"), ep.rotary_frequencies(64)
+    fresh = lambda stream=None: [*ep.quantize_rows(x, stream=stream), ep.norm(x, stream=stream), *ep.norm(x, residual=x, out_dtype=ep.FP8_E4M3, stream=stream)[0],  # noqa: E731
+                                 ep.int8_matmul(qx, ones, qx, stream=stream), ep.rotary(heads, at, f, stream=stream)]
+    same = lambda a, b: len(a) == len(b) and all([torch.equal(s.view(torch.uint8), t.view(torch.uint8)) for s, t in zip(a, b)])  # noqa: E731
+    calls()
+    want, stream = [t.clone() for t in flat()] + fresh(), torch.cuda.Stream()
+    for busy in (False, True):
+        for t in flat():
+            t.zero_()
+        torch.cuda.synchronize()
+        if busy:
+            torch.cuda._sleep(4_000_000_000)
+        calls(stream)
+        new = fresh(stream)
+        with torch.cuda.stream(stream):
+            got = [t.clone() for t in flat() + new]
+            assert same(got, want)
+        stream.synchronize()
+        assert torch.cuda.current_stream().query() != busy
+        torch.cuda.synchronize()
+
+
+@gpu
+@pytest.mark.parametrize("dtype,wide", [(torch.bfloat16, torch.bfloat16), (torch.float16, torch.float32), (torch.float32, torch.float32)])
+@pytest.mark.parametrize("T,C,groups", [(40000, 128, 1), (30011, 64, 1), (9000, 256, 1), (1300, 1000, 1), (2501, 2048, 1), (1190, 12808, 1), (2400, 12800, 2), (2400, 12800, 4), (1200, 16384, 3)])
+def test_norm_of_many_rows_with_an_offset(T, C, groups, dtype, wide):
+    # weights stored without their 1, vectors of 16 bits where they have to wait as they lie in memory, alone and for each group; a row of zeros and one that is not finite
+    x, v = norm_inputs(T, C, dtype, wide, groups, T + C)
+    zero, bad = T // 3, T // 2
+    x[zero] = v["residual"][zero] = 0
+    x[bad, C - 1] = math.inf
+    fine = torch.arange(T, device="cuda") != bad
+    for center in (False, True):
+        for left in ((), ("gate",), ("post_weight", "bias")):
+            given = {k: t for k, t in v.items() if k not in left}
+            z, r = ep.norm(x, weight_offset=1.0, residual_scale=0.7, center=center, **given)
+            want, r_want = normed(x, weight_offset=1.0, residual_scale=0.7, center=center, **given)
+            assert near(z[fine], tuple(t[fine] for t in want)) and near(r[fine], tuple(t[fine] for t in r_want))
+            assert z[bad].isnan().any() and (r[zero] == 0).all()
+            assert torch.equal(z[zero], rows_of(v["bias"], T)[zero].to(dtype) if "bias" in given else torch.zeros_like(z[zero]))
+    assert ep.last_device_status() == 0
+
+
+@gpu
+@pytest.mark.parametrize("dtype,wide", [(torch.bfloat16, torch.float32), (torch.float32, torch.float16)])
+@pytest.mark.parametrize("c0", [0, 8, 1, 3])
+def test_norm_to_int8_in_views(c0, dtype, wide):
+    # values and scales of rows of any distance and alignment are those of the 32-bit result
+    T, C = 33, 200
+    x, v = norm_inputs(T, C + 20, dtype, wide, 3, 20 + c0)
+    x, v = x[..., c0:c0 + C], {k: t[..., c0:c0 + C] for k, t in v.items()}
+    values, scales = torch.full((T, C + 29), 3, dtype=torch.int8, device="cuda"), torch.full((T + 2,), 3.0, device="cuda")
+    out = (values[:, c0:c0 + C], scales[1:T + 1])
+    got, r = ep.norm(x, **v, out=out)
+    z, r32 = ep.norm(x, **v, out_dtype=ep.FP32)
+    q, s = ep.quantize_rows(z)
+    assert got is out and torch.equal(got[0], q) and torch.equal(got[1], s) and torch.equal(r, r32)
+    assert (values[:, :c0] == 3).all() and (values[:, c0 + C:] == 3).all() and scales[0] == scales[T + 1] == 3
