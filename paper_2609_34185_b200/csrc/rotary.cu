@@ -325,6 +325,7 @@ extern "C" int ep_rotary_frequencies(uint32_t pairs, double base, double stretch
             k = k < 0.0 ? 0.0 : k > 1.0 ? 1.0 : k;
         }
         out[i] = f * (k + (1.0 - k) / stretch);
+        if (!std::isfinite(out[i])) return EP_ERR_BAD_ARG;                              // (of a base next to 0, of bounds that are infinite)
     }
     return EP_OK;
 }

@@ -123,3 +123,12 @@ def test_results_in_the_place_of_operands():
         assert rows_job(T=0, **w) == 0 and rows_job(x=P, **w) == BAD, w
     for w in (dict(x=P, w=2 * P), dict(x=2 * P, w=P), dict(x=P, w=2 * P, dtype=ep.FP32)):
         assert matmul_job(T=0, y=P, **w) == 0 and matmul_job(y=P, **w) == BAD, w
+
+
+def test_frequencies_that_are_none():
+    """What is not a finite number is refused, wherever it comes from: header and kernels ask for finite frequencies."""
+    for kw in (dict(original=10.0, fast=math.inf, slow=-math.inf), dict(original=10.0, fast=1.0, slow=-math.inf), dict(original=1e308, base=5e-324), dict(base=5e-324)):
+        with pytest.raises(ep.EntroPackError) as e:
+            ep.rotary_frequencies(256, device="cpu", **kw)
+        assert e.value.status == BAD
+    assert np.isfinite(ep.rotary_frequencies(256, device="cpu", original=10.0, stretch=2.0, fast=math.inf).numpy()).all()
