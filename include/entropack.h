@@ -481,7 +481,9 @@ int ep_rotary(const ep_rotary_job *job, void *stream);
  * as long as the one of `original` positions that the model was trained on: a frequency that makes fewer than `slow` turns in that context is divided by
  * stretch, one that makes more than `fast` stays, and between the two
  *     out[i] = f (k + (1 - k) / stretch),   k = (original f / 2 pi - slow) / (fast - slow)
- * With original = 0 every frequency is divided by stretch.  (Models stretched like this are usually run with factor = 0.1 ln(stretch) + 1.) */
+ * With original = 0 every frequency is divided by stretch.  The share k is linear in the turns that a pair makes.  Programs that run checkpoints with factor = 0.1 ln(stretch) + 1
+ * often share out linearly in the pair's index i, between the indexes that make `fast` and `slow` turns: that is another rule with other frequencies, which a caller
+ * works out and passes to ep_rotary like any others. */
 int ep_rotary_frequencies(uint32_t pairs, double base, double stretch, double original, double fast, double slow, double *out);
 
 /* Device-side integrity word (no counterpart in the paper; it uses the fact that the encoder of Eq. 17 starts

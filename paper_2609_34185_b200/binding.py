@@ -792,7 +792,8 @@ def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, 
 def rotary_frequencies(dim: int, base: float = 10000.0, stretch: float = 1.0, original: float = 0.0, fast: float = 32.0, slow: float = 1.0, device="cuda"):
     """The dim / 2 frequencies base^(-2 i / dim) in radians per position, float64 on `device`, for a context `stretch` times as long as the model was
     trained for: with `original`, the length of that one, those that turn fewer than `slow` times in it are divided by stretch, those that turn more than `fast`
-    times stay, and it is shared out between; without, all are divided.  See ep_rotary_frequencies."""
+    times stay, and between it is shared out linearly in the turns (not in the pair's index, as many checkpoints with a factor of 0.1 ln(stretch) + 1 have it: work
+    those out and pass them to rotary); without, all are divided.  See ep_rotary_frequencies."""
     torch = _torch()
     if dim < 2 or dim % 2:
         raise ValueError("dim must be even")
