@@ -758,11 +758,14 @@ def norm(x, weight=None, bias=None, residual=None, residual_scale: float = 1.0, 
     z, s, scales, ld_scales = out, None, 0, 0
     if isinstance(out, (tuple, list)):
         z, s = out
-        if z.dtype == e4m3:
-            scales, ld_scales = s.data_ptr(), _matrix(s, e8m0, (T, -(-Cc // 128)), dev, "out[1]")
-        elif s is not None:
-            scales = _floats(s, T, dev, "out[1]")
-        z_code = FP8_E4M3 if z.dtype == e4m3 else INT8 if z.dtype == torch.int8 and s is not None else None
+        if s is not None:
+            if z.dtype == e4m3:
+                scales, ld_scales = s.data_ptr(), _matrix(s, e8m0, (T, -(-Cc // 128)), dev, "out[1]")
+            else:
+                scales = _floats(s, T, dev, "out[1]")
+            z_code = FP8_E4M3 if z.dtype == e4m3 else INT8 if z.dtype == torch.int8 else None
+        else:
+            z_code = None
     else:
         z_code = codes.get(z.dtype)
     if z_code is None:

@@ -998,3 +998,13 @@ def test_norm_to_int8_in_views(c0, dtype, wide):
     q, s = ep.quantize_rows(z)
     assert got is out and torch.equal(got[0], q) and torch.equal(got[1], s) and torch.equal(r, r32)
     assert (values[:, :c0] == 3).all() and (values[:, c0 + C:] == 3).all() and scales[0] == scales[T + 1] == 3
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [E4M3, torch.int8])
+def test_norm_refuses_values_without_their_scales(dtype):
+    x, q = torch.zeros(4, 256, device="cuda"), torch.zeros(4, 256, dtype=torch.uint8, device="cuda").view(dtype)
+    with pytest.raises(ValueError):
+        ep.norm(x, out=(q, None))
+    with pytest.raises(ValueError):
+        ep.norm(x, out=(q,))
