@@ -438,7 +438,9 @@ typedef struct {
  * norm(v) = (v - mean) / sqrt(mean((v - mean)^2) + eps), the mean taken as 0 unless `center`; o = weight_offset, 0 or 1 as the weights are
  * stored (o + weight is 1 where there is no weight).  Everything is held in fp32, r too: it is rounded where it is written, not before z is computed.  z is
  * rounded once: to a 16- or 32-bit type, to E4M3 with the scales of ep_quantize_blocks (block_rows 1), or to INT8 with the scale of ep_quantize_rows.
- * C up to 32768, else EP_ERR_UNSUPPORTED.  d_z or d_residual_out, one of them, may be d_x, and one of them d_residual, with the type and ld of what was there: a
+ * C up to 32768, else EP_ERR_UNSUPPORTED.  A sum of squares has to stay inside fp32: values of more than 1.8e19 / sqrt(C) make zeros of their row.  Fastest are rows and vectors that begin on
+ * 16 bytes (outputs of 32 bits on 32), C a multiple of 8, and x and residual of one type or a 16-bit x beside an FP32 residual; anything else is taken by a general kernel.  A row's last bits
+ * depend on which kernel that is.  d_z or d_residual_out, one of them, may be d_x, and one of them d_residual, with the type and ld of what was there: a
  * row is read before it is written.  (Another type or ld there is EP_ERR_BAD_ARG, as is d_z for d_residual_out; no other overlap of what is read and what is
  * written is allowed.) */
 typedef struct {

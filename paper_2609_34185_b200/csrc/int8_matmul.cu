@@ -381,7 +381,7 @@ int launch_strip(ProductParams P, const Operands &o, const StripPlan &plan, uint
     const uint32_t block = P.w_block + P.x_block;
     P.whole = o.C / 128u;
     // One CTA to an SM with all of its memory; or two that share it, the next one beginning while the last one ends, where there are more CTAs than SMs or
-    // a CTA's share is not much more than fits (4096 x 4096, 1 token: 5.8 us, 6.4 with all memory; 5120 x 17408 19.9, 17.8).
+    // a CTA's share is not much more than fits (4096 x 4096, 1 token: 5.8 us, 6.4 with all memory; 5120 x 17408 19.9, 17.8: the border between the two is known no better than that).
     // (The place of a cluster's sums comes off it.)
     const uint32_t join = plan.split > 1 ? 512u * plan.split * (((plan.tokens + plan.split - 1u) / plan.split + 3u) / 4u * 4u) : 0u, room = (plan.grid > sms || plan.split > 2 || uint64_t(block) * P.blocks / plan.split <= 310u * 1024u ? 92u : 204u) * 1024u - join;
     // Four blocks to a stage where three stages of them fit: a stage costs the issuing warps some 250 cycles, a block's instructions 130
@@ -408,7 +408,7 @@ int launch_strip(ProductParams P, const Operands &o, const StripPlan &plan, uint
 // ---- many tokens: a pair of CTAs per tile -----------------------------------------------------------------------------------
 // Two CTAs share tiles of 256 rows of the weight by N tokens (tcgen05 cta_group::2): each has half of the weight's rows and half of the tokens
 // in its shared memory, and keeps the sums of its 128 rows with all tokens in its tensor memory, twice, so that a tile is read out while the next one
-// is summed.  8192^3 in 334 - 355 us (3.1 - 3.3 PFLOP/s; operands from L2 at 12 TB/s), 777 x 3000 x 1744 in 10.1.
+// is summed.  8192^3 in 334 - 373 us in a short graph of calls (3.0 - 3.3 PFLOP/s; operands from L2 at 12 TB/s), 371 - 434 called one after another, where the power cap lowers the clock; 777 x 3000 x 1744 in 10.1.
 //   warp 0        brings the operands in
 //   warp 1        of the first CTA issues the products
 //   warps 2 - 9   sums to y: two warps to each quarter of the rows, half of the tokens each

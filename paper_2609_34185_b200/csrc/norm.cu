@@ -29,7 +29,7 @@ struct NormParams {
     uint8_t *r, *z, *s;
     int64_t ldx, ldh, ldr, ldz, lds;      // bytes; scales: elements
     NormVector w, d, g, p;
-    float c, offset, eps, columns, inverse;      // (inverse: of columns; a mean is divided, so that a row of equal values has none but zeros left)
+    float c, offset, eps, columns, inverse;      // (inverse: of columns; a mean is divided, so that a row of equal 16-bit values, whose sum is exact, has none but zeros left)
     uint32_t T, C;
     uint32_t warps, rows;         // warps of a row, rows of a CTA
     uint32_t lanes;               // of a row that takes less than a warp (32: whole warps)
@@ -136,6 +136,8 @@ __device__ __forceinline__ void e4m3_pieces(const RowGroup &group, Pair (&v)[N][
 }
 
 // ---- any rows: straight from memory -------------------------------------------------------------------------------------------
+// Any types, alignment and up to 32768 columns.  Conversions and vectors from L1 bound it where rows begin on 16 bytes (8192 x 5120 BF16 beside FP16 62.8 us, with both norms 81.7); where they
+// begin anywhere, the way from L1: eight loads one after another take the same sectors (2300 x 3427 FP32 with a residual 50 us, floor 19.6, L2 brings 480 MB for 126).
 template <uint32_t XBITS, uint32_t HBITS, uint32_t N, uint32_t THREADS>
 __global__ void __launch_bounds__(THREADS) norm_kernel(const __grid_constant__ NormParams P) {
     __shared__ uint32_t room[64];
