@@ -463,7 +463,7 @@ int ep_norm(const ep_norm_job *job, void *stream);
  * becomes factor * (u cos a - v sin a, v cos a + u sin a) for a = position * frequency[i]; the other values of the head stay.  The angle is kept as a
  * fraction of a turn in 64 bits and is off by up to |position| (2^-52 |frequency| + 2^-61) radians before it becomes a float: twice what the frequency's own last bit
  * makes of it, and beside that 2e-9 radians at position 2^32, 5e-7 at 2^40.  Everything else is fp32, rounded once.  d_out may
- * be d_x (with the same strides): the rotation is then in place.  Its values lie apart: all heads of a row before the next row (ldo >= (heads - 1) ldo_head +
+ * be d_x (with the same strides): the rotation is then in place; else the two do not overlap.  d_out's values lie apart: all heads of a row before the next row (ldo >= (heads - 1) ldo_head +
  * dim), or all rows of a head before the next head, else EP_ERR_BAD_ARG. */
 typedef struct {
     const void *d_x;                /* device: T x heads x dim of dtype */
